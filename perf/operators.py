@@ -217,7 +217,8 @@ def _prepare_attn(case, dr, handles):
     if handles:
         from paper_2606_19004_amd import ditstep as lib
         o = st["o"] if case["kind"] == "grad" else torch.empty((st["q_off"][-1], H, d), dtype=dt, device="cuda")
-        cfg = lib.packed_config(st["q"], st["k"], st["v"], o, len(lens), causal=case["causal"], scale=st["scale"])
+        cfg = lib.packed_config(st["q"], st["k"], st["v"], o, len(lens), causal=case["causal"], scale=st["scale"],
+                                max_q=case["new"] or max(lens))
         st["cfg"] = cfg
         if case["kind"] == "grad":
             dqkv = torch.empty_like(qkv)
