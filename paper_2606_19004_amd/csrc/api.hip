@@ -6,15 +6,19 @@
 #include <atomic>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <limits>
 #include <map>
 #include <mutex>
 #include <string>
 #include <vector>
 
+#include "../../include/ditpolicy.h"
 #include "../../include/ditstep.h"
 #include "internal.h"
 #include "host_checks.h"
+#include "packed.h"
+#include "policy_checks.h"
 
 using namespace dit;
 using dit::set_error;
@@ -1251,6 +1255,271 @@ dit_status dit_profile_end(dit_kernel_stat* stats, int32_t capacity, int32_t* co
   }
   if (count) *count = n;
   return st;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// policy update (ditpolicy.h)
+// ---------------------------------------------------------------------------
+namespace {
+
+// queries a sequence has at most
+int most_queries(const dit_packed_config* c, const int32_t* q_offsets) {
+  const int most = q_offsets || c->sequences == 0 ? c->total_q : c->total_q / c->sequences;
+  return c->max_q > 0 ? std::min(c->max_q, most) : most;
+}
+
+dit_status packed_args(const dit_packed_config* c, const int32_t* q_offsets, const int32_t* k_offsets,
+                       const int32_t* k_lengths, PackedArgs* a) {
+  dit_status st = check_packed(c);
+  if (st) return st;
+  if ((st = check_lengths("q", q_offsets, c->total_q, c->sequences))) return st;
+  if ((st = check_lengths("k", k_offsets, c->total_k, c->sequences))) return st;
+  if (!q_offsets && c->sequences > 0 && c->max_q > 0 && c->max_q < c->total_q / c->sequences)
+    return set_error(DIT_ERR_SHAPE, "max_q %d is below the %d queries of every sequence", c->max_q, c->total_q / c->sequences);
+  const int n = std::max(c->sequences, 1);
+  a->qr = PackedRows{q_offsets, c->total_q, c->total_q / n};
+  a->kr = PackedRows{k_offsets, c->total_k, c->total_k / n};
+  a->k_len = k_lengths;
+  a->nseq = c->sequences;
+  a->H = c->heads;
+  a->Hkv = c->kv_heads;
+  a->G = c->heads / c->kv_heads;
+  a->max_q = most_queries(c, q_offsets);
+  a->causal = c->causal != 0;
+  a->scale = c->scale;
+  a->q_row = c->q_row;
+  a->q_head = c->q_head;
+  a->k_row = c->k_row;
+  a->k_head = c->k_head;
+  a->v_row = c->v_row;
+  a->v_head = c->v_head;
+  a->o_row = c->o_row;
+  a->o_head = c->o_head;
+  return DIT_OK;
+}
+
+dit_status check_offsets_aligned(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs)
+    if ((uintptr_t)p & 3) return set_error(DIT_ERR_INVALID_ARG, "offsets, lengths and fp32 tensors must be 4-byte aligned");
+  return DIT_OK;
+}
+
+// workspace of a call, whatever its max_q and offsets turn out to be
+size_t packed_forward_ws(const dit_packed_config* c) {
+  if (c->sequences == 0) return 0;
+  size_t need = 0;
+  const int tight = c->max_q > 0 ? std::min(c->max_q, c->total_q) : c->total_q;
+  for (int most : {tight, std::min(tight, c->total_q / c->sequences)})
+    need = std::max(need, packed_plan(c->dtype, c->sequences, c->heads, c->kv_heads, c->head_dim, c->total_q, c->total_k, most).ws);
+  return al256(need);
+}
+
+dit_status gated_norm_args(const dit_gated_norm_config* c, const void* post_w, const void* pre_w, const float* gate,
+                           const float* scale, const int32_t* offsets, GatedNormArgs* a) {
+  dit_status st = check_gated_norm(c);
+  if (st) return st;
+  if ((st = check_lengths("rows", offsets, c->rows, c->sequences))) return st;
+  if ((st = check_offsets_aligned({gate, scale, offsets}))) return st;
+  a->post_w = post_w;
+  a->pre_w = pre_w;
+  a->gate = gate;
+  a->scale = scale;
+  a->pr = PackedRows{offsets, c->rows, c->rows / std::max(c->sequences, 1)};
+  a->nseq = c->sequences;
+  a->rows = c->rows;
+  a->D = c->hidden;
+  a->post = c->post_norm;
+  a->pre = c->pre_norm;
+  a->eps = c->eps;
+  a->alpha = c->residual_scale;
+  a->x_row = c->x_row;
+  a->y_row = c->y_row;
+  a->h_row = c->h_row;
+  a->mod_row = c->mod_row;
+  return DIT_OK;
+}
+
+dit_status check_elements(std::initializer_list<const void*> ptrs, int32_t dtype) {
+  for (const void* p : ptrs)
+    if ((uintptr_t)p % esize(dtype)) return set_error(DIT_ERR_INVALID_ARG, "row tensors and norm weights must be aligned to their type");
+  return DIT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t packed_attention_workspace_bytes(const dit_packed_config* c) { return check_packed(c) ? 0 : packed_forward_ws(c); }
+
+size_t packed_attention_backward_workspace_bytes(const dit_packed_config* c) {
+  return check_packed(c) ? 0 : al256(packed_backward_ws(c->sequences, c->heads, c->total_q));
+}
+
+dit_status packed_attention(const dit_packed_config* c, const void* q, const void* k, const void* v,
+                            const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths, void* o,
+                            float* lse, void* ws, size_t ws_bytes, dit_stream stream) {
+  PackedArgs a{};
+  dit_status st = packed_args(c, q_offsets, k_offsets, k_lengths, &a);
+  if (st) return st;
+  if (c->sequences == 0 || c->total_q == 0) return DIT_OK;
+  if (!q || !o || (c->total_k > 0 && (!k || !v))) return set_error(DIT_ERR_INVALID_ARG, "q/k/v/o NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o))
+    return set_error(DIT_ERR_INVALID_ARG, "q/k/v/o must be 16-byte aligned");
+  if ((st = check_offsets_aligned({q_offsets, k_offsets, k_lengths, lse}))) return st;
+  if ((st = check_ws(ws, ws_bytes, packed_forward_ws(c)))) return st;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = o;
+  a.lse = lse;
+  // (the visible pairs are on the device: the class's flops count every pair of equal lengths)
+  const double pairs = (double)c->total_q * c->total_k / c->sequences * (c->causal && c->total_q == c->total_k ? 0.5 : 1.0);
+  TIMED("packed_attention", 4.0 * pairs * c->heads * c->head_dim, 0, hs(stream),
+        packed_attention_fwd(a, c->dtype, c->head_dim, c->total_k, ws, hs(stream)));
+  return DIT_OK;
+}
+
+dit_status packed_attention_backward(const dit_packed_config* c, const void* q, const void* k, const void* v,
+                                     const void* o, const float* lse, const void* d_o, const int32_t* q_offsets,
+                                     const int32_t* k_offsets, const int32_t* k_lengths, void* dq, void* dk, void* dv,
+                                     void* ws, size_t ws_bytes, dit_stream stream) {
+  PackedArgs a{};
+  dit_status st = packed_args(c, q_offsets, k_offsets, k_lengths, &a);
+  if (st) return st;
+  if ((st = check_packed_gradients(c))) return st;
+  if (c->sequences == 0 || (c->total_q == 0 && c->total_k == 0)) return DIT_OK;
+  if (c->total_q > 0 && (!q || !o || !lse || !d_o || !dq)) return set_error(DIT_ERR_INVALID_ARG, "q/o/lse/d_o/dq NULL");
+  if (c->total_k > 0 && (!k || !v || !dk || !dv)) return set_error(DIT_ERR_INVALID_ARG, "k/v/dk/dv NULL");
+  for (const void* p : {q, k, v, o, d_o, (const void*)dq, (const void*)dk, (const void*)dv})
+    if (!aligned16(p)) return set_error(DIT_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
+  if ((st = check_offsets_aligned({q_offsets, k_offsets, k_lengths, lse}))) return st;
+  if ((st = check_ws(ws, ws_bytes, al256(packed_backward_ws(c->sequences, c->heads, c->total_q))))) return st;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.o = const_cast<void*>(o);
+  a.lse = const_cast<float*>(lse);
+  a.d_o = d_o;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  const double pairs = (double)c->total_q * c->total_k / c->sequences * (c->causal && c->total_q == c->total_k ? 0.5 : 1.0);
+  const double product = 2.0 * pairs * c->heads * c->head_dim;
+  TIMED("packed_attention_delta", 0, 2.0 * c->total_q * c->heads * c->head_dim * esize(c->dtype), hs(stream),
+        packed_attention_delta(a, c->dtype, c->head_dim, ws, hs(stream)));
+  TIMED("packed_attention_dkdv", 4 * product, 0, hs(stream),
+        packed_attention_dkdv(a, c->dtype, c->head_dim, c->total_k, ws, hs(stream)));
+  TIMED("packed_attention_dq", 3 * product, 0, hs(stream), packed_attention_dq(a, c->dtype, c->head_dim, ws, hs(stream)));
+  return DIT_OK;
+}
+
+dit_status gated_norm(const dit_gated_norm_config* c, const void* x, const void* y, const void* post_w,
+                      const void* pre_w, const float* gate, const float* scale, const float* shift,
+                      const int32_t* offsets, void* x_out, void* h, dit_stream stream) {
+  GatedNormArgs a{};
+  dit_status st = gated_norm_args(c, post_w, pre_w, gate, scale, offsets, &a);
+  if (st) return st;
+  if (c->rows == 0 || (!x_out && !h)) return DIT_OK;
+  if (!x) return set_error(DIT_ERR_INVALID_ARG, "x NULL");
+  if ((st = check_offsets_aligned({shift}))) return st;
+  if ((st = check_elements({x, y, post_w, pre_w, x_out, h}, c->dtype))) return st;
+  a.x = x;
+  a.y = y;
+  a.shift = shift;
+  a.x_out = x_out;
+  a.h = h;
+  const double passes = 1 + (y != nullptr) + (x_out != nullptr) + (h != nullptr);
+  TIMED("gated_norm", 0, passes * c->rows * c->hidden * esize(c->dtype), hs(stream), gated_norm_fwd(a, c->dtype, hs(stream)));
+  return DIT_OK;
+}
+
+size_t gated_norm_backward_workspace_bytes(const dit_gated_norm_config* c) {
+  return check_gated_norm(c) ? 0 : al256(gated_norm_ws(c->sequences, c->rows, c->hidden));
+}
+
+dit_status gated_norm_backward(const dit_gated_norm_config* c, const void* x_out, const void* y, const void* post_w,
+                               const void* pre_w, const float* gate, const float* scale, const int32_t* offsets,
+                               const void* dx_out, const void* dh, void* dx, void* dy, float* dgate, float* dscale,
+                               float* dshift, float* dpost_w, float* dpre_w, void* ws, size_t ws_bytes,
+                               dit_stream stream) {
+  GatedNormArgs a{};
+  dit_status st = gated_norm_args(c, post_w, pre_w, gate, scale, offsets, &a);
+  if (st) return st;
+  if (c->rows > 0 && !x_out) return set_error(DIT_ERR_INVALID_ARG, "x_out NULL");
+  if (!y && (dy || dgate || dpost_w)) return set_error(DIT_ERR_INVALID_ARG, "dy/dgate/dpost_w wanted without a branch y");
+  if ((st = check_offsets_aligned({dgate, dscale, dshift, dpost_w, dpre_w}))) return st;
+  if ((st = check_elements({x_out, y, post_w, pre_w, dx_out, dh, dx, dy}, c->dtype))) return st;
+  const bool columns = dgate || dscale || dshift || dpost_w || dpre_w;
+  if (!columns && (c->rows == 0 || (!dx && !dy))) return DIT_OK;
+  if (c->sequences == 0 && !dpost_w && !dpre_w) return DIT_OK;
+  if ((st = check_ws(ws, ws_bytes, al256(gated_norm_ws(c->sequences, c->rows, c->hidden))))) return st;
+  a.x = x_out;
+  a.y = y;
+  a.dx_out = dx_out;
+  a.dh = dh;
+  a.dx = dx;
+  a.dy = dy;
+  a.dgate = dgate;
+  a.dscale = dscale;
+  a.dshift = dshift;
+  a.dpost_w = dpost_w;
+  a.dpre_w = dpre_w;
+  a.parts = columns ? (float*)ws : nullptr;
+  a.chunks = gated_norm_chunks(c->sequences, c->rows);
+  const double passes = 1 + (y != nullptr) + (dx_out != nullptr) + (dh != nullptr) + (dx != nullptr) + (dy != nullptr);
+  if (c->rows > 0)
+    TIMED("gated_norm_backward", 0, passes * c->rows * c->hidden * esize(c->dtype), hs(stream),
+          gated_norm_rows_bwd(a, c->dtype, hs(stream)));
+  if (columns)
+    TIMED("gated_norm_columns", 0, 12.0 * a.chunks * c->hidden, hs(stream), gated_norm_columns_bwd(a, c->dtype, hs(stream)));
+  return DIT_OK;
+}
+
+size_t flow_policy_loss_workspace_bytes(int32_t batch, int64_t n) {
+  if (batch <= 0 || n <= 0) return 0;
+  return al256((size_t)batch * policy_loss_chunks(batch, n) * 2 * sizeof(double));
+}
+
+dit_status flow_policy_loss(const float* x, const float* v, const float* x_next, const float* v_ref, int32_t batch,
+                            int64_t n, float t, float t_next, float noise_level, const double* logp_old,
+                            const float* adv, double logp_scale, double clip_low, double clip_high, double kl_weight,
+                            double* loss, double* logp, double* ratio, float* dv, void* ws, size_t ws_bytes,
+                            dit_stream stream) {
+  dit_status st = check_policy_loss(batch, n, logp_scale, clip_low, clip_high, kl_weight);
+  if (st) return st;
+  PolicyLossArgs a{};
+  if ((st = flow_density_terms(n, t, t_next, noise_level, &a.cx, &a.cv, &a.var, &a.cst))) return st;
+  if (batch == 0 || n == 0) return DIT_OK;
+  if (!x || !v || !x_next || !logp_old || !adv) return set_error(DIT_ERR_INVALID_ARG, "x/v/x_next/logp_old/adv NULL");
+  if (!loss && !logp && !ratio && !dv) return set_error(DIT_ERR_INVALID_ARG, "no output wanted");
+  if ((st = check_offsets_aligned({x, v, x_next, v_ref, adv, dv}))) return st;
+  for (const void* p : {(const void*)logp_old, (const void*)loss, (const void*)logp, (const void*)ratio})
+    if ((uintptr_t)p & 7) return set_error(DIT_ERR_INVALID_ARG, "fp64 tensors must be 8-byte aligned");
+  if ((st = check_ws(ws, ws_bytes, flow_policy_loss_workspace_bytes(batch, n)))) return st;
+  a.x = x;
+  a.v = v;
+  a.xn = x_next;
+  a.v_ref = kl_weight > 0.0 ? v_ref : nullptr;
+  a.batch = batch;
+  a.n = n;
+  a.logp_old = logp_old;
+  a.adv = adv;
+  a.logp_scale = logp_scale;
+  a.clip_low = clip_low;
+  a.clip_high = clip_high;
+  a.kl_weight = kl_weight;
+  a.loss = loss;
+  a.logp = logp;
+  a.ratio = ratio;
+  a.dv = dv;
+  a.parts = (double*)ws;
+  a.chunks = policy_loss_chunks(batch, n);
+  const double reads = 4.0 * batch * n * (a.v_ref ? 4 : 3);
+  TIMED("policy_loss_sums", 0, reads, hs(stream), policy_loss_sums(a, hs(stream)));
+  TIMED("policy_loss_finish", 0, dv ? reads + 4.0 * batch * n : 0.0, hs(stream), policy_loss_finish(a, hs(stream)));
+  return DIT_OK;
 }
 
 }  // extern "C"

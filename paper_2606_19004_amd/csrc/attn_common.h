@@ -1,0 +1,126 @@
+// Pieces that the attention kernels share: exchanges between the halves of a wave, loads that go straight
+// into LDS, and the tile layout whose rows are read both as they are and transposed.
+#pragma once
+#include <type_traits>
+
+#include "internal.h"
+
+namespace dit {
+
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+
+// Combine the values of lanes l and l ^ 32 through v_permlane32_swap (a VALU exchange of the two
+// 32-lane halves) instead of an LDS permute. With both operands v, the swap's two results hold, in
+// every lane, v[l] and v[l ^ 32] (which of the two is which depends on the half), so only symmetric
+// combinations are formed from them.
+__device__ __forceinline__ void half_pair(float v, float& a, float& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float pair_max(float v) {
+  float a, b;
+  half_pair(v, a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float pair_sum(float v) {
+  float a, b;
+  half_pair(v, a, b);
+  return a + b;
+}
+
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+
+// Four direct-to-LDS loads under one M0 value: destination M0 + 1024 i + 16 lane, global offset
+// v[i] + 1024 i (the instruction offset moves both addresses). Issued back to back they hold the
+// wave's issue for less than four separately issued loads, each of which sets M0 on its own.
+// Inline assembly, so the compiler does not track these loads: the wait before the barrier that
+// hands a stage over is the explicit s_waitcnt(0) of the loop.
+__device__ __forceinline__ void dma4_b128(u32x4_t rsrc, uint32_t m0v, uint32_t v0, uint32_t v1, uint32_t v2,
+                                          uint32_t v3) {
+  uint32_t saved;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+               "buffer_load_dwordx4 %2, %6, 0 offen lds\n\t"
+               "buffer_load_dwordx4 %3, %6, 0 offen offset:1024 lds\n\t"
+               "buffer_load_dwordx4 %4, %6, 0 offen offset:2048 lds\n\t"
+               "buffer_load_dwordx4 %5, %6, 0 offen offset:3072 lds\n\t"
+               "s_mov_b32 m0, %0"
+               : "=&s"(saved) : "s"(m0v), "v"(v0), "v"(v1), "v"(v2), "v"(v3), "s"(rsrc) : "memory");
+}
+
+// One or two such loads.
+__device__ __forceinline__ void dma1_b128(u32x4_t rsrc, uint32_t m0v, uint32_t v0) {
+  uint32_t saved;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+               "buffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+               "s_mov_b32 m0, %0"
+               : "=&s"(saved) : "s"(m0v), "v"(v0), "s"(rsrc) : "memory");
+}
+__device__ __forceinline__ void dma2_b128(u32x4_t rsrc, uint32_t m0v, uint32_t v0, uint32_t v1) {
+  uint32_t saved;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+               "buffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+               "buffer_load_dwordx4 %3, %4, 0 offen offset:1024 lds\n\t"
+               "s_mov_b32 m0, %0"
+               : "=&s"(saved) : "s"(m0v), "v"(v0), "v"(v1), "s"(rsrc) : "memory");
+}
+
+template <int N> __device__ __forceinline__ void wait_loads() {   // until at most N of this wave's loads are in flight
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+
+// A tile of ROWS rows of D bf16 in LDS, loaded by NW waves straight from global memory. 16-byte chunk c of
+// row r sits in slot c ^ tile_swizzle<D>(r): sixteen successive rows (eight, two to a 256-byte line, at D = 64)
+// put the same chunk into different banks, which serves the b128 reads of rows, and any four aligned rows put
+// a 64-byte piece into four different quarters of the banks, which serves the transposing reads.
+template <int D> __device__ __forceinline__ int tile_swizzle(int r) {
+  return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+template <int D, int ROWS, int NW> struct RowTile {
+  static constexpr int CH = D / 8, RB = D * 2, BYTES = ROWS * RB;
+  static constexpr int KPI = 64 / CH, LOADS = ROWS / KPI / NW;   // rows per 1 KB wave load, loads per wave
+  static_assert(LOADS >= 1 && LOADS <= 8, "");
+  uint32_t off[LOADS];   // global offset of this lane's chunk of load i, less the instruction's own offset
+  uint32_t dst, stride;
+  // (the descriptor starts 4 KB early so that no offset goes negative)
+  __device__ __forceinline__ void init(int wave, int lane, int64_t row_stride) {
+    stride = (uint32_t)(row_stride * 2);
+    dst = (uint32_t)(__builtin_amdgcn_readfirstlane(wave) * LOADS * 1024);
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+      const int row = (wave * LOADS + i) * KPI + lane / CH, slot = lane % CH;
+      off[i] = row * stride + ((slot ^ tile_swizzle<D>(row)) << 4) + 4096u - 1024u * (i & 3);
+    }
+  }
+  // rows: how many of the tile's rows exist (uniform); the others read as zeros
+  __device__ __forceinline__ void load(const u16* base, int rows, uint32_t lds) const {
+    const uint64_t b = (uint64_t)base - 4096;
+    const uint32_t nrec = rows > 0 ? (uint32_t)(min(rows, ROWS) - 1) * stride + RB + 4096u : 0u;
+    const u32x4_t rs = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b),
+                        (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32) & 0xffffu),
+                        (uint32_t)__builtin_amdgcn_readfirstlane(nrec), 0x00020000u};
+    const uint32_t d = lds + dst;
+    if constexpr (LOADS == 1) dma1_b128(rs, d, off[0]);
+    else if constexpr (LOADS == 2) dma2_b128(rs, d, off[0], off[1]);
+    else
+#pragma unroll
+      for (int i = 0; i < LOADS; i += 4) dma4_b128(rs, d + 1024u * i, off[i], off[i + 1], off[i + 2], off[i + 3]);
+  }
+  // 8 elements of row `row`, chunk c
+  static __device__ __forceinline__ bf16x8 read(const char* tile, int row, int c) {
+    return *(const bf16x8*)(tile + row * RB + ((c ^ tile_swizzle<D>(row)) << 4));
+  }
+};
+
+// Four rows k0..k0+3 of one dim each, transposed: lane s of 16 gives the address of 4 dims of row k0 + s / 4 and gets
+// rows k0..k0+3 of dim s of the 16 dims that the group covers.
+__device__ __forceinline__ i16x4 read_tr(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p));
+}
+__device__ __forceinline__ bf16x8 join_tr(i16x4 lo, i16x4 hi) {
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+}  // namespace dit

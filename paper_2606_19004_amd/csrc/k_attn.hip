@@ -39,52 +39,9 @@
 //     contiguous range of (sample, head, query block) tiles, so the query blocks
 //     of one (sample, head) read its K/V through the same L2.
 // fp32 path: the same orientation on the fp32 matrix instruction, 64 queries per workgroup.
-#include "internal.h"
+#include "attn_common.h"
 
 namespace dit {
-
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
-
-// Combine the values of lanes l and l ^ 32 through v_permlane32_swap (a VALU exchange of the two
-// 32-lane halves) instead of an LDS permute. With both operands v, the swap's two results hold, in
-// every lane, v[l] and v[l ^ 32] (which of the two is which depends on the half), so only symmetric
-// combinations are formed from them.
-__device__ __forceinline__ void half_pair(float v, float& a, float& b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  a = __uint_as_float(r[0]);
-  b = __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float pair_max(float v) {
-  float a, b;
-  half_pair(v, a, b);
-  return fmaxf(a, b);
-}
-__device__ __forceinline__ float pair_sum(float v) {
-  float a, b;
-  half_pair(v, a, b);
-  return a + b;
-}
-
-typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
-
-// Four direct-to-LDS loads under one M0 value: destination M0 + 1024 i + 16 lane, global offset
-// v[i] + 1024 i (the instruction offset moves both addresses). Issued back to back they hold the
-// wave's issue for less than four separately issued loads, each of which sets M0 on its own.
-// Inline assembly, so the compiler does not track these loads: the wait before the barrier that
-// hands a stage over is the explicit s_waitcnt(0) of the loop.
-__device__ __forceinline__ void dma4_b128(u32x4_t rsrc, uint32_t m0v, uint32_t v0, uint32_t v1, uint32_t v2,
-                                          uint32_t v3) {
-  uint32_t saved;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
-               "buffer_load_dwordx4 %2, %6, 0 offen lds\n\t"
-               "buffer_load_dwordx4 %3, %6, 0 offen offset:1024 lds\n\t"
-               "buffer_load_dwordx4 %4, %6, 0 offen offset:2048 lds\n\t"
-               "buffer_load_dwordx4 %5, %6, 0 offen offset:3072 lds\n\t"
-               "s_mov_b32 m0, %0"
-               : "=&s"(saved) : "s"(m0v), "v"(v0), "v"(v1), "v"(v2), "v"(v3), "s"(rsrc) : "memory");
-}
 
 template <int D>
 __global__ void __launch_bounds__(256, 2) attn_fwd_bf16(AttnArgs a) {

@@ -1,0 +1,513 @@
+// Attention over packed sequences on gfx950: o = softmax(scale q k^T) v per sequence, with grouped heads and an
+// optional causal mask (the last query of a sequence sees its last key).
+//
+// Rows. The G = heads / kv_heads query heads that share a key/value head are rows of one problem: row r of a
+// sequence of m queries is query r / G, head r % G of the group, r < m G. Keys and values are then read once per
+// tile of rows for the whole group, one new token of G heads is a tile of G rows, and a causal tile of R rows
+// spans only R / G diagonal positions.
+//
+// bf16: flash-style with v_mfma_f32_32x32x16_bf16, 4 waves of 32 rows, 64-key tiles of K and V in two LDS buffers
+// each. Scores are computed transposed (S^T = K Q^T), so that a lane owns one row and its probabilities are
+// operand B of O^T = V^T P^T as they stand; the exponentials of tile t share one instruction stream with the score
+// MFMAs of tile t + 1. Probabilities are rounded to bf16 for the second product (half a step, 2^-9 relative, of each:
+// averaged over the keys it is below the rounding of o itself); sums and maxima stay fp32.
+#include <algorithm>
+
+#include "attn_common.h"
+#include "packed.h"
+
+namespace dit {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float M_FLOOR = -1e37f;   // running maximum of a row that has seen no key: finite, so differences are too
+
+// What a workgroup works on: rows [row0, row0 + rows of the tile) of sequence seq, key/value head g, keys
+// [key0, key1) of the n of the sequence.
+struct PackedTile {
+  int g, seq, rt, part, parts, m, n;
+  int64_t slot;   // of its partial result
+  bool any;
+};
+template <int ROWS>
+__device__ __forceinline__ PackedTile packed_tile(const PackedArgs& a) {
+  PackedTile t{};
+  t.g = blockIdx.x % a.Hkv;
+  const int u = blockIdx.x / a.Hkv;
+  t.slot = (int64_t)t.g * a.units + u;
+  auto parts_of = [&](int i) { return a.part_tiles ? max(cdiv(cdiv(a.keys(i), 64), a.part_tiles), 1) : 1; };
+  int local;
+  t.any = find_unit(a.nseq, u, [&](int i) { return cdiv((int64_t)a.queries(i) * a.G, ROWS) * parts_of(i); }, t.seq, local);
+  if (!t.any) return t;
+  t.m = __builtin_amdgcn_readfirstlane(a.queries(t.seq));
+  t.n = __builtin_amdgcn_readfirstlane(a.keys(t.seq));
+  t.parts = __builtin_amdgcn_readfirstlane(parts_of(t.seq));
+  t.rt = local / t.parts;
+  t.part = local - t.rt * t.parts;
+  if (a.causal) t.rt = cdiv((int64_t)t.m * a.G, ROWS) - 1 - t.rt;   // the rows that see most keys first
+  return t;
+}
+
+template <int D, bool PARTS>
+__global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
+  constexpr int ROWS = 128, KB = 64, NDB = D / 32, NKS = D / 16;
+  constexpr float TAU = 8.f;           // lazy-rescale threshold (log2 units)
+  using Tile = RowTile<D, KB, 4>;
+  constexpr int CH = Tile::CH, RB = Tile::RB, TILE = Tile::BYTES;
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];   // [K0][K1][V0][V1]
+  const PackedTile t = packed_tile<ROWS>(a);
+  if (!t.any) return;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int half = lane >> 5, l32 = lane & 31;
+  const int rows = t.m * a.G, row0 = t.rt * ROWS;
+  const int q0 = a.qr.begin(t.seq);
+  const int64_t k0 = a.kr.begin(t.seq);
+  const u16* Kg = (const u16*)a.k + k0 * a.k_row + (int64_t)t.g * a.k_head;
+  const u16* Vg = (const u16*)a.v + k0 * a.v_row + (int64_t)t.g * a.v_head;
+
+  // this lane's row and its Q fragments: q[row][16 s + 8 half + 0..7]; vis keys are visible to it
+  const int row = min(row0 + wave * 32 + l32, rows - 1);
+  const int tok = row / a.G, head = t.g * a.G + (row - tok * a.G);
+  const int vis = a.causal ? min(tok + t.n - t.m + 1, t.n) : t.n;
+  bf16x8 qf[NKS];
+  {
+    const u16* qrow = (const u16*)a.q + (int64_t)(q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < NKS; s++) qf[s] = *(const bf16x8*)(qrow + 16 * s + 8 * half);
+  }
+  // keys the tile needs: those of its last row; keys every row of this wave sees: those of its first
+  const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
+  const int nvis = a.causal ? min(max(last_tok + t.n - t.m + 1, 0), t.n) : t.n;
+  const int all_vis = __builtin_amdgcn_readfirstlane(vis);
+  int kt0 = 0, nt = cdiv(nvis, KB);
+  if (PARTS) {
+    kt0 = min(t.part * a.part_tiles, nt);
+    nt = min(kt0 + a.part_tiles, nt);
+  }
+
+  Tile tk, tv;
+  tk.init(wave, lane, a.k_row);
+  tv.init(wave, lane, a.v_row);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  auto issue_k = [&](int kt) { tk.load(Kg + (int64_t)kt * KB * a.k_row, t.n - kt * KB, lds0 + (kt & 1) * TILE); };
+  auto issue_v = [&](int kt) { tv.load(Vg + (int64_t)kt * KB * a.v_row, t.n - kt * KB, lds0 + (2 + (kt & 1)) * TILE); };
+
+  // V^T fragment quarters: this lane points at 4 dims of key 4 half + (lane >> 2) % 4 of a step
+  const int vkey = 4 * half + ((lane >> 2) & 3);
+  int vbase[NDB][2];
+#pragma unroll
+  for (int db = 0; db < NDB; db++) {
+    const int ch = 4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+#pragma unroll
+    for (int e = 0; e < 2; e++)   // (the swizzle has period 16, a step's keys)
+      vbase[db][e] = (vkey + 8 * e) * RB + ((ch ^ tile_swizzle<D>(vkey + 8 * e)) << 4) + 8 * (lane & 1);
+  }
+
+  f32x16 o[NDB];
+#pragma unroll
+  for (int i = 0; i < NDB; i++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) o[i][r] = 0.f;
+  const f32x16 zero = {};
+  const float c = a.scale * LOG2E;
+  float m_run = M_FLOOR, l_run = 0.f;
+
+  auto scores = [&](int kt, f32x16* sn) {
+    const char* sk = smem + (kt & 1) * TILE;
+    constexpr int NS = NKS / 4;
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+      bf16x8 kf[NS][KB / 32];
+#pragma unroll
+      for (int s = 0; s < NS; s++)
+#pragma unroll
+        for (int kb = 0; kb < KB / 32; kb++) kf[s][kb] = Tile::read(sk, 32 * kb + l32, 2 * (g * NS + s) + half);
+#pragma unroll
+      for (int s = 0; s < NS; s++)
+#pragma unroll
+        for (int kb = 0; kb < KB / 32; kb++) {
+          const int sg = g * NS + s;
+          sn[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s][kb], qf[sg], sg == 0 ? zero : sn[kb], 0, 0, 0);
+        }
+    }
+  };
+  // hidden keys score -inf; returns this lane's max
+  auto mask_max = [&](int kt, f32x16* sn) {
+    if ((kt + 1) * KB > all_vis) {
+#pragma unroll
+      for (int kb = 0; kb < KB / 32; kb++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) {
+          const int key = kt * KB + 32 * kb + 8 * (r >> 2) + 4 * half + (r & 3);
+          if (key >= vis) sn[kb][r] = -INFINITY;
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KB / 32; kb++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) mx = fmaxf(mx, sn[kb][r]);
+    return mx;
+  };
+  auto step = [&](int kt, f32x16* st, float& mx, f32x16* sn, float& mxn, auto next_c) {
+    constexpr bool NEXT = decltype(next_c)::value;
+    // every wave is done with K buffer kt&1 and V buffer (kt+1)&1; the loads of the buffers read below have landed
+    __syncthreads();
+    if (kt + 2 < nt) issue_k(kt + 2);
+    const char* sv = smem + (2 + (kt & 1)) * TILE;
+    mx = pair_max(mx);
+    const float mxs = mx * c;
+    if (__ballot(mxs > m_run + TAU) != 0) {
+      const float m_new = fmaxf(m_run, mxs);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int i = 0; i < NDB; i++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) o[i][r] *= alpha;
+    }
+    float psum = 0.f;
+    bf16x8 pf[KB / 32][2];
+#pragma unroll
+    for (int kb = 0; kb < KB / 32; kb++)
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(st[kb][8 * h + j], c, -m_run));
+          psum += p;
+          pf[kb][h][j] = (__bf16)p;
+        }
+    if constexpr (NEXT) scores(kt + 1, sn);
+    l_run += psum;
+    if (NEXT) issue_v(kt + 1);
+    // keys 16 q + {4 half + 0..3, 8 + 4 half + 0..3}: the order of the score accumulator
+#pragma unroll
+    for (int q = 0; q < KB / 16; q++) {
+      bf16x8 vf[NDB];
+#pragma unroll
+      for (int db = 0; db < NDB; db++)
+        vf[db] = join_tr(read_tr(sv + 16 * q * RB + vbase[db][0]), read_tr(sv + 16 * q * RB + vbase[db][1]));
+#pragma unroll
+      for (int db = 0; db < NDB; db++)
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[db], pf[q >> 1][q & 1], o[db], 0, 0, 0);
+    }
+    if constexpr (NEXT) mxn = mask_max(kt + 1, sn);
+    __builtin_amdgcn_s_waitcnt(0);
+  };
+
+  if (kt0 < nt) {
+    issue_k(kt0);
+    issue_v(kt0);
+    if (kt0 + 1 < nt) issue_k(kt0 + 1);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    f32x16 sa[KB / 32], sb[KB / 32];
+    float ma, mb = -INFINITY;
+    scores(kt0, sa);
+    ma = mask_max(kt0, sa);
+    int kt = kt0;
+    for (; kt + 2 < nt; kt += 2) {
+      step(kt, sa, ma, sb, mb, std::true_type());
+      step(kt + 1, sb, mb, sa, ma, std::true_type());
+    }
+    if (kt + 1 < nt) {
+      step(kt, sa, ma, sb, mb, std::true_type());
+      step(kt + 1, sb, mb, sa, ma, std::false_type());
+    } else {
+      step(kt, sa, ma, sb, mb, std::false_type());
+    }
+  }
+
+  const float l_all = pair_sum(l_run);
+  const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;   // (a NaN stays one)
+  const float lse = l_all == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_all)) * LN2;
+  const bool real = row0 + wave * 32 + l32 < rows;
+  if (PARTS && t.parts > 1) {
+    const int64_t slot = t.slot * ROWS + wave * 32 + l32;
+    if (real) {
+      if (half == 0) a.part_lse[slot] = lse;
+      float* po = a.part_o + slot * D;
+#pragma unroll
+      for (int db = 0; db < NDB; db++)
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+          *(float4*)(po + 32 * db + 8 * g + 4 * half) = make_float4(o[db][4 * g] * inv, o[db][4 * g + 1] * inv,
+                                                                   o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
+    }
+    return;
+  }
+  if (a.lse && real && half == 0) a.lse[(int64_t)(q0 + tok) * a.H + head] = lse;
+  // The output leaves through the 32 rows of the K buffers that belong to this wave, so that a store writes whole
+  // rows. (Both K buffers were last read before the last step's barrier.)
+  {
+    char* so = smem + wave * 32 * RB;
+#pragma unroll
+    for (int db = 0; db < NDB; db++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        const int ch = 4 * db + g;
+        uint2 u;
+        u.x = pack_bf16x2(o[db][4 * g] * inv, o[db][4 * g + 1] * inv);
+        u.y = pack_bf16x2(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
+        *(uint2*)(so + l32 * RB + ((ch ^ (l32 % CH)) << 4) + 8 * half) = u;
+      }
+    constexpr int RPI = 64 / CH;
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; i++) {
+      const int r = i * RPI + lane / CH, ch = lane % CH;
+      const uint4 v = *(const uint4*)(so + r * RB + ((ch ^ (r % CH)) << 4));
+      const int rr = row0 + wave * 32 + r;
+      if (rr < rows) {
+        const int tk_ = rr / a.G, hd = t.g * a.G + (rr - tk_ * a.G);
+        *(uint4*)((u16*)a.o + (int64_t)(q0 + tk_) * a.o_row + (int64_t)hd * a.o_head + 8 * ch) = v;
+      }
+    }
+  }
+#endif
+}
+
+// ---------------------------------------------------------------------------
+// fp32 on v_mfma_f32_16x16x4_f32 (fp32 operands, products and sums): 4 waves of 16 rows share K/V tiles of 32 keys (16
+// at D = 128), staged through registers one tile ahead; the same transposed orientation, one rescale per tile.
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
+  constexpr int ROWS = 64, KB = D == 64 ? 32 : 16, NKB = KB / 16, LD = D + 4, NDB = D / 16, NKC = D / 16;
+  constexpr int CPT = KB * D / 4 / 256;   // 16-byte chunks of K (and of V) each thread stages per tile
+  __shared__ __attribute__((aligned(16))) float sk[2][KB * LD];
+  __shared__ __attribute__((aligned(16))) float sv[2][KB * LD];
+  const PackedTile t = packed_tile<ROWS>(a);
+  if (!t.any) return;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int l16 = lane & 15, g4 = lane >> 4;
+  const int rows = t.m * a.G, row0 = t.rt * ROWS;
+  const int q0 = a.qr.begin(t.seq);
+  const int64_t k0 = a.kr.begin(t.seq);
+  const float* Kg = (const float*)a.k + k0 * a.k_row + (int64_t)t.g * a.k_head;
+  const float* Vg = (const float*)a.v + k0 * a.v_row + (int64_t)t.g * a.v_head;
+  const int row = min(row0 + wave * 16 + l16, rows - 1);
+  const int tok = row / a.G, head = t.g * a.G + (row - tok * a.G);
+  const int vis = a.causal ? min(tok + t.n - t.m + 1, t.n) : t.n;
+  f32x4 qf[NKC];   // scaled before the products, which may overflow without
+  {
+    const float* qrow = (const float*)a.q + (int64_t)(q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int c = 0; c < NKC; c++) {
+      qf[c] = *(const f32x4*)(qrow + 16 * c + 4 * g4);
+#pragma unroll
+      for (int e = 0; e < 4; e++) qf[c][e] *= a.scale;
+    }
+  }
+  const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
+  const int nvis = a.causal ? min(max(last_tok + t.n - t.m + 1, 0), t.n) : t.n;
+  int kt0 = 0, nt = cdiv(nvis, KB);
+  if (a.part_tiles) {
+    const int per = a.part_tiles * (64 / KB);
+    kt0 = min(t.part * per, nt);
+    nt = min(kt0 + per, nt);
+  }
+  f32x4 rk[CPT], rv[CPT];
+  // rows past the end repeat the last key, whose scores are masked there, with a value of zero
+  auto fetch = [&](int kt) {
+#pragma unroll
+    for (int i = 0; i < CPT; i++) {
+      const int idx = tid + 256 * i, r = min(kt * KB + idx / (D / 4), t.n - 1), c = idx % (D / 4);
+      rk[i] = *(const f32x4*)(Kg + r * a.k_row + 4 * c);
+      rv[i] = *(const f32x4*)(Vg + r * a.v_row + 4 * c);
+    }
+  };
+  auto stage = [&](int kt) {
+    const int buf = kt & 1;
+#pragma unroll
+    for (int i = 0; i < CPT; i++) {
+      const int idx = tid + 256 * i, r = idx / (D / 4), c = idx % (D / 4);
+      *(f32x4*)(&sk[buf][r * LD + 4 * c]) = rk[i];
+      *(f32x4*)(&sv[buf][r * LD + 4 * c]) = kt * KB + r < t.n ? rv[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  f32x4 o[NDB];
+#pragma unroll
+  for (int i = 0; i < NDB; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = M_FLOOR, l_run = 0.f;
+  if (kt0 < nt) {
+    fetch(kt0);
+    stage(kt0);
+  }
+  for (int kt = kt0; kt < nt; kt++) {
+    const int buf = kt & 1;
+    __syncthreads();   // tile kt is staged, and every wave is done with the other buffer
+    if (kt + 1 < nt) fetch(kt + 1);
+    f32x4 s[NKB];
+    {
+      f32x4 kf[NKB][NKC];
+#pragma unroll
+      for (int kb = 0; kb < NKB; kb++)
+#pragma unroll
+        for (int c = 0; c < NKC; c++) kf[kb][c] = *(const f32x4*)(&sk[buf][(16 * kb + l16) * LD + 16 * c + 4 * g4]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kb = 0; kb < NKB; kb++) s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NKC; c++)
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+#pragma unroll
+          for (int kb = 0; kb < NKB; kb++)
+            s[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[kb][c][e], qf[c][e], s[kb], 0, 0, 0);
+    }
+    float vf[NKB][4][NDB];
+#pragma unroll
+    for (int kb = 0; kb < NKB; kb++)
+#pragma unroll
+      for (int r = 0; r < 4; r++)
+#pragma unroll
+        for (int i = 0; i < NDB; i++) vf[kb][r][i] = sv[buf][(16 * kb + 4 * g4 + r) * LD + l16 + 16 * i];
+    __builtin_amdgcn_sched_barrier(0);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < NKB; kb++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) {
+        if (kt * KB + 16 * kb + 4 * g4 + r >= vis) s[kb][r] = -INFINITY;
+        mx = fmaxf(mx, s[kb][r]);
+      }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(m_run, mx);
+    const float alpha = __builtin_amdgcn_exp2f((m_run - m_new) * LOG2E);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int i = 0; i < NDB; i++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) o[i][r] *= alpha;
+    float psum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < NKB; kb++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) {
+        s[kb][r] = __builtin_amdgcn_exp2f((s[kb][r] - m_new) * LOG2E);
+        psum += s[kb][r];
+      }
+    l_run += psum;
+#pragma unroll
+    for (int kb = 0; kb < NKB; kb++)
+#pragma unroll
+      for (int r = 0; r < 4; r++)
+#pragma unroll
+        for (int i = 0; i < NDB; i++) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[kb][r][i], s[kb][r], o[i], 0, 0, 0);
+    if (kt + 1 < nt) stage(kt + 1);
+  }
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (row0 + wave * 16 + l16 >= rows) return;
+  const float inv = l_run > 0.f ? 1.0f / l_run : l_run == 0.f ? 0.f : l_run;
+  const float lse = l_run == 0.f ? -INFINITY : m_run + __builtin_amdgcn_logf(l_run) * LN2;
+  float* orow = (float*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head;
+  float* olse = a.lse ? a.lse + (int64_t)(q0 + tok) * a.H + head : nullptr;
+  if (a.part_tiles && t.parts > 1) {
+    const int64_t slot = t.slot * ROWS + wave * 16 + l16;
+    orow = a.part_o + slot * D;
+    olse = a.part_lse + slot;
+  }
+  if (olse && g4 == 0) *olse = lse;
+#pragma unroll
+  for (int i = 0; i < NDB; i++)   // dims 16 i + 4 g4 + 0..3 of this lane's row
+    *(float4*)(orow + 16 * i + 4 * g4) = make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
+}
+
+// Joins the parts of each row: o = sum_p exp(lse_p - lse) o_p, in the order of the parts. One wave per row.
+template <typename T, int ROWS>
+__global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
+  const int g = blockIdx.x % a.Hkv, u = blockIdx.x / a.Hkv;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int seq, rt;
+  if (!find_unit(a.nseq, u, [&](int i) { return cdiv((int64_t)a.queries(i) * a.G, ROWS); }, seq, rt)) return;
+  auto parts_of = [&](int i) { return max(cdiv(cdiv(a.keys(i), 64), a.part_tiles), 1); };
+  const int parts = parts_of(seq);
+  if (parts <= 1) return;
+  // units before this sequence's
+  int64_t before = 0;
+  for (int i = lane; i < seq; i += 64) before += (int64_t)cdiv((int64_t)a.queries(i) * a.G, ROWS) * parts_of(i);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
+  const int m = a.queries(seq), rows = m * a.G, q0 = a.qr.begin(seq);
+  const int place = a.causal ? cdiv(rows, ROWS) - 1 - rt : rt;   // where the tile stands in the order of the units
+  if (before + (int64_t)(place + 1) * parts > a.units) return;   // (offsets that are not increasing: no such units ran)
+  const int64_t slot = ((int64_t)g * a.units + before + place * parts) * ROWS;
+  for (int r = wave; r < ROWS && rt * ROWS + r < rows; r += 4) {
+    const int row = rt * ROWS + r, tok = row / a.G, head = g * a.G + row - tok * a.G;
+    float top = -INFINITY;
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_lse[slot + (int64_t)p * ROWS + r]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    float total = 0.f, acc0 = 0.f, acc1 = 0.f;
+    if (top > -INFINITY || top != top)
+      for (int p = 0; p < parts; p++) {
+        const int64_t at = slot + (int64_t)p * ROWS + r;
+        const float w = __builtin_amdgcn_exp2f((a.part_lse[at] - top) * LOG2E);
+        total += w;
+        if (w != 0.f) {
+          acc0 = fmaf(w, a.part_o[at * d + lane], acc0);
+          if (d > 64) acc1 = fmaf(w, a.part_o[at * d + 64 + lane], acc1);
+        }
+      }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    T* orow = (T*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head;
+    orow[lane] = from_f32<T>(acc0 * inv);
+    if (d > 64) orow[64 + lane] = from_f32<T>(acc1 * inv);
+    if (a.lse && lane == 0)
+      a.lse[(int64_t)(q0 + tok) * a.H + head] = total == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(total) * LN2;
+  }
+}
+
+// Tiles and parts. Keys are shared out only where the tiles of rows alone leave half of the chip idle (fewer than one
+// workgroup per CU), in parts of at least 4 key tiles, for about two workgroups per CU.
+PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q) {
+  PackedPlan p{};
+  const int G = H / Hkv;
+  p.rows = dtype == DT_BF16 ? 128 : 64;
+  const int64_t per_seq = cdiv((int64_t)max_q * G, p.rows);   // no sequence has more row tiles
+  p.row_tiles = p.units = (int)std::min<int64_t>((int64_t)total_q * G / p.rows + nseq, nseq * per_seq);
+  const int64_t groups = (int64_t)p.row_tiles * Hkv;
+  constexpr int CUS = 256;
+  if (groups == 0 || groups >= CUS) return p;
+  const int64_t tiles = (int64_t)cdiv(total_k, 64);
+  const int64_t per = std::max<int64_t>(4, (tiles * groups + 2 * CUS * (int64_t)nseq - 1) / (2 * CUS * (int64_t)nseq));
+  const int64_t units = per_seq * (tiles / per + nseq);   // a sequence of n tiles has at most n / per + 1 parts
+  if (tiles <= per || units * Hkv > 16 * CUS) return p;
+  p.part_tiles = (int)per;
+  p.units = (int)units;
+  p.ws = (size_t)Hkv * units * p.rows * (d + 1) * 4;
+  return p;
+}
+
+template <int D>
+static void fwd_launch(const PackedArgs& a, int dtype, int64_t grid, hipStream_t s) {
+  if (dtype == DT_F32) packed_fwd_f32<D><<<grid, 256, 0, s>>>(a);
+  else if (a.part_tiles) packed_fwd_bf16<D, true><<<grid, 256, 0, s>>>(a);
+  else packed_fwd_bf16<D, false><<<grid, 256, 0, s>>>(a);
+}
+
+hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s) {
+  const PackedPlan p = packed_plan(dtype, a.nseq, a.H, a.Hkv, d, a.qr.total, total_k, a.max_q);
+  if (p.row_tiles == 0) return hipSuccess;
+  a.part_tiles = p.part_tiles;
+  a.units = p.units;
+  a.row_tiles = p.row_tiles;
+  a.part_o = (float*)ws;
+  a.part_lse = (float*)ws + (int64_t)a.Hkv * p.units * p.rows * d;
+  const int64_t grid = (int64_t)p.units * a.Hkv;
+  if (d == 128) fwd_launch<128>(a, dtype, grid, s);
+  else fwd_launch<64>(a, dtype, grid, s);
+  if (p.part_tiles) {
+    const int64_t jg = (int64_t)p.row_tiles * a.Hkv;
+    if (dtype == DT_BF16) packed_join<u16, 128><<<jg, 256, 0, s>>>(a, d);
+    else packed_join<float, 64><<<jg, 256, 0, s>>>(a, d);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace dit

@@ -1,0 +1,561 @@
+// Gradients of packed attention on gfx950. With s = scale q k^T, p = exp(s - lse) and delta = rowsum(do o),
+//   dv = p^T do,   ds = p (do v^T - delta),   dq = scale ds k,   dk = scale ds^T q.
+//
+// Two kernels recompute p, so that every gradient is summed by one workgroup in a fixed order (no atomics, no
+// partial gradients in memory): one owns query rows and walks the keys (dq: 3 products), one owns keys and walks
+// the query rows of all heads that share them (dk, dv: 4 products). That is 7 products where 5 would do with
+// atomics on dq.
+//
+// bf16, v_mfma_f32_32x32x16_bf16, 4 waves: an owned row (or key) is a column of the score block, so that p and ds
+// of a lane belong to one owned row and are operand B of the next product as they stand, rounded to bf16 (2^-9
+// relative of each term, averaged over the sum). The walked rows are in LDS twice over time, never in two
+// layouts: a tile is read by rows for the scores and by columns (transposing reads) for the gradients.
+#include <algorithm>
+
+#include "attn_common.h"
+#include "packed.h"
+
+namespace dit {
+
+namespace {
+constexpr float LOG2E = 1.4426950408889634f;
+
+// delta[tok][head] = sum_e do o. D / 8 (bf16) or D / 4 lanes per row, 16 bytes each.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) delta_kernel(PackedArgs a) {
+  constexpr int EL = 16 / sizeof(T), LPR = D / EL;
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
+  const int c = threadIdx.x % LPR;
+  if (row >= (int64_t)a.qr.total * a.H) return;
+  const int tok = row / a.H, head = row % a.H;
+  const int64_t at = (int64_t)tok * a.o_row + (int64_t)head * a.o_head + EL * c;
+  const T* x = (const T*)a.o + at;
+  const T* y = (const T*)a.d_o + at;
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < EL; i += 4) {
+    float f[4], g[4];
+    load4<T>(x + i, f);
+    load4<T>(y + i, g);
+#pragma unroll
+    for (int j = 0; j < 4; j++) s = fmaf(f[j], g[j], s);
+  }
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (c == 0) a.delta[row] = s;
+}
+
+// lse in log2 units, or what makes every p of a row without visible keys 0
+__device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
+
+// Address parts of a transposing read of a tile: this lane's 4 dims of dim block db, row 4 half + (lane >> 2) % 4 + 8 e of a step
+template <int D>
+__device__ __forceinline__ void tr_bases(int lane, int (*base)[2]) {
+  const int r = 4 * (lane >> 5) + ((lane >> 2) & 3);
+#pragma unroll
+  for (int db = 0; db < D / 32; db++) {
+    const int ch = 4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+#pragma unroll
+    for (int e = 0; e < 2; e++)
+      base[db][e] = (r + 8 * e) * (2 * D) + ((ch ^ tile_swizzle<D>(r + 8 * e)) << 4) + 8 * (lane & 1);
+  }
+}
+
+// acc[dim][column] of this wave's 32 columns, times f, to rows of bf16 through 32 rows of LDS: store(column, chunk, value)
+template <int D, typename F>
+__device__ __forceinline__ void store_columns(char* so, const f32x16* acc, float f, int lane, F&& store) {
+  constexpr int CH = D / 8, RB = D * 2;
+  const int half = lane >> 5, l32 = lane & 31;
+#pragma unroll
+  for (int db = 0; db < D / 32; db++)
+#pragma unroll
+    for (int g = 0; g < 4; g++) {
+      uint2 u;
+      u.x = pack_bf16x2(acc[db][4 * g] * f, acc[db][4 * g + 1] * f);
+      u.y = pack_bf16x2(acc[db][4 * g + 2] * f, acc[db][4 * g + 3] * f);
+      *(uint2*)(so + l32 * RB + (((4 * db + g) ^ (l32 % CH)) << 4) + 8 * half) = u;
+    }
+  constexpr int RPI = 64 / CH;
+#pragma unroll
+  for (int i = 0; i < 32 / RPI; i++) {
+    const int r = i * RPI + lane / CH, ch = lane % CH;
+    store(r, ch, *(const uint4*)(so + r * RB + ((ch ^ (r % CH)) << 4)));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dq: 128 query rows (row r: query r / G, head r % G of the group) against 64-key tiles
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(256, 2) packed_dq_bf16(PackedArgs a) {
+  constexpr int ROWS = 128, KB = 64, NDB = D / 32, NKS = D / 16;
+  using Tile = RowTile<D, KB, 4>;
+  constexpr int TILE = Tile::BYTES, RB = Tile::RB;
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];   // [K0][K1][V0][V1]
+  const int g = blockIdx.x % a.Hkv;
+  int seq, rt;
+  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv((int64_t)a.queries(i) * a.G, ROWS); }, seq, rt)) return;
+  const int m = __builtin_amdgcn_readfirstlane(a.queries(seq)), n = __builtin_amdgcn_readfirstlane(a.keys(seq));
+  const int rows = m * a.G;
+  if (a.causal) rt = cdiv(rows, ROWS) - 1 - rt;
+  const int row0 = rt * ROWS;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int half = lane >> 5, l32 = lane & 31;
+  const int q0 = a.qr.begin(seq);
+  const int64_t k0 = a.kr.begin(seq);
+  const u16* Kg = (const u16*)a.k + k0 * a.k_row + (int64_t)g * a.k_head;
+  const u16* Vg = (const u16*)a.v + k0 * a.v_row + (int64_t)g * a.v_head;
+  const int row = min(row0 + wave * 32 + l32, rows - 1);
+  const int tok = row / a.G, head = g * a.G + (row - tok * a.G);
+  const int vis = a.causal ? min(tok + n - m + 1, n) : n;
+  bf16x8 qf[NKS], df[NKS];
+  {
+    const u16* qrow = (const u16*)a.q + (int64_t)(q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+    const u16* drow = (const u16*)a.d_o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head;
+#pragma unroll
+    for (int s = 0; s < NKS; s++) {
+      qf[s] = *(const bf16x8*)(qrow + 16 * s + 8 * half);
+      df[s] = *(const bf16x8*)(drow + 16 * s + 8 * half);
+    }
+  }
+  const float lse2 = lse2_of(a.lse[(int64_t)(q0 + tok) * a.H + head]);
+  const float delta = a.delta[(int64_t)(q0 + tok) * a.H + head];
+  const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
+  const int nvis = a.causal ? min(max(last_tok + n - m + 1, 0), n) : n;
+  const int all_vis = __builtin_amdgcn_readfirstlane(vis);
+  const int nt = cdiv(nvis, KB);
+  Tile tk, tv;
+  tk.init(wave, lane, a.k_row);
+  tv.init(wave, lane, a.v_row);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  auto issue = [&](int kt) {
+    tk.load(Kg + (int64_t)kt * KB * a.k_row, n - kt * KB, lds0 + (kt & 1) * TILE);
+    tv.load(Vg + (int64_t)kt * KB * a.v_row, n - kt * KB, lds0 + (2 + (kt & 1)) * TILE);
+  };
+  int kbase[NDB][2];
+  tr_bases<D>(lane, kbase);
+  f32x16 dq[NDB];
+#pragma unroll
+  for (int i = 0; i < NDB; i++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) dq[i][r] = 0.f;
+  const f32x16 zero = {};
+  const float c = a.scale * LOG2E;
+  if (nt > 0) issue(0);
+  for (int kt = 0; kt < nt; kt++) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();   // tile kt has landed, and every wave is done with the other buffers
+    if (kt + 1 < nt) issue(kt + 1);
+    const char* sk = smem + (kt & 1) * TILE;
+    const char* sv = smem + (2 + (kt & 1)) * TILE;
+    const bool mask = (kt + 1) * KB > all_vis;
+#pragma unroll
+    for (int kb = 0; kb < KB / 32; kb++) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int x = 0; x < NKS; x++) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::read(sk, 32 * kb + l32, 2 * x + half), qf[x], x == 0 ? zero : s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::read(sv, 32 * kb + l32, 2 * x + half), df[x], x == 0 ? zero : dp, 0, 0, 0);
+      }
+      if (mask) {
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          if (kt * KB + 32 * kb + 8 * (r >> 2) + 4 * half + (r & 3) >= vis) s[r] = -INFINITY;
+      }
+      bf16x8 ds[2];
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[8 * h + j], c, -lse2));
+          ds[h][j] = (__bf16)(p * (dp[8 * h + j] - delta));
+        }
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int db = 0; db < NDB; db++) {
+          const char* p0 = sk + (32 * kb + 16 * h) * RB;
+          dq[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join_tr(read_tr(p0 + kbase[db][0]), read_tr(p0 + kbase[db][1])),
+                                                           ds[h], dq[db], 0, 0, 0);
+        }
+    }
+  }
+  __syncthreads();   // every wave is done with the K buffers
+  store_columns<D>(smem + wave * 32 * RB, dq, a.scale, lane, [&](int r, int ch, uint4 v) {
+    const int rr = row0 + wave * 32 + r;
+    if (rr < rows) {
+      const int t = rr / a.G, hd = g * a.G + (rr - t * a.G);
+      *(uint4*)((u16*)a.dq + (int64_t)(q0 + t) * a.q_row + (int64_t)hd * a.q_head + 8 * ch) = v;
+    }
+  });
+#endif
+}
+
+// ---------------------------------------------------------------------------
+// dk, dv: 128 keys of one key/value head against 64-query tiles of every head of its group in turn
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
+  constexpr int KEYS = 128, QB = 64, NDB = D / 32, NKS = D / 16;
+  using Tile = RowTile<D, QB, 4>;
+  constexpr int TILE = Tile::BYTES, RB = Tile::RB;
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];   // [Q0][Q1][dO0][dO1]
+  __shared__ float4 stat[2][2][QB / 4];                            // lse (log2 units) and delta of a tile's rows
+  const int g = blockIdx.x % a.Hkv;
+  int seq, kt;
+  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  const int m = __builtin_amdgcn_readfirstlane(a.queries(seq)), n = __builtin_amdgcn_readfirstlane(a.keys(seq));
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int half = lane >> 5, l32 = lane & 31;
+  const int64_t q0 = a.qr.begin(seq), k0 = a.kr.begin(seq);
+  const int key = kt * KEYS + wave * 32 + l32;
+  bf16x8 kf[NKS], vf[NKS];
+  {
+    const int64_t kr = k0 + min(key, n - 1);
+    const u16* krow = (const u16*)a.k + kr * a.k_row + (int64_t)g * a.k_head;
+    const u16* vrow = (const u16*)a.v + kr * a.v_row + (int64_t)g * a.v_head;
+#pragma unroll
+    for (int s = 0; s < NKS; s++) {
+      kf[s] = *(const bf16x8*)(krow + 16 * s + 8 * half);
+      vf[s] = *(const bf16x8*)(vrow + 16 * s + 8 * half);
+    }
+  }
+  // the first query that sees any of the tile's keys; queries from `first` of this lane on see its key
+  const int first = a.causal ? key - (n - m) : 0;
+  const int t0 = a.causal ? min(max(kt * KEYS - (n - m), 0), m) / QB : 0;
+  const int wave_first = a.causal ? kt * KEYS + __builtin_amdgcn_readfirstlane(wave) * 32 + 31 - (n - m) : 0;
+  const int per = cdiv(m, QB) - t0, steps = per * a.G;   // tiles of one head, of all heads
+  Tile tq, td;
+  tq.init(wave, lane, a.q_row);
+  td.init(wave, lane, a.o_row);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  int ih = 0, it = t0;   // head and tile of the next loads
+  float nlse = INFINITY, ndelta = 0.f;
+  auto issue = [&](int i) {
+    const int64_t head = (int64_t)g * a.G + ih;
+    tq.load((const u16*)a.q + (q0 + it * QB) * a.q_row + head * a.q_head, m - it * QB, lds0 + (i & 1) * TILE);
+    td.load((const u16*)a.d_o + (q0 + it * QB) * a.o_row + head * a.o_head, m - it * QB, lds0 + (2 + (i & 1)) * TILE);
+    if (tid < QB) {
+      const int t = it * QB + tid;
+      nlse = INFINITY;   // rows past the end: p = 0
+      ndelta = 0.f;
+      if (t < m) {
+        nlse = lse2_of(a.lse[(q0 + t) * a.H + head]);
+        ndelta = a.delta[(q0 + t) * a.H + head];
+      }
+    }
+    if (++it == t0 + per) {
+      it = t0;
+      ih++;
+    }
+  };
+  auto put_stats = [&](int i) {
+    if (tid < QB) {
+      ((float*)stat[i & 1][0])[tid] = nlse;
+      ((float*)stat[i & 1][1])[tid] = ndelta;
+    }
+  };
+  int base[NDB][2];
+  tr_bases<D>(lane, base);
+  f32x16 dk[NDB], dv[NDB];
+#pragma unroll
+  for (int i = 0; i < NDB; i++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) dk[i][r] = dv[i][r] = 0.f;
+  const f32x16 zero = {};
+  const float c = a.scale * LOG2E;
+  if (steps > 0) {
+    issue(0);
+    put_stats(0);
+  }
+  int ct = t0;
+  for (int i = 0; i < steps; i++) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();   // tile i has landed, and every wave is done with the other buffers
+    if (i + 1 < steps) issue(i + 1);
+    const char* sq = smem + (i & 1) * TILE;
+    const char* sd = smem + (2 + (i & 1)) * TILE;
+#pragma unroll
+    for (int qb = 0; qb < QB / 32; qb++) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int x = 0; x < NKS; x++) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::read(sq, 32 * qb + l32, 2 * x + half), kf[x], x == 0 ? zero : s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::read(sd, 32 * qb + l32, 2 * x + half), vf[x], x == 0 ? zero : dp, 0, 0, 0);
+      }
+      const int r0 = ct * QB + 32 * qb;
+      if (r0 < wave_first) {
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          if (r0 + 8 * (r >> 2) + 4 * half + (r & 3) < first) s[r] = -INFINITY;
+      }
+      bf16x8 pf[2], ds[2];
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int j4 = 0; j4 < 2; j4++) {
+          const float4 l4 = stat[i & 1][0][8 * qb + 4 * h + 2 * j4 + half], d4 = stat[i & 1][1][8 * qb + 4 * h + 2 * j4 + half];
+          const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, de[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            const int x = 8 * h + 4 * j4 + j;
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[x], c, -ls[j]));
+            pf[h][4 * j4 + j] = (__bf16)p;
+            ds[h][4 * j4 + j] = (__bf16)(p * (dp[x] - de[j]));
+          }
+        }
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int db = 0; db < NDB; db++) {
+          const int at = (32 * qb + 16 * h) * RB;
+          dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              join_tr(read_tr(sd + at + base[db][0]), read_tr(sd + at + base[db][1])), pf[h], dv[db], 0, 0, 0);
+          dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              join_tr(read_tr(sq + at + base[db][0]), read_tr(sq + at + base[db][1])), ds[h], dk[db], 0, 0, 0);
+        }
+    }
+    if (i + 1 < steps) put_stats(i + 1);
+    if (++ct == t0 + per) ct = t0;
+  }
+  __syncthreads();
+  auto rows_to = [&](void* dst, int64_t row_stride, int64_t head_stride) {
+    return [=](int r, int ch, uint4 v) {
+      const int kk = kt * KEYS + wave * 32 + r;
+      if (kk < n) *(uint4*)((u16*)dst + (k0 + kk) * row_stride + (int64_t)g * head_stride + 8 * ch) = v;
+    };
+  };
+  store_columns<D>(smem + wave * 32 * RB, dk, a.scale, lane, rows_to(a.dk, a.k_row, a.k_head));
+  store_columns<D>(smem + wave * 32 * RB, dv, 1.f, lane, rows_to(a.dv, a.v_row, a.v_head));
+#endif
+}
+
+// ---------------------------------------------------------------------------
+// fp32, v_mfma_f32_16x16x4_f32: 4 waves own 16 rows (or keys) each and walk tiles of 16 keys (rows) of both
+// operands, staged through registers one tile ahead.
+// ---------------------------------------------------------------------------
+// The walked tile: NROW rows of two tensors
+template <int D> struct WalkF32 {
+  static constexpr int NROW = 16, LD = D + 4, CPT = NROW * D / 4 / 256;
+  f32x4 ra[CPT], rb[CPT];
+  // rows past `left` repeat the last one (their p is 0) with zeros, as 0 times an infinity would be NaN
+  __device__ __forceinline__ void fetch(const float* a, int64_t as, const float* b, int64_t bs, int left) {
+#pragma unroll
+    for (int i = 0; i < CPT; i++) {
+      const int idx = threadIdx.x + 256 * i, r = idx / (D / 4), c = idx % (D / 4), rr = min(r, left - 1);
+      ra[i] = *(const f32x4*)(a + rr * as + 4 * c);
+      rb[i] = *(const f32x4*)(b + rr * bs + 4 * c);
+      if (r >= left) ra[i] = rb[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  __device__ __forceinline__ void stage(float* sa, float* sb) const {
+#pragma unroll
+    for (int i = 0; i < CPT; i++) {
+      const int idx = threadIdx.x + 256 * i, r = idx / (D / 4), c = idx % (D / 4);
+      *(f32x4*)(sa + r * LD + 4 * c) = ra[i];
+      *(f32x4*)(sb + r * LD + 4 * c) = rb[i];
+    }
+  }
+  // [walked row][owned] products of both tensors with the owned fragments
+  static __device__ __forceinline__ f32x4 dot(const float* st, const f32x4* own, int l16, int g4) {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < D / 16; c++) {
+      const f32x4 w = *(const f32x4*)(st + l16 * LD + 16 * c + 4 * g4);
+#pragma unroll
+      for (int e = 0; e < 4; e++) s = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], own[c][e], s, 0, 0, 0);
+    }
+    return s;
+  }
+  // acc[dim][owned] += sum over the walked rows of st[row][dim] w[row][owned]
+  static __device__ __forceinline__ void add(f32x4* acc, const float* st, const f32x4& w, int l16, int g4) {
+#pragma unroll
+    for (int r = 0; r < 4; r++)
+#pragma unroll
+      for (int i = 0; i < D / 16; i++)
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(st[(4 * g4 + r) * LD + l16 + 16 * i], w[r], acc[i], 0, 0, 0);
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(256) packed_dq_f32(PackedArgs a) {
+  constexpr int ROWS = 64, NKC = D / 16;
+  using W = WalkF32<D>;
+  __shared__ __attribute__((aligned(16))) float sk[2][W::NROW * W::LD], sv[2][W::NROW * W::LD];
+  const int g = blockIdx.x % a.Hkv;
+  int seq, rt;
+  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv((int64_t)a.queries(i) * a.G, ROWS); }, seq, rt)) return;
+  const int m = a.queries(seq), n = a.keys(seq), rows = m * a.G;
+  if (a.causal) rt = cdiv(rows, ROWS) - 1 - rt;
+  const int row0 = rt * ROWS, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int64_t q0 = a.qr.begin(seq), k0 = a.kr.begin(seq);
+  const float* Kg = (const float*)a.k + k0 * a.k_row + (int64_t)g * a.k_head;
+  const float* Vg = (const float*)a.v + k0 * a.v_row + (int64_t)g * a.v_head;
+  const int row = min(row0 + wave * 16 + l16, rows - 1);
+  const int tok = row / a.G, head = g * a.G + (row - tok * a.G);
+  const int vis = a.causal ? min(tok + n - m + 1, n) : n;
+  f32x4 qf[NKC], df[NKC];
+  {
+    const float* qrow = (const float*)a.q + (q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+    const float* drow = (const float*)a.d_o + (q0 + tok) * a.o_row + (int64_t)head * a.o_head;
+#pragma unroll
+    for (int c = 0; c < NKC; c++) {
+      qf[c] = *(const f32x4*)(qrow + 16 * c + 4 * g4);
+#pragma unroll
+      for (int e = 0; e < 4; e++) qf[c][e] *= a.scale;
+      df[c] = *(const f32x4*)(drow + 16 * c + 4 * g4);
+    }
+  }
+  const float lse = a.lse[(q0 + tok) * a.H + head], delta = a.delta[(q0 + tok) * a.H + head];
+  const bool none = lse == -INFINITY;
+  const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
+  const int nvis = a.causal ? min(max(last_tok + n - m + 1, 0), n) : n;
+  const int nt = cdiv(nvis, W::NROW);
+  f32x4 dq[NKC];
+#pragma unroll
+  for (int i = 0; i < NKC; i++) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  W w;
+  auto fetch = [&](int kt) {
+    w.fetch(Kg + (int64_t)kt * W::NROW * a.k_row, a.k_row, Vg + (int64_t)kt * W::NROW * a.v_row, a.v_row, n - kt * W::NROW);
+  };
+  if (nt > 0) {
+    fetch(0);
+    w.stage(sk[0], sv[0]);
+  }
+  for (int kt = 0; kt < nt; kt++) {
+    const int buf = kt & 1;
+    __syncthreads();
+    if (kt + 1 < nt) fetch(kt + 1);
+    f32x4 s = W::dot(sk[buf], qf, l16, g4), dp = W::dot(sv[buf], df, l16, g4);
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const bool hidden = none || kt * W::NROW + 4 * g4 + r >= vis;
+      s[r] = hidden ? 0.f : __builtin_amdgcn_exp2f((s[r] - lse) * LOG2E) * (dp[r] - delta);
+    }
+    W::add(dq, sk[buf], s, l16, g4);
+    if (kt + 1 < nt) w.stage(sk[buf ^ 1], sv[buf ^ 1]);
+  }
+  if (row0 + wave * 16 + l16 >= rows) return;
+  float* out = (float*)a.dq + (q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+  for (int i = 0; i < NKC; i++)
+    *(float4*)(out + 16 * i + 4 * g4) = make_float4(dq[i][0] * a.scale, dq[i][1] * a.scale, dq[i][2] * a.scale, dq[i][3] * a.scale);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
+  constexpr int KEYS = 64, NKC = D / 16;
+  using W = WalkF32<D>;
+  __shared__ __attribute__((aligned(16))) float sq[2][W::NROW * W::LD], sd[2][W::NROW * W::LD];
+  const int g = blockIdx.x % a.Hkv;
+  int seq, kt;
+  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  const int m = a.queries(seq), n = a.keys(seq);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int64_t q0 = a.qr.begin(seq), k0 = a.kr.begin(seq);
+  const int key = kt * KEYS + wave * 16 + l16;
+  f32x4 kf[NKC], vf[NKC];
+  {
+    const int64_t kr = k0 + min(key, n - 1);
+    const float* krow = (const float*)a.k + kr * a.k_row + (int64_t)g * a.k_head;
+    const float* vrow = (const float*)a.v + kr * a.v_row + (int64_t)g * a.v_head;
+#pragma unroll
+    for (int c = 0; c < NKC; c++) {
+      kf[c] = *(const f32x4*)(krow + 16 * c + 4 * g4);
+#pragma unroll
+      for (int e = 0; e < 4; e++) kf[c][e] *= a.scale;
+      vf[c] = *(const f32x4*)(vrow + 16 * c + 4 * g4);
+    }
+  }
+  const int first = a.causal ? key - (n - m) : 0;
+  const int t0 = a.causal ? min(max(kt * KEYS - (n - m), 0), m) / W::NROW : 0;
+  const int per = cdiv(m, W::NROW) - t0;
+  f32x4 dk[NKC], dv[NKC];
+#pragma unroll
+  for (int i = 0; i < NKC; i++) dk[i] = dv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  W w;
+  auto fetch = [&](int h, int t) {
+    const int64_t head = (int64_t)g * a.G + h, at = q0 + t * W::NROW;
+    w.fetch((const float*)a.q + at * a.q_row + head * a.q_head, a.q_row,
+            (const float*)a.d_o + at * a.o_row + head * a.o_head, a.o_row, m - t * W::NROW);
+  };
+  int h = 0, t = t0;
+  if (per > 0) {
+    fetch(0, t0);
+    w.stage(sq[0], sd[0]);
+  }
+  for (int i = 0; i < per * a.G; i++) {
+    const int buf = i & 1;
+    __syncthreads();
+    const int nh = t + 1 == t0 + per ? h + 1 : h, nt = t + 1 == t0 + per ? t0 : t + 1;
+    if (i + 1 < per * a.G) fetch(nh, nt);
+    f32x4 s = W::dot(sq[buf], kf, l16, g4), dp = W::dot(sd[buf], vf, l16, g4);
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      const int tok = t * W::NROW + 4 * g4 + r;
+      const int64_t at = (q0 + min(tok, m - 1)) * a.H + (int64_t)g * a.G + h;
+      const float lse = a.lse[at];
+      const bool hidden = tok >= m || tok < first || lse == -INFINITY;
+      s[r] = hidden ? 0.f : __builtin_amdgcn_exp2f((s[r] - lse) * LOG2E);
+      dp[r] = hidden ? 0.f : s[r] * (dp[r] - a.delta[at]);
+    }
+    W::add(dv, sd[buf], s, l16, g4);
+    W::add(dk, sq[buf], dp, l16, g4);
+    if (i + 1 < per * a.G) w.stage(sq[buf ^ 1], sd[buf ^ 1]);
+    h = nh;
+    t = nt;
+  }
+  if (key >= n) return;
+  float* ok = (float*)a.dk + (k0 + key) * a.k_row + (int64_t)g * a.k_head;
+  float* ov = (float*)a.dv + (k0 + key) * a.v_row + (int64_t)g * a.v_head;
+#pragma unroll
+  for (int i = 0; i < NKC; i++) {
+    *(float4*)(ok + 16 * i + 4 * g4) = make_float4(dk[i][0] * a.scale, dk[i][1] * a.scale, dk[i][2] * a.scale, dk[i][3] * a.scale);
+    *(float4*)(ov + 16 * i + 4 * g4) = make_float4(dv[i][0], dv[i][1], dv[i][2], dv[i][3]);
+  }
+}
+
+}  // namespace
+
+// row sums of do o
+size_t packed_backward_ws(int nseq, int H, int total_q) { return (size_t)total_q * H * 4; }
+
+hipError_t packed_attention_delta(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
+  a.delta = (float*)ws;
+  const int64_t lanes = (int64_t)a.qr.total * a.H * (d * (dtype == DT_BF16 ? 2 : 4) / 16);
+  const int64_t grid = (lanes + 255) / 256;
+  if (grid == 0) return hipSuccess;
+  if (dtype == DT_BF16 && d == 128) delta_kernel<u16, 128><<<grid, 256, 0, s>>>(a);
+  else if (dtype == DT_BF16) delta_kernel<u16, 64><<<grid, 256, 0, s>>>(a);
+  else if (d == 128) delta_kernel<float, 128><<<grid, 256, 0, s>>>(a);
+  else delta_kernel<float, 64><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s) {
+  a.delta = (float*)ws;
+  const int keys = dtype == DT_BF16 ? 128 : 64;
+  const int64_t grid = ((int64_t)total_k / keys + a.nseq) * a.Hkv;
+  if (total_k == 0) return hipSuccess;
+  if (dtype == DT_BF16 && d == 128) packed_dkdv_bf16<128><<<grid, 256, 0, s>>>(a);
+  else if (dtype == DT_BF16) packed_dkdv_bf16<64><<<grid, 256, 0, s>>>(a);
+  else if (d == 128) packed_dkdv_f32<128><<<grid, 256, 0, s>>>(a);
+  else packed_dkdv_f32<64><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t packed_attention_dq(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
+  a.delta = (float*)ws;
+  const int rows = dtype == DT_BF16 ? 128 : 64;
+  const int64_t grid = std::min<int64_t>((int64_t)a.qr.total * a.G / rows + a.nseq, (int64_t)a.nseq * cdiv((int64_t)a.max_q * a.G, rows)) * a.Hkv;
+  if (grid == 0) return hipSuccess;
+  if (dtype == DT_BF16 && d == 128) packed_dq_bf16<128><<<grid, 256, 0, s>>>(a);
+  else if (dtype == DT_BF16) packed_dq_bf16<64><<<grid, 256, 0, s>>>(a);
+  else if (d == 128) packed_dq_f32<128><<<grid, 256, 0, s>>>(a);
+  else packed_dq_f32<64><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace dit

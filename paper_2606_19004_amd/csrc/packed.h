@@ -1,0 +1,119 @@
+// Packed sequences and the operands of the kernels that work on them (device side), and the entry points
+// of k_packed_attn.hip, k_packed_attn_bwd.hip, k_gated_norm.hip and k_policy_loss.hip.
+#pragma once
+#include "internal.h"
+
+namespace dit {
+
+// Rows of the sequences of a packed tensor: offsets on the device, or equal lengths (off null).
+struct PackedRows {
+  const int* off;
+  int total, len;   // rows of the tensor; of each sequence where off is null
+  __device__ __forceinline__ int begin(int i) const { return off ? min(max(off[i], 0), total) : i * len; }
+  __device__ __forceinline__ int count(int i) const {
+    if (!off) return len;
+    const int b = min(max(off[i], 0), total);
+    return max(min(off[i + 1], total), b) - b;
+  }
+};
+
+struct PackedArgs {
+  const void* q; const void* k; const void* v; void* o;
+  float* lse;                       // [total_q][H], null: not wanted (forward)
+  PackedRows qr, kr;
+  const int* k_len;                 // or null
+  int nseq, H, Hkv, G, max_q, causal;
+  float scale;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+  // long keys shared out in parts of part_tiles 64-key tiles (0: one part), whose results meet in the workspace
+  int part_tiles, units;            // units: upper bound on (sequence, row tile, part) per key/value head
+  float* part_o; float* part_lse;   // [Hkv * units][row tile][d], [Hkv * units][row tile]
+  int row_tiles;                    // upper bound on (sequence, row tile) per key/value head
+  // backward
+  const void* d_o; void* dq; void* dk; void* dv;
+  float* delta;                     // [total_q][H] rowsum(d_o o)
+  int key_tiles;                    // upper bound on (sequence, key tile)
+  __device__ __forceinline__ int queries(int i) const { return min(qr.count(i), max_q); }
+  __device__ __forceinline__ int keys(int i) const {
+    const int c = kr.count(i);
+    return k_len ? min(max(k_len[i], 0), c) : c;
+  }
+};
+
+// The sequence that unit u belongs to, where sequence i has count(i) units, and u's place in it. Every wave finds it by
+// itself, 64 sequences at a time: no host-made list of tiles, no empty workgroups where lengths are unlike.
+template <typename F>
+__device__ __forceinline__ bool find_unit(int nseq, int u, F&& count, int& seq, int& local) {
+  const int lane = threadIdx.x & 63;
+  unsigned carry = 0;   // <= u
+  for (int base = 0; base < nseq; base += 64) {
+    // (no count of a tensor within the entry points' limits is larger, and 64 of these fit)
+    const unsigned c = base + lane < nseq ? min(count(base + lane), 1 << 25) : 0;
+    unsigned incl = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const unsigned up = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += up;
+    }
+    const unsigned total = __builtin_amdgcn_readlane(incl, 63);
+    if ((unsigned)u < carry + total) {
+      const int l = __builtin_ctzll(__ballot(carry + incl > (unsigned)u));
+      seq = base + l;
+      local = u - (int)(carry + __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l));
+      return true;
+    }
+    carry += total;
+  }
+  return false;
+}
+
+// How a call runs (host): see packed_plan in k_packed_attn.hip
+struct PackedPlan {
+  int rows;         // query rows of a workgroup's tile
+  int part_tiles;   // 64-key tiles of a part, 0: keys are not shared out
+  int row_tiles, units;
+  size_t ws;        // bytes
+};
+PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q);
+hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s);
+size_t packed_backward_ws(int nseq, int H, int total_q);
+hipError_t packed_attention_delta(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
+hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s);
+hipError_t packed_attention_dq(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
+
+enum NormKind { NORM_NONE = 0, NORM_LAYER = 1, NORM_RMS = 2 };
+struct GatedNormArgs {
+  const void* x; const void* y; const void* post_w; const void* pre_w;
+  const float* gate; const float* scale; const float* shift;
+  PackedRows pr;
+  int nseq, rows, D, post, pre;
+  float eps, alpha;
+  int64_t x_row, y_row, h_row, mod_row;
+  void* x_out; void* h;
+  // backward (x is the forward's x_out)
+  const void* dx_out; const void* dh; void* dx; void* dy;
+  float* dgate; float* dscale; float* dshift; float* dpost_w; float* dpre_w;
+  float* parts;   // [chunks][3][D] column sums of the row chunks
+  int chunks;     // upper bound on (sequence, chunk)
+};
+hipError_t gated_norm_fwd(const GatedNormArgs& a, int dtype, hipStream_t s);
+int gated_norm_chunks(int nseq, int rows);   // row chunks of the backward pass, at most
+size_t gated_norm_ws(int nseq, int rows, int D);
+hipError_t gated_norm_rows_bwd(const GatedNormArgs& a, int dtype, hipStream_t s);
+hipError_t gated_norm_columns_bwd(const GatedNormArgs& a, int dtype, hipStream_t s);
+
+struct PolicyLossArgs {
+  const float* x; const float* v; const float* xn; const float* v_ref;
+  int batch; int64_t n;
+  double cx, cv, var, cst;   // mean = cx x + cv v; cst: the constant of logp
+  const double* logp_old; const float* adv;
+  double logp_scale, clip_low, clip_high, kl_weight;
+  double* loss; double* logp; double* ratio; float* dv;
+  double* parts;   // [batch][chunks][2] sums of (x_next - mean)^2 and (v - v_ref)^2
+  int chunks;
+};
+int policy_loss_chunks(int batch, int64_t n);
+hipError_t policy_loss_sums(const PolicyLossArgs& a, hipStream_t s);
+hipError_t policy_loss_finish(const PolicyLossArgs& a, hipStream_t s);
+
+}  // namespace dit

@@ -1,4 +1,4 @@
-"""Thin Python binding of libditstep.so (include/ditstep.h).
+"""Thin Python binding of libditstep.so (include/ditstep.h, include/ditpolicy.h).
 
 Argument marshalling only: every function takes torch tensors that already
 live on the GPU, passes their device pointers, sizes and the current HIP
@@ -30,7 +30,10 @@ EXPORTS = ("dit_abi_version", "dit_status_string", "dit_last_error_message", "di
            "dit_block_forward", "dit_block_mlp", "joint_attention", "flow_step", "flow_logprob", "group_reward_stats",
            "group_reward_stats_async", "dit_timestep_embed", "dit_timestep_embed_noalloc", "dit_patch_embed", "dit_final_layer", "dit_denoise_workspace_bytes",
            "dit_denoise_step", "dit_profile_begin", "dit_profile_end", "dit_teacache_init", "dit_teacache_gate",
-           "dit_teacache_cache_bytes", "dit_denoise_step_teacache")
+           "dit_teacache_cache_bytes", "dit_denoise_step_teacache",
+           "packed_attention_workspace_bytes", "packed_attention", "packed_attention_backward_workspace_bytes",
+           "packed_attention_backward", "gated_norm", "gated_norm_backward_workspace_bytes", "gated_norm_backward",
+           "flow_policy_loss_workspace_bytes", "flow_policy_loss")
 
 
 class DitError(RuntimeError):
@@ -62,6 +65,18 @@ class StepWeights(C.Structure):
 class TeaCacheState(C.Structure):
     _fields_ = [("threshold", C.c_double), ("n_coef", C.c_int32), ("coef", C.c_double * 8),
                 ("accumulated", C.c_double), ("has_prev", C.c_int32), ("has_residual", C.c_int32)]
+
+
+class PackedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("sequences", "heads", "kv_heads", "head_dim", "total_q", "total_k", "max_q",
+                                         "causal", "dtype")] + [("scale", C.c_float)] + [
+        (n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "o_row", "o_head")]
+
+
+class GatedNormConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("sequences", "rows", "hidden", "dtype", "post_norm", "pre_norm")] + [
+        ("eps", C.c_float), ("residual_scale", C.c_float)] + [
+        (n, C.c_int64) for n in ("x_row", "y_row", "h_row", "mod_row")]
 
 
 class KernelStat(C.Structure):
@@ -101,6 +116,16 @@ _sigs = {
                                    _i32, _i32, _f32, _f32, _f32, _vp, _vp, _vp, _vp, C.POINTER(TeaCacheState), _i32,
                                    _vp, _sz, C.POINTER(_i32), C.POINTER(C.c_double), _vp, _sz, _stream], _i32),
     "dit_profile_end": ([C.POINTER(KernelStat), _i32, C.POINTER(_i32)], _i32),
+    "packed_attention_workspace_bytes": ([C.POINTER(PackedConfig)], _sz),
+    "packed_attention": ([C.POINTER(PackedConfig)] + [_vp] * 9 + [_sz, _stream], _i32),
+    "packed_attention_backward_workspace_bytes": ([C.POINTER(PackedConfig)], _sz),
+    "packed_attention_backward": ([C.POINTER(PackedConfig)] + [_vp] * 13 + [_sz, _stream], _i32),
+    "gated_norm": ([C.POINTER(GatedNormConfig)] + [_vp] * 10 + [_stream], _i32),
+    "gated_norm_backward_workspace_bytes": ([C.POINTER(GatedNormConfig)], _sz),
+    "gated_norm_backward": ([C.POINTER(GatedNormConfig)] + [_vp] * 17 + [_sz, _stream], _i32),
+    "flow_policy_loss_workspace_bytes": ([_i32, _i64], _sz),
+    "flow_policy_loss": ([_vp, _vp, _vp, _vp, _i32, _i64, _f32, _f32, _f32, _vp, _vp, C.c_double, C.c_double,
+                          C.c_double, C.c_double, _vp, _vp, _vp, _vp, _vp, _sz, _stream], _i32),
 }
 for _name, (_args, _res) in _sigs.items():
     _fn = getattr(_lib, _name)
@@ -281,6 +306,104 @@ def dit_denoise_step_teacache(cfg, sw, blocks, t, t_next, noise_level, latent, x
                                           cache.numel(), C.byref(ran), C.byref(rel), _ptr(ws), ws.numel(),
                                           _s(stream)))
     return bool(ran.value), rel.value
+
+
+# ---------------------------------------------------------------------------
+# policy update (include/ditpolicy.h)
+# ---------------------------------------------------------------------------
+NORM_KINDS = {"none": 0, "layer": 1, "rms": 2}
+
+
+def _ws_args(ws):
+    return (_ptr(ws), ws.numel() if ws is not None else 0)
+
+
+def packed_config(q, k, v, o, sequences, causal=False, scale=None, max_q=0) -> PackedConfig:
+    """Shapes and strides of q, o [rows][heads][d] and k, v [rows][kv_heads][d] (views are fine, e contiguous).
+    max_q: no sequence has more queries (0: not known)."""
+    for t in (q, k, v, o):
+        if t.dim() != 3 or (t.numel() and t.stride(2) != 1):
+            raise ValueError("q, k, v and o are [rows][heads][head_dim] with the last index contiguous")
+        if t.dtype != q.dtype or t.shape[2] != q.shape[2]:
+            raise ValueError("q, k, v and o have one type and one head_dim")
+    if k.shape != v.shape or o.shape != q.shape:
+        raise ValueError("k and v, and q and o, have one shape")
+    d = q.shape[2]
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    strides = [s for t in (q, k, v, o) for s in (t.stride(0), t.stride(1))]
+    return PackedConfig(sequences, q.shape[1], k.shape[1], d, q.shape[0], k.shape[0], max_q, int(bool(causal)),
+                        _dtype_code(q.dtype), scale, *strides)
+
+
+def packed_attention_workspace_bytes(cfg) -> int:
+    return _lib.packed_attention_workspace_bytes(C.byref(cfg))
+
+
+def packed_attention(cfg, q, k, v, o, lse=None, q_offsets=None, k_offsets=None, k_lengths=None, ws=None, stream=None):
+    """Tensors laid out as those cfg was made from; offsets and lengths: device int32, or None (equal lengths)."""
+    _check(_lib.packed_attention(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(q_offsets), _ptr(k_offsets),
+                                 _ptr(k_lengths), _ptr(o), _ptr(lse), *_ws_args(ws), _s(stream)))
+
+
+def packed_attention_backward_workspace_bytes(cfg) -> int:
+    return _lib.packed_attention_backward_workspace_bytes(C.byref(cfg))
+
+
+def packed_attention_backward(cfg, q, k, v, o, lse, d_o, dq, dk, dv, q_offsets=None, k_offsets=None, k_lengths=None,
+                              ws=None, stream=None):
+    """d_o laid out like o, dq, dk, dv like q, k, v."""
+    _check(_lib.packed_attention_backward(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o),
+                                          _ptr(q_offsets), _ptr(k_offsets), _ptr(k_lengths), _ptr(dq), _ptr(dk),
+                                          _ptr(dv), *_ws_args(ws), _s(stream)))
+
+
+def gated_norm_config(x, sequences, post="none", pre="layer", eps=1e-6, residual_scale=1.0, y_row=None, h_row=None,
+                      mod_row=None) -> GatedNormConfig:
+    """x [rows][hidden] (a row stride is fine); row strides of y and h are x's, that of gate, scale and shift is hidden, unless given."""
+    if x.dim() != 2 or (x.numel() and x.stride(1) != 1):
+        raise ValueError("x is [rows][hidden] with the last index contiguous")
+    rows, hidden = x.shape
+    row = x.stride(0) if rows > 1 else max(x.stride(0), hidden)
+    return GatedNormConfig(sequences, rows, hidden, _dtype_code(x.dtype), NORM_KINDS[post], NORM_KINDS[pre], eps,
+                           residual_scale, row, row if y_row is None else y_row, row if h_row is None else h_row,
+                           hidden if mod_row is None else mod_row)
+
+
+def gated_norm(cfg, x, y, x_out, h, gate=None, scale=None, shift=None, post_w=None, pre_w=None, offsets=None,
+               stream=None):
+    _check(_lib.gated_norm(C.byref(cfg), _ptr(x), _ptr(y), _ptr(post_w), _ptr(pre_w), _ptr(gate), _ptr(scale),
+                           _ptr(shift), _ptr(offsets), _ptr(x_out), _ptr(h), _s(stream)))
+
+
+def gated_norm_backward_workspace_bytes(cfg) -> int:
+    return _lib.gated_norm_backward_workspace_bytes(C.byref(cfg))
+
+
+def gated_norm_backward(cfg, x_out, y, dx_out, dh, dx, dy, gate=None, scale=None, post_w=None, pre_w=None, offsets=None,
+                        dgate=None, dscale=None, dshift=None, dpost_w=None, dpre_w=None, ws=None, stream=None):
+    """x_out: the forward call's output. Any gradient may be None."""
+    _check(_lib.gated_norm_backward(C.byref(cfg), _ptr(x_out), _ptr(y), _ptr(post_w), _ptr(pre_w), _ptr(gate),
+                                    _ptr(scale), _ptr(offsets), _ptr(dx_out), _ptr(dh), _ptr(dx), _ptr(dy),
+                                    _ptr(dgate), _ptr(dscale), _ptr(dshift), _ptr(dpost_w), _ptr(dpre_w),
+                                    *_ws_args(ws), _s(stream)))
+
+
+def flow_policy_loss_workspace_bytes(batch, n_per_sample) -> int:
+    return _lib.flow_policy_loss_workspace_bytes(batch, n_per_sample)
+
+
+def flow_policy_loss(x, v, x_next, logp_old, adv, t, t_next, noise_level, loss, dv=None, logp=None, ratio=None,
+                     v_ref=None, logp_scale=None, clip_low=0.2, clip_high=0.2, kl_weight=0.0, ws=None, stream=None):
+    """x, v, x_next, v_ref, dv: [batch][n] fp32 (any trailing shape); logp_old, logp, ratio: [batch] fp64; adv: [batch]
+    fp32; loss: one fp64. logp_scale None: 1 / n."""
+    b = x.shape[0] if x.dim() > 0 else 0
+    n = x.numel() // b if b else 0
+    if logp_scale is None:
+        logp_scale = 1.0 / max(n, 1)
+    _check(_lib.flow_policy_loss(_ptr(x), _ptr(v), _ptr(x_next), _ptr(v_ref), b, n, t, t_next, noise_level,
+                                 _ptr(logp_old), _ptr(adv), logp_scale, clip_low, clip_high, kl_weight, _ptr(loss),
+                                 _ptr(logp), _ptr(ratio), _ptr(dv), *_ws_args(ws), _s(stream)))
 
 
 def dit_profile_begin():

@@ -1,0 +1,128 @@
+"""What the policy-update entry points refuse before any launch, and their workspace sizes (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+from paper_2606_19004_amd import ditstep as d
+
+lib = d.lib()
+INVALID, SHAPE, DOMAIN, UNSUPPORTED, WORKSPACE = 1, 2, 3, 5, 7
+A = 1 << 20      # a 16-byte aligned stand-in for a device pointer: every call here fails before it is used
+
+
+def packed(**kw):
+    f = dict(sequences=2, heads=4, kv_heads=2, head_dim=64, total_q=100, total_k=100, max_q=0, causal=1, dtype=1, scale=0.125,
+             q_row=512, q_head=64, k_row=512, k_head=64, v_row=512, v_head=64, o_row=256, o_head=64)
+    f.update(kw)
+    return d.PackedConfig(*[f[n] for n, _ in d.PackedConfig._fields_])
+
+
+def forward(cfg, q=A, k=A, v=A, q_off=A, k_off=A, k_len=None, o=A, lse=A, ws=None, n=0):
+    return lib.packed_attention(C.byref(cfg) if cfg else None, q, k, v, q_off, k_off, k_len, o, lse, ws, n, None)
+
+
+def backward(cfg, q=A, k=A, v=A, o=A, lse=A, do=A, q_off=A, k_off=A, k_len=None, dq=A, dk=A, dv=A, ws=A, n=1 << 30):
+    return lib.packed_attention_backward(C.byref(cfg), q, k, v, o, lse, do, q_off, k_off, k_len, dq, dk, dv, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=2), INVALID), (dict(sequences=-1), INVALID), (dict(total_q=-1), INVALID), (dict(max_q=-1), INVALID),
+    (dict(heads=5), SHAPE), (dict(kv_heads=0), SHAPE), (dict(heads=0), SHAPE), (dict(head_dim=96), UNSUPPORTED),
+    (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID),
+    (dict(q_row=63), INVALID), (dict(k_row=-512), INVALID), (dict(v_head=-64), INVALID), (dict(q_row=513), INVALID),
+    (dict(k_row=1 << 24), UNSUPPORTED), (dict(o_head=32), INVALID), (dict(o_row=192), INVALID), (dict(o_head=0), INVALID),
+    (dict(total_q=1 << 28), UNSUPPORTED), (dict(sequences=1 << 21), UNSUPPORTED)])
+def test_packed_config(kw, status):
+    cfg = packed(**kw)
+    assert forward(cfg, ws=A, n=1 << 40) == status
+    assert d.packed_attention_workspace_bytes(cfg) == 0 and d.packed_attention_backward_workspace_bytes(cfg) == 0
+
+
+def test_packed_calls():
+    assert forward(None) == INVALID
+    cfg = packed()
+    for kw in (dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(q=A + 8), dict(v=A + 2), dict(q_off=A + 2), dict(lse=A + 1)):
+        assert forward(cfg, ws=A, n=1 << 40, **kw) == INVALID, kw
+    assert forward(packed(total_q=101), q_off=None, ws=A, n=1 << 40) == SHAPE
+    assert forward(packed(total_k=99), k_off=None, ws=A, n=1 << 40) == SHAPE
+    assert forward(packed(max_q=49), q_off=None, ws=A, n=1 << 40) == SHAPE
+    assert forward(packed(sequences=0)) == 0 and forward(packed(total_q=0)) == 0
+    few = packed(sequences=2, total_q=2, max_q=1, total_k=40000)      # keys are shared out: scratch is needed
+    need = d.packed_attention_workspace_bytes(few)
+    assert need > 0
+    for kw in (dict(ws=None, n=need), dict(ws=A, n=need - 1), dict(ws=A + 16, n=need)):
+        assert forward(few, **kw) == WORKSPACE, kw
+    for kw in (dict(q=None), dict(lse=None), dict(do=None), dict(dk=None), dict(dq=A + 8)):
+        assert backward(cfg, **kw) == INVALID, kw
+    assert backward(cfg, ws=None) == WORKSPACE and backward(cfg, n=100 * 4 * 4 - 1) == WORKSPACE
+    # inputs may repeat a head (stride 0), gradients may not
+    assert backward(packed(k_head=0)) == INVALID and b"overlap" in lib.dit_last_error_message()
+    assert backward(packed(sequences=0)) == 0
+
+
+def norm_cfg(**kw):
+    f = dict(sequences=2, rows=10, hidden=64, dtype=1, post_norm=2, pre_norm=1, eps=1e-6, residual_scale=1.0, x_row=64, y_row=64,
+             h_row=64, mod_row=64)
+    f.update(kw)
+    return d.GatedNormConfig(*[f[n] for n, _ in d.GatedNormConfig._fields_])
+
+
+def norm(cfg, x=A, y=A, pw=None, rw=None, gate=None, scale=None, shift=None, off=A, xo=A, h=A):
+    return lib.gated_norm(C.byref(cfg) if cfg else None, x, y, pw, rw, gate, scale, shift, off, xo, h, None)
+
+
+def norm_back(cfg, xo=A, y=A, pw=None, rw=None, gate=None, scale=None, off=A, dxo=A, dh=A, dx=A, dy=A, dg=None, ds=None, dt=None,
+              dpw=None, drw=None, ws=A, n=1 << 30):
+    return lib.gated_norm_backward(C.byref(cfg), xo, y, pw, rw, gate, scale, off, dxo, dh, dx, dy, dg, ds, dt, dpw, drw, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=3), INVALID), (dict(rows=-1), INVALID), (dict(sequences=0), SHAPE), (dict(hidden=0), SHAPE), (dict(hidden=8193, x_row=9000), UNSUPPORTED),
+    (dict(post_norm=3), INVALID), (dict(pre_norm=-1), INVALID), (dict(eps=0.0), INVALID), (dict(eps=float("nan")), INVALID),
+    (dict(residual_scale=float("inf")), INVALID), (dict(x_row=63), INVALID), (dict(mod_row=0), INVALID), (dict(sequences=1 << 20), UNSUPPORTED)])
+def test_gated_norm_config(kw, status):
+    assert norm(norm_cfg(**kw)) == status
+    assert norm_back(norm_cfg(**kw)) == status
+    assert d.gated_norm_backward_workspace_bytes(norm_cfg(**kw)) == 0
+
+
+def test_gated_norm_calls():
+    assert norm(None) == INVALID
+    c = norm_cfg()
+    assert norm(c, x=None) == INVALID and norm(c, x=A + 1) == INVALID and norm(c, shift=A + 2) == INVALID
+    assert norm(norm_cfg(rows=11), off=None) == SHAPE
+    assert norm(norm_cfg(rows=0, sequences=0)) == 0 and norm(c, xo=None, h=None) == 0
+    assert norm_back(c, xo=None) == INVALID
+    for kw in (dict(dy=A), dict(dg=A), dict(dpw=A)):
+        assert norm_back(c, y=None, **{"dy": None, **kw}) == INVALID, kw
+    assert norm_back(c, dt=A, ws=None) == WORKSPACE
+    assert norm_back(c, dx=None, dy=None) == 0
+    assert d.gated_norm_backward_workspace_bytes(c) > 0
+
+
+def loss(B=2, n=8, x=A, v=A, xn=A, ref=None, t=0.6, tn=0.5, lvl=0.7, old=A, adv=A, sc=1.0, lo=0.2, hi=0.2, kl=0.0, out=A, dv=A, ws=A,
+         nb=1 << 20):
+    return lib.flow_policy_loss(x, v, xn, ref, B, n, t, tn, lvl, old, adv, sc, lo, hi, kl, out, None, None, dv, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(B=-1), INVALID), (dict(n=-1), INVALID), (dict(x=None), INVALID), (dict(old=None), INVALID), (dict(adv=None), INVALID),
+    (dict(out=None, dv=None), INVALID), (dict(dv=A + 2), INVALID), (dict(old=A + 4), INVALID), (dict(t=1.0), DOMAIN), (dict(t=0.0), DOMAIN),
+    (dict(tn=0.6), DOMAIN), (dict(lvl=0.0), DOMAIN), (dict(lvl=float("nan")), DOMAIN), (dict(sc=0.0), DOMAIN), (dict(sc=float("inf")), DOMAIN),
+    (dict(lo=-0.1), DOMAIN), (dict(lo=1.5), DOMAIN), (dict(hi=-0.1), DOMAIN), (dict(kl=-1.0), DOMAIN), (dict(kl=float("nan")), DOMAIN),
+    (dict(ws=None), WORKSPACE), (dict(nb=15), WORKSPACE), (dict(B=0), 0), (dict(n=0), 0)])
+def test_policy_loss_calls(kw, status):
+    assert loss(**kw) == status
+
+
+def test_python_configs_check_shapes():
+    import torch
+    q, k = torch.zeros(5, 4, 64), torch.zeros(7, 2, 64)
+    cfg = d.packed_config(q, k, k, q, 1)
+    assert (cfg.heads, cfg.kv_heads, cfg.total_q, cfg.total_k, cfg.q_row, cfg.k_row) == (4, 2, 5, 7, 256, 128)
+    for bad in ((q, k, k[:3], q), (q, k, k, q[:2]), (q.transpose(1, 2), k, k, q), (q, k.bfloat16(), k, q), (q[0], k, k, q)):
+        with pytest.raises(ValueError):
+            d.packed_config(*bad, 1)
+    with pytest.raises(ValueError):
+        d.gated_norm_config(torch.zeros(4, 8).t(), 1)
+    assert d.gated_norm_config(torch.zeros(4, 8), 2).mod_row == 8
