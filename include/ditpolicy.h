@@ -139,13 +139,14 @@ size_t flow_policy_loss_workspace_bytes(int32_t batch, int64_t n_per_sample);
  *   dv = d loss / d v   (a clipped sample has none from the first term; where both terms are equal the
  *                        unclipped one counts)
  * mean_ref is mean at the reference policy's velocity v_ref (NULL: no such term). logp_scale = 1 / n_per_sample
- * takes the density per element. logp_old (fp64) and adv (fp32) are device [batch]. A sample with adv = 0 adds nothing, whatever its ratio.
+ * takes the density per element. t, t_next and noise_level are doubles (flow_logprob's are fp32: for a logp_old of its
+ * making pass the values it was given, rounded to fp32). logp_old (fp64) and adv (fp32) are device [batch]. A sample with adv = 0 adds nothing, whatever its ratio.
  * Outputs (device), each may be NULL but one: loss [1], logp, ratio [batch], all fp64; dv [batch][n_per_sample]
  * fp32, which may be v. Sums are fp64. batch == 0 or n_per_sample == 0 writes nothing.
  * Errors: as flow_logprob; DIT_ERR_DOMAIN unless 0 <= clip_low <= 1, 0 <= clip_high, 0 <= kl_weight,
  * 0 < logp_scale, all finite; DIT_ERR_WORKSPACE. */
 dit_status flow_policy_loss(const float* x, const float* v, const float* x_next, const float* v_ref, int32_t batch,
-                            int64_t n_per_sample, float t, float t_next, float noise_level, const double* logp_old,
+                            int64_t n_per_sample, double t, double t_next, double noise_level, const double* logp_old,
                             const float* adv, double logp_scale, double clip_low, double clip_high, double kl_weight,
                             double* loss, double* logp, double* ratio, float* dv, void* workspace,
                             size_t workspace_bytes, dit_stream stream);

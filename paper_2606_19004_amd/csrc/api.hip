@@ -1483,7 +1483,7 @@ size_t flow_policy_loss_workspace_bytes(int32_t batch, int64_t n) {
 }
 
 dit_status flow_policy_loss(const float* x, const float* v, const float* x_next, const float* v_ref, int32_t batch,
-                            int64_t n, float t, float t_next, float noise_level, const double* logp_old,
+                            int64_t n, double t, double t_next, double noise_level, const double* logp_old,
                             const float* adv, double logp_scale, double clip_low, double clip_high, double kl_weight,
                             double* loss, double* logp, double* ratio, float* dv, void* ws, size_t ws_bytes,
                             dit_stream stream) {

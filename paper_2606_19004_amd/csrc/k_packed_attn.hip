@@ -418,6 +418,194 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
     *(float4*)(orow + 16 * i + 4 * g4) = make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
 }
 
+// ---------------------------------------------------------------------------
+// bf16, few rows: a new token (or a few) of each sequence against its keys, bound by reading K and V once. Tiles of 16 rows on
+// v_mfma_f32_16x16x32_bf16; the 4 waves of a workgroup do not share rows but keys: wave w takes the 32-key stages w, w + 4, ...
+// of the part with a running maximum, sum and output of its own, so no barrier stands in the loop, and the four meet
+// at the end. K goes to registers (a lane's 16 bytes are operand A as they stand), V straight to LDS for the
+// transposing read; both one stage ahead, 16 KB per wave in flight.
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
+  constexpr int ROWS = 16, KB = 32, NKS = D / 32, NDB = D / 16;
+  using Tile = RowTile<D, KB, 1>;
+  constexpr int RB = Tile::RB, TILE = Tile::BYTES;
+  constexpr int MERGE = 4 * ROWS * (D + 4) * 4 + 4 * ROWS * 8;
+  constexpr int LDS = 8 * TILE > MERGE ? 8 * TILE : MERGE;
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char smem[LDS];   // per wave [V0][V1]
+  const PackedTile t = packed_tile<ROWS>(a);
+  if (!t.any) return;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int l16 = lane & 15, g4 = lane >> 4;
+  const int rows = t.m * a.G, row0 = t.rt * ROWS;
+  const int q0 = a.qr.begin(t.seq);
+  const int64_t k0 = a.kr.begin(t.seq);
+  const u16* Kg = (const u16*)a.k + k0 * a.k_row + (int64_t)t.g * a.k_head;
+  const u16* Vg = (const u16*)a.v + k0 * a.v_row + (int64_t)t.g * a.v_head;
+  const int row = min(row0 + l16, rows - 1);
+  const int tok = row / a.G, head = t.g * a.G + (row - tok * a.G);
+  const int vis = a.causal ? min(tok + t.n - t.m + 1, t.n) : t.n;
+  const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
+  const int nvis = a.causal ? min(max(last_tok + t.n - t.m + 1, 0), t.n) : t.n;
+  const int all_vis = __builtin_amdgcn_readfirstlane(vis);
+  int begin = 0, end = nvis;
+  if (a.part_tiles) {
+    begin = min(t.part * a.part_tiles * 64, nvis);
+    end = min(begin + a.part_tiles * 64, nvis);
+  }
+  bf16x8 qf[NKS];   // q[row][32 s + 8 g4 + 0..7]
+  {
+    const u16* qrow = (const u16*)a.q + (int64_t)(q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < NKS; s++) qf[s] = *(const bf16x8*)(qrow + 32 * s + 8 * g4);
+  }
+  Tile tv;
+  tv.init(0, lane, a.v_row);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + wave * 2 * TILE;
+  const char* sv0 = smem + wave * 2 * TILE;
+  auto load_k = [&](int key0, bf16x8 (*kf)[2]) {
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++) {
+      const u16* krow = Kg + (int64_t)min(key0 + 16 * kb + l16, end - 1) * a.k_row + 8 * g4;
+#pragma unroll
+      for (int s = 0; s < NKS; s++) kf[s][kb] = *(const bf16x8*)(krow + 32 * s);
+    }
+  };
+  auto load_v = [&](int key0, int buf) { tv.load(Vg + (int64_t)key0 * a.v_row, end - key0, lds0 + buf * TILE); };
+  int vbase[NDB][2];   // 4 dims of key 4 g4 + (lane >> 2) % 4 (+ 16)
+#pragma unroll
+  for (int db = 0; db < NDB; db++)
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+      const int r = 4 * g4 + ((lane >> 2) & 3) + 16 * e, ch = 2 * db + ((lane >> 1) & 1);
+      vbase[db][e] = r * RB + ((ch ^ tile_swizzle<D>(r)) << 4) + 8 * (lane & 1);
+    }
+  f32x4 o[NDB];
+#pragma unroll
+  for (int i = 0; i < NDB; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float c = a.scale * LOG2E;
+  float m_run = M_FLOOR, l_run = 0.f;
+  auto step = [&](int key0, int buf, bf16x8 (*kf)[2], bf16x8 (*kn)[2]) {
+    // the next stage's loads go out in any case, so that the number in flight is known: past the end they repeat the
+    // last key and read no value
+    const int next = key0 + 4 * KB;
+    load_k(next, kn);
+    f32x4 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++) {
+      s[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < NKS; x++) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[x][kb], qf[x], s[kb], 0, 0, 0);
+    }
+    load_v(next, buf ^ 1);
+    if (key0 + KB > min(all_vis, end)) {
+#pragma unroll
+      for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          const int key = key0 + 16 * kb + 4 * g4 + r;
+          if (key >= vis || key >= end) s[kb][r] = -INFINITY;
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) mx = fmaxf(mx, s[kb][r]);
+    mx = pair_max(fmaxf(mx, __shfl_xor(mx, 16, 64)));
+    const float mxs = mx * c;
+    if (__ballot(mxs > m_run) != 0) {
+      const float m_new = fmaxf(m_run, mxs), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int i = 0; i < NDB; i++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) o[i][r] *= alpha;
+    }
+    bf16x8 pf;   // keys 4 g4 + 0..3, 16 + 4 g4 + 0..3
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][r], c, -m_run));
+        l_run += p;
+        pf[4 * kb + r] = (__bf16)p;
+      }
+    wait_loads<2 * NKS + Tile::LOADS>();   // only the next stage's loads are still in flight
+    __builtin_amdgcn_sched_barrier(0);
+    const char* sv = sv0 + buf * TILE;
+#pragma unroll
+    for (int db = 0; db < NDB; db++)
+      o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join_tr(read_tr(sv + vbase[db][0]), read_tr(sv + vbase[db][1])), pf, o[db], 0, 0, 0);
+    // (the reads are complete before the MFMAs that use them, so the buffer may be loaded again)
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  {
+    int key0 = begin + wave * KB;
+    bf16x8 ka[NKS][2], kb[NKS][2];
+    if (key0 < end) {
+      load_k(key0, ka);
+      load_v(key0, 0);
+    }
+    while (key0 < end) {
+      step(key0, 0, ka, kb);
+      key0 += 4 * KB;
+      if (key0 >= end) break;
+      step(key0, 1, kb, ka);
+      key0 += 4 * KB;
+    }
+  }
+  wait_loads<0>();   // (loads past the end write their zeros to LDS too)
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run = pair_sum(l_run);
+  // the waves' results meet: [wave][row][D + 4] outputs, [wave][row] maxima and sums
+  __syncthreads();
+  float* mo = (float*)smem;
+  float2* ml = (float2*)(smem + 4 * ROWS * (D + 4) * 4);
+#pragma unroll
+  for (int db = 0; db < NDB; db++) *(f32x4*)(mo + (wave * ROWS + l16) * (D + 4) + 16 * db + 4 * g4) = o[db];
+  if (g4 == 0) ml[wave * ROWS + l16] = make_float2(m_run, l_run);
+  __syncthreads();
+  constexpr int EPT = ROWS * D / 256;   // 8 or 4 elements of a row per thread
+  const int r = tid / (D / EPT), e0 = (tid % (D / EPT)) * EPT, rr = row0 + r;
+  if (rr >= rows) return;
+  float m = M_FLOOR, l = 0.f, acc[EPT];
+#pragma unroll
+  for (int w = 0; w < 4; w++) m = fmaxf(m, ml[w * ROWS + r].x);
+#pragma unroll
+  for (int e = 0; e < EPT; e++) acc[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; w++) {
+    const float2 x = ml[w * ROWS + r];
+    const float f = __builtin_amdgcn_exp2f(x.x - m);
+    l = fmaf(f, x.y, l);
+#pragma unroll
+    for (int e = 0; e < EPT; e += 4) {
+      const f32x4 y = *(const f32x4*)(mo + (w * ROWS + r) * (D + 4) + e0 + e);
+#pragma unroll
+      for (int j = 0; j < 4; j++) acc[e + j] = fmaf(f, y[j], acc[e + j]);
+    }
+  }
+  const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+  const float lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+#pragma unroll
+  for (int e = 0; e < EPT; e++) acc[e] *= inv;
+  if (a.part_tiles && t.parts > 1) {
+    const int64_t slot = t.slot * ROWS + r;
+    if (e0 == 0) a.part_lse[slot] = lse;
+#pragma unroll
+    for (int e = 0; e < EPT; e += 4) store4<float>(a.part_o + slot * D + e0 + e, acc + e);
+    return;
+  }
+  const int tk = rr / a.G, hd = t.g * a.G + (rr - tk * a.G);
+  if (a.lse && e0 == 0) a.lse[(int64_t)(q0 + tk) * a.H + hd] = lse;
+#pragma unroll
+  for (int e = 0; e < EPT; e += 4) store4<u16>((u16*)a.o + (int64_t)(q0 + tk) * a.o_row + (int64_t)hd * a.o_head + e0 + e, acc + e);
+#endif
+}
+
 // Joins the parts of each row: o = sum_p exp(lse_p - lse) o_p, in the order of the parts. One wave per row.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
@@ -463,21 +651,25 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
   }
 }
 
-// Tiles and parts. Keys are shared out only where the tiles of rows alone leave half of the chip idle (fewer than one
-// workgroup per CU), in parts of at least 4 key tiles, for about two workgroups per CU.
+// Tiles and parts.
+//   rows   bf16: 16 where no sequence has more than FEW_ROWS (query, head) rows per key/value head, else 128; fp32: 64
+//   parts  16-row tiles: keys are shared out wherever sequences may have more than 1024, in parts that give the chip about
+//          four workgroups per CU, since lengths are unlike. Other tiles: only where they alone leave CUs without a
+//          workgroup.
 PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q) {
+  constexpr int CUS = 256, FEW_ROWS = 32;
   PackedPlan p{};
   const int G = H / Hkv;
-  p.rows = dtype == DT_BF16 ? 128 : 64;
+  const bool few = (int64_t)max_q * G <= FEW_ROWS;
+  p.rows = dtype == DT_F32 ? 64 : few ? 16 : 128;
   const int64_t per_seq = cdiv((int64_t)max_q * G, p.rows);   // no sequence has more row tiles
   p.row_tiles = p.units = (int)std::min<int64_t>((int64_t)total_q * G / p.rows + nseq, nseq * per_seq);
   const int64_t groups = (int64_t)p.row_tiles * Hkv;
-  constexpr int CUS = 256;
-  if (groups == 0 || groups >= CUS) return p;
-  const int64_t tiles = (int64_t)cdiv(total_k, 64);
-  const int64_t per = std::max<int64_t>(4, (tiles * groups + 2 * CUS * (int64_t)nseq - 1) / (2 * CUS * (int64_t)nseq));
+  if (groups == 0 || (!few && groups >= CUS)) return p;
+  const int64_t tiles = (int64_t)cdiv(total_k, 64), work = tiles * groups / nseq, goal = few ? 4 * CUS : 2 * CUS;
+  const int64_t per = std::max<int64_t>(few ? 16 : 4, (work + goal - 1) / goal);
   const int64_t units = per_seq * (tiles / per + nseq);   // a sequence of n tiles has at most n / per + 1 parts
-  if (tiles <= per || units * Hkv > 16 * CUS) return p;
+  if (tiles <= per || (!few && units * Hkv > 16 * CUS)) return p;
   p.part_tiles = (int)per;
   p.units = (int)units;
   p.ws = (size_t)Hkv * units * p.rows * (d + 1) * 4;
@@ -485,8 +677,9 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
 }
 
 template <int D>
-static void fwd_launch(const PackedArgs& a, int dtype, int64_t grid, hipStream_t s) {
+static void fwd_launch(const PackedArgs& a, int dtype, int rows, int64_t grid, hipStream_t s) {
   if (dtype == DT_F32) packed_fwd_f32<D><<<grid, 256, 0, s>>>(a);
+  else if (rows == 16) packed_few_bf16<D><<<grid, 256, 0, s>>>(a);
   else if (a.part_tiles) packed_fwd_bf16<D, true><<<grid, 256, 0, s>>>(a);
   else packed_fwd_bf16<D, false><<<grid, 256, 0, s>>>(a);
 }
@@ -500,11 +693,12 @@ hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, int total_k, voi
   a.part_o = (float*)ws;
   a.part_lse = (float*)ws + (int64_t)a.Hkv * p.units * p.rows * d;
   const int64_t grid = (int64_t)p.units * a.Hkv;
-  if (d == 128) fwd_launch<128>(a, dtype, grid, s);
-  else fwd_launch<64>(a, dtype, grid, s);
+  if (d == 128) fwd_launch<128>(a, dtype, p.rows, grid, s);
+  else fwd_launch<64>(a, dtype, p.rows, grid, s);
   if (p.part_tiles) {
     const int64_t jg = (int64_t)p.row_tiles * a.Hkv;
-    if (dtype == DT_BF16) packed_join<u16, 128><<<jg, 256, 0, s>>>(a, d);
+    if (p.rows == 16) packed_join<u16, 16><<<jg, 256, 0, s>>>(a, d);
+    else if (dtype == DT_BF16) packed_join<u16, 128><<<jg, 256, 0, s>>>(a, d);
     else packed_join<float, 64><<<jg, 256, 0, s>>>(a, d);
   }
   return hipGetLastError();

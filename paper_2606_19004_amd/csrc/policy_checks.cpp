@@ -79,17 +79,17 @@ dit_status check_gated_norm(const dit_gated_norm_config* c) {
   return DIT_OK;
 }
 
-dit_status flow_density_terms(int64_t n, float t, float t_next, float noise_level, double* cx, double* cv, double* var,
+dit_status flow_density_terms(int64_t n, double t, double t_next, double noise_level, double* cx, double* cv, double* var,
                               double* cst) {
-  if (!(noise_level > 0.f) || !std::isfinite(noise_level))
+  if (!(noise_level > 0.0) || !std::isfinite(noise_level))
     return set_error(DIT_ERR_DOMAIN, "the density needs a finite noise_level > 0 (the ODE step has none)");
-  if (!(t > 0.f && t < 1.f) || !std::isfinite(t_next) || !(t_next < t))
+  if (!(t > 0.0 && t < 1.0) || !std::isfinite(t_next) || !(t_next < t))
     return set_error(DIT_ERR_DOMAIN, "the density needs 0 < t < 1 and t_next < t (t=%g, t_next=%g)", t, t_next);
-  const double td = t, h = (double)t_next - td, a = noise_level;
-  const double k1 = 0.5 * a * a / (1.0 - td);   // sigma^2 / (2 t)
-  *var = a * a * td / (1.0 - td) * -h;
+  const double h = t_next - t;
+  const double k1 = 0.5 * noise_level * noise_level / (1.0 - t);   // sigma^2 / (2 t)
+  *var = noise_level * noise_level * t / (1.0 - t) * -h;
   *cx = 1.0 + h * k1;
-  *cv = h * (1.0 + k1 * (1.0 - td));
+  *cv = h * (1.0 + k1 * (1.0 - t));
   *cst = -0.5 * (double)n * std::log(2.0 * M_PI * *var);
   return DIT_OK;
 }

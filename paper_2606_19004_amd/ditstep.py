@@ -124,8 +124,7 @@ _sigs = {
     "gated_norm_backward_workspace_bytes": ([C.POINTER(GatedNormConfig)], _sz),
     "gated_norm_backward": ([C.POINTER(GatedNormConfig)] + [_vp] * 17 + [_sz, _stream], _i32),
     "flow_policy_loss_workspace_bytes": ([_i32, _i64], _sz),
-    "flow_policy_loss": ([_vp, _vp, _vp, _vp, _i32, _i64, _f32, _f32, _f32, _vp, _vp, C.c_double, C.c_double,
-                          C.c_double, C.c_double, _vp, _vp, _vp, _vp, _vp, _sz, _stream], _i32),
+    "flow_policy_loss": ([_vp, _vp, _vp, _vp, _i32, _i64] + [C.c_double] * 3 + [_vp, _vp] + [C.c_double] * 4 + [ _vp, _vp, _vp, _vp, _vp, _sz, _stream], _i32),
 }
 for _name, (_args, _res) in _sigs.items():
     _fn = getattr(_lib, _name)
