@@ -1300,6 +1300,10 @@ dit_status packed_args(const dit_packed_config* c, const int32_t* q_offsets, con
   return DIT_OK;
 }
 
+size_t packed_grad_ws(const dit_packed_config* c) {
+  return al256(packed_backward_ws(c->dtype, c->sequences, c->heads, c->kv_heads, c->head_dim, c->total_q, c->total_k, c->causal));
+}
+
 dit_status check_offsets_aligned(std::initializer_list<const void*> ptrs) {
   for (const void* p : ptrs)
     if ((uintptr_t)p & 3) return set_error(DIT_ERR_INVALID_ARG, "offsets, lengths and fp32 tensors must be 4-byte aligned");
@@ -1354,7 +1358,7 @@ extern "C" {
 size_t packed_attention_workspace_bytes(const dit_packed_config* c) { return check_packed(c) ? 0 : packed_forward_ws(c); }
 
 size_t packed_attention_backward_workspace_bytes(const dit_packed_config* c) {
-  return check_packed(c) ? 0 : al256(packed_backward_ws(c->sequences, c->heads, c->total_q));
+  return check_packed(c) ? 0 : packed_grad_ws(c);
 }
 
 dit_status packed_attention(const dit_packed_config* c, const void* q, const void* k, const void* v,
@@ -1395,7 +1399,7 @@ dit_status packed_attention_backward(const dit_packed_config* c, const void* q, 
   for (const void* p : {q, k, v, o, d_o, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!aligned16(p)) return set_error(DIT_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
   if ((st = check_offsets_aligned({q_offsets, k_offsets, k_lengths, lse}))) return st;
-  if ((st = check_ws(ws, ws_bytes, al256(packed_backward_ws(c->sequences, c->heads, c->total_q))))) return st;
+  if ((st = check_ws(ws, ws_bytes, packed_grad_ws(c)))) return st;
   a.q = q;
   a.k = k;
   a.v = v;

@@ -193,45 +193,60 @@ __global__ void __launch_bounds__(256, 2) packed_dq_bf16(PackedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// dk, dv: 128 keys of one key/value head against 64-query tiles of every head of its group in turn
+// dk, dv: 128 keys of one key/value head against 32-query tiles of every head of its group in turn. V stays in LDS and K in
+// registers: with both in registers 40 of them spilled at two waves per SIMD (joint attention at 512x512: 232 us against 197).
+// The tiles may be shared out between a.shares workgroups, whose sums meet in the workspace (shares_join).
 // ---------------------------------------------------------------------------
+// The first of `steps` that share i of n takes.
+__device__ __forceinline__ int share_begin(int steps, int i, int n) { return (int)((int64_t)steps * i / n); }
+// Where share i keeps dk (without the factor scale) and dv of a key: 2 D floats.
+__device__ __forceinline__ float* share_row(const PackedArgs& a, int D, int i, int64_t key_row, int g) {
+  return a.share_sums + (((int64_t)i * a.kr.total + key_row) * a.Hkv + g) * 2 * D;
+}
+
 template <int D>
 __global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
-  constexpr int KEYS = 128, QB = 64, NDB = D / 32, NKS = D / 16;
+  constexpr int KEYS = 128, QB = 32, NDB = D / 32, NKS = D / 16;
   using Tile = RowTile<D, QB, 4>;
   constexpr int TILE = Tile::BYTES, RB = Tile::RB;
 #if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];   // [Q0][Q1][dO0][dO1]
+  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE + KEYS * RB];
   __shared__ float4 stat[2][2][QB / 4];                            // lse (log2 units) and delta of a tile's rows
   const int g = blockIdx.x % a.Hkv;
   int seq, kt;
-  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  if (!find_unit(a.nseq, blockIdx.x / (a.Hkv * a.shares), [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  const int share = blockIdx.x / a.Hkv % a.shares;
   const int m = __builtin_amdgcn_readfirstlane(a.queries(seq)), n = __builtin_amdgcn_readfirstlane(a.keys(seq));
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int half = lane >> 5, l32 = lane & 31;
   const int64_t q0 = a.qr.begin(seq), k0 = a.kr.begin(seq);
   const int key = kt * KEYS + wave * 32 + l32;
-  bf16x8 kf[NKS], vf[NKS];
+  bf16x8 kf[NKS];
   {
     const int64_t kr = k0 + min(key, n - 1);
     const u16* krow = (const u16*)a.k + kr * a.k_row + (int64_t)g * a.k_head;
-    const u16* vrow = (const u16*)a.v + kr * a.v_row + (int64_t)g * a.v_head;
 #pragma unroll
     for (int s = 0; s < NKS; s++) {
       kf[s] = *(const bf16x8*)(krow + 16 * s + 8 * half);
-      vf[s] = *(const bf16x8*)(vrow + 16 * s + 8 * half);
     }
   }
   // the first query that sees any of the tile's keys; queries from `first` of this lane on see its key
   const int first = a.causal ? key - (n - m) : 0;
   const int t0 = a.causal ? min(max(kt * KEYS - (n - m), 0), m) / QB : 0;
   const int wave_first = a.causal ? kt * KEYS + __builtin_amdgcn_readfirstlane(wave) * 32 + 31 - (n - m) : 0;
-  const int per = cdiv(m, QB) - t0, steps = per * a.G;   // tiles of one head, of all heads
+  const int per = cdiv(m, QB) - t0;   // tiles of one head
+  const int begin = share_begin(per * a.G, share, a.shares), steps = share_begin(per * a.G, share + 1, a.shares) - begin;
   Tile tq, td;
   tq.init(wave, lane, a.q_row);
   td.init(wave, lane, a.o_row);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
-  int ih = 0, it = t0;   // head and tile of the next loads
+  {
+    RowTile<D, KEYS, 4> tv;
+    tv.init(wave, lane, a.v_row);
+    tv.load((const u16*)a.v + (k0 + kt * KEYS) * a.v_row + (int64_t)g * a.v_head, n - kt * KEYS, lds0 + 4 * TILE);
+  }
+  const char* sv = smem + 4 * TILE + wave * 32 * RB;
+  int ih = per > 0 ? begin / per : 0, it = t0 + begin - ih * per;   // head and tile of the next loads
   float nlse = INFINITY, ndelta = 0.f;
   auto issue = [&](int i) {
     const int64_t head = (int64_t)g * a.G + ih;
@@ -266,11 +281,12 @@ __global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
     for (int r = 0; r < 16; r++) dk[i][r] = dv[i][r] = 0.f;
   const f32x16 zero = {};
   const float c = a.scale * LOG2E;
+  const int it0 = it;
   if (steps > 0) {
     issue(0);
     put_stats(0);
   }
-  int ct = t0;
+  int ct = it0;
   for (int i = 0; i < steps; i++) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();   // tile i has landed, and every wave is done with the other buffers
@@ -283,7 +299,7 @@ __global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
 #pragma unroll
       for (int x = 0; x < NKS; x++) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::read(sq, 32 * qb + l32, 2 * x + half), kf[x], x == 0 ? zero : s, 0, 0, 0);
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::read(sd, 32 * qb + l32, 2 * x + half), vf[x], x == 0 ? zero : dp, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::read(sd, 32 * qb + l32, 2 * x + half), Tile::read(sv, l32, 2 * x + half), x == 0 ? zero : dp, 0, 0, 0);
       }
       const int r0 = ct * QB + 32 * qb;
       if (r0 < wave_first) {
@@ -319,6 +335,20 @@ __global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
     }
     if (i + 1 < steps) put_stats(i + 1);
     if (++ct == t0 + per) ct = t0;
+  }
+  if (a.shares > 1) {
+    if (key < n) {
+      float* pk = share_row(a, D, share, k0 + key, g);
+#pragma unroll
+      for (int db = 0; db < NDB; db++)
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+          const int e = 32 * db + 8 * q + 4 * half;
+          *(float4*)(pk + e) = make_float4(dk[db][4 * q], dk[db][4 * q + 1], dk[db][4 * q + 2], dk[db][4 * q + 3]);
+          *(float4*)(pk + D + e) = make_float4(dv[db][4 * q], dv[db][4 * q + 1], dv[db][4 * q + 2], dv[db][4 * q + 3]);
+        }
+    }
+    return;
   }
   __syncthreads();
   auto rows_to = [&](void* dst, int64_t row_stride, int64_t head_stride) {
@@ -451,7 +481,8 @@ __global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
   __shared__ __attribute__((aligned(16))) float sq[2][W::NROW * W::LD], sd[2][W::NROW * W::LD];
   const int g = blockIdx.x % a.Hkv;
   int seq, kt;
-  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  if (!find_unit(a.nseq, blockIdx.x / (a.Hkv * a.shares), [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  const int share = blockIdx.x / a.Hkv % a.shares;
   const int m = a.queries(seq), n = a.keys(seq);
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int64_t q0 = a.qr.begin(seq), k0 = a.kr.begin(seq);
@@ -481,16 +512,17 @@ __global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
     w.fetch((const float*)a.q + at * a.q_row + head * a.q_head, a.q_row,
             (const float*)a.d_o + at * a.o_row + head * a.o_head, a.o_row, m - t * W::NROW);
   };
-  int h = 0, t = t0;
-  if (per > 0) {
-    fetch(0, t0);
+  const int begin = share_begin(per * a.G, share, a.shares), steps = share_begin(per * a.G, share + 1, a.shares) - begin;
+  int h = per > 0 ? begin / per : 0, t = t0 + begin - h * per;
+  if (steps > 0) {
+    fetch(h, t);
     w.stage(sq[0], sd[0]);
   }
-  for (int i = 0; i < per * a.G; i++) {
+  for (int i = 0; i < steps; i++) {
     const int buf = i & 1;
     __syncthreads();
     const int nh = t + 1 == t0 + per ? h + 1 : h, nt = t + 1 == t0 + per ? t0 : t + 1;
-    if (i + 1 < per * a.G) fetch(nh, nt);
+    if (i + 1 < steps) fetch(nh, nt);
     f32x4 s = W::dot(sq[buf], kf, l16, g4), dp = W::dot(sd[buf], vf, l16, g4);
 #pragma unroll
     for (int r = 0; r < 4; r++) {
@@ -503,24 +535,74 @@ __global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
     }
     W::add(dv, sd[buf], s, l16, g4);
     W::add(dk, sq[buf], dp, l16, g4);
-    if (i + 1 < per * a.G) w.stage(sq[buf ^ 1], sd[buf ^ 1]);
+    if (i + 1 < steps) w.stage(sq[buf ^ 1], sd[buf ^ 1]);
     h = nh;
     t = nt;
   }
   if (key >= n) return;
   float* ok = (float*)a.dk + (k0 + key) * a.k_row + (int64_t)g * a.k_head;
   float* ov = (float*)a.dv + (k0 + key) * a.v_row + (int64_t)g * a.v_head;
+  float f = a.scale;
+  if (a.shares > 1) {
+    ok = share_row(a, D, share, k0 + key, g);
+    ov = ok + D;
+    f = 1.f;
+  }
 #pragma unroll
   for (int i = 0; i < NKC; i++) {
-    *(float4*)(ok + 16 * i + 4 * g4) = make_float4(dk[i][0] * a.scale, dk[i][1] * a.scale, dk[i][2] * a.scale, dk[i][3] * a.scale);
+    *(float4*)(ok + 16 * i + 4 * g4) = make_float4(dk[i][0] * f, dk[i][1] * f, dk[i][2] * f, dk[i][3] * f);
     *(float4*)(ov + 16 * i + 4 * g4) = make_float4(dv[i][0], dv[i][1], dv[i][2], dv[i][3]);
   }
 }
 
+// dk and dv of a key from its shares, in their order. Workgroup: 64 keys of one key/value head.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) shares_join(PackedArgs a) {
+  constexpr int KEYS = 64, LPR = D / 4;
+  const int g = blockIdx.x % a.Hkv;
+  int seq, kt;
+  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  const int n = a.keys(seq), e = 4 * (threadIdx.x % LPR);
+  const int64_t k0 = a.kr.begin(seq);
+  for (int r = threadIdx.x / LPR; r < KEYS && kt * KEYS + r < n; r += 256 / LPR) {
+    const int64_t key = k0 + kt * KEYS + r;
+    float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < a.shares; i++) {
+      const float* p = share_row(a, D, i, key, g) + e;
+      const float4 x = *(const float4*)p, y = *(const float4*)(p + D);
+      k[0] += x.x; k[1] += x.y; k[2] += x.z; k[3] += x.w;
+      v[0] += y.x; v[1] += y.y; v[2] += y.z; v[3] += y.w;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) k[j] *= a.scale;
+    store4<T>((T*)a.dk + key * a.k_row + (int64_t)g * a.k_head + e, k);
+    store4<T>((T*)a.dv + key * a.v_row + (int64_t)g * a.v_head + e, v);
+  }
+}
+
+size_t delta_bytes(int H, int total_q) { return ((size_t)total_q * H * 4 + 255) & ~(size_t)255; }
+
+// Into how many workgroups the rows that a key tile walks are shared out. A share costs a write and a read of its fp32 sums,
+// about what 350 rows cost to walk.
+//   fewer key tiles than CUs      as many as fill two workgroups per CU, of 256 rows at least
+//   causal, fewer than 1024       two: the tiles' work falls from all rows to none, and without a second round of workgroups
+//                                 the longest ones run alone (8192 keys of 8 heads, 4 query heads each: 1952 us in one
+//                                 share)
+int shares_of(int dtype, int nseq, int H, int Hkv, int total_q, int total_k, int causal) {
+  const int keys = dtype == DT_BF16 ? 128 : 64;
+  const int64_t units = ((int64_t)total_k / keys + nseq) * Hkv, rows = (int64_t)total_q * (H / Hkv) / nseq;
+  if (units < 256) return (int)std::max<int64_t>(1, std::min<int64_t>(512 / units, rows / (dtype == DT_BF16 ? 256 : 64)));
+  return causal && units < 1024 && rows >= 4096 ? 2 : 1;
+}
+
 }  // namespace
 
-// row sums of do o
-size_t packed_backward_ws(int nseq, int H, int total_q) { return (size_t)total_q * H * 4; }
+// row sums of do o; the shares of dk and dv
+size_t packed_backward_ws(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal) {
+  if (nseq == 0) return 0;
+  const int shares = shares_of(dtype, nseq, H, Hkv, total_q, total_k, causal);
+  return delta_bytes(H, total_q) + (shares > 1 ? (size_t)shares * total_k * Hkv * 2 * d * 4 : 0);
+}
 
 hipError_t packed_attention_delta(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
   a.delta = (float*)ws;
@@ -534,15 +616,23 @@ hipError_t packed_attention_delta(PackedArgs a, int dtype, int d, void* ws, hipS
   return hipGetLastError();
 }
 
+template <int D>
+static void dkdv_launch(const PackedArgs& a, int dtype, int64_t units, int64_t joins, hipStream_t s) {
+  if (dtype == DT_BF16) packed_dkdv_bf16<D><<<units, 256, 0, s>>>(a);
+  else packed_dkdv_f32<D><<<units, 256, 0, s>>>(a);
+  if (a.shares <= 1) return;
+  if (dtype == DT_BF16) shares_join<u16, D><<<joins, 256, 0, s>>>(a);
+  else shares_join<float, D><<<joins, 256, 0, s>>>(a);
+}
 hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s) {
-  a.delta = (float*)ws;
-  const int keys = dtype == DT_BF16 ? 128 : 64;
-  const int64_t grid = ((int64_t)total_k / keys + a.nseq) * a.Hkv;
   if (total_k == 0) return hipSuccess;
-  if (dtype == DT_BF16 && d == 128) packed_dkdv_bf16<128><<<grid, 256, 0, s>>>(a);
-  else if (dtype == DT_BF16) packed_dkdv_bf16<64><<<grid, 256, 0, s>>>(a);
-  else if (d == 128) packed_dkdv_f32<128><<<grid, 256, 0, s>>>(a);
-  else packed_dkdv_f32<64><<<grid, 256, 0, s>>>(a);
+  a.delta = (float*)ws;
+  a.shares = shares_of(dtype, a.nseq, a.H, a.Hkv, a.qr.total, total_k, a.causal);
+  a.share_sums = (float*)((char*)ws + delta_bytes(a.H, a.qr.total));
+  const int keys = dtype == DT_BF16 ? 128 : 64;
+  const int64_t units = ((int64_t)total_k / keys + a.nseq) * a.Hkv * a.shares, joins = ((int64_t)total_k / 64 + a.nseq) * a.Hkv;
+  if (d == 128) dkdv_launch<128>(a, dtype, units, joins, s);
+  else dkdv_launch<64>(a, dtype, units, joins, s);
   return hipGetLastError();
 }
 

@@ -32,7 +32,7 @@ struct PackedArgs {
   // backward
   const void* d_o; void* dq; void* dk; void* dv;
   float* delta;                     // [total_q][H] rowsum(d_o o)
-  int key_tiles;                    // upper bound on (sequence, key tile)
+  int shares; float* share_sums;    // workgroups that share a key tile's rows, and their sums
   __device__ __forceinline__ int queries(int i) const { return min(qr.count(i), max_q); }
   __device__ __forceinline__ int keys(int i) const {
     const int c = kr.count(i);
@@ -76,7 +76,7 @@ struct PackedPlan {
 };
 PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q);
 hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s);
-size_t packed_backward_ws(int nseq, int H, int total_q);
+size_t packed_backward_ws(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal);
 hipError_t packed_attention_delta(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s);
 hipError_t packed_attention_dq(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
