@@ -1471,7 +1471,7 @@ dit_status gated_norm_backward(const dit_gated_norm_config* c, const void* x_out
   a.dpost_w = dpost_w;
   a.dpre_w = dpre_w;
   a.parts = columns ? (float*)ws : nullptr;
-  a.chunks = gated_norm_chunks(c->sequences, c->rows);
+  a.chunks = gated_norm_chunks(c->sequences, c->rows, c->hidden);
   const double passes = 1 + (y != nullptr) + (dx_out != nullptr) + (dh != nullptr) + (dx != nullptr) + (dy != nullptr);
   if (c->rows > 0)
     TIMED("gated_norm_backward", 0, passes * c->rows * c->hidden * esize(c->dtype), hs(stream),

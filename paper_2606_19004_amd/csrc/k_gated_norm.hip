@@ -2,8 +2,7 @@
 //   x_out = alpha x + gate u, u = post(y) post_w;   h = pre(x_out) pre_w (1 + scale) + shift,
 // and its gradients. Bound by memory: 4 row tensors pass forward, 6 backward.
 //
-// Forward: a row is held by 64 lanes (fewer where it is short), 8 elements per lane and chunk, so that the two-pass mean
-// and variance need no second read. Backward: see rows_kernel.
+// A row is held in registers, 8 elements per lane, so that the two passes of its mean and variance need no second read.
 #include <algorithm>
 
 #include "packed.h"
@@ -11,8 +10,8 @@
 namespace dit {
 namespace {
 
-// Elements of a row that a lane holds: 8 successive ones per chunk (VEC: D a multiple of 8, everything 16-byte
-// aligned) or 8 that are LPR apart.
+// The 8 elements of a row that a lane holds: successive ones (VEC: D a multiple of 8, everything 16-byte aligned) or ones
+// that are `step` apart.
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const T* p, int at, int step, int D, float* f) {
   if (VEC) {
@@ -41,9 +40,57 @@ __device__ __forceinline__ void store8(T* p, int at, int step, int D, const floa
       if (at + i * step < D) p[at + i * step] = from_f32<T>(f[i]);
   }
 }
-// place of a lane's first element of chunk c, of the LPR lanes of a row
-template <bool VEC>
-__device__ __forceinline__ int place(int c, int l, int lpr) { return VEC ? (c * lpr + l) * 8 : c * lpr * 8 + l; }
+// The same as it was loaded: a row on its way while the one before it is worked on.
+template <typename T, bool VEC> struct Raw {
+  float f[8];
+  __device__ __forceinline__ void load(const T* p, int at, int step, int D) { load8<T, VEC>(p, at, step, D, f); }
+  __device__ __forceinline__ void get(float* o) const {
+#pragma unroll
+    for (int i = 0; i < 8; i++) o[i] = f[i];
+  }
+};
+template <> struct Raw<u16, true> {
+  uint4 u;
+  __device__ __forceinline__ void load(const u16* p, int at, int, int D) { u = at < D ? *(const uint4*)(p + at) : make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(float* o) const {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      o[2 * i] = __uint_as_float(w[i] << 16);
+      o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+};
+
+// place of a lane's first element, and whether its element i is one of the row's D
+template <bool VEC> __device__ __forceinline__ int place(int l) { return VEC ? l * 8 : l; }
+template <bool VEC> __device__ __forceinline__ bool inside(int at, int i, int lpr, int D) { return VEC ? at < D : at + i * lpr < D; }
+// ky = gate post_w, kh = (1 + scale) pre_w; 0 past the row
+template <typename T, bool VEC>
+__device__ __forceinline__ void gains(const GatedNormArgs& a, int64_t mo, int at, int lpr, float* ky, float* kh) {
+  float m[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) ky[i] = kh[i] = 1.f;
+  if (a.gate) load8<float, VEC>(a.gate + mo, at, lpr, a.D, ky);
+  if (a.post_w) {
+    load8<T, VEC>((const T*)a.post_w, at, lpr, a.D, m);
+#pragma unroll
+    for (int i = 0; i < 8; i++) ky[i] *= m[i];
+  }
+  if (a.scale) {
+    load8<float, VEC>(a.scale + mo, at, lpr, a.D, m);
+#pragma unroll
+    for (int i = 0; i < 8; i++) kh[i] += m[i];
+  }
+  if (a.pre_w) {
+    load8<T, VEC>((const T*)a.pre_w, at, lpr, a.D, m);
+#pragma unroll
+    for (int i = 0; i < 8; i++) kh[i] *= m[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    if (!inside<VEC>(at, i, lpr, a.D)) ky[i] = kh[i] = 0.f;
+}
 
 __device__ __forceinline__ float lanes_sum(float v, int lpr) {
   for (int o = lpr >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -71,265 +118,374 @@ __device__ __forceinline__ int sequence_of(const GatedNormArgs& a, int row) {
 struct Norm {
   float mean, r;
 };
-template <int CH>
-__device__ __forceinline__ Norm statistics(int kind, const float (*v)[8], const GatedNormArgs& a, int l, int lpr, bool vec) {
+// of a row of up to 512 elements, held by lpr lanes; at: this lane's first element
+template <bool VEC>
+__device__ __forceinline__ Norm statistics(int kind, const float* v, const GatedNormArgs& a, int at, int lpr) {
   Norm n{0.f, 1.f};
   if (kind == NORM_NONE) return n;
   if (kind == NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
-    for (int c = 0; c < CH; c++)
-#pragma unroll
-      for (int i = 0; i < 8; i++) s += v[c][i];
+    for (int i = 0; i < 8; i++) s += v[i];
     n.mean = lanes_sum(s, lpr) / (float)a.D;
   }
   float q = 0.f;
 #pragma unroll
-  for (int c = 0; c < CH; c++)
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const int at = vec ? (c * lpr + l) * 8 + i : c * lpr * 8 + l + i * lpr;
-      const float d = at < a.D ? v[c][i] - n.mean : 0.f;
-      q = fmaf(d, d, q);
-    }
+  for (int i = 0; i < 8; i++) {
+    const float d = inside<VEC>(at, i, lpr, a.D) ? v[i] - n.mean : 0.f;
+    q = fmaf(d, d, q);
+  }
   n.r = rsqrtf(lanes_sum(q, lpr) / (float)a.D + a.eps);
   return n;
 }
 
-template <typename T, int CH, bool VEC>
-__global__ void __launch_bounds__(256) forward_kernel(GatedNormArgs a, int lpr) {
+// Rows of up to 512 elements: 64 / lpr rows per wave, 4 waves.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) forward_narrow(GatedNormArgs a, int lpr) {
   const int lane = threadIdx.x & 63, per = 64 / lpr, l = lane & (lpr - 1);
   const int64_t row64 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * per + lane / lpr;
   const int row = (int)min(row64, (int64_t)a.rows - 1);
   const int seq = sequence_of(a, row);
-  const bool real = row64 < a.rows && seq >= 0;
-  if (!real) return;   // (whole groups of lpr lanes: the sums below stay inside a group)
-  const int D = a.D;
-  const T* x = (const T*)a.x + row * a.x_row;
+  if (row64 >= a.rows || seq < 0) return;   // (whole groups of lpr lanes: the sums below stay inside a group)
+  const int D = a.D, at = place<VEC>(l);
   const int64_t mo = seq * a.mod_row;
-  float v[CH][8];
+  float v[8], w[8];
+  load8<T, VEC>((const T*)a.x + row * a.x_row, at, lpr, D, v);
+#pragma unroll
+  for (int i = 0; i < 8; i++) v[i] *= a.alpha;
   if (a.y) {
-    const T* y = (const T*)a.y + row * a.y_row;
+    float u[8];
+    load8<T, VEC>((const T*)a.y + row * a.y_row, at, lpr, D, u);
+    const Norm n = statistics<VEC>(a.post, u, a, at, lpr);
 #pragma unroll
-    for (int c = 0; c < CH; c++) load8<T, VEC>(y, place<VEC>(c, l, lpr), lpr, D, v[c]);
-    const Norm n = statistics<CH>(a.post, v, a, l, lpr, VEC);
+    for (int i = 0; i < 8; i++) u[i] = (u[i] - n.mean) * n.r;
+    if (a.post_w) {
+      load8<T, VEC>((const T*)a.post_w, at, lpr, D, w);
 #pragma unroll
-    for (int c = 0; c < CH; c++) {
-      const int at = place<VEC>(c, l, lpr);
-      float xv[8], w[8], g[8];
-      load8<T, VEC>(x, at, lpr, D, xv);
-      if (a.post_w) load8<T, VEC>((const T*)a.post_w, at, lpr, D, w);
-      if (a.gate) load8<float, VEC>(a.gate + mo, at, lpr, D, g);
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        float u = (v[c][i] - n.mean) * n.r;
-        if (a.post_w) u *= w[i];
-        if (a.gate) u *= g[i];
-        v[c][i] = fmaf(a.alpha, xv[i], u);
-      }
+      for (int i = 0; i < 8; i++) u[i] *= w[i];
     }
-  } else {
+    if (a.gate) {
+      load8<float, VEC>(a.gate + mo, at, lpr, D, w);
 #pragma unroll
-    for (int c = 0; c < CH; c++) {
-      load8<T, VEC>(x, place<VEC>(c, l, lpr), lpr, D, v[c]);
-#pragma unroll
-      for (int i = 0; i < 8; i++) v[c][i] *= a.alpha;
+      for (int i = 0; i < 8; i++) u[i] *= w[i];
     }
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = inside<VEC>(at, i, lpr, D) ? v[i] + u[i] : 0.f;
   }
-  if (!VEC) {   // lanes past the row hold what the mean of y left there
-#pragma unroll
-    for (int c = 0; c < CH; c++)
-#pragma unroll
-      for (int i = 0; i < 8; i++)
-        if (place<VEC>(c, l, lpr) + i * lpr >= D) v[c][i] = 0.f;
-  } else {
-#pragma unroll
-    for (int c = 0; c < CH; c++)
-      if (place<VEC>(c, l, lpr) >= D)
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[c][i] = 0.f;
-  }
-  if (a.x_out) {
-    T* xo = (T*)a.x_out + row * a.x_row;
-#pragma unroll
-    for (int c = 0; c < CH; c++) store8<T, VEC>(xo, place<VEC>(c, l, lpr), lpr, D, v[c]);
-  }
+  if (a.x_out) store8<T, VEC>((T*)a.x_out + row * a.x_row, at, lpr, D, v);
   if (!a.h) return;
-  const Norm n = statistics<CH>(a.pre, v, a, l, lpr, VEC);
-  T* h = (T*)a.h + row * a.h_row;
+  const Norm n = statistics<VEC>(a.pre, v, a, at, lpr);
 #pragma unroll
-  for (int c = 0; c < CH; c++) {
-    const int at = place<VEC>(c, l, lpr);
-    float w[8], sc[8], sh[8], o[8];
-    if (a.pre_w) load8<T, VEC>((const T*)a.pre_w, at, lpr, D, w);
-    if (a.scale) load8<float, VEC>(a.scale + mo, at, lpr, D, sc);
-    if (a.shift) load8<float, VEC>(a.shift + mo, at, lpr, D, sh);
+  for (int i = 0; i < 8; i++) v[i] = (v[i] - n.mean) * n.r;
+  if (a.pre_w) {
+    load8<T, VEC>((const T*)a.pre_w, at, lpr, D, w);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] *= w[i];
+  }
+  if (a.scale) {
+    load8<float, VEC>(a.scale + mo, at, lpr, D, w);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = fmaf(v[i], w[i], v[i]);
+  }
+  if (a.shift) {
+    load8<float, VEC>(a.shift + mo, at, lpr, D, w);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] += w[i];
+  }
+  store8<T, VEC>((T*)a.h + row * a.h_row, at, lpr, D, v);
+}
+
+// ---------------------------------------------------------------------------
+// Longer rows take a workgroup of D / 8 lanes, which walks a chunk of rows of one sequence: gate, scale, shift and weights stay in
+// registers (read per row they are half again as many bytes as the rows, from L2), and the next row is on its way while the
+// sums of a row pass their barriers.
+// ---------------------------------------------------------------------------
+constexpr int MAX_WAVES = 16;   // of 8192 / 8 lanes
+
+// v of the lane that a step of a sum over the wave takes it from (0 where there is none): 1, 2, 4, 8 lanes before, which puts the sum of
+// a row of 16 lanes into its lane 15, then the rows before. VALU moves, no LDS.
+template <int CTRL, int ROWS> __device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+template <int STEP> __device__ __forceinline__ float before(float v) {
+  if constexpr (STEP < 4) return moved<0x110 + (1 << STEP), 0xf>(v);
+  else if constexpr (STEP == 4) return moved<0x142, 0xa>(v);
+  else return moved<0x143, 0xc>(v);
+}
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+// sum over the wave, and over its first 16 lanes, in every lane
+__device__ __forceinline__ float row_sum(float v) {
+  v += before<0>(v);
+  v += before<1>(v);
+  v += before<2>(v);
+  v += before<3>(v);
+  return v;
+}
+__device__ __forceinline__ float wave_total(float v) {
+  v = row_sum(v);
+  v += before<4>(v);
+  v += before<5>(v);
+  return lane_of(v, 63);
+}
+__device__ __forceinline__ float first_row_total(float v) { return lane_of(row_sum(v), 15); }
+
+// What is known of a set of row elements v with weights g: sum v, sum (v - m)^2 and sum g (v - m) about the set's own mean m (rms: 0),
+// sum g. Sets are joined by the formulas for the sums about another point, which lose nothing where the mean is large.
+struct Moments {
+  float s, q, sg, c;
+};
+// one step of the sum over a wave: a lane's set of n elements and another of as many
+template <int STEP, bool WITH_G> __device__ __forceinline__ void join_equal(bool layer, Moments& m, float half_inverse) {
+  const float s = before<STEP>(m.s), sg = WITH_G ? before<STEP>(m.sg) : 0.f;
+  m.q += before<STEP>(m.q);
+  if (WITH_G) m.c += before<STEP>(m.c);
+  if (layer) {   // half_inverse = 1 / (2 n)
+    const float d = m.s - s;
+    m.q = fmaf(d * d, half_inverse, m.q);
+    if (WITH_G) m.c = fmaf(d * (m.sg - sg), half_inverse, m.c);
+    m.s += s;
+  }
+  if (WITH_G) m.sg += sg;
+}
+template <bool WITH_G>
+__device__ __forceinline__ Moments wave_moments(int kind, const float* v, const float* g, const bool* in, float count) {
+  Moments m{0.f, 0.f, 0.f, 0.f};
+  const bool layer = kind == NORM_LAYER;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    if (layer) m.s += v[i];
+    if (WITH_G) m.sg += g[i];
+  }
+  if (count == 512.f) {
+    const float mean = m.s * 0.125f;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      o[i] = (v[c][i] - n.mean) * n.r;
-      if (a.pre_w) o[i] *= w[i];
-      if (a.scale) o[i] *= 1.f + sc[i];
-      if (a.shift) o[i] += sh[i];
+      const float d = v[i] - mean;
+      m.q = fmaf(d, d, m.q);
+      if (WITH_G) m.c = fmaf(g[i], d, m.c);
     }
-    store8<T, VEC>(h, at, lpr, D, o);
+    join_equal<0, WITH_G>(layer, m, 1.f / 16);
+    join_equal<1, WITH_G>(layer, m, 1.f / 32);
+    join_equal<2, WITH_G>(layer, m, 1.f / 64);
+    join_equal<3, WITH_G>(layer, m, 1.f / 128);
+    join_equal<4, WITH_G>(layer, m, 1.f / 256);
+    join_equal<5, WITH_G>(layer, m, 1.f / 512);
+    return m;   // (lane 63 has the wave's)
+  }
+  // a wave at the end of the row: its mean first
+  if (WITH_G) m.sg = wave_total(m.sg);
+  float mean = 0.f;
+  if (layer) {
+    m.s = wave_total(m.s);
+    mean = count > 0.f ? m.s / count : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    const float d = in[i] ? v[i] - mean : 0.f;
+    m.q = fmaf(d, d, m.q);
+    if (WITH_G) m.c = fmaf(g[i], d, m.c);
+  }
+  m.q = wave_total(m.q);
+  if (WITH_G) m.c = wave_total(m.c);
+  return m;
+}
+// mean, 1 / deviation, sum g, sum g (v - mean) r of a row from its waves' moments (m: [MAX_WAVES], zeros past the last), each of `count`
+// elements; lane w looks at wave w's
+struct RowStats {
+  float mean, r, sg, c;
+};
+template <bool WITH_G>
+__device__ __forceinline__ RowStats join_moments(int kind, const float4* m, float count, float inv_d, float eps) {
+  const float4 x = m[threadIdx.x & 15];
+  RowStats o{0.f, 1.f, 0.f, 0.f};
+  float off = 0.f;
+  if (kind == NORM_LAYER) {
+    o.mean = first_row_total(x.x) * inv_d;
+    off = count > 0.f ? x.x / count - o.mean : 0.f;
+  }
+  if (kind != NORM_NONE) o.r = rsqrtf(first_row_total(fmaf(count * off, off, x.y)) * inv_d + eps);
+  if (WITH_G) {
+    o.sg = first_row_total(x.z);
+    o.c = first_row_total(fmaf(x.z, off, x.w)) * o.r;
+  }
+  return o;
+}
+// elements of the row in wave w = lane % 16
+__device__ __forceinline__ float wave_count(bool vec, int lpr, int D) {
+  const int w = threadIdx.x & 15;
+  if (vec) return (float)min(max(D - 512 * w, 0), 512);
+  int n = 0;
+  for (int i = 0; i < 8; i++) n += min(max(min(lpr, D - i * lpr) - 64 * w, 0), 64);
+  return (float)n;
+}
+
+// A barrier for what the waves exchange through LDS. __syncthreads() would also wait for the loads of the next row and the stores of
+// the last one, which no other wave looks at (512x512, 16 seeds, forward: 164 us).
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(1024) forward_wide(GatedNormArgs a, int lpr, int chunk_rows) {
+  __shared__ float4 red[2][MAX_WAVES];
+  int seq, chunk;
+  if (!find_unit(a.nseq, blockIdx.x, [&](int i) { return cdiv(a.pr.count(i), chunk_rows); }, seq, chunk)) return;
+  // every chunks-th row: the workgroups that run together then work on neighbouring rows
+  const int count_ = a.pr.count(seq), begin = a.pr.begin(seq) + chunk, end = a.pr.begin(seq) + count_, step = cdiv(count_, chunk_rows);
+  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = l < lpr ? place<VEC>(l) : D;
+  const int64_t mo = seq * a.mod_row;
+  Raw<T, VEC> nx, ny;
+  auto fetch = [&](int64_t row) {
+    nx.load((const T*)a.x + row * a.x_row, at, lpr, D);
+    if (a.y) ny.load((const T*)a.y + row * a.y_row, at, lpr, D);
+  };
+  fetch(begin);
+  bool in[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) in[i] = inside<VEC>(at, i, lpr, D);
+  if (l < 2 * MAX_WAVES) red[l >> 4][l & 15] = make_float4(0.f, 0.f, 0.f, 0.f);
+  __syncthreads();
+  const float counts = wave_count(VEC, lpr, D), count = lane_of(counts, wave), inv_d = 1.f / (float)D;
+  float ky[8], kh[8], sh[8];   // gate post_w; (1 + scale) pre_w; shift
+  gains<T, VEC>(a, mo, at, lpr, ky, kh);
+#pragma unroll
+  for (int i = 0; i < 8; i++) sh[i] = 0.f;
+  if (a.shift && a.h) load8<float, VEC>(a.shift + mo, at, lpr, D, sh);
+  int turn = 0;   // (a buffer is written again two barriers after it was)
+  auto stats = [&](int kind, const float* v) {
+    const Moments m = wave_moments<false>(kind, v, nullptr, in, count);
+    if ((l & 63) == 63) red[turn][wave] = make_float4(m.s, m.q, 0.f, 0.f);
+    lds_barrier();
+    const RowStats n = join_moments<false>(kind, red[turn], counts, inv_d, a.eps);
+    turn ^= 1;
+    return n;
+  };
+  for (int64_t row = begin; row < end; row += step) {
+    float v[8], u[8];
+    nx.get(v);
+    if (a.y) ny.get(u);
+    if (row + step < end) fetch(row + step);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] *= a.alpha;
+    if (a.y) {
+      if (a.post != NORM_NONE) {
+        const RowStats n = stats(a.post, u);
+#pragma unroll
+        for (int i = 0; i < 8; i++) u[i] = (u[i] - n.mean) * n.r;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i++) v[i] = fmaf(u[i], ky[i], v[i]);   // (past the row ky is 0)
+    }
+    if (a.x_out) store8<T, VEC>((T*)a.x_out + row * a.x_row, at, lpr, D, v);
+    if (!a.h) continue;
+    RowStats n{0.f, 1.f, 0.f, 0.f};
+    if (a.pre != NORM_NONE) n = stats(a.pre, v);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = fmaf((v[i] - n.mean) * n.r, kh[i], sh[i]);
+    store8<T, VEC>((T*)a.h + row * a.h_row, at, lpr, D, v);
   }
 }
 
 // ---------------------------------------------------------------------------
-// Backward. A workgroup takes a chunk of rows of one sequence, so that its gate and scale are read once, and adds
-// the column sums of the chunk up in registers: a lane holds the same 8 columns of every row. Rows of up to 512
-// elements share a wave (lpr lanes each); longer ones take the whole workgroup, D / 8 lanes. With xh = pre(x_out), yh = post(y) the
-// normalised rows and t = dx_out + pre'(dh (1 + scale) pre_w),
+// Backward. A workgroup takes a chunk of rows of one sequence and adds its column sums up in registers: a lane holds the
+// same 8 columns of every row. With xh = pre(x_out), yh = post(y) the normalised rows and t = dx_out + pre'(dh (1 + scale) pre_w),
 //   dx = alpha t,  dy = post'(gate post_w t),  norm'(g) = r (g - [mean g] - xh mean(g xh));
 // the sums over the rows are R = sum dh, P = sum dh xh, Q = sum t yh, from which every vector's gradient follows
 // (columns_kernel). R, P and Q of a chunk go to the workspace.
 // ---------------------------------------------------------------------------
-// Sums of two values over the lanes of a row.
-template <bool WIDE>
-__device__ __forceinline__ void row_sums(float& u, float& v, int lpr, float2* red) {
-  if (!WIDE) {
-    u = lanes_sum(u, lpr);
-    v = lanes_sum(v, lpr);
-    return;
-  }
-  u = lanes_sum(u, 64);
-  v = lanes_sum(v, 64);
-  const int waves = blockDim.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(u, v);
-  __syncthreads();
-  u = v = 0.f;
-  for (int w = 0; w < waves; w++) {
-    u += red[w].x;
-    v += red[w].y;
+// What both kernels do with a row once its statistics are known. t: dx_out, becomes its total; xv, yv: become the normalised rows.
+struct RowGradient {
+  float mean, r, mg, mgx;   // of x_out: mean, 1 / deviation, mean g, mean g xh (0 where the norm has none)
+};
+__device__ __forceinline__ RowGradient row_gradient(int kind, const RowStats& n, float inv_d) {
+  return RowGradient{n.mean, n.r, kind == NORM_LAYER ? n.sg * inv_d : 0.f, kind != NORM_NONE ? n.c * inv_d : 0.f};
+}
+struct Columns {
+  float R[8], P[8], Q[8];   // sums of dh, dh xh, t yh over the chunk's rows
+};
+// g = dh kh; t += pre'(g), and the columns' shares
+__device__ __forceinline__ void add_pre(const RowGradient& n, float* xv, const float* dh, const float* kh, float* t, bool live, Columns& s) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    xv[i] = (xv[i] - n.mean) * n.r;   // (past the row dh and the gains are 0, and t is not kept)
+    t[i] += n.r * (dh[i] * kh[i] - n.mg - xv[i] * n.mgx);
+    if (live) {
+      s.R[i] += dh[i];
+      s.P[i] = fmaf(dh[i], xv[i], s.P[i]);
+    }
   }
 }
 
-template <typename T, bool VEC, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 1024 : 256) rows_kernel(GatedNormArgs a, int lpr, int chunk_rows) {
-  __shared__ float2 red[16];
-  __shared__ float cols[WIDE ? 1 : 256 * 24];
+template <bool VEC>
+__device__ __forceinline__ void store_columns(const GatedNormArgs& a, int at, int lpr, const Columns& s) {
+  float* out = a.parts + (int64_t)blockIdx.x * 3 * a.D;
+  store8<float, VEC>(out, at, lpr, a.D, s.R);
+  store8<float, VEC>(out + a.D, at, lpr, a.D, s.P);
+  store8<float, VEC>(out + 2 * a.D, at, lpr, a.D, s.Q);
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_rows(const GatedNormArgs& a, int64_t row, int at, int lpr, float* xv, float* yv, float* t, float* dh) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) yv[i] = t[i] = dh[i] = 0.f;
+  load8<T, VEC>((const T*)a.x + row * a.x_row, at, lpr, a.D, xv);
+  if (a.y) load8<T, VEC>((const T*)a.y + row * a.y_row, at, lpr, a.D, yv);
+  if (a.dx_out) load8<T, VEC>((const T*)a.dx_out + row * a.x_row, at, lpr, a.D, t);
+  if (a.dh) load8<T, VEC>((const T*)a.dh + row * a.h_row, at, lpr, a.D, dh);
+}
+
+// Rows of up to 512 elements: groups of lpr lanes take a row each.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) rows_narrow(GatedNormArgs a, int lpr, int chunk_rows) {
+  __shared__ float cols[256 * 25];   // (25: an odd stride keeps lanes on different banks)
   int seq, chunk;
   if (!find_unit(a.nseq, blockIdx.x, [&](int i) { return cdiv(a.pr.count(i), chunk_rows); }, seq, chunk)) return;
   const int begin = a.pr.begin(seq) + chunk * chunk_rows;
   const int end = min(begin + chunk_rows, a.pr.begin(seq) + a.pr.count(seq));
-  const int D = a.D, groups = WIDE ? 1 : blockDim.x / lpr, l = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lpr - 1);
-  const int grp = WIDE ? 0 : threadIdx.x / lpr;
-  const int at = l < lpr ? place<VEC>(0, l, lpr) : a.D;
-  const int64_t mo = seq * a.mod_row;
-  float kh[8], ky[8], R[8], P[8], Q[8];   // (1 + scale) pre_w; gate post_w
+  const int D = a.D, groups = 256 / lpr, l = threadIdx.x & (lpr - 1), grp = threadIdx.x / lpr, at = place<VEC>(l);
+  float ky[8], kh[8];
+  gains<T, VEC>(a, seq * a.mod_row, at, lpr, ky, kh);
   bool in[8];
-  {
-    float w[8], m[8];
+  Columns cs;
 #pragma unroll
-    for (int i = 0; i < 8; i++) kh[i] = ky[i] = 1.f;
-    if (a.scale) {
-      load8<float, VEC>(a.scale + mo, at, lpr, D, m);
-#pragma unroll
-      for (int i = 0; i < 8; i++) kh[i] += m[i];
-    }
-    if (a.pre_w) {
-      load8<T, VEC>((const T*)a.pre_w, at, lpr, D, w);
-#pragma unroll
-      for (int i = 0; i < 8; i++) kh[i] *= w[i];
-    }
-    if (a.gate) {
-      load8<float, VEC>(a.gate + mo, at, lpr, D, m);
-#pragma unroll
-      for (int i = 0; i < 8; i++) ky[i] *= m[i];
-    }
-    if (a.post_w) {
-      load8<T, VEC>((const T*)a.post_w, at, lpr, D, w);
-#pragma unroll
-      for (int i = 0; i < 8; i++) ky[i] *= w[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      in[i] = VEC ? at < D : at + i * lpr < D;
-      R[i] = P[i] = Q[i] = 0.f;
-    }
+  for (int i = 0; i < 8; i++) {
+    in[i] = inside<VEC>(at, i, lpr, D);
+    cs.R[i] = cs.P[i] = cs.Q[i] = 0.f;
   }
   const float inv_d = 1.f / (float)D;
-  // (every group makes the same number of turns, so that barriers meet; a turn without a row works on the last one and keeps nothing)
+  // (a turn without a row works on the chunk's last one and keeps nothing: every lane takes part in the sums)
   for (int r0 = begin; r0 < end; r0 += groups) {
     const bool live = r0 + grp < end;
     const int64_t row = min(r0 + grp, end - 1);
     float xv[8], yv[8], t[8], dh[8];
-    load8<T, VEC>((const T*)a.x + row * a.x_row, at, lpr, D, xv);
-    if (a.y) load8<T, VEC>((const T*)a.y + row * a.y_row, at, lpr, D, yv);
-    if (a.dx_out) load8<T, VEC>((const T*)a.dx_out + row * a.x_row, at, lpr, D, t);
-    if (a.dh) load8<T, VEC>((const T*)a.dh + row * a.h_row, at, lpr, D, dh);
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      if (!a.y) yv[i] = 0.f;
-      if (!a.dx_out) t[i] = 0.f;
-      if (!a.dh) dh[i] = 0.f;
-    }
-    float u = 0.f, w = 0.f, mx = 0.f, my = 0.f, rx = 1.f, ry = 1.f;
-    if (a.pre == NORM_LAYER || a.post == NORM_LAYER) {
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        u += xv[i];
-        w += yv[i];
-      }
-      row_sums<WIDE>(u, w, lpr, red);
-      if (a.pre == NORM_LAYER) mx = u * inv_d;
-      if (a.post == NORM_LAYER) my = w * inv_d;
-    }
-    u = w = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      xv[i] = in[i] ? xv[i] - mx : 0.f;
-      yv[i] = in[i] ? yv[i] - my : 0.f;
-      u = fmaf(xv[i], xv[i], u);
-      w = fmaf(yv[i], yv[i], w);
-    }
-    if (a.pre != NORM_NONE || a.post != NORM_NONE) {
-      row_sums<WIDE>(u, w, lpr, red);
-      if (a.pre != NORM_NONE) rx = rsqrtf(u * inv_d + a.eps);
-      if (a.post != NORM_NONE) ry = rsqrtf(w * inv_d + a.eps);
-    }
+    load_rows<T, VEC>(a, row, at, lpr, xv, yv, t, dh);
     if (a.dh) {
-      u = w = 0.f;
-      float gx[8];
+      const Norm n = statistics<VEC>(a.pre, xv, a, at, lpr);
+      RowStats st{n.mean, n.r, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 8; i++) {
-        xv[i] *= rx;
-        gx[i] = dh[i] * kh[i];
-        u += gx[i];
-        w = fmaf(gx[i], xv[i], w);
+        const float g = dh[i] * kh[i];
+        st.sg += g;
+        st.c = fmaf(g, (xv[i] - n.mean) * n.r, st.c);
       }
-      if (a.pre != NORM_NONE) row_sums<WIDE>(u, w, lpr, red);
-      const float mg = a.pre == NORM_LAYER ? u * inv_d : 0.f, mgx = a.pre != NORM_NONE ? w * inv_d : 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        t[i] += rx * (gx[i] - mg - xv[i] * mgx);
-        if (live) {
-          R[i] += dh[i];
-          P[i] = fmaf(dh[i], xv[i], P[i]);
-        }
-      }
+      st.sg = lanes_sum(st.sg, lpr);
+      st.c = lanes_sum(st.c, lpr);
+      add_pre(row_gradient(a.pre, st, inv_d), xv, dh, kh, t, live, cs);
     }
     if (a.y) {
+      const Norm n = statistics<VEC>(a.post, yv, a, at, lpr);
+      float g[8], u = 0.f, w = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; i++) {
-        yv[i] *= ry;
-        if (live) Q[i] = fmaf(t[i], yv[i], Q[i]);
+        yv[i] = in[i] ? (yv[i] - n.mean) * n.r : 0.f;
+        if (live) cs.Q[i] = fmaf(t[i], yv[i], cs.Q[i]);
+        g[i] = in[i] ? t[i] * ky[i] : 0.f;
+        u += g[i];
+        w = fmaf(g[i], yv[i], w);
       }
       if (a.dy) {
-        float gy[8];
-        u = w = 0.f;
+        u = a.post == NORM_LAYER ? lanes_sum(u, lpr) * inv_d : 0.f;
+        w = a.post != NORM_NONE ? lanes_sum(w, lpr) * inv_d : 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-          gy[i] = in[i] ? t[i] * ky[i] : 0.f;
-          u += gy[i];
-          w = fmaf(gy[i], yv[i], w);
-        }
-        if (a.post != NORM_NONE) row_sums<WIDE>(u, w, lpr, red);
-        const float mg = a.post == NORM_LAYER ? u * inv_d : 0.f, mgy = a.post != NORM_NONE ? w * inv_d : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; i++) gy[i] = ry * (gy[i] - mg - yv[i] * mgy);
-        if (live) store8<T, VEC>((T*)a.dy + row * a.y_row, at, lpr, D, gy);
+        for (int i = 0; i < 8; i++) g[i] = n.r * (g[i] - u - yv[i] * w);
+        if (live) store8<T, VEC>((T*)a.dy + row * a.y_row, at, lpr, D, g);
       }
     }
     if (a.dx && live) {
@@ -339,35 +495,124 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) rows_kernel(GatedNormArgs a
     }
   }
   if (!a.parts) return;
-  float* out = a.parts + (int64_t)blockIdx.x * 3 * D;
-  if (!WIDE) {   // the groups of rows, in order
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    cols[threadIdx.x * 25 + i] = cs.R[i];
+    cols[threadIdx.x * 25 + 8 + i] = cs.P[i];
+    cols[threadIdx.x * 25 + 16 + i] = cs.Q[i];
+  }
+  __syncthreads();
+  if (grp > 0) return;
+  for (int g = 1; g < groups; g++)   // the groups in order
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      cols[threadIdx.x * 24 + i] = R[i];
-      cols[threadIdx.x * 24 + 8 + i] = P[i];
-      cols[threadIdx.x * 24 + 16 + i] = Q[i];
+      cs.R[i] += cols[(g * lpr + l) * 25 + i];
+      cs.P[i] += cols[(g * lpr + l) * 25 + 8 + i];
+      cs.Q[i] += cols[(g * lpr + l) * 25 + 16 + i];
     }
-    __syncthreads();
-    if (grp > 0) return;
-    for (int g = 1; g < groups; g++)
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        R[i] += cols[(g * lpr + l) * 24 + i];
-        P[i] += cols[(g * lpr + l) * 24 + 8 + i];
-        Q[i] += cols[(g * lpr + l) * 24 + 16 + i];
-      }
-  }
-  store8<float, VEC>(out, at, lpr, D, R);
-  store8<float, VEC>(out + D, at, lpr, D, P);
-  store8<float, VEC>(out + 2 * D, at, lpr, D, Q);
+  store_columns<VEC>(a, at, lpr, cs);
 }
 
-// Sums of the chunks of one sequence, 64 columns per workgroup, its 4 waves sharing the chunks:
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int lpr, int chunk_rows) {
+  __shared__ float4 redx[2][MAX_WAVES], redy[2][MAX_WAVES];
+  __shared__ float2 redg[2][MAX_WAVES];
+  int seq, chunk;
+  if (!find_unit(a.nseq, blockIdx.x, [&](int i) { return cdiv(a.pr.count(i), chunk_rows); }, seq, chunk)) return;
+  // every chunks-th row: the workgroups that run together then work on neighbouring rows
+  const int count_ = a.pr.count(seq), begin = a.pr.begin(seq) + chunk, end = a.pr.begin(seq) + count_, step = cdiv(count_, chunk_rows);
+  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = l < lpr ? place<VEC>(l) : D;
+  Raw<T, VEC> nx, ny, nt, nh;
+  auto fetch = [&](int64_t row) {
+    nx.load((const T*)a.x + row * a.x_row, at, lpr, D);
+    if (a.y) ny.load((const T*)a.y + row * a.y_row, at, lpr, D);
+    if (a.dx_out) nt.load((const T*)a.dx_out + row * a.x_row, at, lpr, D);
+    if (a.dh) nh.load((const T*)a.dh + row * a.h_row, at, lpr, D);
+  };
+  fetch(begin);
+  float ky[8], kh[8];
+  gains<T, VEC>(a, seq * a.mod_row, at, lpr, ky, kh);
+  bool in[8];
+  Columns cs;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    in[i] = inside<VEC>(at, i, lpr, D);
+    cs.R[i] = cs.P[i] = cs.Q[i] = 0.f;
+  }
+  if (l < 2 * MAX_WAVES) {
+    redx[l >> 4][l & 15] = redy[l >> 4][l & 15] = make_float4(0.f, 0.f, 0.f, 0.f);
+    redg[l >> 4][l & 15] = make_float2(0.f, 0.f);
+  }
+  __syncthreads();
+  const float counts = wave_count(VEC, lpr, D), count = lane_of(counts, wave), inv_d = 1.f / (float)D;
+  int turn = 0;   // (a buffer is written again two barriers after it was)
+  for (int64_t row = begin; row < end; row += step, turn ^= 1) {
+    float xv[8], yv[8], t[8], dh[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) yv[i] = t[i] = dh[i] = 0.f;
+    nx.get(xv);
+    if (a.y) ny.get(yv);
+    if (a.dx_out) nt.get(t);
+    if (a.dh) nh.get(dh);
+    if (row + step < end) fetch(row + step);
+    if (a.dh) {
+      float g[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) g[i] = dh[i] * kh[i];
+      const Moments m = wave_moments<true>(a.pre, xv, g, in, count);
+      if ((l & 63) == 63) redx[turn][wave] = make_float4(m.s, m.q, m.sg, m.c);
+    }
+    if (a.y && a.post != NORM_NONE) {
+      const Moments m = wave_moments<false>(a.post, yv, nullptr, in, count);
+      if ((l & 63) == 63) redy[turn][wave] = make_float4(m.s, m.q, 0.f, 0.f);
+    }
+    lds_barrier();
+    if (a.dh) add_pre(row_gradient(a.pre, join_moments<true>(a.pre, redx[turn], counts, inv_d, a.eps), inv_d), xv, dh, kh, t, true, cs);
+    if (a.dx) {
+      float o[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) o[i] = t[i] * a.alpha;
+      store8<T, VEC>((T*)a.dx + row * a.x_row, at, lpr, D, o);
+    }
+    if (!a.y) continue;
+    RowStats n{0.f, 1.f, 0.f, 0.f};
+    if (a.post != NORM_NONE) n = join_moments<false>(a.post, redy[turn], counts, inv_d, a.eps);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      yv[i] = (yv[i] - n.mean) * n.r;
+      cs.Q[i] = fmaf(t[i], yv[i], cs.Q[i]);
+      t[i] *= ky[i];   // (past the row ky is 0)
+    }
+    if (!a.dy) continue;
+    float u = 0.f, w = 0.f;
+    if (a.post != NORM_NONE) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        u += t[i];
+        w = fmaf(t[i], yv[i], w);
+      }
+      u = wave_total(u);
+      w = wave_total(w);
+      if ((l & 63) == 63) redg[turn][wave] = make_float2(u, w);
+      lds_barrier();
+      const float2 x = redg[turn][threadIdx.x & 15];
+      u = a.post == NORM_LAYER ? first_row_total(x.x) * inv_d : 0.f;
+      w = first_row_total(x.y) * inv_d;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) t[i] = n.r * (t[i] - u - yv[i] * w);
+    store8<T, VEC>((T*)a.dy + row * a.y_row, at, lpr, D, t);
+  }
+  if (a.parts) store_columns<VEC>(a, at, lpr, cs);
+}
+
+// Sums of the chunks of one sequence, 64 columns per workgroup, its 16 waves sharing the chunks:
 //   dshift = R, dscale = P pre_w, dgate = Q post_w.
 // P and Q stay behind for the weights' gradients (in the sequence's place after the chunks).
 template <typename T>
-__global__ void __launch_bounds__(256) columns_kernel(GatedNormArgs a, int chunk_rows) {
-  __shared__ float red[3][4][64];
+__global__ void __launch_bounds__(1024) columns_kernel(GatedNormArgs a, int chunk_rows) {
+  constexpr int WAVES = 16;
+  __shared__ float red[3][WAVES][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.D;
   const int blocks = cdiv(D, 64), seq = blockIdx.x / blocks, col = (blockIdx.x - seq * blocks) * 64 + lane;
   int64_t before = 0;
@@ -377,7 +622,7 @@ __global__ void __launch_bounds__(256) columns_kernel(GatedNormArgs a, int chunk
   const int n = (int)min((int64_t)cdiv(a.pr.count(seq), chunk_rows), a.chunks - before);
   float s[3] = {0.f, 0.f, 0.f};
   if (col < D)
-    for (int c = wave; c < n; c += 4) {
+    for (int c = wave; c < n; c += WAVES) {
       const float* p = a.parts + (before + c) * 3 * D + col;
 #pragma unroll
       for (int k = 0; k < 3; k++) s[k] += p[(int64_t)k * D];
@@ -386,8 +631,9 @@ __global__ void __launch_bounds__(256) columns_kernel(GatedNormArgs a, int chunk
   for (int k = 0; k < 3; k++) red[k][wave][lane] = s[k];
   __syncthreads();
   if (wave > 0 || col >= D) return;
+  for (int w = 1; w < WAVES; w++)
 #pragma unroll
-  for (int k = 0; k < 3; k++) s[k] = red[k][0][lane] + red[k][1][lane] + red[k][2][lane] + red[k][3][lane];
+    for (int k = 0; k < 3; k++) s[k] += red[k][w][lane];
   const int64_t at = seq * a.mod_row + col;
   if (a.dshift) a.dshift[at] = s[0];
   if (a.dscale) a.dscale[at] = a.pre_w ? s[1] * to_f32(((const T*)a.pre_w)[col]) : s[1];
@@ -428,54 +674,61 @@ int lanes_of(int D) {
   return l;
 }
 
-template <typename T, int CH>
-void forward_launch(const GatedNormArgs& a, hipStream_t s) {
-  const int lpr = lanes_of(a.D);
-  const int grid = cdiv(a.rows, 4 * (64 / lpr));
-  if (vectors(a)) forward_kernel<T, CH, true><<<grid, 256, 0, s>>>(a, lpr);
-  else forward_kernel<T, CH, false><<<grid, 256, 0, s>>>(a, lpr);
-}
-template <typename T>
-void forward_chunks(const GatedNormArgs& a, hipStream_t s) {
-  const int ch = cdiv(a.D, 512);
-  if (ch <= 1) forward_launch<T, 1>(a, s);
-  else if (ch <= 2) forward_launch<T, 2>(a, s);
-  else if (ch <= 4) forward_launch<T, 4>(a, s);
-  else if (ch <= 6) forward_launch<T, 6>(a, s);
-  else if (ch <= 8) forward_launch<T, 8>(a, s);
-  else forward_launch<T, 16>(a, s);
+// rows of up to 512 elements: lanes of a wave; longer ones: lanes of a workgroup
+bool narrow(int D) { return D <= 512; }
+int wide_threads(int D) { return cdiv(cdiv(D, 8), 64) * 64; }
+
+// Rows of a chunk of the backward pass: as many as let all chunks run at once (16 waves per CU, which their registers allow). Half as
+// many rows need a second round of workgroups for what the first leaves over (8 x about 1300 rows of 3072: CHUNK_COMPARISON),
+// and write twice the sums.
+int chunk_rows_of(int nseq, int rows, int D) {
+  const int waves = narrow(D) ? 4 : wide_threads(D) / 64, slots = 256 * std::max(16 / waves, 1);
+  return std::max(4, cdiv(rows, std::max(slots - nseq, slots / 2)));
 }
 
-// Rows of a chunk: enough chunks to fill the chip, long enough that their sums (3 fp32 rows out and in again) stay
-// small beside their rows.
-int chunk_rows_of(int rows) { return std::min(64, std::max(8, rows / 1024)); }
+// rows a workgroup walks forward: few, so that the workgroups are many rounds of the chip
+int forward_rows_of(int rows) { return std::min(8, std::max(1, rows / 1024)); }
+
+template <typename T>
+void forward_launch(const GatedNormArgs& a, hipStream_t s) {
+  const bool vec = vectors(a);
+  if (narrow(a.D)) {
+    const int lpr = lanes_of(a.D), grid = cdiv(a.rows, 4 * (64 / lpr));
+    if (vec) forward_narrow<T, true><<<grid, 256, 0, s>>>(a, lpr);
+    else forward_narrow<T, false><<<grid, 256, 0, s>>>(a, lpr);
+  } else {
+    const int cr = forward_rows_of(a.rows), grid = a.rows / cr + a.nseq, threads = wide_threads(a.D);
+    if (vec) forward_wide<T, true><<<grid, threads, 0, s>>>(a, cdiv(a.D, 8), cr);
+    else forward_wide<T, false><<<grid, threads, 0, s>>>(a, cdiv(a.D, 8), cr);
+  }
+}
 
 template <typename T>
 void rows_launch(const GatedNormArgs& a, hipStream_t s) {
-  const int lpr = a.D > 512 ? cdiv(a.D, 8) : lanes_of(a.D), cr = chunk_rows_of(a.rows);
+  const int cr = chunk_rows_of(a.nseq, a.rows, a.D);
   const bool vec = vectors(a);
-  if (a.D > 512) {
-    const int threads = cdiv(lpr, 64) * 64;
-    if (vec) rows_kernel<T, true, true><<<a.chunks, threads, 0, s>>>(a, lpr, cr);
-    else rows_kernel<T, false, true><<<a.chunks, threads, 0, s>>>(a, lpr, cr);
-  } else if (vec) {
-    rows_kernel<T, true, false><<<a.chunks, 256, 0, s>>>(a, lpr, cr);
+  if (narrow(a.D)) {
+    const int lpr = lanes_of(a.D);
+    if (vec) rows_narrow<T, true><<<a.chunks, 256, 0, s>>>(a, lpr, cr);
+    else rows_narrow<T, false><<<a.chunks, 256, 0, s>>>(a, lpr, cr);
   } else {
-    rows_kernel<T, false, false><<<a.chunks, 256, 0, s>>>(a, lpr, cr);
+    const int lpr = cdiv(a.D, 8), threads = wide_threads(a.D);
+    if (vec) rows_wide<T, true><<<a.chunks, threads, 0, s>>>(a, lpr, cr);
+    else rows_wide<T, false><<<a.chunks, threads, 0, s>>>(a, lpr, cr);
   }
 }
 
 }  // namespace
 
 hipError_t gated_norm_fwd(const GatedNormArgs& a, int dtype, hipStream_t s) {
-  if (dtype == DT_BF16) forward_chunks<u16>(a, s);
-  else forward_chunks<float>(a, s);
+  if (dtype == DT_BF16) forward_launch<u16>(a, s);
+  else forward_launch<float>(a, s);
   return hipGetLastError();
 }
 
-int gated_norm_chunks(int nseq, int rows) { return (int)std::min<int64_t>((int64_t)rows / chunk_rows_of(rows) + nseq, 0x7fffffff); }
+int gated_norm_chunks(int nseq, int rows, int D) { return rows / chunk_rows_of(nseq, rows, D) + nseq; }
 size_t gated_norm_ws(int nseq, int rows, int D) {
-  return ((size_t)gated_norm_chunks(nseq, rows) * 3 + 2 * (size_t)nseq) * D * 4;
+  return ((size_t)gated_norm_chunks(nseq, rows, D) * 3 + 2 * (size_t)nseq) * D * 4;
 }
 
 hipError_t gated_norm_rows_bwd(const GatedNormArgs& a, int dtype, hipStream_t s) {
@@ -486,10 +739,10 @@ hipError_t gated_norm_rows_bwd(const GatedNormArgs& a, int dtype, hipStream_t s)
 
 hipError_t gated_norm_columns_bwd(const GatedNormArgs& a, int dtype, hipStream_t s) {
   const int64_t grid = (int64_t)cdiv(a.D, 64) * a.nseq;
-  const int cr = chunk_rows_of(a.rows);
+  const int cr = chunk_rows_of(a.nseq, a.rows, a.D);
   if (grid == 0) {
-  } else if (dtype == DT_BF16) columns_kernel<u16><<<grid, 256, 0, s>>>(a, cr);
-  else columns_kernel<float><<<grid, 256, 0, s>>>(a, cr);
+  } else if (dtype == DT_BF16) columns_kernel<u16><<<grid, 1024, 0, s>>>(a, cr);
+  else columns_kernel<float><<<grid, 1024, 0, s>>>(a, cr);
   if (a.dpre_w || a.dpost_w) weights_kernel<<<cdiv(a.D, 256), 256, 0, s>>>(a);
   return hipGetLastError();
 }

@@ -97,7 +97,7 @@ struct GatedNormArgs {
   int chunks;     // upper bound on (sequence, chunk)
 };
 hipError_t gated_norm_fwd(const GatedNormArgs& a, int dtype, hipStream_t s);
-int gated_norm_chunks(int nseq, int rows);   // row chunks of the backward pass, at most
+int gated_norm_chunks(int nseq, int rows, int D);   // row chunks of the backward pass, at most
 size_t gated_norm_ws(int nseq, int rows, int D);
 hipError_t gated_norm_rows_bwd(const GatedNormArgs& a, int dtype, hipStream_t s);
 hipError_t gated_norm_columns_bwd(const GatedNormArgs& a, int dtype, hipStream_t s);
