@@ -1316,7 +1316,8 @@ size_t packed_forward_ws(const dit_packed_config* c) {
   size_t need = 0;
   const int tight = c->max_q > 0 ? std::min(c->max_q, c->total_q) : c->total_q;
   for (int most : {tight, std::min(tight, c->total_q / c->sequences)})
-    need = std::max(need, packed_plan(c->dtype, c->sequences, c->heads, c->kv_heads, c->head_dim, c->total_q, c->total_k, most).ws);
+    for (int keys : {c->total_k, c->total_k / c->sequences})
+      need = std::max(need, packed_plan(c->dtype, c->sequences, c->heads, c->kv_heads, c->head_dim, c->total_q, c->total_k, most, keys).ws);
   return al256(need);
 }
 
@@ -1381,7 +1382,7 @@ dit_status packed_attention(const dit_packed_config* c, const void* q, const voi
   // (the visible pairs are on the device: the class's flops count every pair of equal lengths)
   const double pairs = (double)c->total_q * c->total_k / c->sequences * (c->causal && c->total_q == c->total_k ? 0.5 : 1.0);
   TIMED("packed_attention", 4.0 * pairs * c->heads * c->head_dim, 0, hs(stream),
-        packed_attention_fwd(a, c->dtype, c->head_dim, c->total_k, ws, hs(stream)));
+        packed_attention_fwd(a, c->dtype, c->head_dim, ws, hs(stream)));
   return DIT_OK;
 }
 
@@ -1414,7 +1415,7 @@ dit_status packed_attention_backward(const dit_packed_config* c, const void* q, 
   TIMED("packed_attention_delta", 0, 2.0 * c->total_q * c->heads * c->head_dim * esize(c->dtype), hs(stream),
         packed_attention_delta(a, c->dtype, c->head_dim, ws, hs(stream)));
   TIMED("packed_attention_dkdv", 4 * product, 0, hs(stream),
-        packed_attention_dkdv(a, c->dtype, c->head_dim, c->total_k, ws, hs(stream)));
+        packed_attention_dkdv(a, c->dtype, c->head_dim, ws, hs(stream)));
   TIMED("packed_attention_dq", 3 * product, 0, hs(stream), packed_attention_dq(a, c->dtype, c->head_dim, ws, hs(stream)));
   return DIT_OK;
 }

@@ -111,8 +111,14 @@ __device__ __forceinline__ int sequence_of(const GatedNormArgs& a, int row) {
   }
   while (seq < a.nseq && a.pr.off[seq + 1] <= row) seq++;
   if (seq >= a.nseq) return -1;
-  const int b = a.pr.begin(seq);
-  return row >= b && row < b + a.pr.count(seq) ? seq : -1;
+  const RowSpan r = a.pr.span(seq);
+  return row >= r.begin && row < r.begin + r.count ? seq : -1;
+}
+
+// the sequence, and its chunk of chunk_rows rows, that this workgroup works on
+__device__ __forceinline__ bool find_chunk(const GatedNormArgs& a, int chunk_rows, int& seq, int& chunk, RowSpan& rows) {
+  return find_unit(a.nseq, blockIdx.x, [&](int i) { return a.pr.span(i); },
+                   [&](const RowSpan& r) { return cdiv(r.count, chunk_rows); }, seq, chunk, rows);
 }
 
 struct Norm {
@@ -329,9 +335,10 @@ template <typename T, bool VEC, bool FULL>
 __global__ void __launch_bounds__(1024) forward_wide(GatedNormArgs a, int lpr, int chunk_rows) {
   __shared__ float4 red[2][MAX_WAVES];
   int seq, chunk;
-  if (!find_unit(a.nseq, blockIdx.x, [&](int i) { return cdiv(a.pr.count(i), chunk_rows); }, seq, chunk)) return;
+  RowSpan rows;
+  if (!find_chunk(a, chunk_rows, seq, chunk, rows)) return;
   // every chunks-th row: the workgroups that run together then work on neighbouring rows
-  const int count_ = a.pr.count(seq), begin = a.pr.begin(seq) + chunk, end = a.pr.begin(seq) + count_, step = cdiv(count_, chunk_rows);
+  const int begin = rows.begin + chunk, end = rows.begin + rows.count, step = cdiv(rows.count, chunk_rows);
   const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = l < lpr ? place<VEC>(l) : D;
   const int64_t mo = seq * a.mod_row;
   const bool has_y = FULL || a.y, has_xo = FULL || a.x_out, has_h = FULL || a.h;
@@ -439,9 +446,9 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) rows_narrow(GatedNormArgs a, int lpr, int chunk_rows) {
   __shared__ float cols[256 * 25];   // (25: an odd stride keeps lanes on different banks)
   int seq, chunk;
-  if (!find_unit(a.nseq, blockIdx.x, [&](int i) { return cdiv(a.pr.count(i), chunk_rows); }, seq, chunk)) return;
-  const int begin = a.pr.begin(seq) + chunk * chunk_rows;
-  const int end = min(begin + chunk_rows, a.pr.begin(seq) + a.pr.count(seq));
+  RowSpan rows;
+  if (!find_chunk(a, chunk_rows, seq, chunk, rows)) return;
+  const int begin = rows.begin + chunk * chunk_rows, end = min(begin + chunk_rows, rows.begin + rows.count);
   const int D = a.D, groups = 256 / lpr, l = threadIdx.x & (lpr - 1), grp = threadIdx.x / lpr, at = place<VEC>(l);
   float ky[8], kh[8];
   gains<T, VEC>(a, seq * a.mod_row, at, lpr, ky, kh);
@@ -522,9 +529,10 @@ __global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int lpr, int 
   __shared__ float4 redx[2][MAX_WAVES], redy[2][MAX_WAVES];
   __shared__ float2 redg[2][MAX_WAVES];
   int seq, chunk;
-  if (!find_unit(a.nseq, blockIdx.x, [&](int i) { return cdiv(a.pr.count(i), chunk_rows); }, seq, chunk)) return;
+  RowSpan rows;
+  if (!find_chunk(a, chunk_rows, seq, chunk, rows)) return;
   // every chunks-th row: the workgroups that run together then work on neighbouring rows
-  const int count_ = a.pr.count(seq), begin = a.pr.begin(seq) + chunk, end = a.pr.begin(seq) + count_, step = cdiv(count_, chunk_rows);
+  const int begin = rows.begin + chunk, end = rows.begin + rows.count, step = cdiv(rows.count, chunk_rows);
   const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = l < lpr ? place<VEC>(l) : D;
   const bool has_y = FULL || a.y, has_dxo = FULL || a.dx_out, has_dh = FULL || a.dh, has_dx = FULL || a.dx, has_dy = FULL || a.dy;
   Raw<T, VEC> nx, ny, nt, nh;
@@ -621,10 +629,10 @@ __global__ void __launch_bounds__(1024) columns_kernel(GatedNormArgs a, int chun
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.D;
   const int blocks = cdiv(D, 64), seq = blockIdx.x / blocks, col = (blockIdx.x - seq * blocks) * 64 + lane;
   int64_t before = 0;
-  for (int i = lane; i < seq; i += 64) before += cdiv(a.pr.count(i), chunk_rows);
+  for (int i = lane; i < seq; i += 64) before += cdiv(a.pr.span(i).count, chunk_rows);
   for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
   // (offsets that are not increasing can promise more chunks than there are)
-  const int n = (int)min((int64_t)cdiv(a.pr.count(seq), chunk_rows), a.chunks - before);
+  const int n = (int)min((int64_t)cdiv(a.pr.span(seq).count, chunk_rows), a.chunks - before);
   float s[3] = {0.f, 0.f, 0.f};
   if (col < D)
     for (int c = wave; c < n; c += WAVES) {

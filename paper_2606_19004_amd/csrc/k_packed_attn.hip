@@ -21,29 +21,33 @@ namespace dit {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float M_FLOOR = -1e37f;   // running maximum of a row that has seen no key: finite, so differences are too
 
-// What a workgroup works on: rows [row0, row0 + rows of the tile) of sequence seq, key/value head g, keys
-// [key0, key1) of the n of the sequence.
+// What a workgroup works on: rows [ROWS rt, ...) of a sequence, key/value head g, part `part` of its keys.
 struct PackedTile {
-  int g, seq, rt, part, parts, m, n;
+  PackedSeq s;
+  int g, rt, part, parts;
   int64_t slot;   // of its partial result
   bool any;
 };
+__device__ __forceinline__ int parts_of(const PackedArgs& a, const PackedSeq& s) {
+  return a.part_tiles ? max(cdiv(cdiv(s.n, 64), a.part_tiles), 1) : 1;
+}
+template <int ROWS> __device__ __forceinline__ int row_tiles_of(const PackedArgs& a, const PackedSeq& s) {
+  return (s.m * a.G + ROWS - 1) / ROWS;
+}
 template <int ROWS>
 __device__ __forceinline__ PackedTile packed_tile(const PackedArgs& a) {
   PackedTile t{};
-  t.g = blockIdx.x % a.Hkv;
   const int u = blockIdx.x / a.Hkv;
+  t.g = blockIdx.x - u * a.Hkv;
   t.slot = (int64_t)t.g * a.units + u;
-  auto parts_of = [&](int i) { return a.part_tiles ? max(cdiv(cdiv(a.keys(i), 64), a.part_tiles), 1) : 1; };
-  int local;
-  t.any = find_unit(a.nseq, u, [&](int i) { return cdiv((int64_t)a.queries(i) * a.G, ROWS) * parts_of(i); }, t.seq, local);
+  int local, seq;
+  t.any = find_unit(a.nseq, u, [&](int i) { return a.sequence(i); },
+                    [&](const PackedSeq& s) { return row_tiles_of<ROWS>(a, s) * parts_of(a, s); }, seq, local, t.s);
   if (!t.any) return t;
-  t.m = __builtin_amdgcn_readfirstlane(a.queries(t.seq));
-  t.n = __builtin_amdgcn_readfirstlane(a.keys(t.seq));
-  t.parts = __builtin_amdgcn_readfirstlane(parts_of(t.seq));
+  t.parts = parts_of(a, t.s);
   t.rt = local / t.parts;
   t.part = local - t.rt * t.parts;
-  if (a.causal) t.rt = cdiv((int64_t)t.m * a.G, ROWS) - 1 - t.rt;   // the rows that see most keys first
+  if (a.causal) t.rt = row_tiles_of<ROWS>(a, t.s) - 1 - t.rt;   // the rows that see most keys first
   return t;
 }
 
@@ -59,16 +63,16 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
   if (!t.any) return;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int half = lane >> 5, l32 = lane & 31;
-  const int rows = t.m * a.G, row0 = t.rt * ROWS;
-  const int q0 = a.qr.begin(t.seq);
-  const int64_t k0 = a.kr.begin(t.seq);
+  const int rows = t.s.m * a.G, row0 = t.rt * ROWS;
+  const int q0 = t.s.q0;
+  const int64_t k0 = t.s.k0;
   const u16* Kg = (const u16*)a.k + k0 * a.k_row + (int64_t)t.g * a.k_head;
   const u16* Vg = (const u16*)a.v + k0 * a.v_row + (int64_t)t.g * a.v_head;
 
   // this lane's row and its Q fragments: q[row][16 s + 8 half + 0..7]; vis keys are visible to it
   const int row = min(row0 + wave * 32 + l32, rows - 1);
   const int tok = row / a.G, head = t.g * a.G + (row - tok * a.G);
-  const int vis = a.causal ? min(tok + t.n - t.m + 1, t.n) : t.n;
+  const int vis = a.causal ? min(tok + t.s.n - t.s.m + 1, t.s.n) : t.s.n;
   bf16x8 qf[NKS];
   {
     const u16* qrow = (const u16*)a.q + (int64_t)(q0 + tok) * a.q_row + (int64_t)head * a.q_head;
@@ -77,7 +81,7 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
   }
   // keys the tile needs: those of its last row; keys every row of this wave sees: those of its first
   const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
-  const int nvis = a.causal ? min(max(last_tok + t.n - t.m + 1, 0), t.n) : t.n;
+  const int nvis = a.causal ? min(max(last_tok + t.s.n - t.s.m + 1, 0), t.s.n) : t.s.n;
   const int all_vis = __builtin_amdgcn_readfirstlane(vis);
   int kt0 = 0, nt = cdiv(nvis, KB);
   if (PARTS) {
@@ -89,8 +93,8 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
   tk.init(wave, lane, a.k_row);
   tv.init(wave, lane, a.v_row);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
-  auto issue_k = [&](int kt) { tk.load(Kg + (int64_t)kt * KB * a.k_row, t.n - kt * KB, lds0 + (kt & 1) * TILE); };
-  auto issue_v = [&](int kt) { tv.load(Vg + (int64_t)kt * KB * a.v_row, t.n - kt * KB, lds0 + (2 + (kt & 1)) * TILE); };
+  auto issue_k = [&](int kt) { tk.load(Kg + (int64_t)kt * KB * a.k_row, t.s.n - kt * KB, lds0 + (kt & 1) * TILE); };
+  auto issue_v = [&](int kt) { tv.load(Vg + (int64_t)kt * KB * a.v_row, t.s.n - kt * KB, lds0 + (2 + (kt & 1)) * TILE); };
 
   // V^T fragment quarters: this lane points at 4 dims of key 4 half + (lane >> 2) % 4 of a step
   const int vkey = 4 * half + ((lane >> 2) & 3);
@@ -282,14 +286,14 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
   if (!t.any) return;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int l16 = lane & 15, g4 = lane >> 4;
-  const int rows = t.m * a.G, row0 = t.rt * ROWS;
-  const int q0 = a.qr.begin(t.seq);
-  const int64_t k0 = a.kr.begin(t.seq);
+  const int rows = t.s.m * a.G, row0 = t.rt * ROWS;
+  const int q0 = t.s.q0;
+  const int64_t k0 = t.s.k0;
   const float* Kg = (const float*)a.k + k0 * a.k_row + (int64_t)t.g * a.k_head;
   const float* Vg = (const float*)a.v + k0 * a.v_row + (int64_t)t.g * a.v_head;
   const int row = min(row0 + wave * 16 + l16, rows - 1);
   const int tok = row / a.G, head = t.g * a.G + (row - tok * a.G);
-  const int vis = a.causal ? min(tok + t.n - t.m + 1, t.n) : t.n;
+  const int vis = a.causal ? min(tok + t.s.n - t.s.m + 1, t.s.n) : t.s.n;
   f32x4 qf[NKC];   // scaled before the products, which may overflow without
   {
     const float* qrow = (const float*)a.q + (int64_t)(q0 + tok) * a.q_row + (int64_t)head * a.q_head;
@@ -301,7 +305,7 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
     }
   }
   const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
-  const int nvis = a.causal ? min(max(last_tok + t.n - t.m + 1, 0), t.n) : t.n;
+  const int nvis = a.causal ? min(max(last_tok + t.s.n - t.s.m + 1, 0), t.s.n) : t.s.n;
   int kt0 = 0, nt = cdiv(nvis, KB);
   if (a.part_tiles) {
     const int per = a.part_tiles * (64 / KB);
@@ -313,7 +317,7 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
   auto fetch = [&](int kt) {
 #pragma unroll
     for (int i = 0; i < CPT; i++) {
-      const int idx = tid + 256 * i, r = min(kt * KB + idx / (D / 4), t.n - 1), c = idx % (D / 4);
+      const int idx = tid + 256 * i, r = min(kt * KB + idx / (D / 4), t.s.n - 1), c = idx % (D / 4);
       rk[i] = *(const f32x4*)(Kg + r * a.k_row + 4 * c);
       rv[i] = *(const f32x4*)(Vg + r * a.v_row + 4 * c);
     }
@@ -324,7 +328,7 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
     for (int i = 0; i < CPT; i++) {
       const int idx = tid + 256 * i, r = idx / (D / 4), c = idx % (D / 4);
       *(f32x4*)(&sk[buf][r * LD + 4 * c]) = rk[i];
-      *(f32x4*)(&sv[buf][r * LD + 4 * c]) = kt * KB + r < t.n ? rv[i] : f32x4{0.f, 0.f, 0.f, 0.f};
+      *(f32x4*)(&sv[buf][r * LD + 4 * c]) = kt * KB + r < t.s.n ? rv[i] : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
   f32x4 o[NDB];
@@ -420,34 +424,34 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
 
 // ---------------------------------------------------------------------------
 // bf16, few rows: a new token (or a few) of each sequence against its keys, bound by reading K and V once. Tiles of 16 rows on
-// v_mfma_f32_16x16x32_bf16; the 4 waves of a workgroup do not share rows but keys: wave w takes the 32-key stages w, w + 4, ...
-// of the part with a running maximum, sum and output of its own, so no barrier stands in the loop, and the four meet
-// at the end. K goes to registers (a lane's 16 bytes are operand A as they stand), V straight to LDS for the
+// v_mfma_f32_16x16x32_bf16; the NW waves of a workgroup do not share rows but keys: wave w takes the 32-key stages w, w + NW, ...
+// of the part with a running maximum, sum and output of its own, so no barrier stands in the loop, and they meet at
+// the end. K goes to registers (a lane's 16 bytes are operand A as they stand), V straight to LDS for the
 // transposing read; both one stage ahead, 16 KB per wave in flight.
 // ---------------------------------------------------------------------------
-template <int D>
-__global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
+template <int D, int NW>
+__global__ void __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) packed_few_bf16(PackedArgs a) {
   constexpr int ROWS = 16, KB = 32, NKS = D / 32, NDB = D / 16;
   using Tile = RowTile<D, KB, 1>;
   constexpr int RB = Tile::RB, TILE = Tile::BYTES;
-  constexpr int MERGE = 4 * ROWS * (D + 4) * 4 + 4 * ROWS * 8;
-  constexpr int LDS = 8 * TILE > MERGE ? 8 * TILE : MERGE;
+  constexpr int MERGE = NW * ROWS * (D + 4) * 4 + NW * ROWS * 8;
+  constexpr int LDS = 2 * NW * TILE > MERGE ? 2 * NW * TILE : MERGE;
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ __attribute__((aligned(1024))) char smem[LDS];   // per wave [V0][V1]
   const PackedTile t = packed_tile<ROWS>(a);
   if (!t.any) return;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int l16 = lane & 15, g4 = lane >> 4;
-  const int rows = t.m * a.G, row0 = t.rt * ROWS;
-  const int q0 = a.qr.begin(t.seq);
-  const int64_t k0 = a.kr.begin(t.seq);
+  const int rows = t.s.m * a.G, row0 = t.rt * ROWS;
+  const int q0 = t.s.q0;
+  const int64_t k0 = t.s.k0;
   const u16* Kg = (const u16*)a.k + k0 * a.k_row + (int64_t)t.g * a.k_head;
   const u16* Vg = (const u16*)a.v + k0 * a.v_row + (int64_t)t.g * a.v_head;
   const int row = min(row0 + l16, rows - 1);
   const int tok = row / a.G, head = t.g * a.G + (row - tok * a.G);
-  const int vis = a.causal ? min(tok + t.n - t.m + 1, t.n) : t.n;
+  const int vis = a.causal ? min(tok + t.s.n - t.s.m + 1, t.s.n) : t.s.n;
   const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
-  const int nvis = a.causal ? min(max(last_tok + t.n - t.m + 1, 0), t.n) : t.n;
+  const int nvis = a.causal ? min(max(last_tok + t.s.n - t.s.m + 1, 0), t.s.n) : t.s.n;
   const int all_vis = __builtin_amdgcn_readfirstlane(vis);
   int begin = 0, end = nvis;
   if (a.part_tiles) {
@@ -489,7 +493,7 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
   auto step = [&](int key0, int buf, bf16x8 (*kf)[2], bf16x8 (*kn)[2]) {
     // the next stage's loads go out in any case, so that the number in flight is known: past the end they repeat the
     // last key and read no value
-    const int next = key0 + 4 * KB;
+    const int next = key0 + NW * KB;
     load_k(next, kn);
     f32x4 s[2];
 #pragma unroll
@@ -551,10 +555,10 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
     }
     while (key0 < end) {
       step(key0, 0, ka, kb);
-      key0 += 4 * KB;
+      key0 += NW * KB;
       if (key0 >= end) break;
       step(key0, 1, kb, ka);
-      key0 += 4 * KB;
+      key0 += NW * KB;
     }
   }
   wait_loads<0>();   // (loads past the end write their zeros to LDS too)
@@ -563,21 +567,21 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
   // the waves' results meet: [wave][row][D + 4] outputs, [wave][row] maxima and sums
   __syncthreads();
   float* mo = (float*)smem;
-  float2* ml = (float2*)(smem + 4 * ROWS * (D + 4) * 4);
+  float2* ml = (float2*)(smem + NW * ROWS * (D + 4) * 4);
 #pragma unroll
   for (int db = 0; db < NDB; db++) *(f32x4*)(mo + (wave * ROWS + l16) * (D + 4) + 16 * db + 4 * g4) = o[db];
   if (g4 == 0) ml[wave * ROWS + l16] = make_float2(m_run, l_run);
   __syncthreads();
-  constexpr int EPT = ROWS * D / 256;   // 8 or 4 elements of a row per thread
-  const int r = tid / (D / EPT), e0 = (tid % (D / EPT)) * EPT, rr = row0 + r;
-  if (rr >= rows) return;
+  constexpr int EPT = 8, LPR = D / EPT;   // elements of a row per thread, threads per row
+  const int r = tid / LPR, e0 = (tid % LPR) * EPT, rr = row0 + r;
+  if (r >= ROWS || rr >= rows) return;
   float m = M_FLOOR, l = 0.f, acc[EPT];
 #pragma unroll
-  for (int w = 0; w < 4; w++) m = fmaxf(m, ml[w * ROWS + r].x);
+  for (int w = 0; w < NW; w++) m = fmaxf(m, ml[w * ROWS + r].x);
 #pragma unroll
   for (int e = 0; e < EPT; e++) acc[e] = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; w++) {
+  for (int w = 0; w < NW; w++) {
     const float2 x = ml[w * ROWS + r];
     const float f = __builtin_amdgcn_exp2f(x.x - m);
     l = fmaf(f, x.y, l);
@@ -612,16 +616,20 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
   const int g = blockIdx.x % a.Hkv, u = blockIdx.x / a.Hkv;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int seq, rt;
-  if (!find_unit(a.nseq, u, [&](int i) { return cdiv((int64_t)a.queries(i) * a.G, ROWS); }, seq, rt)) return;
-  auto parts_of = [&](int i) { return max(cdiv(cdiv(a.keys(i), 64), a.part_tiles), 1); };
-  const int parts = parts_of(seq);
+  PackedSeq sq;
+  if (!find_unit(a.nseq, u, [&](int i) { return a.sequence(i); }, [&](const PackedSeq& s) { return row_tiles_of<ROWS>(a, s); }, seq, rt, sq))
+    return;
+  const int parts = parts_of(a, sq);
   if (parts <= 1) return;
   // units before this sequence's
   int64_t before = 0;
-  for (int i = lane; i < seq; i += 64) before += (int64_t)cdiv((int64_t)a.queries(i) * a.G, ROWS) * parts_of(i);
+  for (int i = lane; i < seq; i += 64) {
+    const PackedSeq s = a.sequence(i);
+    before += (int64_t)row_tiles_of<ROWS>(a, s) * parts_of(a, s);
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
-  const int m = a.queries(seq), rows = m * a.G, q0 = a.qr.begin(seq);
+  const int rows = sq.m * a.G, q0 = sq.q0;
   const int place = a.causal ? cdiv(rows, ROWS) - 1 - rt : rt;   // where the tile stands in the order of the units
   if (before + (int64_t)(place + 1) * parts > a.units) return;   // (offsets that are not increasing: no such units ran)
   const int64_t slot = ((int64_t)g * a.units + before + place * parts) * ROWS;
@@ -653,11 +661,13 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
 
 // Tiles and parts.
 //   rows   bf16: 16 where no sequence has more than FEW_ROWS (query, head) rows per key/value head, else 128; fp32: 64
-//   parts  16-row tiles: keys are shared out wherever sequences may have more than 1024, in parts that give the chip about
-//          four workgroups per CU, since lengths are unlike. Other tiles: only where they alone leave CUs without a
-//          workgroup.
-PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q) {
-  constexpr int CUS = 256, FEW_ROWS = 32;
+//   parts  16-row tiles: one CU streams keys at 60 GB/s (128 keys of K and V at head_dim 128 in 1.05 us, after 4.4 us for a call), and
+//          the launch that joins parts costs 4 us. So keys are shared out where a sequence may have more than 12 tiles, for about
+//          two workgroups per CU (32 tokens, 90 k keys of 8 heads: 80 us; four per CU: 88), in parts of at least 4 tiles (one
+//          token, 2048 keys: 11.4 us; 16 tiles: 16.7), or of 12 where the sequences alone fill the chip (32 tokens, 300 keys
+//          each: 11.2 us; 4 tiles: 15.5). Other tiles: only where they alone leave CUs without a workgroup.
+PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q, int max_k) {
+  constexpr int CUS = 256, FEW_ROWS = 32, MIN_PART = 4, WHOLE = 12;
   PackedPlan p{};
   const int G = H / Hkv;
   const bool few = (int64_t)max_q * G <= FEW_ROWS;
@@ -666,10 +676,10 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
   p.row_tiles = p.units = (int)std::min<int64_t>((int64_t)total_q * G / p.rows + nseq, nseq * per_seq);
   const int64_t groups = (int64_t)p.row_tiles * Hkv;
   if (groups == 0 || (!few && groups >= CUS)) return p;
-  const int64_t tiles = (int64_t)cdiv(total_k, 64), work = tiles * groups / nseq, goal = few ? 4 * CUS : 2 * CUS;
-  const int64_t per = std::max<int64_t>(few ? 16 : 4, (work + goal - 1) / goal);
+  const int64_t tiles = cdiv(total_k, 64), work = tiles * groups / nseq;
+  const int64_t per = std::max<int64_t>(groups < CUS ? MIN_PART : WHOLE, (work + 2 * CUS - 1) / (2 * CUS));
   const int64_t units = per_seq * (tiles / per + nseq);   // a sequence of n tiles has at most n / per + 1 parts
-  if (tiles <= per || (!few && units * Hkv > 16 * CUS)) return p;
+  if (cdiv(max_k, 64) <= std::max<int64_t>(WHOLE, per) || (!few && units * Hkv > 16 * CUS)) return p;
   p.part_tiles = (int)per;
   p.units = (int)units;
   p.ws = (size_t)Hkv * units * p.rows * (d + 1) * 4;
@@ -679,13 +689,13 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
 template <int D>
 static void fwd_launch(const PackedArgs& a, int dtype, int rows, int64_t grid, hipStream_t s) {
   if (dtype == DT_F32) packed_fwd_f32<D><<<grid, 256, 0, s>>>(a);
-  else if (rows == 16) packed_few_bf16<D><<<grid, 256, 0, s>>>(a);
+  else if (rows == 16) packed_few_bf16<D, 4><<<grid, 256, 0, s>>>(a);
   else if (a.part_tiles) packed_fwd_bf16<D, true><<<grid, 256, 0, s>>>(a);
   else packed_fwd_bf16<D, false><<<grid, 256, 0, s>>>(a);
 }
 
-hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s) {
-  const PackedPlan p = packed_plan(dtype, a.nseq, a.H, a.Hkv, d, a.qr.total, total_k, a.max_q);
+hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
+  const PackedPlan p = packed_plan(dtype, a.nseq, a.H, a.Hkv, d, a.qr.total, a.kr.total, a.max_q, a.kr.off ? a.kr.total : a.kr.len);
   if (p.row_tiles == 0) return hipSuccess;
   a.part_tiles = p.part_tiles;
   a.units = p.units;

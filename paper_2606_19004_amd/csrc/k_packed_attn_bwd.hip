@@ -83,6 +83,15 @@ __device__ __forceinline__ void store_columns(char* so, const f32x16* acc, float
   }
 }
 
+template <int ROWS> __device__ __forceinline__ bool find_row_tile(const PackedArgs& a, int& seq, int& tile, PackedSeq& s) {
+  return find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return a.sequence(i); },
+                   [&](const PackedSeq& x) { return (x.m * a.G + ROWS - 1) / ROWS; }, seq, tile, s);
+}
+template <int KEYS> __device__ __forceinline__ bool find_key_tile(const PackedArgs& a, int shares, int& seq, int& tile, PackedSeq& s) {
+  return find_unit(a.nseq, blockIdx.x / (a.Hkv * shares), [&](int i) { return a.sequence(i); },
+                   [&](const PackedSeq& x) { return (x.n + KEYS - 1) / KEYS; }, seq, tile, s);
+}
+
 // ---------------------------------------------------------------------------
 // dq: 128 query rows (row r: query r / G, head r % G of the group) against 64-key tiles
 // ---------------------------------------------------------------------------
@@ -95,15 +104,16 @@ __global__ void __launch_bounds__(256, 2) packed_dq_bf16(PackedArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];   // [K0][K1][V0][V1]
   const int g = blockIdx.x % a.Hkv;
   int seq, rt;
-  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv((int64_t)a.queries(i) * a.G, ROWS); }, seq, rt)) return;
-  const int m = __builtin_amdgcn_readfirstlane(a.queries(seq)), n = __builtin_amdgcn_readfirstlane(a.keys(seq));
+  PackedSeq sq;
+  if (!find_row_tile<ROWS>(a, seq, rt, sq)) return;
+  const int m = sq.m, n = sq.n;
   const int rows = m * a.G;
   if (a.causal) rt = cdiv(rows, ROWS) - 1 - rt;
   const int row0 = rt * ROWS;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int half = lane >> 5, l32 = lane & 31;
-  const int q0 = a.qr.begin(seq);
-  const int64_t k0 = a.kr.begin(seq);
+  const int q0 = sq.q0;
+  const int64_t k0 = sq.k0;
   const u16* Kg = (const u16*)a.k + k0 * a.k_row + (int64_t)g * a.k_head;
   const u16* Vg = (const u16*)a.v + k0 * a.v_row + (int64_t)g * a.v_head;
   const int row = min(row0 + wave * 32 + l32, rows - 1);
@@ -214,12 +224,13 @@ __global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
   __shared__ float4 stat[2][2][QB / 4];                            // lse (log2 units) and delta of a tile's rows
   const int g = blockIdx.x % a.Hkv;
   int seq, kt;
-  if (!find_unit(a.nseq, blockIdx.x / (a.Hkv * a.shares), [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  PackedSeq ps;
+  if (!find_key_tile<KEYS>(a, a.shares, seq, kt, ps)) return;
   const int share = blockIdx.x / a.Hkv % a.shares;
-  const int m = __builtin_amdgcn_readfirstlane(a.queries(seq)), n = __builtin_amdgcn_readfirstlane(a.keys(seq));
+  const int m = ps.m, n = ps.n;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int half = lane >> 5, l32 = lane & 31;
-  const int64_t q0 = a.qr.begin(seq), k0 = a.kr.begin(seq);
+  const int64_t q0 = ps.q0, k0 = ps.k0;
   const int key = kt * KEYS + wave * 32 + l32;
   bf16x8 kf[NKS];
   {
@@ -416,11 +427,12 @@ __global__ void __launch_bounds__(256) packed_dq_f32(PackedArgs a) {
   __shared__ __attribute__((aligned(16))) float sk[2][W::NROW * W::LD], sv[2][W::NROW * W::LD];
   const int g = blockIdx.x % a.Hkv;
   int seq, rt;
-  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv((int64_t)a.queries(i) * a.G, ROWS); }, seq, rt)) return;
-  const int m = a.queries(seq), n = a.keys(seq), rows = m * a.G;
+  PackedSeq sq;
+  if (!find_row_tile<ROWS>(a, seq, rt, sq)) return;
+  const int m = sq.m, n = sq.n, rows = m * a.G;
   if (a.causal) rt = cdiv(rows, ROWS) - 1 - rt;
   const int row0 = rt * ROWS, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
-  const int64_t q0 = a.qr.begin(seq), k0 = a.kr.begin(seq);
+  const int64_t q0 = sq.q0, k0 = sq.k0;
   const float* Kg = (const float*)a.k + k0 * a.k_row + (int64_t)g * a.k_head;
   const float* Vg = (const float*)a.v + k0 * a.v_row + (int64_t)g * a.v_head;
   const int row = min(row0 + wave * 16 + l16, rows - 1);
@@ -481,11 +493,12 @@ __global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
   __shared__ __attribute__((aligned(16))) float sq[2][W::NROW * W::LD], sd[2][W::NROW * W::LD];
   const int g = blockIdx.x % a.Hkv;
   int seq, kt;
-  if (!find_unit(a.nseq, blockIdx.x / (a.Hkv * a.shares), [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
+  PackedSeq ps;
+  if (!find_key_tile<KEYS>(a, a.shares, seq, kt, ps)) return;
   const int share = blockIdx.x / a.Hkv % a.shares;
-  const int m = a.queries(seq), n = a.keys(seq);
+  const int m = ps.m, n = ps.n;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
-  const int64_t q0 = a.qr.begin(seq), k0 = a.kr.begin(seq);
+  const int64_t q0 = ps.q0, k0 = ps.k0;
   const int key = kt * KEYS + wave * 16 + l16;
   f32x4 kf[NKC], vf[NKC];
   {
@@ -561,9 +574,10 @@ __global__ void __launch_bounds__(256) shares_join(PackedArgs a) {
   constexpr int KEYS = 64, LPR = D / 4;
   const int g = blockIdx.x % a.Hkv;
   int seq, kt;
-  if (!find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return cdiv(a.keys(i), KEYS); }, seq, kt)) return;
-  const int n = a.keys(seq), e = 4 * (threadIdx.x % LPR);
-  const int64_t k0 = a.kr.begin(seq);
+  PackedSeq ps;
+  if (!find_key_tile<KEYS>(a, 1, seq, kt, ps)) return;
+  const int n = ps.n, e = 4 * (threadIdx.x % LPR);
+  const int64_t k0 = ps.k0;
   for (int r = threadIdx.x / LPR; r < KEYS && kt * KEYS + r < n; r += 256 / LPR) {
     const int64_t key = k0 + kt * KEYS + r;
     float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -624,7 +638,8 @@ static void dkdv_launch(const PackedArgs& a, int dtype, int64_t units, int64_t j
   if (dtype == DT_BF16) shares_join<u16, D><<<joins, 256, 0, s>>>(a);
   else shares_join<float, D><<<joins, 256, 0, s>>>(a);
 }
-hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s) {
+hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
+  const int total_k = a.kr.total;
   if (total_k == 0) return hipSuccess;
   a.delta = (float*)ws;
   a.shares = shares_of(dtype, a.nseq, a.H, a.Hkv, a.qr.total, total_k, a.causal);

@@ -6,17 +6,25 @@
 namespace dit {
 
 // Rows of the sequences of a packed tensor: offsets on the device, or equal lengths (off null).
+struct RowSpan {
+  int begin, count;
+};
 struct PackedRows {
   const int* off;
   int total, len;   // rows of the tensor; of each sequence where off is null
-  __device__ __forceinline__ int begin(int i) const { return off ? min(max(off[i], 0), total) : i * len; }
-  __device__ __forceinline__ int count(int i) const {
-    if (!off) return len;
-    const int b = min(max(off[i], 0), total);
-    return max(min(off[i + 1], total), b) - b;
+  // the offsets' two entries as loaded, so that a caller's loads can all go out before the first is looked at
+  __device__ __forceinline__ int2 raw(int i) const { return off ? make_int2(off[i], off[i + 1]) : make_int2(i * len, (i + 1) * len); }
+  __device__ __forceinline__ RowSpan clamped(int2 r) const {
+    const int b = min(max(r.x, 0), total);
+    return RowSpan{b, max(min(r.y, total), b) - b};
   }
+  __device__ __forceinline__ RowSpan span(int i) const { return clamped(raw(i)); }
 };
 
+// A sequence's queries q0 .. q0 + m and keys k0 .. k0 + n.
+struct PackedSeq {
+  int q0, m, k0, n;
+};
 struct PackedArgs {
   const void* q; const void* k; const void* v; void* o;
   float* lse;                       // [total_q][H], null: not wanted (forward)
@@ -33,22 +41,29 @@ struct PackedArgs {
   const void* d_o; void* dq; void* dk; void* dv;
   float* delta;                     // [total_q][H] rowsum(d_o o)
   int shares; float* share_sums;    // workgroups that share a key tile's rows, and their sums
-  __device__ __forceinline__ int queries(int i) const { return min(qr.count(i), max_q); }
-  __device__ __forceinline__ int keys(int i) const {
-    const int c = kr.count(i);
-    return k_len ? min(max(k_len[i], 0), c) : c;
+  __device__ __forceinline__ PackedSeq sequence(int i) const {
+    const int2 q = qr.raw(i), k = kr.raw(i);
+    const int used = k_len ? k_len[i] : 0x7fffffff;
+    const RowSpan qs = qr.clamped(q), ks = kr.clamped(k);
+    return PackedSeq{qs.begin, min(qs.count, max_q), ks.begin, min(max(used, 0), ks.count)};
   }
 };
 
-// The sequence that unit u belongs to, where sequence i has count(i) units, and u's place in it. Every wave finds it by
-// itself, 64 sequences at a time: no host-made list of tiles, no empty workgroups where lengths are unlike.
-template <typename F>
-__device__ __forceinline__ bool find_unit(int nseq, int u, F&& count, int& seq, int& local) {
+// The sequence that unit u belongs to, where a sequence with what = load(i) (a struct of int) has count(what) units, and u's place
+// in it. Every wave finds it by itself, 64 sequences at a time: no host-made list of tiles, no empty workgroups where
+// lengths are unlike. What is known of the sequence comes from the lane that looked at it, with no further loads.
+template <typename S, typename L, typename C>
+__device__ __forceinline__ bool find_unit(int nseq, int u, L&& load, C&& count, int& seq, int& local, S& what) {
   const int lane = threadIdx.x & 63;
   unsigned carry = 0;   // <= u
   for (int base = 0; base < nseq; base += 64) {
-    // (no count of a tensor within the entry points' limits is larger, and 64 of these fit)
-    const unsigned c = base + lane < nseq ? min(count(base + lane), 1 << 25) : 0;
+    S mine{};
+    unsigned c = 0;
+    if (base + lane < nseq) {
+      mine = load(base + lane);
+      // (no count of a tensor within the entry points' limits is larger, and 64 of these fit)
+      c = min(count(mine), 1 << 25);
+    }
     unsigned incl = c;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -60,6 +75,14 @@ __device__ __forceinline__ bool find_unit(int nseq, int u, F&& count, int& seq, 
       const int l = __builtin_ctzll(__ballot(carry + incl > (unsigned)u));
       seq = base + l;
       local = u - (int)(carry + __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l));
+      union {
+        S s;
+        int w[sizeof(S) / 4];
+      } in, out;
+      in.s = mine;
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof(S) / 4); i++) out.w[i] = __builtin_amdgcn_readlane(in.w[i], l);
+      what = out.s;
       return true;
     }
     carry += total;
@@ -74,11 +97,11 @@ struct PackedPlan {
   int row_tiles, units;
   size_t ws;        // bytes
 };
-PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q);
-hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s);
+PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q, int max_k);
+hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 size_t packed_backward_ws(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal);
 hipError_t packed_attention_delta(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
-hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, int total_k, void* ws, hipStream_t s);
+hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 hipError_t packed_attention_dq(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 
 enum NormKind { NORM_NONE = 0, NORM_LAYER = 1, NORM_RMS = 2 };

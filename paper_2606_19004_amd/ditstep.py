@@ -145,8 +145,14 @@ def _ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
+# the current stream's handle without a Stream object around it (2.5 us of a call's host time)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _s(stream) -> int | None:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
