@@ -68,24 +68,21 @@ template <bool VEC> __device__ __forceinline__ bool inside(int at, int i, int lp
 // ky = gate post_w, kh = (1 + scale) pre_w; 0 past the row
 template <typename T, bool VEC>
 __device__ __forceinline__ void gains(const GatedNormArgs& a, int64_t mo, int at, int lpr, float* ky, float* kh) {
-  float m[8];
+  // (all loads go out before the first is used)
+  float pw[8], rw[8];
 #pragma unroll
-  for (int i = 0; i < 8; i++) ky[i] = kh[i] = 1.f;
+  for (int i = 0; i < 8; i++) {
+    ky[i] = pw[i] = rw[i] = 1.f;
+    kh[i] = 0.f;
+  }
   if (a.gate) load8<float, VEC>(a.gate + mo, at, lpr, a.D, ky);
-  if (a.post_w) {
-    load8<T, VEC>((const T*)a.post_w, at, lpr, a.D, m);
+  if (a.scale) load8<float, VEC>(a.scale + mo, at, lpr, a.D, kh);
+  if (a.post_w) load8<T, VEC>((const T*)a.post_w, at, lpr, a.D, pw);
+  if (a.pre_w) load8<T, VEC>((const T*)a.pre_w, at, lpr, a.D, rw);
 #pragma unroll
-    for (int i = 0; i < 8; i++) ky[i] *= m[i];
-  }
-  if (a.scale) {
-    load8<float, VEC>(a.scale + mo, at, lpr, a.D, m);
-#pragma unroll
-    for (int i = 0; i < 8; i++) kh[i] += m[i];
-  }
-  if (a.pre_w) {
-    load8<T, VEC>((const T*)a.pre_w, at, lpr, a.D, m);
-#pragma unroll
-    for (int i = 0; i < 8; i++) kh[i] *= m[i];
+  for (int i = 0; i < 8; i++) {
+    ky[i] *= pw[i];
+    kh[i] = (1.f + kh[i]) * rw[i];
   }
 #pragma unroll
   for (int i = 0; i < 8; i++)
@@ -696,7 +693,7 @@ int wide_threads(int D) { return cdiv(cdiv(D, 8), 64) * 64; }
 // and write twice the sums.
 int chunk_rows_of(int nseq, int rows, int D) {
   const int waves = narrow(D) ? 4 : wide_threads(D) / 64, slots = 256 * std::max(16 / waves, 1);
-  return std::max(4, cdiv(rows, std::max(slots - nseq, slots / 2)));
+  return std::max(8, cdiv(rows, std::max(slots - nseq, slots / 2)));
 }
 
 // rows a workgroup walks forward: few, so that the workgroups are many rounds of the chip

@@ -39,7 +39,7 @@ struct PackedArgs {
   int row_tiles;                    // upper bound on (sequence, row tile) per key/value head
   // backward
   const void* d_o; void* dq; void* dk; void* dv;
-  float* delta;                     // [total_q][H] rowsum(d_o o)
+  float2* stats;                    // [H][total_q] (lse in log2 units, rowsum(d_o o))
   int shares; float* share_sums;    // workgroups that share a key tile's rows, and their sums
   __device__ __forceinline__ PackedSeq sequence(int i) const {
     const int2 q = qr.raw(i), k = kr.raw(i);
@@ -100,7 +100,7 @@ struct PackedPlan {
 PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q, int max_k);
 hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 size_t packed_backward_ws(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal);
-hipError_t packed_attention_delta(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
+hipError_t packed_attention_stats(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 hipError_t packed_attention_dq(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 
