@@ -111,6 +111,8 @@ SHAPES = [
     (4, 2, [70, 9, 4], [33, 0, 1], True),
     (2, 1, [5, 0, 3], [0, 40, 100], False),
     (1, 1, [300], [257], True),
+    (4, 1, [700], None, True),
+    (8, 1, [300, 90], None, False),
 ]
 
 
