@@ -145,14 +145,15 @@ def _ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
-# the current stream's handle without a Stream object around it (2.5 us of a call's host time)
+# the current device, and its current stream's handle without a Stream object around it (2.5 us of a call's host time)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _s(stream) -> int | None:
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
@@ -319,8 +320,24 @@ def dit_denoise_step_teacache(cfg, sw, blocks, t, t_next, noise_level, latent, x
 NORM_KINDS = {"none": 0, "layer": 1, "rms": 2}
 
 
+def _elsewhere(t, dev):
+    raise ValueError(f"a tensor on {t.device} in a call on cuda:{dev}")
+
+
+def _here(*tensors):
+    """Device pointers of tensors that have to be on the current device (its stream runs the call)."""
+    dev = _current_device()
+    return [None if t is None else t.data_ptr() if t.get_device() == dev else _elsewhere(t, dev) for t in tensors]
+
+
+def _typed(dtype, *tensors):
+    for t in tensors:
+        if t is not None and t.dtype is not dtype:
+            raise ValueError(f"a tensor of {t.dtype} where {dtype} is wanted")
+
+
 def _ws_args(ws):
-    return (_ptr(ws), ws.numel() if ws is not None else 0)
+    return (*_here(ws), ws.numel() if ws is not None else 0)
 
 
 def packed_config(q, k, v, o, sequences, causal=False, scale=None, max_q=0) -> PackedConfig:
@@ -347,8 +364,9 @@ def packed_attention_workspace_bytes(cfg) -> int:
 
 def packed_attention(cfg, q, k, v, o, lse=None, q_offsets=None, k_offsets=None, k_lengths=None, ws=None, stream=None):
     """Tensors laid out as those cfg was made from; offsets and lengths: device int32, or None (equal lengths)."""
-    _check(_lib.packed_attention(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(q_offsets), _ptr(k_offsets),
-                                 _ptr(k_lengths), _ptr(o), _ptr(lse), *_ws_args(ws), _s(stream)))
+    _typed(torch.int32, q_offsets, k_offsets, k_lengths)
+    _check(_lib.packed_attention(C.byref(cfg), *_here(q, k, v, q_offsets, k_offsets, k_lengths, o, lse), *_ws_args(ws),
+                                 _s(stream)))
 
 
 def packed_attention_backward_workspace_bytes(cfg) -> int:
@@ -358,9 +376,9 @@ def packed_attention_backward_workspace_bytes(cfg) -> int:
 def packed_attention_backward(cfg, q, k, v, o, lse, d_o, dq, dk, dv, q_offsets=None, k_offsets=None, k_lengths=None,
                               ws=None, stream=None):
     """d_o laid out like o, dq, dk, dv like q, k, v."""
-    _check(_lib.packed_attention_backward(C.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o),
-                                          _ptr(q_offsets), _ptr(k_offsets), _ptr(k_lengths), _ptr(dq), _ptr(dk),
-                                          _ptr(dv), *_ws_args(ws), _s(stream)))
+    _typed(torch.int32, q_offsets, k_offsets, k_lengths)
+    _check(_lib.packed_attention_backward(C.byref(cfg), *_here(q, k, v, o, lse, d_o, q_offsets, k_offsets, k_lengths, dq,
+                                                               dk, dv), *_ws_args(ws), _s(stream)))
 
 
 def gated_norm_config(x, sequences, post="none", pre="layer", eps=1e-6, residual_scale=1.0, y_row=None, h_row=None,
@@ -377,8 +395,10 @@ def gated_norm_config(x, sequences, post="none", pre="layer", eps=1e-6, residual
 
 def gated_norm(cfg, x, y, x_out, h, gate=None, scale=None, shift=None, post_w=None, pre_w=None, offsets=None,
                stream=None):
-    _check(_lib.gated_norm(C.byref(cfg), _ptr(x), _ptr(y), _ptr(post_w), _ptr(pre_w), _ptr(gate), _ptr(scale),
-                           _ptr(shift), _ptr(offsets), _ptr(x_out), _ptr(h), _s(stream)))
+    """gate, scale, shift: fp32 [sequences][hidden] at cfg's mod_row; offsets: device int32, or None (equal lengths)."""
+    _typed(torch.int32, offsets)
+    _typed(torch.float32, gate, scale, shift)
+    _check(_lib.gated_norm(C.byref(cfg), *_here(x, y, post_w, pre_w, gate, scale, shift, offsets, x_out, h), _s(stream)))
 
 
 def gated_norm_backward_workspace_bytes(cfg) -> int:
@@ -388,10 +408,10 @@ def gated_norm_backward_workspace_bytes(cfg) -> int:
 def gated_norm_backward(cfg, x_out, y, dx_out, dh, dx, dy, gate=None, scale=None, post_w=None, pre_w=None, offsets=None,
                         dgate=None, dscale=None, dshift=None, dpost_w=None, dpre_w=None, ws=None, stream=None):
     """x_out: the forward call's output. Any gradient may be None."""
-    _check(_lib.gated_norm_backward(C.byref(cfg), _ptr(x_out), _ptr(y), _ptr(post_w), _ptr(pre_w), _ptr(gate),
-                                    _ptr(scale), _ptr(offsets), _ptr(dx_out), _ptr(dh), _ptr(dx), _ptr(dy),
-                                    _ptr(dgate), _ptr(dscale), _ptr(dshift), _ptr(dpost_w), _ptr(dpre_w),
-                                    *_ws_args(ws), _s(stream)))
+    _typed(torch.int32, offsets)
+    _typed(torch.float32, gate, scale, dgate, dscale, dshift, dpost_w, dpre_w)
+    _check(_lib.gated_norm_backward(C.byref(cfg), *_here(x_out, y, post_w, pre_w, gate, scale, offsets, dx_out, dh, dx, dy,
+                                                         dgate, dscale, dshift, dpost_w, dpre_w), *_ws_args(ws), _s(stream)))
 
 
 def flow_policy_loss_workspace_bytes(batch, n_per_sample) -> int:
@@ -406,9 +426,11 @@ def flow_policy_loss(x, v, x_next, logp_old, adv, t, t_next, noise_level, loss, 
     n = x.numel() // b if b else 0
     if logp_scale is None:
         logp_scale = 1.0 / max(n, 1)
-    _check(_lib.flow_policy_loss(_ptr(x), _ptr(v), _ptr(x_next), _ptr(v_ref), b, n, t, t_next, noise_level,
-                                 _ptr(logp_old), _ptr(adv), logp_scale, clip_low, clip_high, kl_weight, _ptr(loss),
-                                 _ptr(logp), _ptr(ratio), _ptr(dv), *_ws_args(ws), _s(stream)))
+    _typed(torch.float32, x, v, x_next, v_ref, adv, dv)
+    _typed(torch.float64, logp_old, loss, logp, ratio)
+    px, pv, pn, pr, old, pa, *outs = _here(x, v, x_next, v_ref, logp_old, adv, loss, logp, ratio, dv)
+    _check(_lib.flow_policy_loss(px, pv, pn, pr, b, n, t, t_next, noise_level, old, pa, logp_scale, clip_low, clip_high,
+                                 kl_weight, *outs, *_ws_args(ws), _s(stream)))
 
 
 def dit_profile_begin():

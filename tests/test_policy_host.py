@@ -126,3 +126,23 @@ def test_python_configs_check_shapes():
     with pytest.raises(ValueError):
         d.gated_norm_config(torch.zeros(4, 8).t(), 1)
     assert d.gated_norm_config(torch.zeros(4, 8), 2).mod_row == 8
+
+
+def test_python_calls_check_types_and_places(monkeypatch):
+    """Tensors of another type, and tensors that are not on the current device, are refused before the library is called."""
+    import torch
+    monkeypatch.setattr(d, "_current_device", lambda: 0)
+    q = torch.zeros(4, 2, 64)
+    cfg = d.packed_config(q, q, q, q, 2)
+    with pytest.raises(ValueError, match="int32"):
+        d.packed_attention(cfg, q, q, q, q, q_offsets=torch.zeros(3, dtype=torch.int64))
+    with pytest.raises(ValueError, match="on cpu"):
+        d.packed_attention(cfg, q, q, q, q)
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="float32"):
+        d.gated_norm(d.gated_norm_config(x, 2), x, x, x, x, gate=torch.zeros(2, 8).double())
+    with pytest.raises(ValueError, match="on cpu"):
+        d.gated_norm_backward(d.gated_norm_config(x, 2), x, x, x, x, x, x)
+    one = torch.zeros(4)
+    with pytest.raises(ValueError, match="float64"):
+        d.flow_policy_loss(x, x, x, one, one, 0.5, 0.4, 0.7, one)
