@@ -10,64 +10,102 @@
 namespace dit {
 namespace {
 
-// The 8 elements of a row that a lane holds: successive ones (VEC: D a multiple of 8, everything 16-byte aligned) or ones
-// that are `step` apart.
+// The 8 successive elements of a row that a lane holds. VEC: D is a multiple of 8 and everything 16-byte aligned. Otherwise the lane
+// at the row's end takes its elements one by one, and the others 16 bytes at the alignment of an element, which the memory unit allows.
+typedef unsigned u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void unpack8(const uint32_t* w, float* f) {
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8_any(const u16* p, float* f) {
+  const u32x4_any2 u = *(const u32x4_any2*)p;
+  const uint32_t w[4] = {u[0], u[1], u[2], u[3]};
+  unpack8(w, f);
+}
+__device__ __forceinline__ void load8_any(const float* p, float* f) {
+  const f32x4_any4 u = *(const f32x4_any4*)p, v = *(const f32x4_any4*)(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    f[i] = u[i];
+    f[4 + i] = v[i];
+  }
+}
+__device__ __forceinline__ void store8_any(u16* p, const float* f) {
+  *(u32x4_any2*)p = u32x4_any2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
+}
+__device__ __forceinline__ void store8_any(float* p, const float* f) {
+  *(f32x4_any4*)p = f32x4_any4{f[0], f[1], f[2], f[3]};
+  *(f32x4_any4*)(p + 4) = f32x4_any4{f[4], f[5], f[6], f[7]};
+}
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, int at, int step, int D, float* f) {
+__device__ __forceinline__ void load8(const T* p, int at, int D, float* f) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) f[i] = 0.f;
   if (VEC) {
     if (at < D) {
       load4<T>(p + at, f);
       load4<T>(p + at + 4, f + 4);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; i++) f[i] = 0.f;
     }
+  } else if (at + 8 <= D) {
+    load8_any(p + at, f);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++) f[i] = at + i * step < D ? to_f32(p[at + i * step]) : 0.f;
+    for (int i = 0; i < 8; i++)
+      if (at + i < D) f[i] = to_f32(p[at + i]);
   }
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, int at, int step, int D, const float* f) {
+__device__ __forceinline__ void store8(T* p, int at, int D, const float* f) {
   if (VEC) {
     if (at < D) {
       store4<T>(p + at, f);
       store4<T>(p + at + 4, f + 4);
     }
+  } else if (at + 8 <= D) {
+    store8_any(p + at, f);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; i++)
-      if (at + i * step < D) p[at + i * step] = from_f32<T>(f[i]);
+      if (at + i < D) p[at + i] = from_f32<T>(f[i]);
   }
 }
 // The same as it was loaded: a row on its way while the one before it is worked on.
 template <typename T, bool VEC> struct Raw {
   float f[8];
-  __device__ __forceinline__ void load(const T* p, int at, int step, int D) { load8<T, VEC>(p, at, step, D, f); }
+  __device__ __forceinline__ void load(const T* p, int at, int D) { load8<T, VEC>(p, at, D, f); }
   __device__ __forceinline__ void get(float* o) const {
 #pragma unroll
     for (int i = 0; i < 8; i++) o[i] = f[i];
   }
 };
-template <> struct Raw<u16, true> {
-  uint4 u;
-  __device__ __forceinline__ void load(const u16* p, int at, int, int D) { u = at < D ? *(const uint4*)(p + at) : make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float* o) const {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+template <bool VEC> struct Raw<u16, VEC> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const u16* p, int at, int D) {
+    w[0] = w[1] = w[2] = w[3] = 0;
+    if (at + 8 <= D) {
+      if constexpr (VEC) {
+        const uint4 u = *(const uint4*)(p + at);
+        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+      } else {
+        const u32x4_any2 u = *(const u32x4_any2*)(p + at);
+        w[0] = u[0]; w[1] = u[1]; w[2] = u[2]; w[3] = u[3];
+      }
+    } else if (!VEC) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      o[2 * i] = __uint_as_float(w[i] << 16);
-      o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      for (int i = 0; i < 8; i++)
+        if (at + i < D) w[i / 2] |= (uint32_t)p[at + i] << (16 * (i & 1));
     }
   }
+  __device__ __forceinline__ void get(float* o) const { unpack8(w, o); }
 };
 
-// place of a lane's first element, and whether its element i is one of the row's D
-template <bool VEC> __device__ __forceinline__ int place(int l) { return VEC ? l * 8 : l; }
-template <bool VEC> __device__ __forceinline__ bool inside(int at, int i, int lpr, int D) { return VEC ? at < D : at + i * lpr < D; }
 // ky = gate post_w, kh = (1 + scale) pre_w; 0 past the row
 template <typename T, bool VEC>
-__device__ __forceinline__ void gains(const GatedNormArgs& a, int64_t mo, int at, int lpr, float* ky, float* kh) {
+__device__ __forceinline__ void gains(const GatedNormArgs& a, int64_t mo, int at, float* ky, float* kh) {
   // (all loads go out before the first is used)
   float pw[8], rw[8];
 #pragma unroll
@@ -75,10 +113,10 @@ __device__ __forceinline__ void gains(const GatedNormArgs& a, int64_t mo, int at
     ky[i] = pw[i] = rw[i] = 1.f;
     kh[i] = 0.f;
   }
-  if (a.gate) load8<float, VEC>(a.gate + mo, at, lpr, a.D, ky);
-  if (a.scale) load8<float, VEC>(a.scale + mo, at, lpr, a.D, kh);
-  if (a.post_w) load8<T, VEC>((const T*)a.post_w, at, lpr, a.D, pw);
-  if (a.pre_w) load8<T, VEC>((const T*)a.pre_w, at, lpr, a.D, rw);
+  if (a.gate) load8<float, VEC>(a.gate + mo, at, a.D, ky);
+  if (a.scale) load8<float, VEC>(a.scale + mo, at, a.D, kh);
+  if (a.post_w) load8<T, VEC>((const T*)a.post_w, at, a.D, pw);
+  if (a.pre_w) load8<T, VEC>((const T*)a.pre_w, at, a.D, rw);
 #pragma unroll
   for (int i = 0; i < 8; i++) {
     ky[i] *= pw[i];
@@ -86,7 +124,7 @@ __device__ __forceinline__ void gains(const GatedNormArgs& a, int64_t mo, int at
   }
 #pragma unroll
   for (int i = 0; i < 8; i++)
-    if (!inside<VEC>(at, i, lpr, a.D)) ky[i] = kh[i] = 0.f;
+    if (at + i >= a.D) ky[i] = kh[i] = 0.f;
 }
 
 __device__ __forceinline__ float lanes_sum(float v, int lpr) {
@@ -121,8 +159,7 @@ __device__ __forceinline__ bool find_chunk(const GatedNormArgs& a, int chunk_row
 struct Norm {
   float mean, r;
 };
-// of a row of up to 512 elements, held by lpr lanes; at: this lane's first element
-template <bool VEC>
+// of a row of up to 256 elements, held by lpr lanes; at: this lane's first element
 __device__ __forceinline__ Norm statistics(int kind, const float* v, const GatedNormArgs& a, int at, int lpr) {
   Norm n{0.f, 1.f};
   if (kind == NORM_NONE) return n;
@@ -135,14 +172,14 @@ __device__ __forceinline__ Norm statistics(int kind, const float* v, const Gated
   float q = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; i++) {
-    const float d = inside<VEC>(at, i, lpr, a.D) ? v[i] - n.mean : 0.f;
+    const float d = at + i < a.D ? v[i] - n.mean : 0.f;
     q = fmaf(d, d, q);
   }
   n.r = rsqrtf(lanes_sum(q, lpr) / (float)a.D + a.eps);
   return n;
 }
 
-// Rows of up to 512 elements: 64 / lpr rows per wave, 4 waves.
+// Rows of up to 256 elements: 64 / lpr rows per wave, 4 waves.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) forward_narrow(GatedNormArgs a, int lpr) {
   const int lane = threadIdx.x & 63, per = 64 / lpr, l = lane & (lpr - 1);
@@ -150,52 +187,52 @@ __global__ void __launch_bounds__(256) forward_narrow(GatedNormArgs a, int lpr) 
   const int row = (int)min(row64, (int64_t)a.rows - 1);
   const int seq = sequence_of(a, row);
   if (row64 >= a.rows || seq < 0) return;   // (whole groups of lpr lanes: the sums below stay inside a group)
-  const int D = a.D, at = place<VEC>(l);
+  const int D = a.D, at = 8 * l;
   const int64_t mo = seq * a.mod_row;
   float v[8], w[8];
-  load8<T, VEC>((const T*)a.x + row * a.x_row, at, lpr, D, v);
+  load8<T, VEC>((const T*)a.x + row * a.x_row, at, D, v);
 #pragma unroll
   for (int i = 0; i < 8; i++) v[i] *= a.alpha;
   if (a.y) {
     float u[8];
-    load8<T, VEC>((const T*)a.y + row * a.y_row, at, lpr, D, u);
-    const Norm n = statistics<VEC>(a.post, u, a, at, lpr);
+    load8<T, VEC>((const T*)a.y + row * a.y_row, at, D, u);
+    const Norm n = statistics(a.post, u, a, at, lpr);
 #pragma unroll
     for (int i = 0; i < 8; i++) u[i] = (u[i] - n.mean) * n.r;
     if (a.post_w) {
-      load8<T, VEC>((const T*)a.post_w, at, lpr, D, w);
+      load8<T, VEC>((const T*)a.post_w, at, D, w);
 #pragma unroll
       for (int i = 0; i < 8; i++) u[i] *= w[i];
     }
     if (a.gate) {
-      load8<float, VEC>(a.gate + mo, at, lpr, D, w);
+      load8<float, VEC>(a.gate + mo, at, D, w);
 #pragma unroll
       for (int i = 0; i < 8; i++) u[i] *= w[i];
     }
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = inside<VEC>(at, i, lpr, D) ? v[i] + u[i] : 0.f;
+    for (int i = 0; i < 8; i++) v[i] = at + i < D ? v[i] + u[i] : 0.f;
   }
-  if (a.x_out) store8<T, VEC>((T*)a.x_out + row * a.x_row, at, lpr, D, v);
+  if (a.x_out) store8<T, VEC>((T*)a.x_out + row * a.x_row, at, D, v);
   if (!a.h) return;
-  const Norm n = statistics<VEC>(a.pre, v, a, at, lpr);
+  const Norm n = statistics(a.pre, v, a, at, lpr);
 #pragma unroll
   for (int i = 0; i < 8; i++) v[i] = (v[i] - n.mean) * n.r;
   if (a.pre_w) {
-    load8<T, VEC>((const T*)a.pre_w, at, lpr, D, w);
+    load8<T, VEC>((const T*)a.pre_w, at, D, w);
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] *= w[i];
   }
   if (a.scale) {
-    load8<float, VEC>(a.scale + mo, at, lpr, D, w);
+    load8<float, VEC>(a.scale + mo, at, D, w);
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = fmaf(v[i], w[i], v[i]);
   }
   if (a.shift) {
-    load8<float, VEC>(a.shift + mo, at, lpr, D, w);
+    load8<float, VEC>(a.shift + mo, at, D, w);
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] += w[i];
   }
-  store8<T, VEC>((T*)a.h + row * a.h_row, at, lpr, D, v);
+  store8<T, VEC>((T*)a.h + row * a.h_row, at, D, v);
 }
 
 // ---------------------------------------------------------------------------
@@ -314,13 +351,7 @@ __device__ __forceinline__ RowStats join_moments(int kind, const float4* m, floa
   return o;
 }
 // elements of the row in wave w = lane % 16
-__device__ __forceinline__ float wave_count(bool vec, int lpr, int D) {
-  const int w = threadIdx.x & 15;
-  if (vec) return (float)min(max(D - 512 * w, 0), 512);
-  int n = 0;
-  for (int i = 0; i < 8; i++) n += min(max(min(lpr, D - i * lpr) - 64 * w, 0), 64);
-  return (float)n;
-}
+__device__ __forceinline__ float wave_count(int D) { return (float)min(max(D - 512 * (int)(threadIdx.x & 15), 0), 512); }
 
 // A barrier for what the waves exchange through LDS. __syncthreads() would also wait for the loads of the next row and the stores of
 // the last one, which no other wave looks at (512x512, 16 seeds, forward: 164 us).
@@ -329,33 +360,33 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // FULL: every row tensor is there. The number of loads and stores of a row is then known to the compiler, which waits for the next
 // row's loads without waiting for the last row's stores (backward, 8 x about 1300 rows of 3072: 127 us without, 101 with).
 template <typename T, bool VEC, bool FULL>
-__global__ void __launch_bounds__(1024) forward_wide(GatedNormArgs a, int lpr, int chunk_rows) {
+__global__ void __launch_bounds__(1024) forward_wide(GatedNormArgs a, int chunk_rows) {
   __shared__ float4 red[2][MAX_WAVES];
   int seq, chunk;
   RowSpan rows;
   if (!find_chunk(a, chunk_rows, seq, chunk, rows)) return;
   // every chunks-th row: the workgroups that run together then work on neighbouring rows
   const int begin = rows.begin + chunk, end = rows.begin + rows.count, step = cdiv(rows.count, chunk_rows);
-  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = l < lpr ? place<VEC>(l) : D;
+  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = 8 * l;
   const int64_t mo = seq * a.mod_row;
   const bool has_y = FULL || a.y, has_xo = FULL || a.x_out, has_h = FULL || a.h;
   Raw<T, VEC> nx, ny;
   auto fetch = [&](int64_t row) {
-    nx.load((const T*)a.x + row * a.x_row, at, lpr, D);
-    if (has_y) ny.load((const T*)a.y + row * a.y_row, at, lpr, D);
+    nx.load((const T*)a.x + row * a.x_row, at, D);
+    if (has_y) ny.load((const T*)a.y + row * a.y_row, at, D);
   };
   fetch(begin);
   bool in[8];
 #pragma unroll
-  for (int i = 0; i < 8; i++) in[i] = inside<VEC>(at, i, lpr, D);
+  for (int i = 0; i < 8; i++) in[i] = at + i < D;
   if (l < 2 * MAX_WAVES) red[l >> 4][l & 15] = make_float4(0.f, 0.f, 0.f, 0.f);
   __syncthreads();
-  const float counts = wave_count(VEC, lpr, D), count = lane_of(counts, wave), inv_d = 1.f / (float)D;
+  const float counts = wave_count(D), count = lane_of(counts, wave), inv_d = 1.f / (float)D;
   float ky[8], kh[8], sh[8];   // gate post_w; (1 + scale) pre_w; shift
-  gains<T, VEC>(a, mo, at, lpr, ky, kh);
+  gains<T, VEC>(a, mo, at, ky, kh);
 #pragma unroll
   for (int i = 0; i < 8; i++) sh[i] = 0.f;
-  if (a.shift && has_h) load8<float, VEC>(a.shift + mo, at, lpr, D, sh);
+  if (a.shift && has_h) load8<float, VEC>(a.shift + mo, at, D, sh);
   int turn = 0;   // (a buffer is written again two barriers after it was)
   auto stats = [&](int kind, const float* v) {
     const Moments m = wave_moments<false>(kind, v, nullptr, in, count);
@@ -381,13 +412,13 @@ __global__ void __launch_bounds__(1024) forward_wide(GatedNormArgs a, int lpr, i
 #pragma unroll
       for (int i = 0; i < 8; i++) v[i] = fmaf(u[i], ky[i], v[i]);   // (past the row ky is 0)
     }
-    if (has_xo) store8<T, VEC>((T*)a.x_out + row * a.x_row, at, lpr, D, v);
+    if (has_xo) store8<T, VEC>((T*)a.x_out + row * a.x_row, at, D, v);
     if (!has_h) continue;
     RowStats n{0.f, 1.f, 0.f, 0.f};
     if (a.pre != NORM_NONE) n = stats(a.pre, v);
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = fmaf((v[i] - n.mean) * n.r, kh[i], sh[i]);
-    store8<T, VEC>((T*)a.h + row * a.h_row, at, lpr, D, v);
+    store8<T, VEC>((T*)a.h + row * a.h_row, at, D, v);
   }
 }
 
@@ -422,23 +453,23 @@ __device__ __forceinline__ void add_pre(const RowGradient& n, float* xv, const f
 }
 
 template <bool VEC>
-__device__ __forceinline__ void store_columns(const GatedNormArgs& a, int at, int lpr, const Columns& s) {
+__device__ __forceinline__ void store_columns(const GatedNormArgs& a, int at, const Columns& s) {
   float* out = a.parts + (int64_t)blockIdx.x * 3 * a.D;
-  store8<float, VEC>(out, at, lpr, a.D, s.R);
-  store8<float, VEC>(out + a.D, at, lpr, a.D, s.P);
-  store8<float, VEC>(out + 2 * a.D, at, lpr, a.D, s.Q);
+  store8<float, VEC>(out, at, a.D, s.R);
+  store8<float, VEC>(out + a.D, at, a.D, s.P);
+  store8<float, VEC>(out + 2 * a.D, at, a.D, s.Q);
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_rows(const GatedNormArgs& a, int64_t row, int at, int lpr, float* xv, float* yv, float* t, float* dh) {
+__device__ __forceinline__ void load_rows(const GatedNormArgs& a, int64_t row, int at, float* xv, float* yv, float* t, float* dh) {
 #pragma unroll
   for (int i = 0; i < 8; i++) yv[i] = t[i] = dh[i] = 0.f;
-  load8<T, VEC>((const T*)a.x + row * a.x_row, at, lpr, a.D, xv);
-  if (a.y) load8<T, VEC>((const T*)a.y + row * a.y_row, at, lpr, a.D, yv);
-  if (a.dx_out) load8<T, VEC>((const T*)a.dx_out + row * a.x_row, at, lpr, a.D, t);
-  if (a.dh) load8<T, VEC>((const T*)a.dh + row * a.h_row, at, lpr, a.D, dh);
+  load8<T, VEC>((const T*)a.x + row * a.x_row, at, a.D, xv);
+  if (a.y) load8<T, VEC>((const T*)a.y + row * a.y_row, at, a.D, yv);
+  if (a.dx_out) load8<T, VEC>((const T*)a.dx_out + row * a.x_row, at, a.D, t);
+  if (a.dh) load8<T, VEC>((const T*)a.dh + row * a.h_row, at, a.D, dh);
 }
 
-// Rows of up to 512 elements: groups of lpr lanes take a row each.
+// Rows of up to 256 elements: groups of lpr lanes take a row each.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) rows_narrow(GatedNormArgs a, int lpr, int chunk_rows) {
   __shared__ float cols[256 * 25];   // (25: an odd stride keeps lanes on different banks)
@@ -446,14 +477,14 @@ __global__ void __launch_bounds__(256) rows_narrow(GatedNormArgs a, int lpr, int
   RowSpan rows;
   if (!find_chunk(a, chunk_rows, seq, chunk, rows)) return;
   const int begin = rows.begin + chunk * chunk_rows, end = min(begin + chunk_rows, rows.begin + rows.count);
-  const int D = a.D, groups = 256 / lpr, l = threadIdx.x & (lpr - 1), grp = threadIdx.x / lpr, at = place<VEC>(l);
+  const int D = a.D, groups = 256 / lpr, l = threadIdx.x & (lpr - 1), grp = threadIdx.x / lpr, at = 8 * l;
   float ky[8], kh[8];
-  gains<T, VEC>(a, seq * a.mod_row, at, lpr, ky, kh);
+  gains<T, VEC>(a, seq * a.mod_row, at, ky, kh);
   bool in[8];
   Columns cs;
 #pragma unroll
   for (int i = 0; i < 8; i++) {
-    in[i] = inside<VEC>(at, i, lpr, D);
+    in[i] = at + i < D;
     cs.R[i] = cs.P[i] = cs.Q[i] = 0.f;
   }
   const float inv_d = 1.f / (float)D;
@@ -462,9 +493,9 @@ __global__ void __launch_bounds__(256) rows_narrow(GatedNormArgs a, int lpr, int
     const bool live = r0 + grp < end;
     const int64_t row = min(r0 + grp, end - 1);
     float xv[8], yv[8], t[8], dh[8];
-    load_rows<T, VEC>(a, row, at, lpr, xv, yv, t, dh);
+    load_rows<T, VEC>(a, row, at, xv, yv, t, dh);
     if (a.dh) {
-      const Norm n = statistics<VEC>(a.pre, xv, a, at, lpr);
+      const Norm n = statistics(a.pre, xv, a, at, lpr);
       RowStats st{n.mean, n.r, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 8; i++) {
@@ -477,7 +508,7 @@ __global__ void __launch_bounds__(256) rows_narrow(GatedNormArgs a, int lpr, int
       add_pre(row_gradient(a.pre, st, inv_d), xv, dh, kh, t, live, cs);
     }
     if (a.y) {
-      const Norm n = statistics<VEC>(a.post, yv, a, at, lpr);
+      const Norm n = statistics(a.post, yv, a, at, lpr);
       float g[8], u = 0.f, w = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; i++) {
@@ -492,13 +523,13 @@ __global__ void __launch_bounds__(256) rows_narrow(GatedNormArgs a, int lpr, int
         w = a.post != NORM_NONE ? lanes_sum(w, lpr) * inv_d : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; i++) g[i] = n.r * (g[i] - u - yv[i] * w);
-        if (live) store8<T, VEC>((T*)a.dy + row * a.y_row, at, lpr, D, g);
+        if (live) store8<T, VEC>((T*)a.dy + row * a.y_row, at, D, g);
       }
     }
     if (a.dx && live) {
 #pragma unroll
       for (int i = 0; i < 8; i++) t[i] *= a.alpha;
-      store8<T, VEC>((T*)a.dx + row * a.x_row, at, lpr, D, t);
+      store8<T, VEC>((T*)a.dx + row * a.x_row, at, D, t);
     }
   }
   if (!a.parts) return;
@@ -517,12 +548,12 @@ __global__ void __launch_bounds__(256) rows_narrow(GatedNormArgs a, int lpr, int
       cs.P[i] += cols[(g * lpr + l) * 25 + 8 + i];
       cs.Q[i] += cols[(g * lpr + l) * 25 + 16 + i];
     }
-  store_columns<VEC>(a, at, lpr, cs);
+  store_columns<VEC>(a, at, cs);
 }
 
 // FULL: as above.
 template <typename T, bool VEC, bool FULL>
-__global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int lpr, int chunk_rows) {
+__global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int chunk_rows) {
   __shared__ float4 redx[2][MAX_WAVES], redy[2][MAX_WAVES];
   __shared__ float2 redg[2][MAX_WAVES];
   int seq, chunk;
@@ -530,23 +561,23 @@ __global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int lpr, int 
   if (!find_chunk(a, chunk_rows, seq, chunk, rows)) return;
   // every chunks-th row: the workgroups that run together then work on neighbouring rows
   const int begin = rows.begin + chunk, end = rows.begin + rows.count, step = cdiv(rows.count, chunk_rows);
-  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = l < lpr ? place<VEC>(l) : D;
+  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = 8 * l;
   const bool has_y = FULL || a.y, has_dxo = FULL || a.dx_out, has_dh = FULL || a.dh, has_dx = FULL || a.dx, has_dy = FULL || a.dy;
   Raw<T, VEC> nx, ny, nt, nh;
   auto fetch = [&](int64_t row) {
-    nx.load((const T*)a.x + row * a.x_row, at, lpr, D);
-    if (has_y) ny.load((const T*)a.y + row * a.y_row, at, lpr, D);
-    if (has_dxo) nt.load((const T*)a.dx_out + row * a.x_row, at, lpr, D);
-    if (has_dh) nh.load((const T*)a.dh + row * a.h_row, at, lpr, D);
+    nx.load((const T*)a.x + row * a.x_row, at, D);
+    if (has_y) ny.load((const T*)a.y + row * a.y_row, at, D);
+    if (has_dxo) nt.load((const T*)a.dx_out + row * a.x_row, at, D);
+    if (has_dh) nh.load((const T*)a.dh + row * a.h_row, at, D);
   };
   fetch(begin);
   float ky[8], kh[8];
-  gains<T, VEC>(a, seq * a.mod_row, at, lpr, ky, kh);
+  gains<T, VEC>(a, seq * a.mod_row, at, ky, kh);
   bool in[8];
   Columns cs;
 #pragma unroll
   for (int i = 0; i < 8; i++) {
-    in[i] = inside<VEC>(at, i, lpr, D);
+    in[i] = at + i < D;
     cs.R[i] = cs.P[i] = cs.Q[i] = 0.f;
   }
   if (l < 2 * MAX_WAVES) {
@@ -554,7 +585,7 @@ __global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int lpr, int 
     redg[l >> 4][l & 15] = make_float2(0.f, 0.f);
   }
   __syncthreads();
-  const float counts = wave_count(VEC, lpr, D), count = lane_of(counts, wave), inv_d = 1.f / (float)D;
+  const float counts = wave_count(D), count = lane_of(counts, wave), inv_d = 1.f / (float)D;
   int turn = 0;   // (a buffer is written again two barriers after it was)
   for (int64_t row = begin; row < end; row += step, turn ^= 1) {
     float xv[8], yv[8], t[8], dh[8];
@@ -582,7 +613,7 @@ __global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int lpr, int 
       float o[8];
 #pragma unroll
       for (int i = 0; i < 8; i++) o[i] = t[i] * a.alpha;
-      store8<T, VEC>((T*)a.dx + row * a.x_row, at, lpr, D, o);
+      store8<T, VEC>((T*)a.dx + row * a.x_row, at, D, o);
     }
     if (!has_y) continue;
     RowStats n{0.f, 1.f, 0.f, 0.f};
@@ -611,17 +642,16 @@ __global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int lpr, int 
     }
 #pragma unroll
     for (int i = 0; i < 8; i++) t[i] = n.r * (t[i] - u - yv[i] * w);
-    store8<T, VEC>((T*)a.dy + row * a.y_row, at, lpr, D, t);
+    store8<T, VEC>((T*)a.dy + row * a.y_row, at, D, t);
   }
-  if (a.parts) store_columns<VEC>(a, at, lpr, cs);
+  if (a.parts) store_columns<VEC>(a, at, cs);
 }
 
-// Sums of the chunks of one sequence, 64 columns per workgroup, its 16 waves sharing the chunks:
+// Sums of the chunks of one sequence, 64 columns per workgroup, whose WAVES waves share the chunks:
 //   dshift = R, dscale = P pre_w, dgate = Q post_w.
 // P and Q stay behind for the weights' gradients (in the sequence's place after the chunks).
-template <typename T>
-__global__ void __launch_bounds__(1024) columns_kernel(GatedNormArgs a, int chunk_rows) {
-  constexpr int WAVES = 16;
+template <typename T, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) columns_kernel(GatedNormArgs a, int chunk_rows) {
   __shared__ float red[3][WAVES][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.D;
   const int blocks = cdiv(D, 64), seq = blockIdx.x / blocks, col = (blockIdx.x - seq * blocks) * 64 + lane;
@@ -655,16 +685,26 @@ __global__ void __launch_bounds__(1024) columns_kernel(GatedNormArgs a, int chun
   }
 }
 
-// dpre_w = sum over the sequences of (1 + scale) P, dpost_w of gate Q.
-__global__ void __launch_bounds__(256) weights_kernel(GatedNormArgs a) {
-  const int col = blockIdx.x * 256 + threadIdx.x, D = a.D;
-  if (col >= D) return;
+// dpre_w = sum over the sequences of (1 + scale) P, dpost_w of gate Q: 64 columns per workgroup, its 16 waves share the sequences.
+__global__ void __launch_bounds__(1024) weights_kernel(GatedNormArgs a) {
+  constexpr int WAVES = 16;
+  __shared__ float red[2][WAVES][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane, D = a.D;
   float p = 0.f, q = 0.f;
-  for (int s = 0; s < a.nseq; s++) {
-    const float* k = a.parts + ((int64_t)a.chunks * 3 + 2 * s) * D + col;
-    const int64_t at = s * a.mod_row + col;
-    p = fmaf(a.scale ? 1.f + a.scale[at] : 1.f, k[0], p);
-    q = fmaf(a.gate ? a.gate[at] : 1.f, k[D], q);
+  if (col < D)
+    for (int s = wave; s < a.nseq; s += WAVES) {
+      const float* k = a.parts + ((int64_t)a.chunks * 3 + 2 * s) * D + col;
+      const int64_t at = s * a.mod_row + col;
+      p = fmaf(a.scale ? 1.f + a.scale[at] : 1.f, k[0], p);
+      q = fmaf(a.gate ? a.gate[at] : 1.f, k[D], q);
+    }
+  red[0][wave][lane] = p;
+  red[1][wave][lane] = q;
+  __syncthreads();
+  if (wave > 0 || col >= D) return;
+  for (int w = 1; w < WAVES; w++) {
+    p += red[0][w][lane];
+    q += red[1][w][lane];
   }
   if (a.dpre_w) a.dpre_w[col] = p;
   if (a.dpost_w) a.dpost_w[col] = q;
@@ -677,27 +717,29 @@ bool vectors(const GatedNormArgs& a) {
     if (!aligned(p)) return false;
   return a.D % 8 == 0 && a.x_row % 8 == 0 && a.y_row % 8 == 0 && a.h_row % 8 == 0 && a.mod_row % 8 == 0;
 }
-// lanes of a row of D elements in a wave
+// lanes of a row of up to 256 elements
 int lanes_of(int D) {
   int l = 8;
-  while (l < 64 && l * 8 < D) l *= 2;
+  while (l * 8 < D) l *= 2;
   return l;
 }
 
-// rows of up to 512 elements: lanes of a wave; longer ones: lanes of a workgroup
-bool narrow(int D) { return D <= 512; }
+// Rows of up to 256 elements share a wave; longer ones take the waves of a workgroup (20000 rows of 512: forward 19.5 us, backward 43;
+// as one row per wave of the narrow kernels 23 and 62. Of 256: 14 and 43 either way).
+bool narrow(int D) { return D <= 256; }
 int wide_threads(int D) { return cdiv(cdiv(D, 8), 64) * 64; }
 
-// Rows of a chunk of the backward pass: as many as let all chunks run at once (16 waves per CU, which their registers allow). Half as
-// many rows need a second round of workgroups for what the first leaves over (8 x about 1300 rows of 3072: CHUNK_COMPARISON),
-// and write twice the sums.
+// Rows of a chunk of the backward pass: as many as let all chunks run at once (16 waves per CU, which their registers allow), but 8 at
+// least. Half as many rows need another round of workgroups for what the first leaves over and write twice the sums (8 sequences
+// of about 1300 rows of 3072: 183 us where all at once take 138).
 int chunk_rows_of(int nseq, int rows, int D) {
   const int waves = narrow(D) ? 4 : wide_threads(D) / 64, slots = 256 * std::max(16 / waves, 1);
   return std::max(8, cdiv(rows, std::max(slots - nseq, slots / 2)));
 }
 
-// rows a workgroup walks forward: few, so that the workgroups are many rounds of the chip
-int forward_rows_of(int rows) { return std::min(8, std::max(1, rows / 1024)); }
+// rows a workgroup walks forward: up to 8 (20480 rows of 3072: 104 us; 20, one round of workgroups: 164), as long as that leaves enough
+// workgroups for the 32 waves a CU can hold
+int forward_rows_of(int rows, int D) { return std::min(8, std::max(1, rows / (256 * 32 / (wide_threads(D) / 64)))); }
 
 template <typename T>
 void forward_launch(const GatedNormArgs& a, hipStream_t s) {
@@ -707,10 +749,10 @@ void forward_launch(const GatedNormArgs& a, hipStream_t s) {
     if (vec) forward_narrow<T, true><<<grid, 256, 0, s>>>(a, lpr);
     else forward_narrow<T, false><<<grid, 256, 0, s>>>(a, lpr);
   } else {
-    const int cr = forward_rows_of(a.rows), grid = a.rows / cr + a.nseq, threads = wide_threads(a.D);
-    if (vec && a.y && a.x_out && a.h) forward_wide<T, true, true><<<grid, threads, 0, s>>>(a, cdiv(a.D, 8), cr);
-    else if (vec) forward_wide<T, true, false><<<grid, threads, 0, s>>>(a, cdiv(a.D, 8), cr);
-    else forward_wide<T, false, false><<<grid, threads, 0, s>>>(a, cdiv(a.D, 8), cr);
+    const int cr = forward_rows_of(a.rows, a.D), grid = a.rows / cr + a.nseq, threads = wide_threads(a.D);
+    if (vec && a.y && a.x_out && a.h) forward_wide<T, true, true><<<grid, threads, 0, s>>>(a, cr);
+    else if (vec) forward_wide<T, true, false><<<grid, threads, 0, s>>>(a, cr);
+    else forward_wide<T, false, false><<<grid, threads, 0, s>>>(a, cr);
   }
 }
 
@@ -723,10 +765,10 @@ void rows_launch(const GatedNormArgs& a, hipStream_t s) {
     if (vec) rows_narrow<T, true><<<a.chunks, 256, 0, s>>>(a, lpr, cr);
     else rows_narrow<T, false><<<a.chunks, 256, 0, s>>>(a, lpr, cr);
   } else {
-    const int lpr = cdiv(a.D, 8), threads = wide_threads(a.D);
-    if (vec && a.y && a.dx_out && a.dh && a.dx && a.dy) rows_wide<T, true, true><<<a.chunks, threads, 0, s>>>(a, lpr, cr);
-    else if (vec) rows_wide<T, true, false><<<a.chunks, threads, 0, s>>>(a, lpr, cr);
-    else rows_wide<T, false, false><<<a.chunks, threads, 0, s>>>(a, lpr, cr);
+    const int threads = wide_threads(a.D);
+    if (vec && a.y && a.dx_out && a.dh && a.dx && a.dy) rows_wide<T, true, true><<<a.chunks, threads, 0, s>>>(a, cr);
+    else if (vec) rows_wide<T, true, false><<<a.chunks, threads, 0, s>>>(a, cr);
+    else rows_wide<T, false, false><<<a.chunks, threads, 0, s>>>(a, cr);
   }
 }
 
@@ -749,13 +791,19 @@ hipError_t gated_norm_rows_bwd(const GatedNormArgs& a, int dtype, hipStream_t s)
   return hipGetLastError();
 }
 
-hipError_t gated_norm_columns_bwd(const GatedNormArgs& a, int dtype, hipStream_t s) {
+template <typename T>
+static void columns_launch(const GatedNormArgs& a, int cr, hipStream_t s) {
   const int64_t grid = (int64_t)cdiv(a.D, 64) * a.nseq;
+  if (a.chunks <= 8 * (int64_t)a.nseq) columns_kernel<T, 4><<<grid, 256, 0, s>>>(a, cr);   // few chunks per sequence
+  else columns_kernel<T, 16><<<grid, 1024, 0, s>>>(a, cr);
+}
+hipError_t gated_norm_columns_bwd(const GatedNormArgs& a, int dtype, hipStream_t s) {
   const int cr = chunk_rows_of(a.nseq, a.rows, a.D);
-  if (grid == 0) {
-  } else if (dtype == DT_BF16) columns_kernel<u16><<<grid, 1024, 0, s>>>(a, cr);
-  else columns_kernel<float><<<grid, 1024, 0, s>>>(a, cr);
-  if (a.dpre_w || a.dpost_w) weights_kernel<<<cdiv(a.D, 256), 256, 0, s>>>(a);
+  if (a.nseq > 0) {
+    if (dtype == DT_BF16) columns_launch<u16>(a, cr, s);
+    else columns_launch<float>(a, cr, s);
+  }
+  if (a.dpre_w || a.dpost_w) weights_kernel<<<cdiv(a.D, 64), 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 

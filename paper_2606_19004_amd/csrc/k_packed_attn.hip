@@ -610,17 +610,20 @@ __global__ void __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) packed_few_bf16(Pack
 #endif
 }
 
-// Joins the parts of each row: o = sum_p exp(lse_p - lse) o_p, in the order of the parts. One wave per row.
+// Joins the parts of each row: o = sum_p exp(lse_p - lse) o_p, in the order of the parts. One wave per row, 4 rows per workgroup;
+// the parts' rows are loaded eight at a time.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
-  const int g = blockIdx.x % a.Hkv, u = blockIdx.x / a.Hkv;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int quad = blockIdx.x % (ROWS / 4), gu = blockIdx.x / (ROWS / 4);
+  const int u = gu / a.Hkv, g = gu - u * a.Hkv;
   int seq, rt;
   PackedSeq sq;
   if (!find_unit(a.nseq, u, [&](int i) { return a.sequence(i); }, [&](const PackedSeq& s) { return row_tiles_of<ROWS>(a, s); }, seq, rt, sq))
     return;
   const int parts = parts_of(a, sq);
-  if (parts <= 1) return;
+  const int rows = sq.m * a.G, q0 = sq.q0, row = rt * ROWS + 4 * quad + wave;
+  if (parts <= 1 || row >= rows) return;
   // units before this sequence's
   int64_t before = 0;
   for (int i = lane; i < seq; i += 64) {
@@ -629,34 +632,45 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
-  const int rows = sq.m * a.G, q0 = sq.q0;
   const int place = a.causal ? cdiv(rows, ROWS) - 1 - rt : rt;   // where the tile stands in the order of the units
   if (before + (int64_t)(place + 1) * parts > a.units) return;   // (offsets that are not increasing: no such units ran)
-  const int64_t slot = ((int64_t)g * a.units + before + place * parts) * ROWS;
-  for (int r = wave; r < ROWS && rt * ROWS + r < rows; r += 4) {
-    const int row = rt * ROWS + r, tok = row / a.G, head = g * a.G + row - tok * a.G;
-    float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_lse[slot + (int64_t)p * ROWS + r]);
+  const int64_t slot = ((int64_t)g * a.units + before + place * parts) * ROWS + 4 * quad + wave;   // of part 0; parts are ROWS apart
+  const float* plse = a.part_lse + slot;
+  const float* po = a.part_o + slot * d;
+  const int tok = row / a.G, head = g * a.G + row - tok * a.G;
+  float top = -INFINITY;
+  for (int p = lane; p < parts; p += 64) top = fmaxf(top, plse[(int64_t)p * ROWS]);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    float total = 0.f, acc0 = 0.f, acc1 = 0.f;
-    if (top > -INFINITY || top != top)
-      for (int p = 0; p < parts; p++) {
-        const int64_t at = slot + (int64_t)p * ROWS + r;
-        const float w = __builtin_amdgcn_exp2f((a.part_lse[at] - top) * LOG2E);
-        total += w;
-        if (w != 0.f) {
-          acc0 = fmaf(w, a.part_o[at * d + lane], acc0);
-          if (d > 64) acc1 = fmaf(w, a.part_o[at * d + 64 + lane], acc1);
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const int e = d > 64 ? 2 * lane : lane;
+  float total = 0.f, acc0 = 0.f, acc1 = 0.f;
+  if (top > -INFINITY || top != top)
+    for (int p0 = 0; p0 < parts; p0 += 64) {
+      const int np = min(parts - p0, 64);
+      float w = 0.f;
+      if (lane < np) w = __builtin_amdgcn_exp2f((plse[(int64_t)(p0 + lane) * ROWS] - top) * LOG2E);
+      for (int p = 0; p < np; p += 8) {
+        float2 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const float* x = po + (int64_t)(p0 + min(p + j, np - 1)) * ROWS * d + e;
+          v[j] = d > 64 ? *(const float2*)x : make_float2(*x, 0.f);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const float wj = p + j < np ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), p + j)) : 0.f;
+          total += wj;
+          acc0 = fmaf(wj, v[j].x, acc0);
+          acc1 = fmaf(wj, v[j].y, acc1);
         }
       }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    T* orow = (T*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head;
-    orow[lane] = from_f32<T>(acc0 * inv);
-    if (d > 64) orow[64 + lane] = from_f32<T>(acc1 * inv);
-    if (a.lse && lane == 0)
-      a.lse[(int64_t)(q0 + tok) * a.H + head] = total == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(total) * LN2;
-  }
+    }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+  T* orow = (T*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head + e;
+  orow[0] = from_f32<T>(acc0 * inv);
+  if (d > 64) orow[1] = from_f32<T>(acc1 * inv);
+  if (a.lse && lane == 0)
+    a.lse[(int64_t)(q0 + tok) * a.H + head] = total == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(total) * LN2;
 }
 
 // Tiles and parts.
@@ -706,7 +720,7 @@ hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStr
   if (d == 128) fwd_launch<128>(a, dtype, p.rows, grid, s);
   else fwd_launch<64>(a, dtype, p.rows, grid, s);
   if (p.part_tiles) {
-    const int64_t jg = (int64_t)p.row_tiles * a.Hkv;
+    const int64_t jg = (int64_t)p.row_tiles * a.Hkv * (p.rows / 4);
     if (p.rows == 16) packed_join<u16, 16><<<jg, 256, 0, s>>>(a, d);
     else if (dtype == DT_BF16) packed_join<u16, 128><<<jg, 256, 0, s>>>(a, d);
     else packed_join<float, 64><<<jg, 256, 0, s>>>(a, d);

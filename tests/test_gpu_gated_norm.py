@@ -1,6 +1,6 @@
 """gated_norm and gated_norm_backward against the float64 oracle.
 
-Bounds: K = (D / 64 + 16) 2^-24 covers the fp32 sums over a row (8 successive terms per lane and chunk, then a tree) and
+Bounds: K = (D / 64 + 16) 2^-24 covers the fp32 sums over a row (8 successive terms per lane, then a tree) and
 the few operations after them; U is the rounding of the output type (2^-8 or 2^-24 relative). A normalised row is off by at
 most 4 K (|xhat| + mean|x| r + 1); what follows from it is multiplied through. Vector gradients add rows 2^-24 for their sums."""
 import numpy as np
@@ -186,7 +186,7 @@ class Problem:
 
 KINDS = [("none", "layer"), ("layer", "rms"), ("rms", "layer"), ("rms", "rms"), ("none", "none")]
 SIZES = [(256, [80, 80]), (8, [3, 1]), (64, [1, 0, 200]), (520, [37, 5]), (1023, [9, 4]), (3, [70]), (513, [2]), (4096, [5, 12]),
-         (8192, [3]), (8191, [2]), (192, [1])]
+         (8192, [3]), (8191, [2]), (192, [1]), (257, [6, 30]), (512, [40, 3]), (300, [20])]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -286,3 +286,21 @@ def test_graph_replays_match_eager(d):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
         both()
+
+
+def test_no_rows(d):
+    """Sequences without rows have gradients of zero; no sequence and no row is a call that writes the weights' zeros."""
+    for S in (3, 0):
+        x = torch.empty((0, 64), device="cuda")
+        cfg = d.gated_norm_config(x, S, "rms", "layer")
+        y = torch.empty((0, 64), device="cuda")
+        v = [torch.full((max(S, 1), 64), 7.0, device="cuda") for _ in range(3)]
+        w = [torch.full((64,), 7.0, device="cuda") for _ in range(2)]
+        ws = d.workspace(d.gated_norm_backward_workspace_bytes(cfg))
+        d.gated_norm(cfg, x, y, x, y)
+        one = torch.zeros((1, 64), device="cuda")     # (an empty tensor has no address)
+        d.gated_norm_backward(cfg, one, one, one, one, one, one, dgate=v[0], dscale=v[1], dshift=v[2], dpost_w=w[0], dpre_w=w[1], ws=ws)
+        torch.cuda.synchronize()
+        for t in v:
+            assert torch.all(t[:S] == 0.0) and torch.all(t[S:] == 7.0)
+        assert all(torch.all(t == 0.0) for t in w)

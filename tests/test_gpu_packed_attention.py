@@ -241,3 +241,64 @@ def test_a_cache_past_32_bit_offsets(d):
     ref = attention_reference(q, k, v, [0, 3], [0, rows], [rows], 0.125, True, "bf16")
     check(host64(o), ref["o"], ref["o_tol"], "o")
     check(lse.double().cpu().numpy(), ref["lse"], ref["lse_tol"], "lse")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_cache_of_equal_regions(d, dtype):
+    """[sequences][room] caches: k_lengths without offsets."""
+    S, room, H, G, hd = 3, 50, 4, 2, 64
+    rng = np.random.default_rng(4)
+    lens = np.array([50, 1, 33])
+    q, k, v = (stored(rng.standard_normal(s), dtype) for s in ((S, H, hd), (S * room, G, hd), (S * room, G, hd)))
+    for i, n in enumerate(lens):
+        k[i * room + n:(i + 1) * room] = v[i * room + n:(i + 1) * room] = np.nan
+    tq, tk, tv = (to_dev(x, dtype) for x in (q, k, v))
+    o, lse = torch.zeros_like(tq), torch.zeros((S, H), device="cuda")
+    cfg = d.packed_config(tq, tk, tv, o, S, True)
+    ws = d.workspace(d.packed_attention_workspace_bytes(cfg))
+    d.packed_attention(cfg, tq, tk, tv, o, lse=lse, k_lengths=i32(lens), ws=ws)
+    ref = attention_reference(q, k, v, list(range(S + 1)), [i * room for i in range(S)], lens, hd ** -0.5, True, dtype)
+    check(host64(o), ref["o"], ref["o_tol"], "o")
+    check(lse.double().cpu().numpy(), ref["lse"], ref["lse_tol"], "lse")
+
+
+def test_two_streams_at_once(d):
+    """Calls on two streams with buffers and workspaces of their own."""
+    ps = [Problem(d, "bf16", 64, 8, 2, [200, 300], None, True, seed=s) for s in (1, 2)]
+    want = []
+    for p in ps:
+        p.forward()
+        want.append((p.to.clone(), p.lse.clone(), [g.clone() for g in p.backward()]))
+    streams = [torch.cuda.Stream() for _ in ps]
+    torch.cuda.synchronize()
+    keep = []
+    for _ in range(3):
+        for p, s in zip(ps, streams):
+            ws = d.workspace(d.packed_attention_workspace_bytes(p.cfg))
+            keep.append(ws)
+            d.packed_attention(p.cfg, p.tq, p.tk, p.tv, p.to, lse=p.lse, q_offsets=p.dq_off, k_offsets=p.dk_off, ws=ws, stream=s)
+    torch.cuda.synchronize()
+    for p, w in zip(ps, want):
+        assert torch.equal(p.to, w[0]) and torch.equal(p.lse, w[1])
+
+
+def test_backward_in_a_graph(d):
+    p = Problem(d, "bf16", 128, 8, 2, [300, 41], None, True, seed=21)
+    want = [g.clone() for g in p.backward()]
+    o, do, lse = to_dev(p.o64, "bf16"), to_dev(p.do, "bf16"), torch.from_numpy(p.lse64).float().cuda()
+    buf = torch.zeros((p.tq.shape[0], 12, 128), dtype=torch.bfloat16, device="cuda")
+    grads = [buf[:, :8], buf[:, 8:10], buf[:, 10:]]
+    ws = d.workspace(d.packed_attention_backward_workspace_bytes(p.cfg))
+
+    def call():
+        d.packed_attention_backward(p.cfg, p.tq, p.tk, p.tv, o, lse, do, *grads, q_offsets=p.dq_off, k_offsets=p.dk_off, ws=ws)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        buf.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(grads, want))
+        call()
