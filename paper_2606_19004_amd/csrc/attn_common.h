@@ -123,4 +123,62 @@ __device__ __forceinline__ bf16x8 join_tr(i16x4 lo, i16x4 hi) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// fp32 on v_mfma_f32_16x16x4_f32: 16 owned rows per wave (fragments own[c]: dims 16 c + 4 g4 + 0..3 of row lane % 16, g4 = lane / 16)
+// against a walked tile of 16 rows of two tensors, staged through registers into LDS by LANES lanes (a workgroup, or a wave
+// with tiles of its own).
+template <int D, int LANES> struct WalkF32 {
+  static constexpr int NROW = 16, LD = D + 4, CPT = NROW * D / 4 / LANES;
+  f32x4 ra[CPT], rb[CPT];
+  // rows past `left` are zeros (what they are multiplied with is 0, but 0 times an infinity would be NaN)
+  __device__ __forceinline__ void fetch(const float* a, int64_t as, const float* b, int64_t bs, int left) {
+#pragma unroll
+    for (int i = 0; i < CPT; i++) {
+      const int idx = threadIdx.x % LANES + LANES * i, r = idx / (D / 4), c = idx % (D / 4), rr = min(r, left - 1);
+      ra[i] = *(const f32x4*)(a + rr * as + 4 * c);
+      rb[i] = *(const f32x4*)(b + rr * bs + 4 * c);
+      if (r >= left) ra[i] = rb[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  __device__ __forceinline__ void stage(float* sa, float* sb) const {
+#pragma unroll
+    for (int i = 0; i < CPT; i++) {
+      const int idx = threadIdx.x % LANES + LANES * i, r = idx / (D / 4), c = idx % (D / 4);
+      *(f32x4*)(sa + r * LD + 4 * c) = ra[i];
+      *(f32x4*)(sb + r * LD + 4 * c) = rb[i];
+    }
+  }
+  // [walked row 4 g4 + r][owned row lane % 16] products
+  static __device__ __forceinline__ f32x4 dot(const float* st, const f32x4* own, int l16, int g4) {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < D / 16; c++) {
+      const f32x4 w = *(const f32x4*)(st + l16 * LD + 16 * c + 4 * g4);
+#pragma unroll
+      for (int e = 0; e < 4; e++) s = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], own[c][e], s, 0, 0, 0);
+    }
+    return s;
+  }
+  // acc[dim][owned] += sum over the walked rows of st[row][dim] w[row][owned]
+  static __device__ __forceinline__ void add(f32x4* acc, const float* st, const f32x4& w, int l16, int g4) {
+#pragma unroll
+    for (int r = 0; r < 4; r++)
+#pragma unroll
+      for (int i = 0; i < D / 16; i++)
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(st[(4 * g4 + r) * LD + l16 + 16 * i], w[r], acc[i], 0, 0, 0);
+  }
+};
+// The sums of four waves that own the same rows, in wave 0, through LDS of 3 x 16 x (D + 4) floats.
+template <int D> __device__ __forceinline__ void join_waves(float* lds, f32x4* acc, int wave, int l16, int g4) {
+  __syncthreads();
+  if (wave > 0)
+#pragma unroll
+    for (int i = 0; i < D / 16; i++) *(f32x4*)(lds + ((wave - 1) * 16 + l16) * (D + 4) + 16 * i + 4 * g4) = acc[i];
+  __syncthreads();
+  if (wave == 0)
+#pragma unroll
+    for (int w = 0; w < 3; w++)
+#pragma unroll
+      for (int i = 0; i < D / 16; i++) acc[i] += *(const f32x4*)(lds + (w * 16 + l16) * (D + 4) + 16 * i + 4 * g4);
+}
+
 }  // namespace dit

@@ -423,6 +423,107 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// fp32 where tiles of 64 rows would leave CUs idle: 16 rows per workgroup, whose 4 waves take every fourth 16-key tile, each staging its
+// own, with a running maximum and sum of their own; they meet at the end.
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
+  constexpr int ROWS = 16, NKC = D / 16;
+  using W = WalkF32<D, 64>;
+  __shared__ __attribute__((aligned(16))) float sk[4][W::NROW * W::LD], sv[4][W::NROW * W::LD];
+  __shared__ float2 ml[4][ROWS];
+  const PackedTile t = packed_tile<ROWS>(a);
+  if (!t.any) return;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int rows = t.s.m * a.G, row0 = t.rt * ROWS, n = t.s.n;
+  const int64_t q0 = t.s.q0, k0 = t.s.k0;
+  const float* Kg = (const float*)a.k + k0 * a.k_row + (int64_t)t.g * a.k_head;
+  const float* Vg = (const float*)a.v + k0 * a.v_row + (int64_t)t.g * a.v_head;
+  const int row = min(row0 + l16, rows - 1);
+  const int tok = row / a.G, head = t.g * a.G + (row - tok * a.G);
+  const int vis = a.causal ? min(tok + n - t.s.m + 1, n) : n;
+  const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
+  const int nvis = a.causal ? min(max(last_tok + n - t.s.m + 1, 0), n) : n;
+  int kt0 = 0, nt = cdiv(nvis, 16);
+  if (a.part_tiles) {
+    kt0 = min(t.part * a.part_tiles * 4, nt);
+    nt = min(kt0 + a.part_tiles * 4, nt);
+  }
+  f32x4 qf[NKC];   // scaled before the products, which may overflow without
+  {
+    const float* qrow = (const float*)a.q + (q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+    for (int c = 0; c < NKC; c++) {
+      qf[c] = *(const f32x4*)(qrow + 16 * c + 4 * g4);
+#pragma unroll
+      for (int e = 0; e < 4; e++) qf[c][e] *= a.scale;
+    }
+  }
+  W w;
+  auto fetch = [&](int kt) { w.fetch(Kg + (int64_t)kt * 16 * a.k_row, a.k_row, Vg + (int64_t)kt * 16 * a.v_row, a.v_row, n - kt * 16); };
+  f32x4 o[NKC];
+#pragma unroll
+  for (int i = 0; i < NKC; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_run = M_FLOOR, l_run = 0.f;
+  if (kt0 + wave < nt) {
+    fetch(kt0 + wave);
+    w.stage(sk[wave], sv[wave]);
+  }
+  for (int kt = kt0 + wave; kt < nt; kt += 4) {
+    if (kt + 4 < nt) fetch(kt + 4);
+    f32x4 s = W::dot(sk[wave], qf, l16, g4);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      if (kt * 16 + 4 * g4 + r >= vis) s[r] = -INFINITY;
+      mx = fmaxf(mx, s[r]);
+    }
+    mx = pair_max(fmaxf(mx, __shfl_xor(mx, 16, 64)));
+    const float m_new = fmaxf(m_run, mx), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * LOG2E);
+    m_run = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int i = 0; i < NKC; i++)
+#pragma unroll
+      for (int r = 0; r < 4; r++) o[i][r] *= alpha;
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+      s[r] = __builtin_amdgcn_exp2f((s[r] - m_new) * LOG2E);
+      l_run += s[r];
+    }
+    W::add(o, sv[wave], s, l16, g4);
+    if (kt + 4 < nt) w.stage(sk[wave], sv[wave]);
+  }
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run = pair_sum(l_run);
+  if (g4 == 0) ml[wave][l16] = make_float2(m_run, l_run);
+  __syncthreads();
+  float m = M_FLOOR, l = 0.f;
+#pragma unroll
+  for (int x = 0; x < 4; x++) m = fmaxf(m, ml[x][l16].x);
+#pragma unroll
+  for (int x = 0; x < 4; x++) l = fmaf(__builtin_amdgcn_exp2f((ml[x][l16].x - m) * LOG2E), ml[x][l16].y, l);
+  const float mine = __builtin_amdgcn_exp2f((m_run - m) * LOG2E);
+#pragma unroll
+  for (int i = 0; i < NKC; i++) o[i] *= mine;
+  join_waves<D>(sk[0], o, wave, l16, g4);
+  if (wave > 0 || row0 + l16 >= rows) return;
+  const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+  const float lse = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l) * LN2;
+  float* orow = (float*)a.o + (q0 + tok) * a.o_row + (int64_t)head * a.o_head;
+  float* olse = a.lse ? a.lse + (q0 + tok) * a.H + head : nullptr;
+  if (a.part_tiles && t.parts > 1) {
+    const int64_t slot = t.slot * ROWS + l16;
+    orow = a.part_o + slot * D;
+    olse = a.part_lse + slot;
+  }
+  if (olse && g4 == 0) *olse = lse;
+#pragma unroll
+  for (int i = 0; i < NKC; i++)
+    *(float4*)(orow + 16 * i + 4 * g4) = make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
+}
+
+// ---------------------------------------------------------------------------
 // bf16, few rows: a new token (or a few) of each sequence against its keys, bound by reading K and V once. Tiles of 16 rows on
 // v_mfma_f32_16x16x32_bf16; the NW waves of a workgroup do not share rows but keys: wave w takes the 32-key stages w, w + NW, ...
 // of the part with a running maximum, sum and output of its own, so no barrier stands in the loop, and they meet at
@@ -674,7 +775,8 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
 }
 
 // Tiles and parts.
-//   rows   bf16: 16 where no sequence has more than FEW_ROWS (query, head) rows per key/value head, else 128; fp32: 64
+//   rows   16 where no sequence has more than FEW_ROWS (query, head) rows per key/value head; else bf16: 128, fp32: 64, or 16 where
+//          tiles of 64 leave CUs without a workgroup
 //   parts  16-row tiles: one CU streams keys at 60 GB/s (128 keys of K and V at head_dim 128 in 1.05 us, after 4.4 us for a call), and
 //          the launch that joins parts costs 4 us. So keys are shared out where a sequence may have more than 12 tiles, for about
 //          two workgroups per CU (32 tokens, 90 k keys of 8 heads: 80 us; four per CU: 88), in parts of at least 4 tiles (one
@@ -685,9 +787,10 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
   PackedPlan p{};
   const int G = H / Hkv;
   const bool few = (int64_t)max_q * G <= FEW_ROWS;
-  p.rows = dtype == DT_F32 ? 64 : few ? 16 : 128;
+  auto tiles_of = [&](int rows) { return std::min<int64_t>((int64_t)total_q * G / rows + nseq, (int64_t)nseq * cdiv((int64_t)max_q * G, rows)); };
+  p.rows = few || (dtype == DT_F32 && tiles_of(64) * Hkv < CUS) ? 16 : dtype == DT_F32 ? 64 : 128;
   const int64_t per_seq = cdiv((int64_t)max_q * G, p.rows);   // no sequence has more row tiles
-  p.row_tiles = p.units = (int)std::min<int64_t>((int64_t)total_q * G / p.rows + nseq, nseq * per_seq);
+  p.row_tiles = p.units = (int)tiles_of(p.rows);
   const int64_t groups = (int64_t)p.row_tiles * Hkv;
   if (groups == 0 || (!few && groups >= CUS)) return p;
   const int64_t tiles = cdiv(total_k, 64), work = tiles * groups / nseq;
@@ -702,7 +805,8 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
 
 template <int D>
 static void fwd_launch(const PackedArgs& a, int dtype, int rows, int64_t grid, hipStream_t s) {
-  if (dtype == DT_F32) packed_fwd_f32<D><<<grid, 256, 0, s>>>(a);
+  if (dtype == DT_F32 && rows == 16) packed_split_f32<D><<<grid, 256, 0, s>>>(a);
+  else if (dtype == DT_F32) packed_fwd_f32<D><<<grid, 256, 0, s>>>(a);
   else if (rows == 16) packed_few_bf16<D, 4><<<grid, 256, 0, s>>>(a);
   else if (a.part_tiles) packed_fwd_bf16<D, true><<<grid, 256, 0, s>>>(a);
   else packed_fwd_bf16<D, false><<<grid, 256, 0, s>>>(a);
@@ -721,7 +825,8 @@ hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStr
   else fwd_launch<64>(a, dtype, p.rows, grid, s);
   if (p.part_tiles) {
     const int64_t jg = (int64_t)p.row_tiles * a.Hkv * (p.rows / 4);
-    if (p.rows == 16) packed_join<u16, 16><<<jg, 256, 0, s>>>(a, d);
+    if (p.rows == 16 && dtype == DT_F32) packed_join<float, 16><<<jg, 256, 0, s>>>(a, d);
+    else if (p.rows == 16) packed_join<u16, 16><<<jg, 256, 0, s>>>(a, d);
     else if (dtype == DT_BF16) packed_join<u16, 128><<<jg, 256, 0, s>>>(a, d);
     else packed_join<float, 64><<<jg, 256, 0, s>>>(a, d);
   }

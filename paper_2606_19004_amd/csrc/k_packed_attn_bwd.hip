@@ -371,68 +371,27 @@ __global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// fp32, v_mfma_f32_16x16x4_f32: 4 waves own 16 rows (or keys) each and walk tiles of 16 keys (rows) of both
-// operands, staged through registers one tile ahead.
+// fp32: 4 waves own 16 rows (or keys) each and share tiles of 16 keys (rows) of both operands. SPLIT, for problems that have too few such
+// workgroups to fill the chip: the waves own the same 16 and take every fourth tile, each staging its own, so that
+// the chain of tiles is a quarter as long; their sums meet at the end.
 // ---------------------------------------------------------------------------
-// The walked tile: NROW rows of two tensors
-template <int D> struct WalkF32 {
-  static constexpr int NROW = 16, LD = D + 4, CPT = NROW * D / 4 / 256;
-  f32x4 ra[CPT], rb[CPT];
-  // rows past `left` repeat the last one (their p is 0) with zeros, as 0 times an infinity would be NaN
-  __device__ __forceinline__ void fetch(const float* a, int64_t as, const float* b, int64_t bs, int left) {
-#pragma unroll
-    for (int i = 0; i < CPT; i++) {
-      const int idx = threadIdx.x + 256 * i, r = idx / (D / 4), c = idx % (D / 4), rr = min(r, left - 1);
-      ra[i] = *(const f32x4*)(a + rr * as + 4 * c);
-      rb[i] = *(const f32x4*)(b + rr * bs + 4 * c);
-      if (r >= left) ra[i] = rb[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-  }
-  __device__ __forceinline__ void stage(float* sa, float* sb) const {
-#pragma unroll
-    for (int i = 0; i < CPT; i++) {
-      const int idx = threadIdx.x + 256 * i, r = idx / (D / 4), c = idx % (D / 4);
-      *(f32x4*)(sa + r * LD + 4 * c) = ra[i];
-      *(f32x4*)(sb + r * LD + 4 * c) = rb[i];
-    }
-  }
-  // [walked row][owned] products of both tensors with the owned fragments
-  static __device__ __forceinline__ f32x4 dot(const float* st, const f32x4* own, int l16, int g4) {
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < D / 16; c++) {
-      const f32x4 w = *(const f32x4*)(st + l16 * LD + 16 * c + 4 * g4);
-#pragma unroll
-      for (int e = 0; e < 4; e++) s = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], own[c][e], s, 0, 0, 0);
-    }
-    return s;
-  }
-  // acc[dim][owned] += sum over the walked rows of st[row][dim] w[row][owned]
-  static __device__ __forceinline__ void add(f32x4* acc, const float* st, const f32x4& w, int l16, int g4) {
-#pragma unroll
-    for (int r = 0; r < 4; r++)
-#pragma unroll
-      for (int i = 0; i < D / 16; i++)
-        acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(st[(4 * g4 + r) * LD + l16 + 16 * i], w[r], acc[i], 0, 0, 0);
-  }
-};
-
-template <int D>
+template <int D, bool SPLIT>
 __global__ void __launch_bounds__(256) packed_dq_f32(PackedArgs a) {
-  constexpr int ROWS = 64, NKC = D / 16;
-  using W = WalkF32<D>;
-  __shared__ __attribute__((aligned(16))) float sk[2][W::NROW * W::LD], sv[2][W::NROW * W::LD];
+  constexpr int ROWS = SPLIT ? 16 : 64, NKC = D / 16, LANES = SPLIT ? 64 : 256, BUFS = SPLIT ? 4 : 2;
+  using W = WalkF32<D, LANES>;
+  __shared__ __attribute__((aligned(16))) float sk[BUFS][W::NROW * W::LD], sv[BUFS][W::NROW * W::LD];
   const int g = blockIdx.x % a.Hkv;
   int seq, rt;
   PackedSeq sq;
   if (!find_row_tile<ROWS>(a, seq, rt, sq)) return;
   const int m = sq.m, n = sq.n, rows = m * a.G;
   if (a.causal) rt = cdiv(rows, ROWS) - 1 - rt;
-  const int row0 = rt * ROWS, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int row0 = rt * ROWS, mine = row0 + (SPLIT ? 0 : wave * 16) + l16;
   const int64_t q0 = sq.q0, k0 = sq.k0;
   const float* Kg = (const float*)a.k + k0 * a.k_row + (int64_t)g * a.k_head;
   const float* Vg = (const float*)a.v + k0 * a.v_row + (int64_t)g * a.v_head;
-  const int row = min(row0 + wave * 16 + l16, rows - 1);
+  const int row = min(mine, rows - 1);
   const int tok = row / a.G, head = g * a.G + (row - tok * a.G);
   const int vis = a.causal ? min(tok + n - m + 1, n) : n;
   f32x4 qf[NKC], df[NKC];
@@ -450,7 +409,7 @@ __global__ void __launch_bounds__(256) packed_dq_f32(PackedArgs a) {
   const float2 st = stats_of(a, q0 + tok, head);
   const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
   const int nvis = a.causal ? min(max(last_tok + n - m + 1, 0), n) : n;
-  const int nt = cdiv(nvis, W::NROW);
+  const int nt = cdiv(nvis, W::NROW), first = SPLIT ? wave : 0, step = SPLIT ? 4 : 1;
   f32x4 dq[NKC];
 #pragma unroll
   for (int i = 0; i < NKC; i++) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -458,14 +417,15 @@ __global__ void __launch_bounds__(256) packed_dq_f32(PackedArgs a) {
   auto fetch = [&](int kt) {
     w.fetch(Kg + (int64_t)kt * W::NROW * a.k_row, a.k_row, Vg + (int64_t)kt * W::NROW * a.v_row, a.v_row, n - kt * W::NROW);
   };
-  if (nt > 0) {
-    fetch(0);
-    w.stage(sk[0], sv[0]);
+  auto buf_of = [&](int kt) { return SPLIT ? wave : kt & 1; };
+  if (first < nt) {
+    fetch(first);
+    w.stage(sk[buf_of(first)], sv[buf_of(first)]);
   }
-  for (int kt = 0; kt < nt; kt++) {
-    const int buf = kt & 1;
-    __syncthreads();
-    if (kt + 1 < nt) fetch(kt + 1);
+  for (int kt = first; kt < nt; kt += step) {
+    const int buf = buf_of(kt);
+    if (!SPLIT) __syncthreads();   // (a wave's own tile needs none)
+    if (kt + step < nt) fetch(kt + step);
     f32x4 s = W::dot(sk[buf], qf, l16, g4), dp = W::dot(sv[buf], df, l16, g4);
 #pragma unroll
     for (int r = 0; r < 4; r++) {
@@ -473,29 +433,33 @@ __global__ void __launch_bounds__(256) packed_dq_f32(PackedArgs a) {
       s[r] = hidden ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], LOG2E, -st.x)) * (dp[r] - st.y);
     }
     W::add(dq, sk[buf], s, l16, g4);
-    if (kt + 1 < nt) w.stage(sk[buf ^ 1], sv[buf ^ 1]);
+    if (kt + step < nt) w.stage(sk[buf_of(kt + step)], sv[buf_of(kt + step)]);
   }
-  if (row0 + wave * 16 + l16 >= rows) return;
+  if (SPLIT) {
+    join_waves<D>(sk[0], dq, wave, l16, g4);
+    if (wave > 0) return;
+  }
+  if (mine >= rows) return;
   float* out = (float*)a.dq + (q0 + tok) * a.q_row + (int64_t)head * a.q_head;
 #pragma unroll
   for (int i = 0; i < NKC; i++)
     *(float4*)(out + 16 * i + 4 * g4) = make_float4(dq[i][0] * a.scale, dq[i][1] * a.scale, dq[i][2] * a.scale, dq[i][3] * a.scale);
 }
 
-template <int D>
+template <int D, bool SPLIT>
 __global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
-  constexpr int KEYS = 64, NKC = D / 16;
-  using W = WalkF32<D>;
-  __shared__ __attribute__((aligned(16))) float sq[2][W::NROW * W::LD], sd[2][W::NROW * W::LD];
+  constexpr int KEYS = SPLIT ? 16 : 64, NKC = D / 16, LANES = SPLIT ? 64 : 256, BUFS = SPLIT ? 4 : 2;
+  using W = WalkF32<D, LANES>;
+  __shared__ __attribute__((aligned(16))) float sq[BUFS][W::NROW * W::LD], sd[BUFS][W::NROW * W::LD];
   const int g = blockIdx.x % a.Hkv;
   int seq, kt;
   PackedSeq ps;
   if (!find_key_tile<KEYS>(a, a.shares, seq, kt, ps)) return;
   const int share = blockIdx.x / a.Hkv % a.shares;
   const int m = ps.m, n = ps.n;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int64_t q0 = ps.q0, k0 = ps.k0;
-  const int key = kt * KEYS + wave * 16 + l16;
+  const int key = kt * KEYS + (SPLIT ? 0 : wave * 16) + l16;
   f32x4 kf[NKC], vf[NKC];
   {
     const int64_t kr = k0 + min(key, n - 1);
@@ -516,36 +480,45 @@ __global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
 #pragma unroll
   for (int i = 0; i < NKC; i++) dk[i] = dv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   W w;
-  auto fetch = [&](int h, int t) {
+  float2 st[4], next[4];   // of rows 4 g4 + r
+  // step i of all heads' tiles in turn: head i / per, tile t0 + i % per
+  auto fetch = [&](int i) {
+    const int h = i / per, t = t0 + i - h * per;
     const int64_t head = (int64_t)g * a.G + h, at = q0 + t * W::NROW;
     w.fetch((const float*)a.q + at * a.q_row + head * a.q_head, a.q_row,
             (const float*)a.d_o + at * a.o_row + head * a.o_head, a.o_row, m - t * W::NROW);
+#pragma unroll
+    for (int r = 0; r < 4; r++) next[r] = stats_of(a, q0 + min(t * W::NROW + 4 * g4 + r, m - 1), head);
   };
-  const int begin = share_begin(per * a.G, share, a.shares), steps = share_begin(per * a.G, share + 1, a.shares) - begin;
-  int h = per > 0 ? begin / per : 0, t = t0 + begin - h * per;
-  if (steps > 0) {
-    fetch(h, t);
-    w.stage(sq[0], sd[0]);
+  const int begin = share_begin(per * a.G, share, a.shares) + (SPLIT ? wave : 0), end = share_begin(per * a.G, share + 1, a.shares);
+  const int step = SPLIT ? 4 : 1;
+  auto buf_of = [&](int i) { return SPLIT ? wave : i & 1; };
+  if (begin < end) {
+    fetch(begin);
+    w.stage(sq[buf_of(begin)], sd[buf_of(begin)]);
   }
-  for (int i = 0; i < steps; i++) {
-    const int buf = i & 1;
-    __syncthreads();
-    const int nh = t + 1 == t0 + per ? h + 1 : h, nt = t + 1 == t0 + per ? t0 : t + 1;
-    if (i + 1 < steps) fetch(nh, nt);
+  for (int i = begin; i < end; i += step) {
+    const int buf = buf_of(i), t = t0 + i % per;
+    if (!SPLIT) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; r++) st[r] = next[r];
+    if (i + step < end) fetch(i + step);
     f32x4 s = W::dot(sq[buf], kf, l16, g4), dp = W::dot(sd[buf], vf, l16, g4);
 #pragma unroll
     for (int r = 0; r < 4; r++) {
       const int tok = t * W::NROW + 4 * g4 + r;
-      const float2 st = stats_of(a, q0 + min(tok, m - 1), (int64_t)g * a.G + h);
       const bool hidden = tok >= m || tok < first;
-      s[r] = hidden ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], LOG2E, -st.x));
-      dp[r] = hidden ? 0.f : s[r] * (dp[r] - st.y);
+      s[r] = hidden ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], LOG2E, -st[r].x));
+      dp[r] = hidden ? 0.f : s[r] * (dp[r] - st[r].y);
     }
     W::add(dv, sd[buf], s, l16, g4);
     W::add(dk, sq[buf], dp, l16, g4);
-    if (i + 1 < steps) w.stage(sq[buf ^ 1], sd[buf ^ 1]);
-    h = nh;
-    t = nt;
+    if (i + step < end) w.stage(sq[buf_of(i + step)], sd[buf_of(i + step)]);
+  }
+  if (SPLIT) {
+    join_waves<D>(sq[0], dk, wave, l16, g4);
+    join_waves<D>(sq[0], dv, wave, l16, g4);
+    if (wave > 0) return;
   }
   if (key >= n) return;
   float* ok = (float*)a.dk + (k0 + key) * a.k_row + (int64_t)g * a.k_head;
@@ -591,6 +564,16 @@ __global__ void __launch_bounds__(256) shares_join(PackedArgs a) {
 
 size_t stats_bytes(int H, int total_q) { return ((size_t)total_q * H * 8 + 255) & ~(size_t)255; }
 
+// Keys (query rows) of a workgroup; fp32: 16, whose walk its waves split, where tiles of 64 would leave CUs without a workgroup (3 sequences
+// of 80 to 333, 4 heads of 64, all gradients: 51 us with tiles of 64)
+int key_tile(int dtype, int nseq, int Hkv, int total_k) {
+  return dtype == DT_BF16 ? 128 : ((int64_t)total_k / 64 + nseq) * Hkv < 256 ? 16 : 64;
+}
+int64_t row_tiles(const PackedArgs& a, int rows) {
+  return std::min<int64_t>((int64_t)a.qr.total * a.G / rows + a.nseq, (int64_t)a.nseq * cdiv((int64_t)a.max_q * a.G, rows)) * a.Hkv;
+}
+int row_tile(const PackedArgs& a, int dtype) { return dtype == DT_BF16 ? 128 : row_tiles(a, 64) < 256 ? 16 : 64; }
+
 // Into how many workgroups the rows that a key tile walks are shared out. A share costs a write and a read of its fp32 sums,
 // about what 350 rows cost to walk.
 //   fewer key tiles than CUs      as many as fill two workgroups per CU, of 256 rows at least
@@ -598,10 +581,9 @@ size_t stats_bytes(int H, int total_q) { return ((size_t)total_q * H * 8 + 255) 
 //                                 the longest ones run alone (8192 keys of 8 heads, 4 query heads each: 1952 us in one
 //                                 share)
 int shares_of(int dtype, int nseq, int H, int Hkv, int total_q, int total_k, int causal) {
-  const int keys = dtype == DT_BF16 ? 128 : 64;
-  const int64_t units = ((int64_t)total_k / keys + nseq) * Hkv, rows = (int64_t)total_q * (H / Hkv) / nseq;
-  if (units < 256) return (int)std::max<int64_t>(1, std::min<int64_t>(512 / units, rows / (dtype == DT_BF16 ? 256 : 64)));
-  return causal && units < 1024 && rows >= 4096 ? 2 : 1;
+  const int64_t units = ((int64_t)total_k / key_tile(dtype, nseq, Hkv, total_k) + nseq) * Hkv, rows = (int64_t)total_q * (H / Hkv) / nseq;
+  if (units < 256) return (int)std::max<int64_t>(1, std::min<int64_t>(512 / units, rows / 256));
+  return causal && dtype == DT_BF16 && units < 1024 && rows >= 4096 ? 2 : 1;
 }
 
 }  // namespace
@@ -626,9 +608,10 @@ hipError_t packed_attention_stats(PackedArgs a, int dtype, int d, void* ws, hipS
 }
 
 template <int D>
-static void dkdv_launch(const PackedArgs& a, int dtype, int64_t units, int64_t joins, hipStream_t s) {
+static void dkdv_launch(const PackedArgs& a, int dtype, int keys, int64_t units, int64_t joins, hipStream_t s) {
   if (dtype == DT_BF16) packed_dkdv_bf16<D><<<units, 256, 0, s>>>(a);
-  else packed_dkdv_f32<D><<<units, 256, 0, s>>>(a);
+  else if (keys == 16) packed_dkdv_f32<D, true><<<units, 256, 0, s>>>(a);
+  else packed_dkdv_f32<D, false><<<units, 256, 0, s>>>(a);
   if (a.shares <= 1) return;
   if (dtype == DT_BF16) shares_join<u16, D><<<joins, 256, 0, s>>>(a);
   else shares_join<float, D><<<joins, 256, 0, s>>>(a);
@@ -639,22 +622,26 @@ hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, void* ws, hipSt
   a.stats = (float2*)ws;
   a.shares = shares_of(dtype, a.nseq, a.H, a.Hkv, a.qr.total, total_k, a.causal);
   a.share_sums = (float*)((char*)ws + stats_bytes(a.H, a.qr.total));
-  const int keys = dtype == DT_BF16 ? 128 : 64;
+  const int keys = key_tile(dtype, a.nseq, a.Hkv, total_k);
   const int64_t units = ((int64_t)total_k / keys + a.nseq) * a.Hkv * a.shares, joins = ((int64_t)total_k / 64 + a.nseq) * a.Hkv;
-  if (d == 128) dkdv_launch<128>(a, dtype, units, joins, s);
-  else dkdv_launch<64>(a, dtype, units, joins, s);
+  if (d == 128) dkdv_launch<128>(a, dtype, keys, units, joins, s);
+  else dkdv_launch<64>(a, dtype, keys, units, joins, s);
   return hipGetLastError();
 }
 
+template <int D>
+static void dq_launch(const PackedArgs& a, int dtype, int rows, int64_t grid, hipStream_t s) {
+  if (dtype == DT_BF16) packed_dq_bf16<D><<<grid, 256, 0, s>>>(a);
+  else if (rows == 16) packed_dq_f32<D, true><<<grid, 256, 0, s>>>(a);
+  else packed_dq_f32<D, false><<<grid, 256, 0, s>>>(a);
+}
 hipError_t packed_attention_dq(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
   a.stats = (float2*)ws;
-  const int rows = dtype == DT_BF16 ? 128 : 64;
-  const int64_t grid = std::min<int64_t>((int64_t)a.qr.total * a.G / rows + a.nseq, (int64_t)a.nseq * cdiv((int64_t)a.max_q * a.G, rows)) * a.Hkv;
+  const int rows = row_tile(a, dtype);
+  const int64_t grid = row_tiles(a, rows);
   if (grid == 0) return hipSuccess;
-  if (dtype == DT_BF16 && d == 128) packed_dq_bf16<128><<<grid, 256, 0, s>>>(a);
-  else if (dtype == DT_BF16) packed_dq_bf16<64><<<grid, 256, 0, s>>>(a);
-  else if (d == 128) packed_dq_f32<128><<<grid, 256, 0, s>>>(a);
-  else packed_dq_f32<64><<<grid, 256, 0, s>>>(a);
+  if (d == 128) dq_launch<128>(a, dtype, rows, grid, s);
+  else dq_launch<64>(a, dtype, rows, grid, s);
   return hipGetLastError();
 }
 
