@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// fp32 where tiles of 64 rows would leave CUs idle: 16 rows per workgroup, whose 4 waves take every fourth 16-key tile, each staging its
+// fp32 where tiles of 64 rows would be few: 16 rows per workgroup, whose 4 waves take every fourth 16-key tile, each staging its
 // own, with a running maximum and sum of their own; they meet at the end.
 // ---------------------------------------------------------------------------
 template <int D>
@@ -776,7 +776,7 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
 
 // Tiles and parts.
 //   rows   16 where no sequence has more than FEW_ROWS (query, head) rows per key/value head; else bf16: 128, fp32: 64, or 16 where
-//          tiles of 64 leave CUs without a workgroup
+//          tiles of 64 are fewer than two workgroups per CU (4 x 300 tokens, 16 heads of 64: 22 us, as tiles of 64 28)
 //   parts  16-row tiles: one CU streams keys at 60 GB/s (128 keys of K and V at head_dim 128 in 1.05 us, after 4.4 us for a call), and
 //          the launch that joins parts costs 4 us. So keys are shared out where a sequence may have more than 12 tiles, for about
 //          two workgroups per CU (32 tokens, 90 k keys of 8 heads: 80 us; four per CU: 88), in parts of at least 4 tiles (one
@@ -788,7 +788,7 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
   const int G = H / Hkv;
   const bool few = (int64_t)max_q * G <= FEW_ROWS;
   auto tiles_of = [&](int rows) { return std::min<int64_t>((int64_t)total_q * G / rows + nseq, (int64_t)nseq * cdiv((int64_t)max_q * G, rows)); };
-  p.rows = few || (dtype == DT_F32 && tiles_of(64) * Hkv < CUS) ? 16 : dtype == DT_F32 ? 64 : 128;
+  p.rows = few || (dtype == DT_F32 && tiles_of(64) * Hkv < 2 * CUS) ? 16 : dtype == DT_F32 ? 64 : 128;
   const int64_t per_seq = cdiv((int64_t)max_q * G, p.rows);   // no sequence has more row tiles
   p.row_tiles = p.units = (int)tiles_of(p.rows);
   const int64_t groups = (int64_t)p.row_tiles * Hkv;

@@ -564,15 +564,16 @@ __global__ void __launch_bounds__(256) shares_join(PackedArgs a) {
 
 size_t stats_bytes(int H, int total_q) { return ((size_t)total_q * H * 8 + 255) & ~(size_t)255; }
 
-// Keys (query rows) of a workgroup; fp32: 16, whose walk its waves split, where tiles of 64 would leave CUs without a workgroup (3 sequences
-// of 80 to 333, 4 heads of 64, all gradients: 51 us with tiles of 64)
+// Keys (query rows) of a workgroup; fp32: 16, whose walk its waves split, where tiles of 64 would be fewer than two workgroups per CU
+// (all gradients, 16 heads of 64, causal: 4 x 300 tokens, 364 tiles of 64: 71 us, as tiles of 64 97; 8 x 300 tokens of 12 heads,
+// 540 tiles: 102 and 106; heads of 128: 206 and 184)
 int key_tile(int dtype, int nseq, int Hkv, int total_k) {
-  return dtype == DT_BF16 ? 128 : ((int64_t)total_k / 64 + nseq) * Hkv < 256 ? 16 : 64;
+  return dtype == DT_BF16 ? 128 : ((int64_t)total_k / 64 + nseq) * Hkv < 512 ? 16 : 64;
 }
 int64_t row_tiles(const PackedArgs& a, int rows) {
   return std::min<int64_t>((int64_t)a.qr.total * a.G / rows + a.nseq, (int64_t)a.nseq * cdiv((int64_t)a.max_q * a.G, rows)) * a.Hkv;
 }
-int row_tile(const PackedArgs& a, int dtype) { return dtype == DT_BF16 ? 128 : row_tiles(a, 64) < 256 ? 16 : 64; }
+int row_tile(const PackedArgs& a, int dtype) { return dtype == DT_BF16 ? 128 : row_tiles(a, 64) < 512 ? 16 : 64; }
 
 // Into how many workgroups the rows that a key tile walks are shared out. A share costs a write and a read of its fp32 sums,
 // about what 350 rows cost to walk.
