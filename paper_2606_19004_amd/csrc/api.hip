@@ -1414,9 +1414,7 @@ dit_status packed_attention_backward(const dit_packed_config* c, const void* q, 
   const double product = 2.0 * pairs * c->heads * c->head_dim;
   TIMED("packed_attention_stats", 0, 2.0 * c->total_q * c->heads * c->head_dim * esize(c->dtype), hs(stream),
         packed_attention_stats(a, c->dtype, c->head_dim, ws, hs(stream)));
-  TIMED("packed_attention_dkdv", 4 * product, 0, hs(stream),
-        packed_attention_dkdv(a, c->dtype, c->head_dim, ws, hs(stream)));
-  TIMED("packed_attention_dq", 3 * product, 0, hs(stream), packed_attention_dq(a, c->dtype, c->head_dim, ws, hs(stream)));
+  TIMED("packed_attention_gradients", 7 * product, 0, hs(stream), packed_attention_gradients(a, c->dtype, c->head_dim, ws, hs(stream)));
   return DIT_OK;
 }
 

@@ -1,10 +1,9 @@
 // Gradients of packed attention on gfx950. With s = scale q k^T, p = exp(s - lse) and delta = rowsum(do o),
 //   dv = p^T do,   ds = p (do v^T - delta),   dq = scale ds k,   dk = scale ds^T q.
 //
-// Two kernels recompute p, so that every gradient is summed by one workgroup in a fixed order (no atomics, no
-// partial gradients in memory): one owns query rows and walks the keys (dq: 3 products), one owns keys and walks
-// the query rows of all heads that share them (dk, dv: 4 products). That is 7 products where 5 would do with
-// atomics on dq.
+// Two kinds of workgroup recompute p, so that every gradient is summed in a fixed order without atomics: one owns
+// query rows and walks the keys (dq: 3 products), one owns keys and walks the query rows of all heads that share them
+// (dk, dv: 4 products). That is 7 products where 5 would do with atomics on dq.
 //
 // bf16, v_mfma_f32_32x32x16_bf16, 4 waves: an owned row (or key) is a column of the score block, so that p and ds
 // of a lane belong to one owned row and are operand B of the next product as they stand, rounded to bf16 (2^-9
@@ -85,12 +84,17 @@ __device__ __forceinline__ void store_columns(char* so, const f32x16* acc, float
   }
 }
 
-template <int ROWS> __device__ __forceinline__ bool find_row_tile(const PackedArgs& a, int& seq, int& tile, PackedSeq& s) {
-  return find_unit(a.nseq, blockIdx.x / a.Hkv, [&](int i) { return a.sequence(i); },
+// Both kinds of workgroup are in one launch, those of the keys, which are the longer, first. In a launch each, every CU waits between
+// them for the last workgroup of the first (all gradients, graph replays, us in two launches / one: fp32 3 x 80..333 tokens 26.1 / 19.8,
+// joint attention of 512 tokens 312 / 297, causal 8192 tokens 1905 / 1862).
+template <int D> constexpr int GRAD_LDS = 4 * 64 * 2 * D + 512;
+
+template <int ROWS> __device__ __forceinline__ bool find_row_tile(const PackedArgs& a, int block, int& seq, int& tile, PackedSeq& s) {
+  return find_unit(a.nseq, block / a.Hkv, [&](int i) { return a.sequence(i); },
                    [&](const PackedSeq& x) { return (x.m * a.G + ROWS - 1) / ROWS; }, seq, tile, s);
 }
-template <int KEYS> __device__ __forceinline__ bool find_key_tile(const PackedArgs& a, int shares, int& seq, int& tile, PackedSeq& s) {
-  return find_unit(a.nseq, blockIdx.x / (a.Hkv * shares), [&](int i) { return a.sequence(i); },
+template <int KEYS> __device__ __forceinline__ bool find_key_tile(const PackedArgs& a, int block, int shares, int& seq, int& tile, PackedSeq& s) {
+  return find_unit(a.nseq, block / (a.Hkv * shares), [&](int i) { return a.sequence(i); },
                    [&](const PackedSeq& x) { return (x.n + KEYS - 1) / KEYS; }, seq, tile, s);
 }
 
@@ -98,16 +102,15 @@ template <int KEYS> __device__ __forceinline__ bool find_key_tile(const PackedAr
 // dq: 128 query rows (row r: query r / G, head r % G of the group) against 64-key tiles
 // ---------------------------------------------------------------------------
 template <int D>
-__global__ void __launch_bounds__(256, 2) packed_dq_bf16(PackedArgs a) {
+__device__ __forceinline__ void dq_bf16(const PackedArgs& a, int block, char* smem) {   // [K0][K1][V0][V1]
   constexpr int ROWS = 128, KB = 64, NDB = D / 32, NKS = D / 16;
   using Tile = RowTile<D, KB, 4>;
   constexpr int TILE = Tile::BYTES, RB = Tile::RB;
-#if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];   // [K0][K1][V0][V1]
-  const int g = blockIdx.x % a.Hkv;
+  static_assert(4 * TILE <= GRAD_LDS<D>, "");
+  const int g = block % a.Hkv;
   int seq, rt;
   PackedSeq sq;
-  if (!find_row_tile<ROWS>(a, seq, rt, sq)) return;
+  if (!find_row_tile<ROWS>(a, block, seq, rt, sq)) return;
   const int m = sq.m, n = sq.n;
   const int rows = m * a.G;
   if (a.causal) rt = cdiv(rows, ROWS) - 1 - rt;
@@ -201,12 +204,12 @@ __global__ void __launch_bounds__(256, 2) packed_dq_bf16(PackedArgs a) {
       *(uint4*)((u16*)a.dq + (int64_t)(q0 + t) * a.q_row + (int64_t)hd * a.q_head + 8 * ch) = v;
     }
   });
-#endif
 }
 
 // ---------------------------------------------------------------------------
 // dk, dv: 128 keys of one key/value head against 32-query tiles of every head of its group in turn. V stays in LDS and K in
-// registers: with both in registers 40 of them spilled at two waves per SIMD (joint attention at 512x512: 232 us against 197).
+// registers: with both in registers 40 of them spilled at two waves per SIMD (these products alone, joint attention at 512x512:
+// 232 us against 197).
 // The tiles may be shared out between a.shares workgroups, whose sums meet in the workspace (shares_join).
 // ---------------------------------------------------------------------------
 // The first of `steps` that share i of n takes.
@@ -217,18 +220,17 @@ __device__ __forceinline__ float* share_row(const PackedArgs& a, int D, int i, i
 }
 
 template <int D>
-__global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
+__device__ __forceinline__ void dkdv_bf16(const PackedArgs& a, int block, char* smem) {   // [Q0][Q1][dO0][dO1][V], then the rows' statistics
   constexpr int KEYS = 128, QB = 32, NDB = D / 32, NKS = D / 16;
   using Tile = RowTile<D, QB, 4>;
   constexpr int TILE = Tile::BYTES, RB = Tile::RB;
-#if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE + KEYS * RB];
-  __shared__ float4 stat[2][2][QB / 4];                            // lse (log2 units) and delta of a tile's rows
-  const int g = blockIdx.x % a.Hkv;
+  static_assert(4 * TILE + KEYS * RB + 4 * QB * 4 <= GRAD_LDS<D>, "");
+  auto stat = (float4(*)[2][QB / 4])(smem + 4 * TILE + KEYS * RB);   // lse (log2 units) and delta of a tile's rows
+  const int g = block % a.Hkv;
   int seq, kt;
   PackedSeq ps;
-  if (!find_key_tile<KEYS>(a, a.shares, seq, kt, ps)) return;
-  const int share = blockIdx.x / a.Hkv % a.shares;
+  if (!find_key_tile<KEYS>(a, block, a.shares, seq, kt, ps)) return;
+  const int share = block / a.Hkv % a.shares;
   const int m = ps.m, n = ps.n;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int half = lane >> 5, l32 = lane & 31;
@@ -367,6 +369,14 @@ __global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
   };
   store_columns<D>(smem + wave * 32 * RB, dk, a.scale, lane, rows_to(a.dk, a.k_row, a.k_head));
   store_columns<D>(smem + wave * 32 * RB, dv, 1.f, lane, rows_to(a.dv, a.v_row, a.v_head));
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) packed_gradients_bf16(PackedArgs a, int key_blocks) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ __attribute__((aligned(1024))) char smem[GRAD_LDS<D>];
+  if ((int)blockIdx.x < key_blocks) dkdv_bf16<D>(a, blockIdx.x, smem);
+  else dq_bf16<D>(a, blockIdx.x - key_blocks, smem);
 #endif
 }
 
@@ -375,15 +385,17 @@ __global__ void __launch_bounds__(256, 2) packed_dkdv_bf16(PackedArgs a) {
 // workgroups to fill the chip: the waves own the same 16 and take every fourth tile, each staging its own, so that
 // the chain of tiles is a quarter as long; their sums meet at the end.
 // ---------------------------------------------------------------------------
+template <int D, bool SPLIT> constexpr int WALK_LDS = (SPLIT ? 4 : 2) * 16 * (D + 4);   // floats of one operand's tiles
+
 template <int D, bool SPLIT>
-__global__ void __launch_bounds__(256) packed_dq_f32(PackedArgs a) {
-  constexpr int ROWS = SPLIT ? 16 : 64, NKC = D / 16, LANES = SPLIT ? 64 : 256, BUFS = SPLIT ? 4 : 2;
+__device__ __forceinline__ void dq_f32(const PackedArgs& a, int block, float* smem) {
+  constexpr int ROWS = SPLIT ? 16 : 64, NKC = D / 16, LANES = SPLIT ? 64 : 256;
   using W = WalkF32<D, LANES>;
-  __shared__ __attribute__((aligned(16))) float sk[BUFS][W::NROW * W::LD], sv[BUFS][W::NROW * W::LD];
-  const int g = blockIdx.x % a.Hkv;
+  auto sk = (float(*)[W::NROW * W::LD])smem, sv = (float(*)[W::NROW * W::LD])(smem + WALK_LDS<D, SPLIT>);
+  const int g = block % a.Hkv;
   int seq, rt;
   PackedSeq sq;
-  if (!find_row_tile<ROWS>(a, seq, rt, sq)) return;
+  if (!find_row_tile<ROWS>(a, block, seq, rt, sq)) return;
   const int m = sq.m, n = sq.n, rows = m * a.G;
   if (a.causal) rt = cdiv(rows, ROWS) - 1 - rt;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
@@ -447,15 +459,15 @@ __global__ void __launch_bounds__(256) packed_dq_f32(PackedArgs a) {
 }
 
 template <int D, bool SPLIT>
-__global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
-  constexpr int KEYS = SPLIT ? 16 : 64, NKC = D / 16, LANES = SPLIT ? 64 : 256, BUFS = SPLIT ? 4 : 2;
+__device__ __forceinline__ void dkdv_f32(const PackedArgs& a, int block, float* smem) {
+  constexpr int KEYS = SPLIT ? 16 : 64, NKC = D / 16, LANES = SPLIT ? 64 : 256;
   using W = WalkF32<D, LANES>;
-  __shared__ __attribute__((aligned(16))) float sq[BUFS][W::NROW * W::LD], sd[BUFS][W::NROW * W::LD];
-  const int g = blockIdx.x % a.Hkv;
+  auto sq = (float(*)[W::NROW * W::LD])smem, sd = (float(*)[W::NROW * W::LD])(smem + WALK_LDS<D, SPLIT>);
+  const int g = block % a.Hkv;
   int seq, kt;
   PackedSeq ps;
-  if (!find_key_tile<KEYS>(a, a.shares, seq, kt, ps)) return;
-  const int share = blockIdx.x / a.Hkv % a.shares;
+  if (!find_key_tile<KEYS>(a, block, a.shares, seq, kt, ps)) return;
+  const int share = block / a.Hkv % a.shares;
   const int m = ps.m, n = ps.n;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
   const int64_t q0 = ps.q0, k0 = ps.k0;
@@ -536,6 +548,13 @@ __global__ void __launch_bounds__(256) packed_dkdv_f32(PackedArgs a) {
   }
 }
 
+template <int D, bool SPLIT>
+__global__ void __launch_bounds__(256) packed_gradients_f32(PackedArgs a, int key_blocks) {
+  __shared__ __attribute__((aligned(16))) float smem[2 * WALK_LDS<D, SPLIT>];
+  if ((int)blockIdx.x < key_blocks) dkdv_f32<D, SPLIT>(a, blockIdx.x, smem);
+  else dq_f32<D, SPLIT>(a, blockIdx.x - key_blocks, smem);
+}
+
 // dk and dv of a key from its shares, in their order. Workgroup: 64 keys of one key/value head.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) shares_join(PackedArgs a) {
@@ -543,7 +562,7 @@ __global__ void __launch_bounds__(256) shares_join(PackedArgs a) {
   const int g = blockIdx.x % a.Hkv;
   int seq, kt;
   PackedSeq ps;
-  if (!find_key_tile<KEYS>(a, 1, seq, kt, ps)) return;
+  if (!find_key_tile<KEYS>(a, blockIdx.x, 1, seq, kt, ps)) return;
   const int n = ps.n, e = 4 * (threadIdx.x % LPR);
   const int64_t k0 = ps.k0;
   for (int r = threadIdx.x / LPR; r < KEYS && kt * KEYS + r < n; r += 256 / LPR) {
@@ -564,27 +583,30 @@ __global__ void __launch_bounds__(256) shares_join(PackedArgs a) {
 
 size_t stats_bytes(int H, int total_q) { return ((size_t)total_q * H * 8 + 255) & ~(size_t)255; }
 
-// Keys (query rows) of a workgroup; fp32: 16, whose walk its waves split, where tiles of 64 would be fewer than two workgroups per CU
-// (all gradients, 16 heads of 64, causal: 4 x 300 tokens, 364 tiles of 64: 71 us, as tiles of 64 97; 8 x 300 tokens of 12 heads,
-// 540 tiles: 102 and 106; heads of 128: 206 and 184)
-int key_tile(int dtype, int nseq, int Hkv, int total_k) {
-  return dtype == DT_BF16 ? 128 : ((int64_t)total_k / 64 + nseq) * Hkv < 512 ? 16 : 64;
+int64_t tiles_of(int nseq, int64_t rows, int64_t most, int tile) {   // of the sequences of a packed tensor, at most
+  return std::min<int64_t>(rows / tile + nseq, (int64_t)nseq * ((most + tile - 1) / tile));
 }
-int64_t row_tiles(const PackedArgs& a, int rows) {
-  return std::min<int64_t>((int64_t)a.qr.total * a.G / rows + a.nseq, (int64_t)a.nseq * cdiv((int64_t)a.max_q * a.G, rows)) * a.Hkv;
+// Keys and query rows of a workgroup; fp32: 16, whose walk its waves split, where tiles of 64 would be fewer than four workgroups per CU
+// (64 dims) or two (128 dims, where the split form's registers leave one workgroup per CU). All gradients, causal, us as tiles of 16 / 64:
+//   64 dims     4 x 200 tokens, 4 heads (128 tiles of 64) 20 / 34;  4 x 300, 16 heads (704) 65 / 74;  8 x 300, 12 heads (1080) 96 / 84
+//   128 dims    4 x 200 tokens, 4 heads (128) 32 / 55;  4 x 300, 16 heads (704) 157 / 113
+int grad_tile(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k) {
+  if (dtype == DT_BF16) return 128;
+  const int64_t rows = (int64_t)total_q * (H / Hkv);
+  return (tiles_of(nseq, total_k, total_k, 64) + tiles_of(nseq, rows, rows, 64)) * Hkv < (d == 64 ? 1024 : 512) ? 16 : 64;
 }
-int row_tile(const PackedArgs& a, int dtype) { return dtype == DT_BF16 ? 128 : row_tiles(a, 64) < 512 ? 16 : 64; }
 
 // Into how many workgroups the rows that a key tile walks are shared out. A share costs a write and a read of its fp32 sums,
 // about what 350 rows cost to walk.
 //   fewer key tiles than CUs      as many as fill two workgroups per CU, of 256 rows at least
-//   causal, fewer than 1024       two: the tiles' work falls from all rows to none, and without a second round of workgroups
-//                                 the longest ones run alone (8192 keys of 8 heads, 4 query heads each: 1952 us in one
-//                                 share)
-int shares_of(int dtype, int nseq, int H, int Hkv, int total_q, int total_k, int causal) {
-  const int64_t units = ((int64_t)total_k / key_tile(dtype, nseq, Hkv, total_k) + nseq) * Hkv, rows = (int64_t)total_q * (H / Hkv) / nseq;
+//   causal, few tiles             two: the tiles' work falls from all rows to none, and the longest ones run alone at the end unless the
+//                                 workgroups of dq, or a second round of tiles, are enough to fill the chip meanwhile. All gradients of
+//                                 128 dims, us in two shares / one: 256 tiles of 8192 rows 307 / 433; 512 tiles of 4096 rows 404 / 355,
+//                                 of 8192 632 / 596, of 16384 1008 / 1047, of 32768 1821 / 1992; 768 of 16384 1518 / 1477
+int shares_of(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal) {
+  const int64_t units = ((int64_t)total_k / grad_tile(dtype, nseq, H, Hkv, d, total_q, total_k) + nseq) * Hkv, rows = (int64_t)total_q * (H / Hkv) / nseq;
   if (units < 256) return (int)std::max<int64_t>(1, std::min<int64_t>(512 / units, rows / 256));
-  return causal && dtype == DT_BF16 && units < 1024 && rows >= 4096 ? 2 : 1;
+  return causal && dtype == DT_BF16 && (units < 400 ? rows >= 4096 : units < 600 && rows >= 16384) ? 2 : 1;   // (units count one more tile a sequence)
 }
 
 }  // namespace
@@ -592,7 +614,7 @@ int shares_of(int dtype, int nseq, int H, int Hkv, int total_q, int total_k, int
 // what is known of each row; the shares of dk and dv
 size_t packed_backward_ws(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal) {
   if (nseq == 0) return 0;
-  const int shares = shares_of(dtype, nseq, H, Hkv, total_q, total_k, causal);
+  const int shares = shares_of(dtype, nseq, H, Hkv, d, total_q, total_k, causal);
   return stats_bytes(H, total_q) + (shares > 1 ? (size_t)shares * total_k * Hkv * 2 * d * 4 : 0);
 }
 
@@ -609,40 +631,25 @@ hipError_t packed_attention_stats(PackedArgs a, int dtype, int d, void* ws, hipS
 }
 
 template <int D>
-static void dkdv_launch(const PackedArgs& a, int dtype, int keys, int64_t units, int64_t joins, hipStream_t s) {
-  if (dtype == DT_BF16) packed_dkdv_bf16<D><<<units, 256, 0, s>>>(a);
-  else if (keys == 16) packed_dkdv_f32<D, true><<<units, 256, 0, s>>>(a);
-  else packed_dkdv_f32<D, false><<<units, 256, 0, s>>>(a);
-  if (a.shares <= 1) return;
+static void gradients_launch(const PackedArgs& a, int dtype, int tile, int key_blocks, int64_t blocks, int64_t joins, hipStream_t s) {
+  if (dtype == DT_BF16) packed_gradients_bf16<D><<<blocks, 256, 0, s>>>(a, key_blocks);
+  else if (tile == 16) packed_gradients_f32<D, true><<<blocks, 256, 0, s>>>(a, key_blocks);
+  else packed_gradients_f32<D, false><<<blocks, 256, 0, s>>>(a, key_blocks);
+  if (a.shares <= 1 || joins == 0) return;
   if (dtype == DT_BF16) shares_join<u16, D><<<joins, 256, 0, s>>>(a);
   else shares_join<float, D><<<joins, 256, 0, s>>>(a);
 }
-hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
-  const int total_k = a.kr.total;
-  if (total_k == 0) return hipSuccess;
+hipError_t packed_attention_gradients(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
+  const int total_q = a.qr.total, total_k = a.kr.total, tile = grad_tile(dtype, a.nseq, a.H, a.Hkv, d, total_q, total_k);
   a.stats = (float2*)ws;
-  a.shares = shares_of(dtype, a.nseq, a.H, a.Hkv, a.qr.total, total_k, a.causal);
-  a.share_sums = (float*)((char*)ws + stats_bytes(a.H, a.qr.total));
-  const int keys = key_tile(dtype, a.nseq, a.Hkv, total_k);
-  const int64_t units = ((int64_t)total_k / keys + a.nseq) * a.Hkv * a.shares, joins = ((int64_t)total_k / 64 + a.nseq) * a.Hkv;
-  if (d == 128) dkdv_launch<128>(a, dtype, keys, units, joins, s);
-  else dkdv_launch<64>(a, dtype, keys, units, joins, s);
-  return hipGetLastError();
-}
-
-template <int D>
-static void dq_launch(const PackedArgs& a, int dtype, int rows, int64_t grid, hipStream_t s) {
-  if (dtype == DT_BF16) packed_dq_bf16<D><<<grid, 256, 0, s>>>(a);
-  else if (rows == 16) packed_dq_f32<D, true><<<grid, 256, 0, s>>>(a);
-  else packed_dq_f32<D, false><<<grid, 256, 0, s>>>(a);
-}
-hipError_t packed_attention_dq(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
-  a.stats = (float2*)ws;
-  const int rows = row_tile(a, dtype);
-  const int64_t grid = row_tiles(a, rows);
-  if (grid == 0) return hipSuccess;
-  if (d == 128) dq_launch<128>(a, dtype, rows, grid, s);
-  else dq_launch<64>(a, dtype, rows, grid, s);
+  a.shares = shares_of(dtype, a.nseq, a.H, a.Hkv, d, total_q, total_k, a.causal);
+  a.share_sums = (float*)((char*)ws + stats_bytes(a.H, total_q));
+  const int64_t keys = total_k > 0 ? tiles_of(a.nseq, total_k, total_k, tile) * a.Hkv * a.shares : 0;
+  const int64_t rows = tiles_of(a.nseq, (int64_t)total_q * a.G, (int64_t)a.max_q * a.G, tile) * a.Hkv;
+  if (keys + rows == 0) return hipSuccess;
+  const int64_t joins = total_k > 0 ? ((int64_t)total_k / 64 + a.nseq) * a.Hkv : 0;
+  if (d == 128) gradients_launch<128>(a, dtype, tile, (int)keys, keys + rows, joins, s);
+  else gradients_launch<64>(a, dtype, tile, (int)keys, keys + rows, joins, s);
   return hipGetLastError();
 }
 

@@ -101,8 +101,7 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
 hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 size_t packed_backward_ws(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal);
 hipError_t packed_attention_stats(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
-hipError_t packed_attention_dkdv(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
-hipError_t packed_attention_dq(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
+hipError_t packed_attention_gradients(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 
 enum NormKind { NORM_NONE = 0, NORM_LAYER = 1, NORM_RMS = 2 };
 struct GatedNormArgs {
