@@ -306,12 +306,7 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
   }
   const int last_tok = (min(row0 + ROWS, rows) - 1) / a.G;
   const int nvis = a.causal ? min(max(last_tok + t.s.n - t.s.m + 1, 0), t.s.n) : t.s.n;
-  int kt0 = 0, nt = cdiv(nvis, KB);
-  if (a.part_tiles) {
-    const int per = a.part_tiles * (64 / KB);
-    kt0 = min(t.part * per, nt);
-    nt = min(kt0 + per, nt);
-  }
+  const int nt = cdiv(nvis, KB);
   f32x4 rk[CPT], rv[CPT];
   // rows past the end repeat the last key, whose scores are masked there, with a value of zero
   auto fetch = [&](int kt) {
@@ -335,11 +330,11 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
 #pragma unroll
   for (int i = 0; i < NDB; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = M_FLOOR, l_run = 0.f;
-  if (kt0 < nt) {
-    fetch(kt0);
-    stage(kt0);
+  if (nt > 0) {
+    fetch(0);
+    stage(0);
   }
-  for (int kt = kt0; kt < nt; kt++) {
+  for (int kt = 0; kt < nt; kt++) {
     const int buf = kt & 1;
     __syncthreads();   // tile kt is staged, and every wave is done with the other buffer
     if (kt + 1 < nt) fetch(kt + 1);
@@ -411,11 +406,6 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
   const float lse = l_run == 0.f ? -INFINITY : m_run + __builtin_amdgcn_logf(l_run) * LN2;
   float* orow = (float*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head;
   float* olse = a.lse ? a.lse + (int64_t)(q0 + tok) * a.H + head : nullptr;
-  if (a.part_tiles && t.parts > 1) {
-    const int64_t slot = t.slot * ROWS + wave * 16 + l16;
-    orow = a.part_o + slot * D;
-    olse = a.part_lse + slot;
-  }
   if (olse && g4 == 0) *olse = lse;
 #pragma unroll
   for (int i = 0; i < NDB; i++)   // dims 16 i + 4 g4 + 0..3 of this lane's row
@@ -525,14 +515,14 @@ __global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
 
 // ---------------------------------------------------------------------------
 // bf16, few rows: a new token (or a few) of each sequence against its keys, bound by reading K and V once. Tiles of 16 rows on
-// v_mfma_f32_16x16x32_bf16; the NW waves of a workgroup do not share rows but keys: wave w takes the 32-key stages w, w + NW, ...
+// v_mfma_f32_16x16x32_bf16; the four waves of a workgroup do not share rows but keys: wave w takes the 32-key stages w, w + 4, ...
 // of the part with a running maximum, sum and output of its own, so no barrier stands in the loop, and they meet at
 // the end. K goes to registers (a lane's 16 bytes are operand A as they stand), V straight to LDS for the
 // transposing read; both one stage ahead, 16 KB per wave in flight.
 // ---------------------------------------------------------------------------
-template <int D, int NW>
-__global__ void __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) packed_few_bf16(PackedArgs a) {
-  constexpr int ROWS = 16, KB = 32, NKS = D / 32, NDB = D / 16;
+template <int D>
+__global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
+  constexpr int NW = 4, ROWS = 16, KB = 32, NKS = D / 32, NDB = D / 16;
   using Tile = RowTile<D, KB, 1>;
   constexpr int RB = Tile::RB, TILE = Tile::BYTES;
   constexpr int MERGE = NW * ROWS * (D + 4) * 4 + NW * ROWS * 8;
@@ -807,7 +797,7 @@ template <int D>
 static void fwd_launch(const PackedArgs& a, int dtype, int rows, int64_t grid, hipStream_t s) {
   if (dtype == DT_F32 && rows == 16) packed_split_f32<D><<<grid, 256, 0, s>>>(a);
   else if (dtype == DT_F32) packed_fwd_f32<D><<<grid, 256, 0, s>>>(a);
-  else if (rows == 16) packed_few_bf16<D, 4><<<grid, 256, 0, s>>>(a);
+  else if (rows == 16) packed_few_bf16<D><<<grid, 256, 0, s>>>(a);
   else if (a.part_tiles) packed_fwd_bf16<D, true><<<grid, 256, 0, s>>>(a);
   else packed_fwd_bf16<D, false><<<grid, 256, 0, s>>>(a);
 }
@@ -817,7 +807,6 @@ hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStr
   if (p.row_tiles == 0) return hipSuccess;
   a.part_tiles = p.part_tiles;
   a.units = p.units;
-  a.row_tiles = p.row_tiles;
   a.part_o = (float*)ws;
   a.part_lse = (float*)ws + (int64_t)a.Hkv * p.units * p.rows * d;
   const int64_t grid = (int64_t)p.units * a.Hkv;
@@ -827,8 +816,7 @@ hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStr
     const int64_t jg = (int64_t)p.row_tiles * a.Hkv * (p.rows / 4);
     if (p.rows == 16 && dtype == DT_F32) packed_join<float, 16><<<jg, 256, 0, s>>>(a, d);
     else if (p.rows == 16) packed_join<u16, 16><<<jg, 256, 0, s>>>(a, d);
-    else if (dtype == DT_BF16) packed_join<u16, 128><<<jg, 256, 0, s>>>(a, d);
-    else packed_join<float, 64><<<jg, 256, 0, s>>>(a, d);
+    else packed_join<u16, 128><<<jg, 256, 0, s>>>(a, d);   // (64-row tiles of fp32 fill the chip by themselves)
   }
   return hipGetLastError();
 }

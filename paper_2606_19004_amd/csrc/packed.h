@@ -36,7 +36,6 @@ struct PackedArgs {
   // long keys shared out in parts of part_tiles 64-key tiles (0: one part), whose results meet in the workspace
   int part_tiles, units;            // units: upper bound on (sequence, row tile, part) per key/value head
   float* part_o; float* part_lse;   // [Hkv * units][row tile][d], [Hkv * units][row tile]
-  int row_tiles;                    // upper bound on (sequence, row tile) per key/value head
   // backward
   const void* d_o; void* dq; void* dk; void* dv;
   float2* stats;                    // [H][total_q] (lse in log2 units, rowsum(d_o o))

@@ -302,3 +302,58 @@ def test_backward_in_a_graph(d):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(grads, want))
         call()
+
+
+# enough workgroups for the widest tiles of each type: many heads, or so many queries that a key tile's rows are shared out
+WIDE = [
+    # H, G, q lengths, k lengths (None: the same), causal
+    (16, 16, [40, 0, 150, 1, 64, 17] * 7, None, True),
+    (32, 16, [33, 9, 65] * 10, [70, 1, 0] * 10, False),
+    (16, 2, [4100, 5000], [20, 33], False),
+]
+
+
+@pytest.mark.parametrize("dtype,hd", [("f32", 128), ("f32", 64), ("bf16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("H,G,ql,kl,causal", WIDE)
+def test_problems_that_fill_the_chip(d, dtype, hd, H, G, ql, kl, causal):
+    p = Problem(d, dtype, hd, H, G, ql, kl, causal, lead=2, tail=3, seed=hd + len(ql))
+    p.check_forward()
+    p.check_backward()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(q_len=[5, 90], k_len=[40, 130]), dict(q_len=[1, 1], k_len=[1500, 3], slack=2)])
+def test_lse_may_be_left_out(d, dtype, kw):
+    p = Problem(d, dtype, 64, 4, 2, causal=True, seed=31, **kw)
+    p.forward()
+    want, lse = p.to.clone(), p.lse.clone()
+    p.to.fill_(SENTINEL)
+    p.lse.fill_(SENTINEL)
+    ws = d.workspace(d.packed_attention_workspace_bytes(p.cfg))
+    d.packed_attention(p.cfg, p.tq, p.tk, p.tv, p.to, q_offsets=p.dq_off, k_offsets=p.dk_off, k_lengths=p.lengths, ws=ws)
+    torch.cuda.synchronize()
+    assert torch.equal(p.to, want) and bool((p.lse == SENTINEL).all())
+    assert lse.isfinite().all()
+
+
+def test_two_captured_calls_share_a_workspace(d):
+    """Graphs of two problems over one workspace, replayed in turn on one stream."""
+    ps = [Problem(d, "bf16", 64, 4, 2, [1, 1], [1500, 900], True, slack=1, seed=s) for s in (41, 42)]
+    ws = d.workspace(max(d.packed_attention_workspace_bytes(p.cfg) for p in ps))
+    assert ws.numel() > 0
+    want, graphs = [], []
+    for p in ps:
+        p.forward()
+        want.append((p.to.clone(), p.lse.clone()))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            d.packed_attention(p.cfg, p.tq, p.tk, p.tv, p.to, lse=p.lse, q_offsets=p.dq_off, k_offsets=p.dk_off,
+                               k_lengths=p.lengths, ws=ws)
+    for _ in range(3):
+        for p in ps:
+            p.to.zero_()
+            p.lse.zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p.to, w[0]) and torch.equal(p.lse, w[1]) for p, w in zip(ps, want))
