@@ -4,7 +4,9 @@
 //           loss in logp, and writes its chunk of dv; the first one also writes the loss
 // Everything is fp64 from the fp32 inputs: x_next - mean is a difference of near values, the sums run over millions
 // of terms, and the arithmetic hides behind the loads. Bound by memory: 12 (16 with a reference) bytes per element read by
-// each pass, 4 written by the second.
+// each pass, 4 written by the second (24 samples of 409600 elements with a reference: 71 us, 5.0 TB/s; a large copy 4.9). dv needs the
+// finished sum of its sample, so one pass would have to keep every element on the chip until a wait across the grid.
+// Small calls are bound by their two launches (16 samples of 65536 elements: 10.6 us).
 #include <algorithm>
 
 #include "packed.h"
