@@ -67,7 +67,8 @@ size_t packed_attention_backward_workspace_bytes(const dit_packed_config* cfg);
  * Keys outside the sequence are never read. A NaN or infinity in a key or value that the causal mask hides
  * from a query, but not from a later query of the same sequence, may still reach that query.
  * Pointers and strides must keep 16-byte alignment of every (row, head); row strides are at least head_dim,
- * and o's (row, head) pieces must not overlap. DIT_ERR_UNSUPPORTED for a row stride of 2^24 elements or more. */
+ * and o's (row, head) pieces must not overlap. DIT_ERR_UNSUPPORTED for a row stride of 2^24 elements or more
+ * or a head stride of 2^40. */
 dit_status packed_attention(const dit_packed_config* cfg, const void* q, const void* k, const void* v,
                             const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,
                             void* o, float* lse, void* workspace, size_t workspace_bytes, dit_stream stream);

@@ -11,16 +11,18 @@ int64_t esize_of(int32_t dtype) { return dtype == DIT_BF16 ? 2 : 4; }
 
 dit_status check_strides(const char* name, int64_t row, int64_t head, int32_t d, int32_t dtype) {
   if (row < d || head < 0) return set_error(DIT_ERR_INVALID_ARG, "%s_row must be at least head_dim, %s_head >= 0", name, name);
+  // (bounded before anything is multiplied by them; 2^40 elements are further than the device's memory)
+  if (row >= (1 << 24)) return set_error(DIT_ERR_UNSUPPORTED, "%s_row %lld is 2^24 or more", name, (long long)row);
+  if (head >= (int64_t(1) << 40)) return set_error(DIT_ERR_UNSUPPORTED, "%s_head %lld is 2^40 or more", name, (long long)head);
   if ((row * esize_of(dtype)) % 16 || (head * esize_of(dtype)) % 16)
     return set_error(DIT_ERR_INVALID_ARG, "%s strides must keep 16-byte rows", name);
-  if (row >= (1 << 24)) return set_error(DIT_ERR_UNSUPPORTED, "%s_row %lld is 2^24 or more", name, (long long)row);
   return DIT_OK;
 }
 
 // whether the (row, head) pieces of a written tensor are apart
 dit_status check_apart(const char* name, int64_t row, int64_t head, int32_t d, int64_t rows, int64_t heads) {
   if (heads <= 1 || rows <= 0) return DIT_OK;
-  const bool heads_inside = head >= d && row >= (heads - 1) * head + d;
+  const bool heads_inside = head >= d && head <= row && row >= (heads - 1) * head + d;   // (row is below 2^24: no overflow)
   const bool rows_inside = head >= (rows - 1) * row + d;
   if (heads_inside || rows_inside || (rows == 1 && head >= d)) return DIT_OK;
   return set_error(DIT_ERR_INVALID_ARG, "%s strides make rows of different heads overlap", name);
