@@ -19,7 +19,7 @@ using namespace dit;
   } while (0)
 
 namespace {
-const int64_t STRIDES[] = {0, 1, 63, 64, 128, 256, 512, 513, (1 << 24) - 8, 1 << 24, int64_t(1) << 40, int64_t(1) << 60, int64_t(1) << 61,
+const int64_t STRIDES[] = {0, 1, 63, 64, 128, 256, 512, 513, (1 << 24) - 8, 1 << 24, (int64_t(1) << 40) - 64, int64_t(1) << 40, int64_t(1) << 60, int64_t(1) << 61,
                            int64_t(1) << 62, std::numeric_limits<int64_t>::max(), -1, -64, std::numeric_limits<int64_t>::min()};
 const int32_t SIZES[] = {0, 1, 2, 7, 100, (1 << 20) - 1, 1 << 20, 1 << 28, std::numeric_limits<int32_t>::max(), -1,
                          std::numeric_limits<int32_t>::min()};
