@@ -662,6 +662,7 @@ __global__ void __launch_bounds__(64 * WAVES) columns_kernel(GatedNormArgs a, in
   const int n = (int)min((int64_t)cdiv(a.pr.span(seq).count, chunk_rows), a.chunks - before);
   float s[3] = {0.f, 0.f, 0.f};
   if (col < D)
+#pragma unroll 4   // (loads of several chunks in flight)
     for (int c = wave; c < n; c += WAVES) {
       const float* p = a.parts + (before + c) * 3 * D + col;
 #pragma unroll
@@ -692,6 +693,7 @@ __global__ void __launch_bounds__(1024) weights_kernel(GatedNormArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane, D = a.D;
   float p = 0.f, q = 0.f;
   if (col < D)
+#pragma unroll 4
     for (int s = wave; s < a.nseq; s += WAVES) {
       const float* k = a.parts + ((int64_t)a.chunks * 3 + 2 * s) * D + col;
       const int64_t at = s * a.mod_row + col;
@@ -729,12 +731,15 @@ int lanes_of(int D) {
 bool narrow(int D) { return D <= 256; }
 int wide_threads(int D) { return cdiv(cdiv(D, 8), 64) * 64; }
 
-// Rows of a chunk of the backward pass: as many as let all chunks run at once (16 waves per CU, which their registers allow), but 8 at
-// least. Half as many rows need another round of workgroups for what the first leaves over and write twice the sums (8 sequences
-// of about 1300 rows of 3072: 120 us where all at once take 97).
+// Rows of a chunk of the backward pass: as many as let all chunks run at once (16 waves per CU, which their registers allow). Half as
+// many rows need another round of workgroups for what the first leaves over and write twice the sums (8 sequences of about 1300
+// rows of 3072: 120 us where all at once take 97). At least, for long rows, what costs less than the sums of more chunks (a row costs
+// its chunk 2 us; gradients in all, us with 8 / 4 / 2 / 1 at least): 64 rows of 1024 22 / 16 / 13 / 12, 512 of 3072 28 / 23 / 22 / 22;
+// 616 of 3072 29 / 23 / 26 / 25, 4000 of 1024 32 / 27 / 33 / 32, 3000 of 512 in one sequence 27 / 25 / 33 / 50. Short rows: 8, which
+// the waves of a workgroup take at once.
 int chunk_rows_of(int nseq, int rows, int D) {
   const int waves = narrow(D) ? 4 : wide_threads(D) / 64, slots = 256 * std::max(16 / waves, 1);
-  return std::max(8, cdiv(rows, std::max(slots - nseq, slots / 2)));
+  return std::max(narrow(D) ? 8 : rows <= 512 ? 2 : 4, cdiv(rows, std::max(slots - nseq, slots / 2)));
 }
 
 // rows a workgroup walks forward: up to 8 (20480 rows of 3072: 103 us; 20, one round of workgroups: 109), as long as that leaves enough
