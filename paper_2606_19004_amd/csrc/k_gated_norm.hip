@@ -42,6 +42,13 @@ __device__ __forceinline__ void store8_any(float* p, const float* f) {
   *(f32x4_any4*)p = f32x4_any4{f[0], f[1], f[2], f[3]};
   *(f32x4_any4*)(p + 4) = f32x4_any4{f[4], f[5], f[6], f[7]};
 }
+typedef unsigned u32x2_any2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef unsigned u32_any2 __attribute__((aligned(2)));
+typedef float f32x2_any4 __attribute__((ext_vector_type(2), aligned(4)));
+__device__ __forceinline__ void store4_any(u16* p, const float* f) { *(u32x2_any2*)p = u32x2_any2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])}; }
+__device__ __forceinline__ void store4_any(float* p, const float* f) { *(f32x4_any4*)p = f32x4_any4{f[0], f[1], f[2], f[3]}; }
+__device__ __forceinline__ void store2_any(u16* p, const float* f) { *(u32_any2*)p = pack_bf16x2(f[0], f[1]); }
+__device__ __forceinline__ void store2_any(float* p, const float* f) { *(f32x2_any4*)p = f32x2_any4{f[0], f[1]}; }
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const T* p, int at, int D, float* f) {
 #pragma unroll
@@ -68,40 +75,70 @@ __device__ __forceinline__ void store8(T* p, int at, int D, const float* f) {
     }
   } else if (at + 8 <= D) {
     store8_any(p + at, f);
-  } else {
+  } else if (at < D) {   // 4, 2 and 1 of the elements left
+    const int left = D - at;
+    float g[4] = {f[0], f[1], f[2], f[3]};
+    p += at;
+    if (left & 4) {
+      store4_any(p, g);
+      p += 4;
 #pragma unroll
-    for (int i = 0; i < 8; i++)
-      if (at + i < D) p[at + i] = from_f32<T>(f[i]);
+      for (int i = 0; i < 4; i++) g[i] = f[4 + i];
+    }
+    if (left & 2) {
+      store2_any(p, g);
+      p += 2;
+      g[0] = g[2];
+    }
+    if (left & 1) *p = from_f32<T>(g[0]);
   }
 }
-// The same as it was loaded: a row on its way while the one before it is worked on.
+// The same as it was loaded, for rows of more than 8: a row on its way while the one before it is worked on. Without VEC every lane
+// loads 16 bytes: the ones at the row's end and past it its last 8 elements, less the first `skip` of them, which are other lanes'
+// (20480 bf16 rows of 3068 forward 107 us, 10400 backward 98; the end element by element 142 and 152).
+template <bool VEC> __device__ __forceinline__ int skip_of(int at, int D) { return VEC ? 0 : min(max(at + 8 - D, 0), 8); }
+// w's elements from `by` on, zeros behind them; PER: elements of a word
+template <int WORDS, int PER> __device__ __forceinline__ void skip_first(uint32_t* w, int by) {
+#pragma unroll
+  for (int step = WORDS; step >= 1; step /= 2)   // words
+    if (by & (step * PER))
+#pragma unroll
+      for (int i = 0; i < WORDS; i++) w[i] = i + step < WORDS ? w[i + step] : 0;
+  if (PER == 2 && (by & 1))
+#pragma unroll
+    for (int i = 0; i < WORDS; i++) w[i] = w[i] >> 16 | (i + 1 < WORDS ? w[i + 1] << 16 : 0);
+}
 template <typename T, bool VEC> struct Raw {
-  float f[8];
-  __device__ __forceinline__ void load(const T* p, int at, int D) { load8<T, VEC>(p, at, D, f); }
-  __device__ __forceinline__ void get(float* o) const {
+  static constexpr int PER = 4 / sizeof(T), WORDS = 8 / PER;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ void load(const T* p, int at, int D) {
+    if (VEC && at >= D) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) o[i] = f[i];
-  }
-};
-template <bool VEC> struct Raw<u16, VEC> {
-  uint32_t w[4];
-  __device__ __forceinline__ void load(const u16* p, int at, int D) {
-    w[0] = w[1] = w[2] = w[3] = 0;
-    if (at + 8 <= D) {
+      for (int i = 0; i < WORDS; i++) w[i] = 0;
+      return;
+    }
+    const T* from = p + (VEC ? at : min(at, D - 8));
+#pragma unroll
+    for (int i = 0; i < WORDS; i += 4) {
       if constexpr (VEC) {
-        const uint4 u = *(const uint4*)(p + at);
-        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+        const uint4 u = *(const uint4*)(from + PER * i);
+        w[i] = u.x; w[i + 1] = u.y; w[i + 2] = u.z; w[i + 3] = u.w;
       } else {
-        const u32x4_any2 u = *(const u32x4_any2*)(p + at);
-        w[0] = u[0]; w[1] = u[1]; w[2] = u[2]; w[3] = u[3];
+        const u32x4_any2 u = *(const u32x4_any2*)(from + PER * i);
+        w[i] = u[0]; w[i + 1] = u[1]; w[i + 2] = u[2]; w[i + 3] = u[3];
       }
-    } else if (!VEC) {
-#pragma unroll
-      for (int i = 0; i < 8; i++)
-        if (at + i < D) w[i / 2] |= (uint32_t)p[at + i] << (16 * (i & 1));
     }
   }
-  __device__ __forceinline__ void get(float* o) const { unpack8(w, o); }
+  __device__ __forceinline__ void get(float* o, int skip) const {
+    uint32_t x[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; i++) x[i] = w[i];
+    if (!VEC) skip_first<WORDS, PER>(x, skip);
+    if constexpr (PER == 2) unpack8(x, o);
+    else
+#pragma unroll
+      for (int i = 0; i < 8; i++) o[i] = __uint_as_float(x[i]);
+  }
 };
 
 // ky = gate post_w, kh = (1 + scale) pre_w; 0 past the row
@@ -366,7 +403,7 @@ __global__ void __launch_bounds__(1024) forward_wide(GatedNormArgs a, int chunk_
   if (!find_chunk(a, chunk_rows, seq, chunk, rows)) return;
   // every chunks-th row: the workgroups that run together then work on neighbouring rows
   const int begin = rows.begin + chunk, end = rows.begin + rows.count, step = cdiv(rows.count, chunk_rows);
-  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = 8 * l;
+  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = 8 * l, skip = skip_of<VEC>(at, D);
   const int64_t mo = seq * a.mod_row;
   const bool has_y = a.y, has_xo = a.x_out, has_h = a.h;
   Raw<T, VEC> nx, ny;
@@ -397,8 +434,8 @@ __global__ void __launch_bounds__(1024) forward_wide(GatedNormArgs a, int chunk_
   };
   for (int64_t row = begin; row < end; row += step) {
     float v[8], u[8];
-    nx.get(v);
-    if (has_y) ny.get(u);
+    nx.get(v, skip);
+    if (has_y) ny.get(u, skip);
     fetch(row + step < end ? row + step : row);
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] *= a.alpha;
@@ -561,7 +598,7 @@ __global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int chunk_row
   if (!find_chunk(a, chunk_rows, seq, chunk, rows)) return;
   // every chunks-th row: the workgroups that run together then work on neighbouring rows
   const int begin = rows.begin + chunk, end = rows.begin + rows.count, step = cdiv(rows.count, chunk_rows);
-  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = 8 * l;
+  const int D = a.D, l = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = 8 * l, skip = skip_of<VEC>(at, D);
   const bool has_y = FULL || a.y, has_dxo = FULL || a.dx_out, has_dh = FULL || a.dh, has_dx = FULL || a.dx, has_dy = FULL || a.dy;
   Raw<T, VEC> nx, ny, nt, nh;
   auto fetch = [&](int64_t row) {
@@ -591,10 +628,10 @@ __global__ void __launch_bounds__(1024) rows_wide(GatedNormArgs a, int chunk_row
     float xv[8], yv[8], t[8], dh[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) yv[i] = t[i] = dh[i] = 0.f;
-    nx.get(xv);
-    if (has_y) ny.get(yv);
-    if (has_dxo) nt.get(t);
-    if (has_dh) nh.get(dh);
+    nx.get(xv, skip);
+    if (has_y) ny.get(yv, skip);
+    if (has_dxo) nt.get(t, skip);
+    if (has_dh) nh.get(dh, skip);
     fetch(row + step < end ? row + step : row);
     if (has_dh) {
       float g[8];

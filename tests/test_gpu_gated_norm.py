@@ -304,3 +304,13 @@ def test_no_rows(d):
         for t in v:
             assert torch.all(t[:S] == 0.0) and torch.all(t[S:] == 7.0)
         assert all(torch.all(t == 0.0) for t in w)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [258, 259, 260, 261, 262, 263, 509, 517, 1, 2, 5, 7, 13, 246, 1535])
+def test_every_end_of_a_row(d, dtype, D):
+    """Rows whose last lane holds one to seven elements, one wave and several; what lies behind a row stays."""
+    for pad in (0, 3):
+        p = Problem(d, dtype, D, [9, 0, 26], "rms", "layer", seed=D, lead=1, tail=2, **({"pad": pad} if pad else {}))
+        p.check_forward()
+        p.check_backward()
