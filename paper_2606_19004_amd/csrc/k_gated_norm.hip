@@ -11,8 +11,9 @@
 namespace dit {
 namespace {
 
-// The 8 successive elements of a row that a lane holds. VEC: D is a multiple of 8 and everything 16-byte aligned. Otherwise the lane
-// at the row's end takes its elements one by one, and the others 16 bytes at the alignment of an element, which the memory unit allows.
+// The 8 successive elements of a row that a lane holds. VEC: D is a multiple of 8 and everything 16-byte aligned. Otherwise a lane
+// takes 16 bytes at the alignment of an element, which the memory unit allows; the one at the row's end loads its elements one by one
+// (the vectors of a chunk, and rows of up to 256 elements; longer rows: Raw) and stores 4, 2 and 1 of them.
 typedef unsigned u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ void unpack8(const uint32_t* w, float* f) {

@@ -598,16 +598,17 @@ int grad_tile(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total
   return (tiles_of(nseq, total_k, total_k, 64) + tiles_of(nseq, rows, rows, 64)) * Hkv < (d == 64 ? 1024 : 512) ? 16 : 64;
 }
 
-// Into how many workgroups the rows that a key tile walks are shared out. A share costs a write and a read of its fp32 sums,
-// about what 350 rows cost to walk.
-//   fewer key tiles than CUs      as many as fill two workgroups per CU, of 256 rows at least
+// Into how many workgroups the rows that a key tile walks are shared out. A share costs a write and a read of its fp32 sums.
+//   fewer key tiles than CUs      as many as fill two workgroups per CU, of 512 rows at least (all gradients, us with 256 / 512 / 1024
+//                                 at least: 1024 causal tokens of 16 over 4 heads 85 / 73 / 76, 4 x 512 66 / 59 / 74, 1000 of 2 over 1
+//                                 50 / 51 / 95)
 //   causal, few tiles             two: the tiles' work falls from all rows to none, and the longest ones run alone at the end unless the
 //                                 workgroups of dq, or a second round of tiles, are enough to fill the chip meanwhile. All gradients of
 //                                 128 dims, us in two shares / one: 256 tiles of 8192 rows 307 / 433; 512 tiles of 4096 rows 404 / 355,
 //                                 of 8192 632 / 596, of 16384 1008 / 1047, of 32768 1821 / 1992; 768 of 16384 1518 / 1477
 int shares_of(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal) {
   const int64_t units = ((int64_t)total_k / grad_tile(dtype, nseq, H, Hkv, d, total_q, total_k) + nseq) * Hkv, rows = (int64_t)total_q * (H / Hkv) / nseq;
-  if (units < 256) return (int)std::max<int64_t>(1, std::min<int64_t>(512 / units, rows / 256));
+  if (units < 256) return (int)std::max<int64_t>(1, std::min<int64_t>(512 / units, rows / 512));
   return causal && dtype == DT_BF16 && (units < 400 ? rows >= 4096 : units < 600 && rows >= 16384) ? 2 : 1;   // (units count one more tile a sequence)
 }
 
