@@ -357,3 +357,14 @@ def test_two_captured_calls_share_a_workspace(d):
             g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p.to, w[0]) and torch.equal(p.lse, w[1]) for p, w in zip(ps, want))
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("H,G,ql,kl,causal", [
+    (2, 1, [40], [3000], True), (2, 2, [33, 130, 0], [3100, 2700, 900], True), (4, 1, [90, 1], [4100, 5], False),
+    (1, 1, [2500], [2500], True)])
+def test_many_queries_against_long_keys(d, dtype, hd, H, G, ql, kl, causal):
+    """So few tiles of rows that their keys are shared out and joined, a part without visible keys among them."""
+    p = Problem(d, dtype, hd, H, G, ql, kl, causal, lead=1, tail=2, seed=hd + len(ql))
+    assert d.packed_attention_workspace_bytes(p.cfg) > 0
+    p.check_forward()
