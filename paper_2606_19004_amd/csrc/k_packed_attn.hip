@@ -773,7 +773,8 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
 //          the launch that joins parts costs 4 us. So keys are shared out where a sequence may have more than 12 tiles, for about
 //          two workgroups per CU (32 tokens, 90 k keys of 8 heads: 80 us; four per CU: 88), in parts of at least 4 tiles (one
 //          token, 2048 keys: 11.4 us; 16 tiles: 16.7), or of 12 where the sequences alone fill the chip (32 tokens, 300 keys
-//          each: 11.2 us; 4 tiles: 15.5). Other tiles: only where they alone leave CUs without a workgroup, and
+//          each: 11.2 us; 4 tiles: 15.5). fp32 tiles take twice as long: parts of 2 at least, from 5 tiles on (700 keys 29 us whole,
+//          18 in parts of 4, 14 in parts of 2; sequences that fill the chip as above). Other tiles: only where they alone leave CUs without a workgroup, and
 //          128 rows only where a part is WORTH tiles shorter than the average sequence: their results are about 67 MB to write and
 //          read however the keys are cut (us whole / shared out: 1024 keys of 16 over 4 heads 23 / 38, 2048 of 8 over 1 38 / 40, of
 //          4 over 4 37 / 32, 4096 of 4 over 1 68 / 51, 8192 of 2 over 1 129 / 72).
@@ -789,10 +790,12 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
   const int64_t groups = (int64_t)p.row_tiles * Hkv;
   if (groups == 0 || (!few && groups >= CUS)) return p;
   const int64_t tiles = cdiv(total_k, 64), work = tiles * groups / nseq;
-  const int64_t per = std::max<int64_t>(groups < CUS ? MIN_PART : WHOLE, (work + 2 * CUS - 1) / (2 * CUS));
+  const bool split_f32 = dtype == DT_F32 && groups < CUS;
+  const int whole = split_f32 ? 4 : WHOLE;
+  const int64_t per = std::max<int64_t>(split_f32 ? 2 : groups < CUS ? MIN_PART : WHOLE, (work + 2 * CUS - 1) / (2 * CUS));
   if (p.rows == 128 && tiles / nseq - per < WORTH) return p;
   const int64_t units = per_seq * (tiles / per + nseq);   // a sequence of n tiles has at most n / per + 1 parts
-  if (cdiv(max_k, 64) <= std::max<int64_t>(WHOLE, per) || (!few && units * Hkv > 16 * CUS)) return p;
+  if (cdiv(max_k, 64) <= std::max<int64_t>(whole, per) || (!few && units * Hkv > 16 * CUS)) return p;
   p.part_tiles = (int)per;
   p.units = (int)units;
   p.ws = (size_t)Hkv * units * p.rows * (d + 1) * 4;

@@ -48,45 +48,61 @@ struct PackedArgs {
   }
 };
 
+// Inclusive sum over the wave: 1, 2, 4 and 8 lanes before within rows of 16 lanes, then the rows before. VALU moves, no LDS.
+template <int CTRL, int ROWS> __device__ __forceinline__ unsigned moved_up(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ unsigned wave_scan(unsigned v) {
+  v += moved_up<0x111, 0xf>(v);
+  v += moved_up<0x112, 0xf>(v);
+  v += moved_up<0x114, 0xf>(v);
+  v += moved_up<0x118, 0xf>(v);
+  v += moved_up<0x142, 0xa>(v);
+  v += moved_up<0x143, 0xc>(v);
+  return v;
+}
+
 // The sequence that unit u belongs to, where a sequence with what = load(i) (a struct of int) has count(what) units, and u's place
 // in it. Every wave finds it by itself, 64 sequences at a time: no host-made list of tiles, no empty workgroups where
 // lengths are unlike. What is known of the sequence comes from the lane that looked at it, with no further loads.
-template <typename S, typename L, typename C>
-__device__ __forceinline__ bool find_unit(int nseq, int u, L&& load, C&& count, int& seq, int& local, S& what) {
+// BLOCKS: how many times 64 sequences are loaded together (1000 sequences of 64 keys, 8 heads, one new token each: 191 us; one block at a
+// time, with a sum by LDS permutes, 239).
+template <int BLOCKS, typename S, typename L, typename C>
+__device__ __forceinline__ bool find_unit_in(int nseq, int u, L&& load, C&& count, int& seq, int& local, S& what) {
   const int lane = threadIdx.x & 63;
   unsigned carry = 0;   // <= u
-  for (int base = 0; base < nseq; base += 64) {
-    S mine{};
-    unsigned c = 0;
-    if (base + lane < nseq) {
-      mine = load(base + lane);
+  for (int base = 0; base < nseq; base += 64 * BLOCKS) {
+    S mine[BLOCKS];
+#pragma unroll
+    for (int b = 0; b < BLOCKS; b++) mine[b] = load(min(base + 64 * b + lane, nseq - 1));
+#pragma unroll
+    for (int b = 0; b < BLOCKS; b++) {
+      if (base + 64 * b >= nseq) return false;
       // (no count of a tensor within the entry points' limits is larger, and 64 of these fit)
-      c = min(count(mine), 1 << 25);
-    }
-    unsigned incl = c;
+      const unsigned c = base + 64 * b + lane < nseq ? min(count(mine[b]), 1 << 25) : 0, incl = wave_scan(c);
+      const unsigned total = __builtin_amdgcn_readlane(incl, 63);
+      if ((unsigned)u < carry + total) {
+        const int l = __builtin_ctzll(__ballot(carry + incl > (unsigned)u));
+        seq = base + 64 * b + l;
+        local = u - (int)(carry + __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l));
+        union {
+          S s;
+          int w[sizeof(S) / 4];
+        } in, out;
+        in.s = mine[b];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned up = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += up;
+        for (int i = 0; i < (int)(sizeof(S) / 4); i++) out.w[i] = __builtin_amdgcn_readlane(in.w[i], l);
+        what = out.s;
+        return true;
+      }
+      carry += total;
     }
-    const unsigned total = __builtin_amdgcn_readlane(incl, 63);
-    if ((unsigned)u < carry + total) {
-      const int l = __builtin_ctzll(__ballot(carry + incl > (unsigned)u));
-      seq = base + l;
-      local = u - (int)(carry + __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(c, l));
-      union {
-        S s;
-        int w[sizeof(S) / 4];
-      } in, out;
-      in.s = mine;
-#pragma unroll
-      for (int i = 0; i < (int)(sizeof(S) / 4); i++) out.w[i] = __builtin_amdgcn_readlane(in.w[i], l);
-      what = out.s;
-      return true;
-    }
-    carry += total;
   }
   return false;
+}
+template <typename S, typename L, typename C>
+__device__ __forceinline__ bool find_unit(int nseq, int u, L&& load, C&& count, int& seq, int& local, S& what) {
+  return nseq <= 64 ? find_unit_in<1>(nseq, u, load, count, seq, local, what) : find_unit_in<4>(nseq, u, load, count, seq, local, what);
 }
 
 // How a call runs (host): see packed_plan in k_packed_attn.hip

@@ -314,3 +314,13 @@ def test_every_end_of_a_row(d, dtype, D):
         p = Problem(d, dtype, D, [9, 0, 26], "rms", "layer", seed=D, lead=1, tail=2, **({"pad": pad} if pad else {}))
         p.check_forward()
         p.check_backward()
+
+
+@pytest.mark.parametrize("D", [64, 320])
+@pytest.mark.parametrize("count", [65, 257, 600])
+def test_hundreds_of_sequences(d, D, count):
+    lengths = np.random.default_rng(count).integers(0, 6, count)
+    lengths[0], lengths[-1] = 0, 2
+    p = Problem(d, "bf16", D, list(lengths), "rms", "layer", seed=count, lead=1, tail=2)
+    p.check_forward()
+    p.check_backward()

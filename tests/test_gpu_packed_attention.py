@@ -368,3 +368,17 @@ def test_many_queries_against_long_keys(d, dtype, hd, H, G, ql, kl, causal):
     p = Problem(d, dtype, hd, H, G, ql, kl, causal, lead=1, tail=2, seed=hd + len(ql))
     assert d.packed_attention_workspace_bytes(p.cfg) > 0
     p.check_forward()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("count", [64, 65, 256, 257, 700])
+def test_hundreds_of_sequences(d, dtype, count):
+    """As many as a wave looks at in one go, and past it, empty ones at both ends among them."""
+    rng = np.random.default_rng(count)
+    ql = rng.integers(0, 7, count)
+    ql[0] = 0
+    ql[-2:] = (3, 0)
+    p = Problem(d, dtype, 64, 4, 2, ql, None, True, lead=2, tail=1, seed=count)
+    p.check_forward()
+    p.check_backward()
+    Problem(d, dtype, 64, 4, 2, np.ones(count, int), rng.integers(0, 50, count), True, slack=1, seed=count + 1).check_forward()
