@@ -769,10 +769,10 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
 // Tiles and parts.
 //   rows   16 where no sequence has more than FEW_ROWS (query, head) rows per key/value head; else bf16: 128, fp32: 64, or 16 where
 //          tiles of 64 are fewer than two workgroups per CU (4 x 300 tokens, 16 heads of 64: 22 us, as tiles of 64 28)
-//   parts  16-row tiles: one CU streams keys at 60 GB/s (128 keys of K and V at head_dim 128 in 1.05 us, after 4.4 us for a call), and
+//   parts  16-row tiles: one CU streams keys at 60 GB/s (128 keys of K and V at head_dim 128 in 1.09 us, after 4.2 us for a call), and
 //          the launch that joins parts costs 4 us. So keys are shared out where a sequence may have more than 12 tiles, for about
 //          two workgroups per CU (32 tokens, 90 k keys of 8 heads: 80 us; four per CU: 88), in parts of at least 4 tiles (one
-//          token, 2048 keys: 11.4 us; 16 tiles: 16.7), or of 12 where the sequences alone fill the chip (32 tokens, 300 keys
+//          token, 2048 keys: 10.5 us; 16 tiles: 16.7), or of 12 where the sequences alone fill the chip (32 tokens, 300 keys
 //          each: 11.2 us; 4 tiles: 15.5). fp32 tiles take twice as long: parts of 2 at least, from 5 tiles on (700 keys 29 us whole,
 //          18 in parts of 4, 14 in parts of 2; sequences that fill the chip as above). Other tiles: only where they alone leave CUs without a workgroup, and
 //          128 rows only where a part is WORTH tiles shorter than the average sequence: their results are about 67 MB to write and
