@@ -227,23 +227,22 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
   }
 
   const float l_all = pair_sum(l_run);
-  const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;   // (a NaN stays one)
-  const float lse = l_all == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_all)) * LN2;
   const bool real = row0 + wave * 32 + l32 < rows;
   if (PARTS && t.parts > 1) {
     const int64_t slot = t.slot * ROWS + wave * 32 + l32;
     if (real) {
-      if (half == 0) a.part_lse[slot] = lse;
+      if (half == 0) a.part_ml[slot] = make_float2(m_run, l_all);
       float* po = a.part_o + slot * D;
 #pragma unroll
       for (int db = 0; db < NDB; db++)
 #pragma unroll
         for (int g = 0; g < 4; g++)
-          *(float4*)(po + 32 * db + 8 * g + 4 * half) = make_float4(o[db][4 * g] * inv, o[db][4 * g + 1] * inv,
-                                                                   o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
+          *(float4*)(po + 32 * db + 8 * g + 4 * half) = make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
     }
     return;
   }
+  const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;   // (a NaN stays one)
+  const float lse = l_all == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_all)) * LN2;
   if (a.lse && real && half == 0) a.lse[(int64_t)(q0 + tok) * a.H + head] = lse;
   // The output leaves through the 32 rows of the K buffers that belong to this wave, so that a store writes whole
   // rows. (Both K buffers were last read before the last step's barrier.)
@@ -500,16 +499,16 @@ __global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
   for (int i = 0; i < NKC; i++) o[i] *= mine;
   join_waves<D>(sk[0], o, wave, l16, g4);
   if (wave > 0 || row0 + l16 >= rows) return;
-  const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
-  const float lse = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l) * LN2;
+  float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
   float* orow = (float*)a.o + (q0 + tok) * a.o_row + (int64_t)head * a.o_head;
-  float* olse = a.lse ? a.lse + (q0 + tok) * a.H + head : nullptr;
   if (a.part_tiles && t.parts > 1) {
     const int64_t slot = t.slot * ROWS + l16;
     orow = a.part_o + slot * D;
-    olse = a.part_lse + slot;
+    inv = 1.f;
+    if (g4 == 0) a.part_ml[slot] = make_float2(m, l);
+  } else if (a.lse && g4 == 0) {
+    a.lse[(q0 + tok) * a.H + head] = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l) * LN2;
   }
-  if (olse && g4 == 0) *olse = lse;
 #pragma unroll
   for (int i = 0; i < NKC; i++)
     *(float4*)(orow + 16 * i + 4 * g4) = make_float4(o[i][0] * inv, o[i][1] * inv, o[i][2] * inv, o[i][3] * inv);
@@ -685,17 +684,17 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
       for (int j = 0; j < 4; j++) acc[e + j] = fmaf(f, y[j], acc[e + j]);
     }
   }
-  const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
-  const float lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
-#pragma unroll
-  for (int e = 0; e < EPT; e++) acc[e] *= inv;
   if (a.part_tiles && t.parts > 1) {
     const int64_t slot = t.slot * ROWS + r;
-    if (e0 == 0) a.part_lse[slot] = lse;
+    if (e0 == 0) a.part_ml[slot] = make_float2(m, l);
 #pragma unroll
     for (int e = 0; e < EPT; e += 4) store4<float>(a.part_o + slot * D + e0 + e, acc + e);
     return;
   }
+  const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+  const float lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+#pragma unroll
+  for (int e = 0; e < EPT; e++) acc[e] *= inv;
   const int tk = rr / a.G, hd = t.g * a.G + (rr - tk * a.G);
   if (a.lse && e0 == 0) a.lse[(int64_t)(q0 + tk) * a.H + hd] = lse;
 #pragma unroll
@@ -703,8 +702,9 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
 #endif
 }
 
-// Joins the parts of each row: o = sum_p exp(lse_p - lse) o_p, in the order of the parts. One wave per row, 4 rows per workgroup;
-// the parts' rows are loaded eight at a time.
+// Joins the parts of each row, in their order: with w_p = exp(m_p - max m), o = sum w_p o_p / sum w_p l_p. (Not from an lse of each part,
+// m_p + log l_p: that loses what l_p says where m_p is large, and a maximum over NaN drops them.) One wave per row, 4 rows per
+// workgroup; the parts' rows are loaded eight at a time.
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -728,42 +728,49 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
   const int place = a.causal ? cdiv(rows, ROWS) - 1 - rt : rt;   // where the tile stands in the order of the units
   if (before + (int64_t)(place + 1) * parts > a.units) return;   // (offsets that are not increasing: no such units ran)
   const int64_t slot = ((int64_t)g * a.units + before + place * parts) * ROWS + 4 * quad + wave;   // of part 0; parts are ROWS apart
-  const float* plse = a.part_lse + slot;
+  const float2* ml = a.part_ml + slot;
   const float* po = a.part_o + slot * d;
   const int tok = row / a.G, head = g * a.G + row - tok * a.G;
-  float top = -INFINITY;
-  for (int p = lane; p < parts; p += 64) top = fmaxf(top, plse[(int64_t)p * ROWS]);
+  constexpr float UNIT = sizeof(T) == 2 ? 1.f : LOG2E;   // of the maxima: log2 units (bf16), natural ones (fp32)
+  float top = M_FLOOR;
+  for (int p = lane; p < parts; p += 64) top = fmaxf(top, ml[(int64_t)p * ROWS].x);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
   const int e = d > 64 ? 2 * lane : lane;
   float total = 0.f, acc0 = 0.f, acc1 = 0.f;
-  if (top > -INFINITY || top != top)
-    for (int p0 = 0; p0 < parts; p0 += 64) {
-      const int np = min(parts - p0, 64);
-      float w = 0.f;
-      if (lane < np) w = __builtin_amdgcn_exp2f((plse[(int64_t)(p0 + lane) * ROWS] - top) * LOG2E);
-      for (int p = 0; p < np; p += 8) {
-        float2 v[8];
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const int np = min(parts - p0, 64);
+    float w = 0.f, l = 0.f;
+    if (lane < np) {
+      const float2 x = ml[(int64_t)(p0 + lane) * ROWS];
+      w = __builtin_amdgcn_exp2f((x.x - top) * UNIT);
+      l = x.y;
+    }
+    for (int p = 0; p < np; p += 8) {
+      float2 v[8];
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-          const float* x = po + (int64_t)(p0 + min(p + j, np - 1)) * ROWS * d + e;
-          v[j] = d > 64 ? *(const float2*)x : make_float2(*x, 0.f);
-        }
+      for (int j = 0; j < 8; j++) {
+        const float* x = po + (int64_t)(p0 + min(p + j, np - 1)) * ROWS * d + e;
+        v[j] = d > 64 ? *(const float2*)x : make_float2(*x, 0.f);
+      }
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-          const float wj = p + j < np ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), p + j)) : 0.f;
-          total += wj;
+      for (int j = 0; j < 8; j++)
+        if (p + j < np) {
+          const float wj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), p + j));
+          total = fmaf(wj, __int_as_float(__builtin_amdgcn_readlane(__float_as_int(l), p + j)), total);
           acc0 = fmaf(wj, v[j].x, acc0);
           acc1 = fmaf(wj, v[j].y, acc1);
         }
-      }
     }
+  }
   const float inv = total == 0.f ? 0.f : 1.f / total;
   T* orow = (T*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head + e;
   orow[0] = from_f32<T>(acc0 * inv);
   if (d > 64) orow[1] = from_f32<T>(acc1 * inv);
-  if (a.lse && lane == 0)
-    a.lse[(int64_t)(q0 + tok) * a.H + head] = total == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(total) * LN2;
+  if (a.lse && lane == 0) {
+    const float lt = __builtin_amdgcn_logf(total);
+    a.lse[(int64_t)(q0 + tok) * a.H + head] = total == 0.f ? -INFINITY : sizeof(T) == 2 ? (top + lt) * LN2 : fmaf(lt, LN2, top);
+  }
 }
 
 // Tiles and parts.
@@ -798,7 +805,7 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
   if (cdiv(max_k, 64) <= std::max<int64_t>(whole, per) || (!few && units * Hkv > 16 * CUS)) return p;
   p.part_tiles = (int)per;
   p.units = (int)units;
-  p.ws = (size_t)Hkv * units * p.rows * (d + 1) * 4;
+  p.ws = (size_t)Hkv * units * p.rows * (d + 2) * 4;
   return p;
 }
 
@@ -817,7 +824,7 @@ hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStr
   a.part_tiles = p.part_tiles;
   a.units = p.units;
   a.part_o = (float*)ws;
-  a.part_lse = (float*)ws + (int64_t)a.Hkv * p.units * p.rows * d;
+  a.part_ml = (float2*)(a.part_o + (int64_t)a.Hkv * p.units * p.rows * d);
   const int64_t grid = (int64_t)p.units * a.Hkv;
   if (d == 128) fwd_launch<128>(a, dtype, p.rows, grid, s);
   else fwd_launch<64>(a, dtype, p.rows, grid, s);

@@ -35,7 +35,7 @@ struct PackedArgs {
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
   // long keys shared out in parts of part_tiles 64-key tiles (0: one part), whose results meet in the workspace
   int part_tiles, units;            // units: upper bound on (sequence, row tile, part) per key/value head
-  float* part_o; float* part_lse;   // [Hkv * units][row tile][d], [Hkv * units][row tile]
+  float* part_o; float2* part_ml;   // [Hkv * units][row tile][d] sums of p v, [Hkv * units][row tile] running maximum and sum of p
   // backward
   const void* d_o; void* dq; void* dk; void* dv;
   float2* stats;                    // [H][total_q] (lse in log2 units, rowsum(d_o o))
