@@ -60,6 +60,7 @@ size_t packed_attention_backward_workspace_bytes(const dit_packed_config* cfg);
 
 /* o[i][h] = sum_j p_ij v_j, p_ij = exp(scale q_i.k_j - lse_i), lse_i = log sum_j exp(scale q_i.k_j), over the
  * visible keys j of the query's sequence; a query that sees none gets o = 0 and lse = -inf.
+ * Scores are fp32, of any size; a query whose visible ones are all -inf (q k^T past the range of fp32) gets NaN in o, -inf in lse.
  *   q_offsets, k_offsets  rows of each sequence (device, or NULL)
  *   k_lengths  device [sequences] or NULL: only the first k_lengths[i] rows of sequence i's keys are used
  *              (a cache with room to grow); clamped to those rows

@@ -21,7 +21,13 @@
 namespace dit {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float M_FLOOR = -1e37f;   // running maximum of a row that has seen no key: finite, so differences are too
+constexpr float M_FLOOR = -3.4028235e38f;   // running maximum of a row that has seen no key: finite, and no finite score is below it
+
+// Whether a query sees any key: o of one that does not is 0 and its lse -inf, whatever its sum is (one whose scores are all -inf
+// has a sum of 0 too).
+__device__ __forceinline__ bool sees_keys(const PackedArgs& a, const PackedSeq& s, int tok) {
+  return s.n > 0 && (!a.causal || tok + s.n - s.m >= 0);
+}
 
 // What a workgroup works on: rows [ROWS rt, ...) of a sequence, key/value head g, part `part` of its keys.
 struct PackedTile {
@@ -116,7 +122,12 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
     for (int r = 0; r < 16; r++) o[i][r] = 0.f;
   const f32x16 zero = {};
   const float c = a.scale * LOG2E;
-  float m_run = M_FLOOR, l_run = 0.f;
+  // p = exp2(c_row s - m_run) in one operation. The rounding of m_run = c_row max s leaves the same factor for every key of the row, which
+  // cancels, as long as it is a number: up to |m_run| = FAR it is within 2^32. Scores past that are at least 2^4 apart in log2
+  // units where they differ at all, so any steeper or flatter exponential tells the largest from the others as well: c_row
+  // becomes the power of two that brings the maximum to 2^28, where neither product rounds.
+  constexpr float FAR = 536870912.f;   // 2^29
+  float c_row = c, m_run = M_FLOOR, l_run = 0.f;
 
   auto scores = [&](int kt, f32x16* sn) {
     const char* sk = smem + (kt & 1) * TILE;
@@ -162,11 +173,20 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
     if (kt + 2 < nt) issue_k(kt + 2);
     const char* sv = smem + (2 + (kt & 1)) * TILE;
     mx = pair_max(mx);
-    const float mxs = mx * c;
+    const float mxs = mx * c_row;
     if (__ballot(mxs > m_run + TAU) != 0) {
-      const float m_new = fmaxf(m_run, mxs);
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      float m_new = fmaxf(m_run, mxs), c_new = c_row;
+      if (mxs > m_run) {
+        c_new = c;
+        m_new = mx * c;
+        if (fabsf(m_new) > FAR) {
+          c_new = __uint_as_float(((127 + 28 + 127) << 23) - (__float_as_uint(mx) & 0x7f800000u));
+          m_new = mx * c_new;
+        }
+      }
+      const float alpha = c_new == c_row ? __builtin_amdgcn_exp2f(m_run - m_new) : 0.f;
       m_run = m_new;
+      c_row = c_new;
       l_run *= alpha;
 #pragma unroll
       for (int i = 0; i < NDB; i++)
@@ -181,7 +201,7 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
       for (int h = 0; h < 2; h++)
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(st[kb][8 * h + j], c, -m_run));
+          const float p = __builtin_amdgcn_exp2f(fmaf(st[kb][8 * h + j], c_row, -m_run));
           psum += p;
           pf[kb][h][j] = (__bf16)p;
         }
@@ -230,19 +250,23 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
   const bool real = row0 + wave * 32 + l32 < rows;
   if (PARTS && t.parts > 1) {
     const int64_t slot = t.slot * ROWS + wave * 32 + l32;
+    // the maximum in units of the scores, and what its rounding changes
+    const float m = m_run == M_FLOOR ? M_FLOOR : m_run / c_row;
+    const float f = m_run == M_FLOOR ? 1.f : __builtin_amdgcn_exp2f(fmaf(-m, c_row, m_run));
     if (real) {
-      if (half == 0) a.part_ml[slot] = make_float2(m_run, l_all);
+      if (half == 0) a.part_ml[slot] = make_float2(m, l_all * f);
       float* po = a.part_o + slot * D;
 #pragma unroll
       for (int db = 0; db < NDB; db++)
 #pragma unroll
         for (int g = 0; g < 4; g++)
-          *(float4*)(po + 32 * db + 8 * g + 4 * half) = make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+          *(float4*)(po + 32 * db + 8 * g + 4 * half) = make_float4(o[db][4 * g] * f, o[db][4 * g + 1] * f, o[db][4 * g + 2] * f, o[db][4 * g + 3] * f);
     }
     return;
   }
-  const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;   // (a NaN stays one)
-  const float lse = l_all == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_all)) * LN2;
+  const bool sees = vis > 0;
+  const float inv = sees ? 1.0f / l_all : 0.f, log2_l = __builtin_amdgcn_logf(l_all);
+  const float lse = !sees ? -INFINITY : c_row == c ? (m_run + log2_l) * LN2 : m_run * __builtin_amdgcn_rcpf(c_row) * a.scale;
   if (a.lse && real && half == 0) a.lse[(int64_t)(q0 + tok) * a.H + head] = lse;
   // The output leaves through the 32 rows of the K buffers that belong to this wave, so that a store writes whole
   // rows. (Both K buffers were last read before the last step's barrier.)
@@ -403,8 +427,9 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
   l_run += __shfl_xor(l_run, 16, 64);
   l_run += __shfl_xor(l_run, 32, 64);
   if (row0 + wave * 16 + l16 >= rows) return;
-  const float inv = l_run > 0.f ? 1.0f / l_run : l_run == 0.f ? 0.f : l_run;
-  const float lse = l_run == 0.f ? -INFINITY : m_run + __builtin_amdgcn_logf(l_run) * LN2;
+  const bool sees = vis > 0;
+  const float inv = sees ? 1.0f / l_run : 0.f;
+  const float lse = sees ? m_run + __builtin_amdgcn_logf(l_run) * LN2 : -INFINITY;
   float* orow = (float*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head;
   float* olse = a.lse ? a.lse + (int64_t)(q0 + tok) * a.H + head : nullptr;
   if (olse && g4 == 0) *olse = lse;
@@ -499,7 +524,8 @@ __global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
   for (int i = 0; i < NKC; i++) o[i] *= mine;
   join_waves<D>(sk[0], o, wave, l16, g4);
   if (wave > 0 || row0 + l16 >= rows) return;
-  float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+  const bool sees = vis > 0;
+  float inv = sees ? 1.0f / l : 0.f;
   float* orow = (float*)a.o + (q0 + tok) * a.o_row + (int64_t)head * a.o_head;
   if (a.part_tiles && t.parts > 1) {
     const int64_t slot = t.slot * ROWS + l16;
@@ -507,7 +533,7 @@ __global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
     inv = 1.f;
     if (g4 == 0) a.part_ml[slot] = make_float2(m, l);
   } else if (a.lse && g4 == 0) {
-    a.lse[(q0 + tok) * a.H + head] = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l) * LN2;
+    a.lse[(q0 + tok) * a.H + head] = sees ? m + __builtin_amdgcn_logf(l) * LN2 : -INFINITY;
   }
 #pragma unroll
   for (int i = 0; i < NKC; i++)
@@ -610,9 +636,8 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
 #pragma unroll
       for (int r = 0; r < 4; r++) mx = fmaxf(mx, s[kb][r]);
     mx = pair_max(fmaxf(mx, __shfl_xor(mx, 16, 64)));
-    const float mxs = mx * c;
-    if (__ballot(mxs > m_run) != 0) {
-      const float m_new = fmaxf(m_run, mxs), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    if (__ballot(mx > m_run) != 0) {
+      const float m_new = fmaxf(m_run, mx), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * c);
       m_run = m_new;
       l_run *= alpha;
 #pragma unroll
@@ -625,7 +650,7 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
     for (int kb = 0; kb < 2; kb++)
 #pragma unroll
       for (int r = 0; r < 4; r++) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][r], c, -m_run));
+        const float p = __builtin_amdgcn_exp2f((s[kb][r] - m_run) * c);   // (the difference first: exact however large they are)
         l_run += p;
         pf[4 * kb + r] = (__bf16)p;
       }
@@ -675,7 +700,7 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
 #pragma unroll
   for (int w = 0; w < NW; w++) {
     const float2 x = ml[w * ROWS + r];
-    const float f = __builtin_amdgcn_exp2f(x.x - m);
+    const float f = __builtin_amdgcn_exp2f((x.x - m) * c);
     l = fmaf(f, x.y, l);
 #pragma unroll
     for (int e = 0; e < EPT; e += 4) {
@@ -691,11 +716,12 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
     for (int e = 0; e < EPT; e += 4) store4<float>(a.part_o + slot * D + e0 + e, acc + e);
     return;
   }
-  const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
-  const float lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+  const int tk = rr / a.G, hd = t.g * a.G + (rr - tk * a.G);
+  const bool sees = sees_keys(a, t.s, tk);
+  const float inv = sees ? 1.0f / l : 0.f;
+  const float lse = sees ? fmaf(m, a.scale, __builtin_amdgcn_logf(l) * LN2) : -INFINITY;
 #pragma unroll
   for (int e = 0; e < EPT; e++) acc[e] *= inv;
-  const int tk = rr / a.G, hd = t.g * a.G + (rr - tk * a.G);
   if (a.lse && e0 == 0) a.lse[(int64_t)(q0 + tk) * a.H + hd] = lse;
 #pragma unroll
   for (int e = 0; e < EPT; e += 4) store4<u16>((u16*)a.o + (int64_t)(q0 + tk) * a.o_row + (int64_t)hd * a.o_head + e0 + e, acc + e);
@@ -731,7 +757,7 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
   const float2* ml = a.part_ml + slot;
   const float* po = a.part_o + slot * d;
   const int tok = row / a.G, head = g * a.G + row - tok * a.G;
-  constexpr float UNIT = sizeof(T) == 2 ? 1.f : LOG2E;   // of the maxima: log2 units (bf16), natural ones (fp32)
+  const float scale = sizeof(T) == 2 ? a.scale : 1.f, c = scale * LOG2E;   // (fp32 scores are scaled)
   float top = M_FLOOR;
   for (int p = lane; p < parts; p += 64) top = fmaxf(top, ml[(int64_t)p * ROWS].x);
 #pragma unroll
@@ -743,7 +769,7 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
     float w = 0.f, l = 0.f;
     if (lane < np) {
       const float2 x = ml[(int64_t)(p0 + lane) * ROWS];
-      w = __builtin_amdgcn_exp2f((x.x - top) * UNIT);
+      w = __builtin_amdgcn_exp2f((x.x - top) * c);
       l = x.y;
     }
     for (int p = 0; p < np; p += 8) {
@@ -763,14 +789,13 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
         }
     }
   }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const bool sees = sees_keys(a, sq, tok);
+  const float inv = sees ? 1.f / total : 0.f;
   T* orow = (T*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head + e;
   orow[0] = from_f32<T>(acc0 * inv);
   if (d > 64) orow[1] = from_f32<T>(acc1 * inv);
-  if (a.lse && lane == 0) {
-    const float lt = __builtin_amdgcn_logf(total);
-    a.lse[(int64_t)(q0 + tok) * a.H + head] = total == 0.f ? -INFINITY : sizeof(T) == 2 ? (top + lt) * LN2 : fmaf(lt, LN2, top);
-  }
+  if (a.lse && lane == 0)
+    a.lse[(int64_t)(q0 + tok) * a.H + head] = sees ? fmaf(top, scale, __builtin_amdgcn_logf(total) * LN2) : -INFINITY;
 }
 
 // Tiles and parts.

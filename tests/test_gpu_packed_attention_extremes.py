@@ -86,3 +86,72 @@ def test_parts_keep_their_weights_at_large_scores(d, H, G, m, n, hd, dtype):
     """Equal scores of 2^18, whose lse is known to 2^-6 only: o is the mean of v, whose parts have unlike means."""
     v = stored(np.repeat((np.arange(n) / n)[:, None], hd, 1), dtype)
     exact_case(d, dtype, hd, H, G, m, n, False, np.full(m, 2.0 ** 9), np.full(n, 2.0 ** 9), v, 1.0)
+
+
+LARGE = [2.0 ** 17, -2.0 ** 17, 2.0 ** 22, -2.0 ** 22, 2.0 ** 33, -2.0 ** 33, 2.0 ** 80, -2.0 ** 80, 2.0 ** 123, -2.0 ** 123, 2.0 ** 125,
+         -2.0 ** 125]
+# H, G, queries, keys, causal: few rows and wide tiles, one key, whole and in parts, rows that see nothing, enough tiles for 64 fp32 rows
+PLACES = [(8, 2, 1, 1, False), (8, 2, 1, 150, False), (8, 2, 1, 2000, False), (2, 1, 40, 1, False), (2, 1, 40, 77, True), (2, 1, 40, 20, True),
+          (2, 1, 40, 3000, False), (16, 16, 2112, 3, False)]
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("H,G,m,n,causal", PLACES)
+def test_large_scores_have_the_softmax_of_their_differences(d, H, G, m, n, causal, dtype, hd):
+    """Equal scores weigh the same; one that is 2^-7 of their size above the others is all that counts."""
+    v = stored(np.random.default_rng(n).standard_normal((n, hd)), dtype)
+    for s in LARGE:
+        q0 = np.full(m, np.copysign(2.0 ** 60, s))
+        k0 = np.full(n, abs(s) * 2.0 ** -59)
+        exact_case(d, dtype, hd, H, G, m, n, causal, q0, k0, v, 0.5)
+        for at in {0, n // 2, n - 1}:
+            k1 = k0.copy()
+            if s > 0:
+                k1[at] *= 1 + 2.0 ** -7
+            else:
+                k1 *= 1 + 2.0 ** -7
+                k1[at] = k0[at]
+            exact_case(d, dtype, hd, H, G, m, n, causal, q0, k1, v, 0.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,m,n", [(8, 2, 1, 2000), (2, 1, 40, 600), (2, 1, 40, 3000)])
+def test_scores_that_grow_along_the_keys(d, H, G, m, n, dtype):
+    """From ordinary ones to 2^40, and rows of ordinary scores beside rows of large ones."""
+    v = stored(np.random.default_rng(n).standard_normal((n, 64)), dtype)
+    k0 = 2.0 ** (np.arange(n) * 40 // n)
+    for k in (k0, -k0, k0[::-1], -k0[::-1]):
+        exact_case(d, dtype, 64, H, G, m, n, False, np.ones(m), k, v, 1.0)
+        exact_case(d, dtype, 64, H, G, m, n, True, np.where(np.arange(m) % 3, 2.0 ** -40, 1.0), k, v, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,m,n", [(8, 2, 1, 300), (2, 1, 40, 300), (2, 1, 40, 3000)])
+def test_neighbouring_large_scores_keep_their_ratio(d, H, G, m, n, dtype):
+    """Scores of a whole number near 726817 (2^20 in log2 units) and of one more: weights of e^-1 and 1, to the bound."""
+    q, k = np.zeros((m, H, 64)), np.zeros((n, G, 64))
+    q[:, :, :3] = 1.0
+    k[:, :, 0], k[:, :, 1] = 704 * 1024, 5888
+    k[:, :, 2] = 33 + (np.arange(n)[:, None] >= n // 2)
+    v = stored(np.random.default_rng(n).standard_normal((n, G, 64)), dtype)
+    tq, tk, tv = (to_dev(x, dtype) for x in (q, k, v))
+    o, lse = torch.zeros_like(tq), torch.zeros((m, H), device="cuda")
+    cfg = d.packed_config(tq, tk, tv, o, 1, False, 1.0, max_q=m)
+    ws = d.workspace(d.packed_attention_workspace_bytes(cfg)).fill_(255)
+    d.packed_attention(cfg, tq, tk, tv, o, lse=lse, ws=ws)
+    ref = attention_reference(q, k, v, [0, m], [0, n], [n], 1.0, False, dtype)
+    tol = UNIT[dtype] * np.abs(ref["o"]) + ((UNIT["bf16"] if dtype == "bf16" else 0.0) + (n + 8) * F32) * np.abs(v).max()
+    check(host64(o), ref["o"], tol, "o")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,m,n", [(8, 2, 1, 150), (8, 2, 1, 2000), (2, 1, 40, 70), (2, 1, 40, 3000)])
+def test_scores_of_minus_infinity_are_not_an_empty_row(d, H, G, m, n, dtype):
+    """A row whose scores all overflow has no softmax: NaN, not the zeros of a row that sees no key."""
+    q, k = np.full((m, H, 64), 2.0 ** 100), np.full((n, G, 64), -2.0 ** 100)
+    tq, tk = to_dev(q, dtype), to_dev(k, dtype)
+    o, lse = torch.zeros_like(tq), torch.zeros((m, H), device="cuda")
+    cfg = d.packed_config(tq, tk, tk, o, 1, False, 1.0, max_q=m)
+    ws = d.workspace(d.packed_attention_workspace_bytes(cfg)).fill_(255)
+    d.packed_attention(cfg, tq, tk, tk, o, lse=lse, ws=ws)
+    assert torch.isnan(o).all() and torch.isneginf(lse).all()
