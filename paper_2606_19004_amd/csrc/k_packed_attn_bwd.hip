@@ -21,10 +21,15 @@ namespace dit {
 namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 
-// lse in log2 units, or what makes every p of a row without visible keys 0
-__device__ __forceinline__ float lse2_of(float lse) { return lse == -INFINITY ? INFINITY : lse * LOG2E; }
+// What p is formed with, or what makes every p of a row without visible keys 0. bf16: lse in log2 units, p = exp2(c s - lse2) in one
+// operation; the rounding of lse2 is below that of p to bf16 (2^-8) while |lse| < 2^16. fp32: lse itself, and the difference
+// from it is taken before it goes to the exponential's base, which rounds it no further.
+template <typename T> __device__ __forceinline__ float lse_of(float lse) {
+  return lse == -INFINITY ? INFINITY : sizeof(T) == 2 ? lse * LOG2E : lse;
+}
+__device__ __forceinline__ float p_f32(float s, float lse) { return __builtin_amdgcn_exp2f((s - lse) * LOG2E); }
 
-// stats[head][tok] = (lse in log2 units, delta = sum_e do o): D / 8 (bf16) or D / 4 lanes per row, 16 bytes each. By head, so that the
+// stats[head][tok] = (lse as above, delta = sum_e do o): D / 8 (bf16) or D / 4 lanes per row, 16 bytes each. By head, so that the
 // rows a key tile walks read theirs in one piece ([tok][head] as lse comes: 1273 us for dk, dv of 8192 keys, 8 of 32 heads).
 template <typename T, int D>
 __global__ void __launch_bounds__(256) stats_kernel(PackedArgs a) {
@@ -47,7 +52,7 @@ __global__ void __launch_bounds__(256) stats_kernel(PackedArgs a) {
   }
 #pragma unroll
   for (int o = LPR / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (c == 0) a.stats[row] = make_float2(lse2_of(a.lse[(int64_t)tok * a.H + head]), s);
+  if (c == 0) a.stats[row] = make_float2(lse_of<T>(a.lse[(int64_t)tok * a.H + head]), s);
 }
 __device__ __forceinline__ float2 stats_of(const PackedArgs& a, int64_t tok, int64_t head) { return a.stats[head * a.qr.total + tok]; }
 
@@ -444,7 +449,7 @@ __device__ __forceinline__ void dq_f32(const PackedArgs& a, int block, float* sm
 #pragma unroll
     for (int r = 0; r < 4; r++) {
       const bool hidden = kt * W::NROW + 4 * g4 + r >= vis;
-      s[r] = hidden ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], LOG2E, -st.x)) * (dp[r] - st.y);
+      s[r] = hidden ? 0.f : p_f32(s[r], st.x) * (dp[r] - st.y);
     }
     W::add(dq, sk[buf], s, l16, g4);
     if (kt + step < nt) w.stage(sk[buf_of(kt + step)], sv[buf_of(kt + step)]);
@@ -522,7 +527,7 @@ __device__ __forceinline__ void dkdv_f32(const PackedArgs& a, int block, float* 
     for (int r = 0; r < 4; r++) {
       const int tok = t * W::NROW + 4 * g4 + r;
       const bool hidden = tok >= m || tok < first;
-      s[r] = hidden ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], LOG2E, -st[r].x));
+      s[r] = hidden ? 0.f : p_f32(s[r], st[r].x);
       dp[r] = hidden ? 0.f : s[r] * (dp[r] - st[r].y);
     }
     W::add(dv, sd[buf], s, l16, g4);

@@ -38,7 +38,7 @@ struct PackedArgs {
   float* part_o; float2* part_ml;   // [Hkv * units][row tile][d] sums of p v, [Hkv * units][row tile] running maximum and sum of p
   // backward
   const void* d_o; void* dq; void* dk; void* dv;
-  float2* stats;                    // [H][total_q] (lse in log2 units, rowsum(d_o o))
+  float2* stats;                    // [H][total_q] (lse, for bf16 in log2 units, rowsum(d_o o))
   int shares; float* share_sums;    // workgroups that share a key tile's rows, and their sums
   __device__ __forceinline__ PackedSeq sequence(int i) const {
     const int2 q = qr.raw(i), k = kr.raw(i);

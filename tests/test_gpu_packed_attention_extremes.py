@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import policy_oracle as P
 from tests.gpu_util import host64
 from tests.policy_util import F32, UNIT, attention_reference, check, stored, to_dev
 from tests.test_gpu_packed_attention import Problem
@@ -155,3 +156,57 @@ def test_scores_of_minus_infinity_are_not_an_empty_row(d, H, G, m, n, dtype):
     ws = d.workspace(d.packed_attention_workspace_bytes(cfg)).fill_(255)
     d.packed_attention(cfg, tq, tk, tk, o, lse=lse, ws=ws)
     assert torch.isnan(o).all() and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("H,G,hd,m", [(4, 2, 64, 70), (2, 1, 128, 33), (16, 16, 64, 2112), (8, 8, 128, 2112)])
+def test_fp32_gradients_take_the_difference_from_lse_first(d, H, G, hd, m):
+    """Whole scores from 4096 on, exact in every kernel, in tiles of 16 and of 64. With e the given lse, p = exp(s - e) is off by 2^-20:
+    s - e is exact (within a factor of two of each other), |s - e| < 10 goes to the base 2 with 2^-24 of itself, twice, and the
+    exponential by 2^-23. The rest is tests/policy_util.py's."""
+    rng = np.random.default_rng(m)
+    scale, n = 0.125, m
+    q, k = np.zeros((m, hd)), np.zeros((n, hd))
+    q[:, 0], k[:, 0] = 256.0, 128 + rng.integers(0, 6, n) / 32
+    v, do = (stored(rng.standard_normal((m, h, hd)), "f32") for h in (G, H))
+    o, lse = np.zeros((m, H, hd)), np.zeros((m, H))
+    for j in range(H):
+        o[:, j], lse[:, j], _ = P.attention(q, k, v[:, j // (H // G)], scale, True)
+    o, lse = stored(o, "f32"), stored(lse, "f32")
+    tq, tk = (to_dev(np.repeat(x[:, None], h, 1), "f32") for x, h in ((q, H), (k, G)))
+    tv, to, tdo = (to_dev(x, "f32") for x in (v, o, do))
+    dq, dk, dv = (torch.zeros_like(t) for t in (tq, tk, tv))
+    cfg = d.packed_config(tq, tk, tv, to, 1, True, scale, max_q=m)
+    ws = d.workspace(d.packed_attention_backward_workspace_bytes(cfg)).fill_(255)
+    d.packed_attention_backward(cfg, tq, tk, tv, to, torch.from_numpy(lse).float().cuda(), tdo, dq, dk, dv, ws=ws)
+    gq, gk, gv = (host64(t) for t in (dq, dk, dv))
+    e_p = 2.0 ** -20
+    wk, wv, tk_, tv_ = (np.zeros((n, G, hd)) for _ in range(4))
+    for j in range(H):
+        g = j // (H // G)
+        wq, k1, v1, p, ds = P.attention_gradients(q, k, v[:, g], o[:, j], lse[:, j], do[:, j], scale, True)
+        e_dp = (hd + 8) * F32 * (np.abs(do[:, j]) @ np.abs(v[:, g]).T + (np.abs(do[:, j]) * np.abs(o[:, j])).sum(1)[:, None])
+        b = (e_p + F32 * 8) * np.abs(ds) + p * e_dp
+        check(gq[:, j], wq, F32 * np.abs(wq) + scale * (b + n * F32 * np.abs(ds)) @ np.abs(k), "dq")
+        wk[:, g] += k1
+        wv[:, g] += v1
+        tk_[:, g] += scale * (b + m * F32 * np.abs(ds)).T @ np.abs(q)
+        tv_[:, g] += ((e_p + m * F32) * p).T @ np.abs(do[:, j])
+    check(gk, wk, tk_ + F32 * np.abs(wk), "dk")
+    check(gv, wv, tv_ + F32 * np.abs(wv), "dv")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(H=2, G=1, q_len=[100, 70], causal=True), dict(H=4, G=4, q_len=[33, 5], k_len=[60, 90])])
+def test_gradients_of_large_scores(d, dtype, kw):
+    """The bounds of tests/policy_util.py, and what underflow adds to them: a probability below 2^-126, the least number the exponential
+    gives, is 0, and so is such a ds = p (dp - delta). That is off by at most t = 2^-126 (1 + |dp| + |delta|), which the products carry
+    into at most rows t scale |q| of dk, keys t scale |k| of dq and rows 2^-126 |do| of dv."""
+    p = Problem(d, dtype, 64, seed=7, q_gain=40.0, **kw)
+    grads = p.backward()
+    ref = attention_reference(p.q, p.k, p.v, p.q_off, p.k_off, p.k_len, p.scale, p.causal, dtype, p.do, p.o64, p.lse64)
+    t = 2.0 ** -126 * (1 + np.nanmax(np.abs(p.do).sum(2)) * (np.nanmax(np.abs(p.v)) + np.nanmax(np.abs(p.o64))))
+    rows = max(p.q_len) * p.q.shape[1] // p.k.shape[1]
+    tiny = {"dq": max(p.k_len) * t * p.scale * np.nanmax(np.abs(p.k)), "dk": rows * t * p.scale * np.nanmax(np.abs(p.q)),
+            "dv": rows * 2.0 ** -126 * np.nanmax(np.abs(p.do))}
+    for n, g in zip(("dq", "dk", "dv"), grads):
+        check(host64(g.contiguous()), ref[n], ref[n + "_tol"] + tiny[n], n)
