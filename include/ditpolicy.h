@@ -93,7 +93,7 @@ typedef enum { DIT_NORM_NONE = 0, DIT_NORM_LAYER = 1, DIT_NORM_RMS = 2 } dit_nor
 
 typedef struct {
   int32_t sequences;     /* >= 1 where rows > 0; each has its own gate, scale and shift */
-  int32_t rows;          /* rows of x, y, h and their gradients */
+  int32_t rows;          /* rows of x, y, h and their gradients: at most 2^28 */
   int32_t hidden;        /* 1..8192 */
   int32_t dtype;         /* dit_dtype of the row tensors and of the norm weights */
   int32_t post_norm;     /* dit_norm_kind of the branch y */

@@ -78,7 +78,8 @@ __device__ __forceinline__ bool find_unit_in(int nseq, int u, L&& load, C&& coun
 #pragma unroll
     for (int b = 0; b < BLOCKS; b++) {
       if (base + 64 * b >= nseq) return false;
-      // (no count of a tensor within the entry points' limits is larger, and 64 of these fit)
+      // (no count of a tensor within the entry points' limits is larger: tiles of 64 of fewer than 2^30 rows, of 16 only where they are
+      // few, chunks of 8 of at most 2^28 rows where there are many; and 64 of these fit)
       const unsigned c = base + 64 * b + lane < nseq ? min(count(mine[b]), 1 << 25) : 0, incl = wave_scan(c);
       const unsigned total = __builtin_amdgcn_readlane(incl, 63);
       if ((unsigned)u < carry + total) {

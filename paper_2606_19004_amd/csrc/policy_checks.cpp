@@ -72,6 +72,8 @@ dit_status check_gated_norm(const dit_gated_norm_config* c) {
   if (c->hidden <= 0) return set_error(DIT_ERR_SHAPE, "hidden %d must be positive", c->hidden);
   if (c->hidden > 8192) return set_error(DIT_ERR_UNSUPPORTED, "hidden %d > 8192", c->hidden);
   if (c->sequences >= (1 << 20)) return set_error(DIT_ERR_UNSUPPORTED, "%d sequences (at most 2^20 - 1)", c->sequences);
+  // (chunks of a sequence, of 8 rows at least where there are many, are counted up to 2^25)
+  if (c->rows > (1 << 28)) return set_error(DIT_ERR_UNSUPPORTED, "%d rows (at most 2^28)", c->rows);
   for (int32_t k : {c->post_norm, c->pre_norm})
     if (k < DIT_NORM_NONE || k > DIT_NORM_RMS) return set_error(DIT_ERR_INVALID_ARG, "norm kind %d invalid", k);
   if (!(c->eps > 0.f) || !std::isfinite(c->eps)) return set_error(DIT_ERR_INVALID_ARG, "eps must be positive");
