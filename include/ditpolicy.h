@@ -18,6 +18,9 @@
  * end is before its start as empty, so bad offsets give wrong results but touch no other memory.
  * Output rows that belong to no sequence are left as they were.
  *
+ * A call whose largest launch would take 2^32 threads or more is refused with DIT_ERR_UNSUPPORTED (attention: 256 to a tile of 16 to
+ * 128 rows or keys of a head, one tile a sequence at least; norm: about hidden, to 8 rows; loss: 256 to a sample at least).
+ *
  * Every result is the same from run to run: sums are taken in a fixed order, with no atomics.
  * Output tensors must not overlap inputs or each other, except where it is said below.
  */

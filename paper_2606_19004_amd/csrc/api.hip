@@ -1310,6 +1310,12 @@ dit_status check_offsets_aligned(std::initializer_list<const void*> ptrs) {
   return DIT_OK;
 }
 
+// the largest launch of a call
+dit_status check_threads(int64_t threads) {
+  if (threads >= int64_t(1) << 32) return set_error(DIT_ERR_UNSUPPORTED, "%lld threads in one launch (fewer than 2^32)", (long long)threads);
+  return DIT_OK;
+}
+
 // workspace of a call, whatever its max_q and offsets turn out to be
 size_t packed_forward_ws(const dit_packed_config* c) {
   if (c->sequences == 0) return 0;
@@ -1373,6 +1379,7 @@ dit_status packed_attention(const dit_packed_config* c, const void* q, const voi
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o))
     return set_error(DIT_ERR_INVALID_ARG, "q/k/v/o must be 16-byte aligned");
   if ((st = check_offsets_aligned({q_offsets, k_offsets, k_lengths, lse}))) return st;
+  if ((st = check_threads(packed_forward_threads(a, c->dtype, c->head_dim)))) return st;
   if ((st = check_ws(ws, ws_bytes, packed_forward_ws(c)))) return st;
   a.q = q;
   a.k = k;
@@ -1400,6 +1407,7 @@ dit_status packed_attention_backward(const dit_packed_config* c, const void* q, 
   for (const void* p : {q, k, v, o, d_o, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!aligned16(p)) return set_error(DIT_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
   if ((st = check_offsets_aligned({q_offsets, k_offsets, k_lengths, lse}))) return st;
+  if ((st = check_threads(packed_backward_threads(a, c->dtype, c->head_dim)))) return st;
   if ((st = check_ws(ws, ws_bytes, packed_grad_ws(c)))) return st;
   a.q = q;
   a.k = k;
@@ -1428,6 +1436,7 @@ dit_status gated_norm(const dit_gated_norm_config* c, const void* x, const void*
   if (!x) return set_error(DIT_ERR_INVALID_ARG, "x NULL");
   if ((st = check_offsets_aligned({shift}))) return st;
   if ((st = check_elements({x, y, post_w, pre_w, x_out, h}, c->dtype))) return st;
+  if ((st = check_threads(gated_norm_forward_threads(a)))) return st;
   a.x = x;
   a.y = y;
   a.shift = shift;
@@ -1457,6 +1466,9 @@ dit_status gated_norm_backward(const dit_gated_norm_config* c, const void* x_out
   const bool columns = dgate || dscale || dshift || dpost_w || dpre_w;
   if (!columns && (c->rows == 0 || (!dx && !dy))) return DIT_OK;
   if (c->sequences == 0 && !dpost_w && !dpre_w) return DIT_OK;
+  a.parts = columns ? (float*)ws : nullptr;
+  a.chunks = gated_norm_chunks(c->sequences, c->rows, c->hidden);
+  if ((st = check_threads(gated_norm_backward_threads(a)))) return st;
   if ((st = check_ws(ws, ws_bytes, al256(gated_norm_ws(c->sequences, c->rows, c->hidden))))) return st;
   a.x = x_out;
   a.y = y;
@@ -1469,8 +1481,6 @@ dit_status gated_norm_backward(const dit_gated_norm_config* c, const void* x_out
   a.dshift = dshift;
   a.dpost_w = dpost_w;
   a.dpre_w = dpre_w;
-  a.parts = columns ? (float*)ws : nullptr;
-  a.chunks = gated_norm_chunks(c->sequences, c->rows, c->hidden);
   const double passes = 1 + (y != nullptr) + (dx_out != nullptr) + (dh != nullptr) + (dx != nullptr) + (dy != nullptr);
   if (c->rows > 0)
     TIMED("gated_norm_backward", 0, passes * c->rows * c->hidden * esize(c->dtype), hs(stream),
@@ -1500,6 +1510,7 @@ dit_status flow_policy_loss(const float* x, const float* v, const float* x_next,
   if ((st = check_offsets_aligned({x, v, x_next, v_ref, adv, dv}))) return st;
   for (const void* p : {(const void*)logp_old, (const void*)loss, (const void*)logp, (const void*)ratio})
     if ((uintptr_t)p & 7) return set_error(DIT_ERR_INVALID_ARG, "fp64 tensors must be 8-byte aligned");
+  if ((st = check_threads(256 * (int64_t)policy_loss_chunks(batch, n) * batch))) return st;
   if ((st = check_ws(ws, ws_bytes, flow_policy_loss_workspace_bytes(batch, n)))) return st;
   a.x = x;
   a.v = v;

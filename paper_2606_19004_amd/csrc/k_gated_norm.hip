@@ -784,17 +784,34 @@ int chunk_rows_of(int nseq, int rows, int D) {
 // workgroups for the 32 waves a CU can hold
 int forward_rows_of(int rows, int D) { return std::min(8, std::max(1, rows / (256 * 32 / (wide_threads(D) / 64)))); }
 
+// Threads of a launch.
+struct Launch {
+  int64_t groups;
+  int threads;
+  int64_t total() const { return groups * threads; }
+};
+Launch forward_of(const GatedNormArgs& a) {
+  if (narrow(a.D)) return {cdiv(a.rows, 4 * (64 / lanes_of(a.D))), 256};
+  return {(int64_t)a.rows / forward_rows_of(a.rows, a.D) + a.nseq, wide_threads(a.D)};
+}
+Launch rows_of(const GatedNormArgs& a) { return {a.chunks, narrow(a.D) ? 256 : wide_threads(a.D)}; }
+Launch columns_of(const GatedNormArgs& a) {
+  return {(int64_t)cdiv(a.D, 64) * a.nseq, a.chunks <= 8 * (int64_t)a.nseq ? 256 : 1024};   // few chunks per sequence: 4 waves
+}
+
 template <typename T>
 void forward_launch(const GatedNormArgs& a, hipStream_t s) {
   const bool vec = vectors(a);
+  const Launch l = forward_of(a);
+  const int grid = (int)l.groups;
   if (narrow(a.D)) {
-    const int lpr = lanes_of(a.D), grid = cdiv(a.rows, 4 * (64 / lpr));
+    const int lpr = lanes_of(a.D);
     if (vec) forward_narrow<T, true><<<grid, 256, 0, s>>>(a, lpr);
     else forward_narrow<T, false><<<grid, 256, 0, s>>>(a, lpr);
   } else {
-    const int cr = forward_rows_of(a.rows, a.D), grid = a.rows / cr + a.nseq, threads = wide_threads(a.D);
-    if (vec) forward_wide<T, true><<<grid, threads, 0, s>>>(a, cr);
-    else forward_wide<T, false><<<grid, threads, 0, s>>>(a, cr);
+    const int cr = forward_rows_of(a.rows, a.D);
+    if (vec) forward_wide<T, true><<<grid, l.threads, 0, s>>>(a, cr);
+    else forward_wide<T, false><<<grid, l.threads, 0, s>>>(a, cr);
   }
 }
 
@@ -807,7 +824,7 @@ void rows_launch(const GatedNormArgs& a, hipStream_t s) {
     if (vec) rows_narrow<T, true><<<a.chunks, 256, 0, s>>>(a, lpr, cr);
     else rows_narrow<T, false><<<a.chunks, 256, 0, s>>>(a, lpr, cr);
   } else {
-    const int threads = wide_threads(a.D);
+    const int threads = rows_of(a).threads;
     if (vec && a.y && a.dx_out && a.dh && a.dx && a.dy) rows_wide<T, true, true><<<a.chunks, threads, 0, s>>>(a, cr);
     else if (vec) rows_wide<T, true, false><<<a.chunks, threads, 0, s>>>(a, cr);
     else rows_wide<T, false, false><<<a.chunks, threads, 0, s>>>(a, cr);
@@ -815,6 +832,11 @@ void rows_launch(const GatedNormArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+int64_t gated_norm_forward_threads(const GatedNormArgs& a) { return forward_of(a).total(); }
+int64_t gated_norm_backward_threads(const GatedNormArgs& a) {
+  return std::max(a.rows > 0 ? rows_of(a).total() : 0, a.parts ? columns_of(a).total() : 0);
+}
 
 hipError_t gated_norm_fwd(const GatedNormArgs& a, int dtype, hipStream_t s) {
   if (dtype == DT_BF16) forward_launch<u16>(a, s);
@@ -835,9 +857,9 @@ hipError_t gated_norm_rows_bwd(const GatedNormArgs& a, int dtype, hipStream_t s)
 
 template <typename T>
 static void columns_launch(const GatedNormArgs& a, int cr, hipStream_t s) {
-  const int64_t grid = (int64_t)cdiv(a.D, 64) * a.nseq;
-  if (a.chunks <= 8 * (int64_t)a.nseq) columns_kernel<T, 4><<<grid, 256, 0, s>>>(a, cr);   // few chunks per sequence
-  else columns_kernel<T, 16><<<grid, 1024, 0, s>>>(a, cr);
+  const Launch l = columns_of(a);
+  if (l.threads == 256) columns_kernel<T, 4><<<l.groups, 256, 0, s>>>(a, cr);
+  else columns_kernel<T, 16><<<l.groups, 1024, 0, s>>>(a, cr);
 }
 hipError_t gated_norm_columns_bwd(const GatedNormArgs& a, int dtype, hipStream_t s) {
   const int cr = chunk_rows_of(a.nseq, a.rows, a.D);

@@ -843,8 +843,17 @@ static void fwd_launch(const PackedArgs& a, int dtype, int rows, int64_t grid, h
   else packed_fwd_bf16<D, false><<<grid, 256, 0, s>>>(a);
 }
 
+static PackedPlan plan_of(const PackedArgs& a, int dtype, int d) {
+  return packed_plan(dtype, a.nseq, a.H, a.Hkv, d, a.qr.total, a.kr.total, a.max_q, a.kr.off ? a.kr.total : a.kr.len);
+}
+static int64_t join_groups(const PackedArgs& a, const PackedPlan& p) { return p.part_tiles ? (int64_t)p.row_tiles * a.Hkv * (p.rows / 4) : 0; }
+int64_t packed_forward_threads(const PackedArgs& a, int dtype, int d) {
+  const PackedPlan p = plan_of(a, dtype, d);
+  return 256 * std::max((int64_t)p.units * a.Hkv, join_groups(a, p));
+}
+
 hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
-  const PackedPlan p = packed_plan(dtype, a.nseq, a.H, a.Hkv, d, a.qr.total, a.kr.total, a.max_q, a.kr.off ? a.kr.total : a.kr.len);
+  const PackedPlan p = plan_of(a, dtype, d);
   if (p.row_tiles == 0) return hipSuccess;
   a.part_tiles = p.part_tiles;
   a.units = p.units;
@@ -854,7 +863,7 @@ hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStr
   if (d == 128) fwd_launch<128>(a, dtype, p.rows, grid, s);
   else fwd_launch<64>(a, dtype, p.rows, grid, s);
   if (p.part_tiles) {
-    const int64_t jg = (int64_t)p.row_tiles * a.Hkv * (p.rows / 4);
+    const int64_t jg = join_groups(a, p);
     if (p.rows == 16 && dtype == DT_F32) packed_join<float, 16><<<jg, 256, 0, s>>>(a, d);
     else if (p.rows == 16) packed_join<u16, 16><<<jg, 256, 0, s>>>(a, d);
     else packed_join<u16, 128><<<jg, 256, 0, s>>>(a, d);   // (64-row tiles of fp32 fill the chip by themselves)

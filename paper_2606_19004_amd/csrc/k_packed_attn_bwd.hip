@@ -626,10 +626,30 @@ size_t packed_backward_ws(int dtype, int nseq, int H, int Hkv, int d, int total_
   return stats_bytes(H, total_q) + (shares > 1 ? (size_t)shares * total_k * Hkv * 2 * d * 4 : 0);
 }
 
+// Workgroups of a call's launches.
+struct BackwardGroups {
+  int tile, shares;
+  int64_t stats, keys, rows, joins;   // (those of keys and rows are in one launch)
+};
+static BackwardGroups groups_of(const PackedArgs& a, int dtype, int d) {
+  const int total_q = a.qr.total, total_k = a.kr.total;
+  BackwardGroups g{};
+  g.tile = grad_tile(dtype, a.nseq, a.H, a.Hkv, d, total_q, total_k);
+  g.shares = shares_of(dtype, a.nseq, a.H, a.Hkv, d, total_q, total_k, a.causal);
+  g.stats = ((int64_t)total_q * a.H * (d * (dtype == DT_BF16 ? 2 : 4) / 16) + 255) / 256;
+  g.keys = total_k > 0 ? tiles_of(a.nseq, total_k, total_k, g.tile) * a.Hkv * g.shares : 0;
+  g.rows = tiles_of(a.nseq, (int64_t)total_q * a.G, (int64_t)a.max_q * a.G, g.tile) * a.Hkv;
+  g.joins = g.shares > 1 && total_k > 0 ? ((int64_t)total_k / 64 + a.nseq) * a.Hkv : 0;
+  return g;
+}
+int64_t packed_backward_threads(const PackedArgs& a, int dtype, int d) {
+  const BackwardGroups g = groups_of(a, dtype, d);
+  return 256 * std::max({g.stats, g.keys + g.rows, g.joins});
+}
+
 hipError_t packed_attention_stats(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
   a.stats = (float2*)ws;
-  const int64_t lanes = (int64_t)a.qr.total * a.H * (d * (dtype == DT_BF16 ? 2 : 4) / 16);
-  const int64_t grid = (lanes + 255) / 256;
+  const int64_t grid = groups_of(a, dtype, d).stats;
   if (grid == 0) return hipSuccess;
   if (dtype == DT_BF16 && d == 128) stats_kernel<u16, 128><<<grid, 256, 0, s>>>(a);
   else if (dtype == DT_BF16) stats_kernel<u16, 64><<<grid, 256, 0, s>>>(a);
@@ -643,21 +663,18 @@ static void gradients_launch(const PackedArgs& a, int dtype, int tile, int key_b
   if (dtype == DT_BF16) packed_gradients_bf16<D><<<blocks, 256, 0, s>>>(a, key_blocks);
   else if (tile == 16) packed_gradients_f32<D, true><<<blocks, 256, 0, s>>>(a, key_blocks);
   else packed_gradients_f32<D, false><<<blocks, 256, 0, s>>>(a, key_blocks);
-  if (a.shares <= 1 || joins == 0) return;
+  if (joins == 0) return;
   if (dtype == DT_BF16) shares_join<u16, D><<<joins, 256, 0, s>>>(a);
   else shares_join<float, D><<<joins, 256, 0, s>>>(a);
 }
 hipError_t packed_attention_gradients(PackedArgs a, int dtype, int d, void* ws, hipStream_t s) {
-  const int total_q = a.qr.total, total_k = a.kr.total, tile = grad_tile(dtype, a.nseq, a.H, a.Hkv, d, total_q, total_k);
+  const BackwardGroups g = groups_of(a, dtype, d);
   a.stats = (float2*)ws;
-  a.shares = shares_of(dtype, a.nseq, a.H, a.Hkv, d, total_q, total_k, a.causal);
-  a.share_sums = (float*)((char*)ws + stats_bytes(a.H, total_q));
-  const int64_t keys = total_k > 0 ? tiles_of(a.nseq, total_k, total_k, tile) * a.Hkv * a.shares : 0;
-  const int64_t rows = tiles_of(a.nseq, (int64_t)total_q * a.G, (int64_t)a.max_q * a.G, tile) * a.Hkv;
-  if (keys + rows == 0) return hipSuccess;
-  const int64_t joins = total_k > 0 ? ((int64_t)total_k / 64 + a.nseq) * a.Hkv : 0;
-  if (d == 128) gradients_launch<128>(a, dtype, tile, (int)keys, keys + rows, joins, s);
-  else gradients_launch<64>(a, dtype, tile, (int)keys, keys + rows, joins, s);
+  a.shares = g.shares;
+  a.share_sums = (float*)((char*)ws + stats_bytes(a.H, a.qr.total));
+  if (g.keys + g.rows == 0) return hipSuccess;
+  if (d == 128) gradients_launch<128>(a, dtype, g.tile, (int)g.keys, g.keys + g.rows, g.joins, s);
+  else gradients_launch<64>(a, dtype, g.tile, (int)g.keys, g.keys + g.rows, g.joins, s);
   return hipGetLastError();
 }
 

@@ -114,6 +114,9 @@ struct PackedPlan {
   size_t ws;        // bytes
 };
 PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q, int max_k);
+// Threads of the largest launch of a call: one takes fewer than 2^32.
+int64_t packed_forward_threads(const PackedArgs& a, int dtype, int d);
+int64_t packed_backward_threads(const PackedArgs& a, int dtype, int d);
 hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
 size_t packed_backward_ws(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int causal);
 hipError_t packed_attention_stats(PackedArgs a, int dtype, int d, void* ws, hipStream_t s);
@@ -134,6 +137,8 @@ struct GatedNormArgs {
   float* parts;   // [chunks][3][D] column sums of the row chunks
   int chunks;     // upper bound on (sequence, chunk)
 };
+int64_t gated_norm_forward_threads(const GatedNormArgs& a);    // of the largest launch
+int64_t gated_norm_backward_threads(const GatedNormArgs& a);
 hipError_t gated_norm_fwd(const GatedNormArgs& a, int dtype, hipStream_t s);
 int gated_norm_chunks(int nseq, int rows, int D);   // row chunks of the backward pass, at most
 size_t gated_norm_ws(int nseq, int rows, int D);

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2606_19004_amd import ditstep as d
-from tests.test_policy_host import A, UNSUPPORTED, norm, norm_back, norm_cfg
+from tests.test_policy_host import A, UNSUPPORTED, backward, forward, loss, norm, norm_back, norm_cfg, packed
 
 
 @pytest.mark.parametrize("hidden", [64, 320, 8192])
@@ -13,3 +13,32 @@ def test_gated_norm_of_too_many_rows(rows, hidden):
     assert norm(c) == UNSUPPORTED
     assert norm_back(c, dt=A) == UNSUPPORTED
     assert d.gated_norm_backward_workspace_bytes(c) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(sequences=(1 << 20) - 1, heads=32, kv_heads=32, total_q=(1 << 20) - 1, total_k=1 << 20, max_q=1),
+                                dict(sequences=(1 << 20) - 1, heads=32, kv_heads=32, total_q=(1 << 20) - 1, total_k=1 << 20, max_q=1, dtype=0,
+                                     q_head=256, k_head=256, v_head=256, o_head=256, q_row=8192, k_row=8192, v_row=8192, o_row=8192)])
+def test_attention_of_more_workgroups_than_a_launch_takes(kw):
+    """256 threads each of 2^25 (sequence, head) pairs: a launch takes fewer than 2^32."""
+    cfg = packed(**{**dict(q_row=2048, k_row=2048, v_row=2048, o_row=2048), **kw})
+    assert forward(cfg, ws=A, n=1 << 50) == UNSUPPORTED
+    assert backward(cfg, n=1 << 50) == UNSUPPORTED
+
+
+def test_attention_gradients_of_more_rows_than_a_launch_takes():
+    """The rows' statistics: 16 lanes to a row of 128 bf16 elements."""
+    cfg = packed(sequences=1, heads=32, kv_heads=32, head_dim=128, total_q=1 << 23, total_k=1 << 23, q_row=4096, k_row=4096, v_row=4096,
+                 o_row=4096, q_head=128, k_head=128, v_head=128, o_head=128)
+    assert backward(cfg, n=1 << 50) == UNSUPPORTED
+
+
+def test_gated_norm_of_more_workgroups_than_a_launch_takes():
+    wide = dict(hidden=8192, x_row=8192, y_row=8192, h_row=8192, mod_row=8192)
+    assert norm(norm_cfg(rows=1 << 26, **wide)) == UNSUPPORTED                      # 1024 threads to 8 rows
+    assert norm(norm_cfg(rows=1 << 28, hidden=256, x_row=256, y_row=256, h_row=256, mod_row=256)) == UNSUPPORTED   # 32 to a row
+    c = norm_cfg(rows=1 << 18, sequences=1 << 18, **wide)
+    assert norm_back(c, dt=A, n=1 << 50) == UNSUPPORTED                             # 256 threads to 64 columns of a sequence
+
+
+def test_policy_loss_of_more_samples_than_a_launch_takes():
+    assert loss(B=1 << 24, n=4, nb=1 << 40) == UNSUPPORTED
