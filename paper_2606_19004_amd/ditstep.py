@@ -324,20 +324,48 @@ def _elsewhere(t, dev):
     raise ValueError(f"a tensor on {t.device} in a call on cuda:{dev}")
 
 
-def _here(*tensors):
-    """Device pointers of tensors that have to be on the current device (its stream runs the call)."""
-    dev = _current_device()
-    return [None if t is None else t.data_ptr() if t.get_device() == dev else _elsewhere(t, dev) for t in tensors]
+_ROW_TYPES = {DIT_BF16: torch.bfloat16, DIT_F32: torch.float32}
 
 
-def _typed(dtype, *tensors):
-    for t in tensors:
-        if t is not None and t.dtype is not dtype:
-            raise ValueError(f"a tensor of {t.dtype} where {dtype} is wanted")
+def _at(t, dev, dtype, shape, strides):
+    """The device pointer of a tensor (or None) that has to be on the current device, whose stream runs the call, and of this type,
+    shape and strides."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.stride() != strides:
+        _check_layout(t, dtype, shape, strides)
+    return t.data_ptr() if t.get_device() == dev else _elsewhere(t, dev)
 
 
-def _ws_args(ws):
-    return (*_here(ws), ws.numel() if ws is not None else 0)
+def _dense(t, dev, dtype, n):
+    """The same of n elements without gaps (or more)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        _check_layout(t, dtype, (n,), (1,))
+    return t.data_ptr() if t.get_device() == dev else _elsewhere(t, dev)
+
+
+def _check_layout(t, dtype, shape, strides):
+    """What else may be read and written as `shape` at `strides`: more rows, any stride of an index that has one value, and, where the
+    elements lie without gaps, as many of them in any contiguous shape."""
+    if dtype is None:   # (a config of an unknown type, which the library refuses)
+        return
+    if t.dtype is not dtype:
+        raise ValueError(f"a tensor of {t.dtype} where {dtype} is wanted")
+    if 0 in shape:
+        return
+    dense = [math.prod(shape[i + 1:]) for i in range(len(shape))]
+    if t.is_contiguous() and t.numel() >= math.prod(shape) and all(n == 1 or a == b for n, a, b in zip(shape, strides, dense)):
+        return
+    if t.dim() != len(shape) or t.shape[0] < shape[0] or t.shape[1:] != shape[1:]:
+        raise ValueError(f"a tensor of shape {tuple(t.shape)} where the call has {shape}")
+    if any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
+        raise ValueError(f"a tensor of strides {t.stride()} where the call has {strides}")
+
+
+def _ws_args(ws, dev):
+    return (None, 0) if ws is None else (ws.data_ptr() if ws.get_device() == dev else _elsewhere(ws, dev), ws.numel())
 
 
 def packed_config(q, k, v, o, sequences, causal=False, scale=None, max_q=0) -> PackedConfig:
@@ -358,15 +386,26 @@ def packed_config(q, k, v, o, sequences, causal=False, scale=None, max_q=0) -> P
                         _dtype_code(q.dtype), scale, *strides)
 
 
+def _attention_layouts(cfg):
+    """(type, shape, strides) of q, k, v, o and their gradients"""
+    dt, d = _ROW_TYPES.get(cfg.dtype), cfg.head_dim
+    q, k = (cfg.total_q, cfg.heads, d), (cfg.total_k, cfg.kv_heads, d)
+    return (dt, q, (cfg.q_row, cfg.q_head, 1)), (dt, k, (cfg.k_row, cfg.k_head, 1)), (dt, k, (cfg.v_row, cfg.v_head, 1)), (
+        dt, q, (cfg.o_row, cfg.o_head, 1))
+
+
 def packed_attention_workspace_bytes(cfg) -> int:
     return _lib.packed_attention_workspace_bytes(C.byref(cfg))
 
 
 def packed_attention(cfg, q, k, v, o, lse=None, q_offsets=None, k_offsets=None, k_lengths=None, ws=None, stream=None):
-    """Tensors laid out as those cfg was made from; offsets and lengths: device int32, or None (equal lengths)."""
-    _typed(torch.int32, q_offsets, k_offsets, k_lengths)
-    _check(_lib.packed_attention(C.byref(cfg), *_here(q, k, v, q_offsets, k_offsets, k_lengths, o, lse), *_ws_args(ws),
-                                 _s(stream)))
+    """Tensors laid out as those cfg was made from; lse: fp32 [rows][heads]; offsets (one more than sequences) and lengths: device
+    int32, or None (equal lengths)."""
+    dev, s, i32 = _current_device(), cfg.sequences, torch.int32
+    lq, lk, lv, lo = _attention_layouts(cfg)
+    qo, ko, kl = _dense(q_offsets, dev, i32, s + 1), _dense(k_offsets, dev, i32, s + 1), _dense(k_lengths, dev, i32, s)
+    _check(_lib.packed_attention(C.byref(cfg), _at(q, dev, *lq), _at(k, dev, *lk), _at(v, dev, *lv), qo, ko, kl, _at(o, dev, *lo),
+                                 _dense(lse, dev, torch.float32, cfg.total_q * cfg.heads), *_ws_args(ws, dev), _s(stream)))
 
 
 def packed_attention_backward_workspace_bytes(cfg) -> int:
@@ -376,9 +415,13 @@ def packed_attention_backward_workspace_bytes(cfg) -> int:
 def packed_attention_backward(cfg, q, k, v, o, lse, d_o, dq, dk, dv, q_offsets=None, k_offsets=None, k_lengths=None,
                               ws=None, stream=None):
     """d_o laid out like o, dq, dk, dv like q, k, v."""
-    _typed(torch.int32, q_offsets, k_offsets, k_lengths)
-    _check(_lib.packed_attention_backward(C.byref(cfg), *_here(q, k, v, o, lse, d_o, q_offsets, k_offsets, k_lengths, dq,
-                                                               dk, dv), *_ws_args(ws), _s(stream)))
+    dev, s, i32 = _current_device(), cfg.sequences, torch.int32
+    lq, lk, lv, lo = _attention_layouts(cfg)
+    qo, ko, kl = _dense(q_offsets, dev, i32, s + 1), _dense(k_offsets, dev, i32, s + 1), _dense(k_lengths, dev, i32, s)
+    _check(_lib.packed_attention_backward(
+        C.byref(cfg), _at(q, dev, *lq), _at(k, dev, *lk), _at(v, dev, *lv), _at(o, dev, *lo),
+        _dense(lse, dev, torch.float32, cfg.total_q * cfg.heads), _at(d_o, dev, *lo), qo, ko, kl, _at(dq, dev, *lq), _at(dk, dev, *lk),
+        _at(dv, dev, *lv), *_ws_args(ws, dev), _s(stream)))
 
 
 def gated_norm_config(x, sequences, post="none", pre="layer", eps=1e-6, residual_scale=1.0, y_row=None, h_row=None,
@@ -395,10 +438,15 @@ def gated_norm_config(x, sequences, post="none", pre="layer", eps=1e-6, residual
 
 def gated_norm(cfg, x, y, x_out, h, gate=None, scale=None, shift=None, post_w=None, pre_w=None, offsets=None,
                stream=None):
-    """gate, scale, shift: fp32 [sequences][hidden] at cfg's mod_row; offsets: device int32, or None (equal lengths)."""
-    _typed(torch.int32, offsets)
-    _typed(torch.float32, gate, scale, shift)
-    _check(_lib.gated_norm(C.byref(cfg), *_here(x, y, post_w, pre_w, gate, scale, shift, offsets, x_out, h), _s(stream)))
+    """x, x_out, y, h: cfg's type, at its x_row, y_row, h_row; post_w, pre_w: [hidden], cfg's type; gate, scale, shift: fp32
+    [sequences][hidden] at its mod_row; offsets: device int32 (one more than sequences), or None (equal lengths)."""
+    dev, dt, f32, hidden, s = _current_device(), _ROW_TYPES.get(cfg.dtype), torch.float32, cfg.hidden, cfg.sequences
+    rows, xs, mods, ms = (cfg.rows, hidden), (cfg.x_row, 1), (s, hidden), (cfg.mod_row, 1)
+    off, g, sc, sh = _dense(offsets, dev, torch.int32, s + 1), _at(gate, dev, f32, mods, ms), _at(scale, dev, f32, mods, ms), _at(
+        shift, dev, f32, mods, ms)
+    _check(_lib.gated_norm(C.byref(cfg), _at(x, dev, dt, rows, xs), _at(y, dev, dt, rows, (cfg.y_row, 1)), _dense(post_w, dev, dt, hidden),
+                           _dense(pre_w, dev, dt, hidden), g, sc, sh, off, _at(x_out, dev, dt, rows, xs),
+                           _at(h, dev, dt, rows, (cfg.h_row, 1)), _s(stream)))
 
 
 def gated_norm_backward_workspace_bytes(cfg) -> int:
@@ -407,11 +455,15 @@ def gated_norm_backward_workspace_bytes(cfg) -> int:
 
 def gated_norm_backward(cfg, x_out, y, dx_out, dh, dx, dy, gate=None, scale=None, post_w=None, pre_w=None, offsets=None,
                         dgate=None, dscale=None, dshift=None, dpost_w=None, dpre_w=None, ws=None, stream=None):
-    """x_out: the forward call's output. Any gradient may be None."""
-    _typed(torch.int32, offsets)
-    _typed(torch.float32, gate, scale, dgate, dscale, dshift, dpost_w, dpre_w)
-    _check(_lib.gated_norm_backward(C.byref(cfg), *_here(x_out, y, post_w, pre_w, gate, scale, offsets, dx_out, dh, dx, dy,
-                                                         dgate, dscale, dshift, dpost_w, dpre_w), *_ws_args(ws), _s(stream)))
+    """x_out: the forward call's output. Any gradient may be None; those of vectors and weights are fp32."""
+    dev, dt, f32, hidden, s = _current_device(), _ROW_TYPES.get(cfg.dtype), torch.float32, cfg.hidden, cfg.sequences
+    lx, ly = (dt, (cfg.rows, hidden), (cfg.x_row, 1)), (dt, (cfg.rows, hidden), (cfg.y_row, 1))
+    lh, lm = (dt, (cfg.rows, hidden), (cfg.h_row, 1)), (f32, (s, hidden), (cfg.mod_row, 1))
+    off, g, sc = _dense(offsets, dev, torch.int32, s + 1), _at(gate, dev, *lm), _at(scale, dev, *lm)
+    _check(_lib.gated_norm_backward(
+        C.byref(cfg), _at(x_out, dev, *lx), _at(y, dev, *ly), _dense(post_w, dev, dt, hidden), _dense(pre_w, dev, dt, hidden), g, sc, off,
+        _at(dx_out, dev, *lx), _at(dh, dev, *lh), _at(dx, dev, *lx), _at(dy, dev, *ly), _at(dgate, dev, *lm), _at(dscale, dev, *lm),
+        _at(dshift, dev, *lm), _dense(dpost_w, dev, f32, hidden), _dense(dpre_w, dev, f32, hidden), *_ws_args(ws, dev), _s(stream)))
 
 
 def flow_policy_loss_workspace_bytes(batch, n_per_sample) -> int:
@@ -420,17 +472,18 @@ def flow_policy_loss_workspace_bytes(batch, n_per_sample) -> int:
 
 def flow_policy_loss(x, v, x_next, logp_old, adv, t, t_next, noise_level, loss, dv=None, logp=None, ratio=None,
                      v_ref=None, logp_scale=None, clip_low=0.2, clip_high=0.2, kl_weight=0.0, ws=None, stream=None):
-    """x, v, x_next, v_ref, dv: [batch][n] fp32 (any trailing shape); logp_old, logp, ratio: [batch] fp64; adv: [batch]
+    """x, v, x_next, v_ref, dv: [batch][n] fp32 (any trailing shape, contiguous); logp_old, logp, ratio: [batch] fp64; adv: [batch]
     fp32; loss: one fp64. logp_scale None: 1 / n."""
     b = x.shape[0] if x.dim() > 0 else 0
     n = x.numel() // b if b else 0
     if logp_scale is None:
         logp_scale = 1.0 / max(n, 1)
-    _typed(torch.float32, x, v, x_next, v_ref, adv, dv)
-    _typed(torch.float64, logp_old, loss, logp, ratio)
-    px, pv, pn, pr, old, pa, *outs = _here(x, v, x_next, v_ref, logp_old, adv, loss, logp, ratio, dv)
-    _check(_lib.flow_policy_loss(px, pv, pn, pr, b, n, t, t_next, noise_level, old, pa, logp_scale, clip_low, clip_high,
-                                 kl_weight, *outs, *_ws_args(ws), _s(stream)))
+    dev, f32, f64, bn = _current_device(), torch.float32, torch.float64, b * n
+    old, pa = _dense(logp_old, dev, f64, b), _dense(adv, dev, f32, b)
+    px, pv, pn, pr, dvp = (_dense(u, dev, f32, bn) for u in (x, v, x_next, v_ref, dv))
+    _check(_lib.flow_policy_loss(px, pv, pn, pr, b, n, t, t_next, noise_level, old, pa, logp_scale, clip_low, clip_high, kl_weight,
+                                 _dense(loss, dev, f64, 1), _dense(logp, dev, f64, b), _dense(ratio, dev, f64, b), dvp,
+                                 *_ws_args(ws, dev), _s(stream)))
 
 
 def dit_profile_begin():
