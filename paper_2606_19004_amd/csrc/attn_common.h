@@ -123,6 +123,13 @@ __device__ __forceinline__ bf16x8 join_tr(i16x4 lo, i16x4 hi) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Between accesses to LDS by which the lanes of one wave hand data to each other without a barrier. The unit keeps a wave's accesses
+// in order; this keeps the compiler from moving a lane's own across it. No instruction.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // fp32 on v_mfma_f32_16x16x4_f32: 16 owned rows per wave (fragments own[c]: dims 16 c + 4 g4 + 0..3 of row lane % 16, g4 = lane / 16)
 // against a walked tile of 16 rows of two tensors, staged through registers into LDS by LANES lanes (a workgroup, or a wave
 // with tiles of its own).

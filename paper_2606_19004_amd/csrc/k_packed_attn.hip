@@ -282,6 +282,7 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
         u.y = pack_bf16x2(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv);
         *(uint2*)(so + l32 * RB + ((ch ^ (l32 % CH)) << 4) + 8 * half) = u;
       }
+    wave_fence();
     constexpr int RPI = 64 / CH;
 #pragma unroll
     for (int i = 0; i < 32 / RPI; i++) {
@@ -484,6 +485,7 @@ __global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
   if (kt0 + wave < nt) {
     fetch(kt0 + wave);
     w.stage(sk[wave], sv[wave]);
+    wave_fence();
   }
   for (int kt = kt0 + wave; kt < nt; kt += 4) {
     if (kt + 4 < nt) fetch(kt + 4);
@@ -508,7 +510,9 @@ __global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
       l_run += s[r];
     }
     W::add(o, sv[wave], s, l16, g4);
+    wave_fence();
     if (kt + 4 < nt) w.stage(sk[wave], sv[wave]);
+    wave_fence();
   }
   l_run += __shfl_xor(l_run, 16, 64);
   l_run = pair_sum(l_run);

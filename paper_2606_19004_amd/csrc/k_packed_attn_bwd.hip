@@ -83,12 +83,14 @@ __device__ __forceinline__ void store_columns(char* so, const f32x16* acc, float
       u.y = pack_bf16x2(acc[db][4 * g + 2] * f, acc[db][4 * g + 3] * f);
       *(uint2*)(so + l32 * RB + (((4 * db + g) ^ (l32 % CH)) << 4) + 8 * half) = u;
     }
+  wave_fence();
   constexpr int RPI = 64 / CH;
 #pragma unroll
   for (int i = 0; i < 32 / RPI; i++) {
     const int r = i * RPI + lane / CH, ch = lane % CH;
     store(r, ch, *(const uint4*)(so + r * RB + ((ch ^ (r % CH)) << 4)));
   }
+  wave_fence();   // (the rows may be written again)
 }
 
 // Both kinds of workgroup are in one launch, those of the keys, which are the longer, first. In a launch each, every CU waits between
@@ -440,6 +442,7 @@ __device__ __forceinline__ void dq_f32(const PackedArgs& a, int block, float* sm
   if (first < nt) {
     fetch(first);
     w.stage(sk[buf_of(first)], sv[buf_of(first)]);
+    if (SPLIT) wave_fence();
   }
   for (int kt = first; kt < nt; kt += step) {
     const int buf = buf_of(kt);
@@ -452,7 +455,9 @@ __device__ __forceinline__ void dq_f32(const PackedArgs& a, int block, float* sm
       s[r] = hidden ? 0.f : p_f32(s[r], st.x) * (dp[r] - st.y);
     }
     W::add(dq, sk[buf], s, l16, g4);
+    if (SPLIT) wave_fence();
     if (kt + step < nt) w.stage(sk[buf_of(kt + step)], sv[buf_of(kt + step)]);
+    if (SPLIT) wave_fence();
   }
   if (SPLIT) {
     join_waves<D>(sk[0], dq, wave, l16, g4);
@@ -515,6 +520,7 @@ __device__ __forceinline__ void dkdv_f32(const PackedArgs& a, int block, float* 
   if (begin < end) {
     fetch(begin);
     w.stage(sq[buf_of(begin)], sd[buf_of(begin)]);
+    if (SPLIT) wave_fence();
   }
   for (int i = begin; i < end; i += step) {
     const int buf = buf_of(i), t = t0 + i % per;
@@ -532,7 +538,9 @@ __device__ __forceinline__ void dkdv_f32(const PackedArgs& a, int block, float* 
     }
     W::add(dv, sd[buf], s, l16, g4);
     W::add(dk, sq[buf], dp, l16, g4);
+    if (SPLIT) wave_fence();
     if (i + step < end) w.stage(sq[buf_of(i + step)], sd[buf_of(i + step)]);
+    if (SPLIT) wave_fence();
   }
   if (SPLIT) {
     join_waves<D>(sq[0], dk, wave, l16, g4);
