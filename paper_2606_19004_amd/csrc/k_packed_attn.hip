@@ -33,7 +33,7 @@ __device__ __forceinline__ bool sees_keys(const PackedArgs& a, const PackedSeq& 
 struct PackedTile {
   PackedSeq s;
   int g, rt, part, parts;
-  int64_t slot;   // of its partial result
+  int seq, local;   // which sequence's, and which of its (row tile, part)
   bool any;
 };
 __device__ __forceinline__ int parts_of(const PackedArgs& a, const PackedSeq& s) {
@@ -47,16 +47,28 @@ __device__ __forceinline__ PackedTile packed_tile(const PackedArgs& a) {
   PackedTile t{};
   const int u = blockIdx.x / a.Hkv;
   t.g = blockIdx.x - u * a.Hkv;
-  t.slot = (int64_t)t.g * a.units + u;
-  int local, seq;
   t.any = find_unit(a.nseq, u, [&](int i) { return a.sequence(i); },
-                    [&](const PackedSeq& s) { return row_tiles_of<ROWS>(a, s) * parts_of(a, s); }, seq, local, t.s);
+                    [&](const PackedSeq& s) { return row_tiles_of<ROWS>(a, s) * parts_of(a, s); }, t.seq, t.local, t.s);
   if (!t.any) return t;
   t.parts = parts_of(a, t.s);
-  t.rt = local / t.parts;
-  t.part = local - t.rt * t.parts;
+  t.rt = t.local / t.parts;
+  t.part = t.local - t.rt * t.parts;
   if (a.causal) t.rt = row_tiles_of<ROWS>(a, t.s) - 1 - t.rt;   // the rows that see most keys first
   return t;
+}
+
+// Where partial results are kept: those of one head lie together, in the order of the sequences that have any. -1: there is no place for
+// `count` of them from the sequence's local-th on (offsets that are not increasing). All lanes of a wave call it.
+template <int ROWS> __device__ __forceinline__ int64_t partial_slot(const PackedArgs& a, int g, int seq, int local, int count) {
+  unsigned before = 0;   // (offsets that are not increasing may wrap it: a place all the same)
+  for (int base = 0; base < seq; base += 64) {
+    const int i = base + (threadIdx.x & 63);
+    const PackedSeq s = a.sequence(min(i, seq));
+    const int parts = parts_of(a, s);
+    before += i < seq && parts > 1 ? row_tiles_of<ROWS>(a, s) * parts : 0;
+  }
+  const int64_t first = (int64_t)(unsigned)__builtin_amdgcn_readlane(seq ? wave_scan(before) : 0, 63) + local;
+  return first + count > a.slots ? -1 : (int64_t)g * a.slots + first;
 }
 
 template <int D, bool PARTS>
@@ -249,7 +261,8 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
   const float l_all = pair_sum(l_run);
   const bool real = row0 + wave * 32 + l32 < rows;
   if (PARTS && t.parts > 1) {
-    const int64_t slot = t.slot * ROWS + wave * 32 + l32;
+    const int64_t place = partial_slot<ROWS>(a, t.g, t.seq, t.local, 1), slot = place * ROWS + wave * 32 + l32;
+    if (place < 0) return;
     // the maximum in units of the scores, and what its rounding changes
     const float m = m_run == M_FLOOR ? M_FLOOR : m_run / c_row;
     const float f = m_run == M_FLOOR ? 1.f : __builtin_amdgcn_exp2f(fmaf(-m, c_row, m_run));
@@ -527,12 +540,15 @@ __global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
 #pragma unroll
   for (int i = 0; i < NKC; i++) o[i] *= mine;
   join_waves<D>(sk[0], o, wave, l16, g4);
-  if (wave > 0 || row0 + l16 >= rows) return;
+  if (wave > 0) return;
+  const bool partial = a.part_tiles && t.parts > 1;
+  const int64_t place = partial ? partial_slot<ROWS>(a, t.g, t.seq, t.local, 1) : 0;
+  if (row0 + l16 >= rows || place < 0) return;
   const bool sees = vis > 0;
   float inv = sees ? 1.0f / l : 0.f;
   float* orow = (float*)a.o + (q0 + tok) * a.o_row + (int64_t)head * a.o_head;
-  if (a.part_tiles && t.parts > 1) {
-    const int64_t slot = t.slot * ROWS + l16;
+  if (partial) {
+    const int64_t slot = place * ROWS + l16;
     orow = a.part_o + slot * D;
     inv = 1.f;
     if (g4 == 0) a.part_ml[slot] = make_float2(m, l);
@@ -695,7 +711,9 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
   __syncthreads();
   constexpr int EPT = 8, LPR = D / EPT;   // elements of a row per thread, threads per row
   const int r = tid / LPR, e0 = (tid % LPR) * EPT, rr = row0 + r;
-  if (r >= ROWS || rr >= rows) return;
+  const bool partial = a.part_tiles && t.parts > 1;
+  const int64_t place = partial ? partial_slot<ROWS>(a, t.g, t.seq, t.local, 1) : 0;
+  if (r >= ROWS || rr >= rows || place < 0) return;
   float m = M_FLOOR, l = 0.f, acc[EPT];
 #pragma unroll
   for (int w = 0; w < NW; w++) m = fmaxf(m, ml[w * ROWS + r].x);
@@ -713,8 +731,8 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
       for (int j = 0; j < 4; j++) acc[e + j] = fmaf(f, y[j], acc[e + j]);
     }
   }
-  if (a.part_tiles && t.parts > 1) {
-    const int64_t slot = t.slot * ROWS + r;
+  if (partial) {
+    const int64_t slot = place * ROWS + r;
     if (e0 == 0) a.part_ml[slot] = make_float2(m, l);
 #pragma unroll
     for (int e = 0; e < EPT; e += 4) store4<float>(a.part_o + slot * D + e0 + e, acc + e);
@@ -747,17 +765,10 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
   const int parts = parts_of(a, sq);
   const int rows = sq.m * a.G, q0 = sq.q0, row = rt * ROWS + 4 * quad + wave;
   if (parts <= 1 || row >= rows) return;
-  // units before this sequence's
-  int64_t before = 0;
-  for (int i = lane; i < seq; i += 64) {
-    const PackedSeq s = a.sequence(i);
-    before += (int64_t)row_tiles_of<ROWS>(a, s) * parts_of(a, s);
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, 64);
   const int place = a.causal ? cdiv(rows, ROWS) - 1 - rt : rt;   // where the tile stands in the order of the units
-  if (before + (int64_t)(place + 1) * parts > a.units) return;   // (offsets that are not increasing: no such units ran)
-  const int64_t slot = ((int64_t)g * a.units + before + place * parts) * ROWS + 4 * quad + wave;   // of part 0; parts are ROWS apart
+  const int64_t first = partial_slot<ROWS>(a, g, seq, place * parts, parts);
+  if (first < 0) return;
+  const int64_t slot = first * ROWS + 4 * quad + wave;   // of part 0; parts are ROWS apart
   const float2* ml = a.part_ml + slot;
   const float* po = a.part_o + slot * d;
   const int tok = row / a.G, head = g * a.G + row - tok * a.G;
@@ -834,7 +845,9 @@ PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, 
   if (cdiv(max_k, 64) <= std::max<int64_t>(whole, per) || (!few && units * Hkv > 16 * CUS)) return p;
   p.part_tiles = (int)per;
   p.units = (int)units;
-  p.ws = (size_t)Hkv * units * p.rows * (d + 2) * 4;
+  // sequences of more than one part have more than 64 per keys, n keys in fewer than n / (64 per) + 1 parts: fewer than 2 n / (64 per)
+  p.slots = (int)std::min(units, per_seq * (total_k / (32 * per)));
+  p.ws = (size_t)Hkv * p.slots * p.rows * (d + 2) * 4;
   return p;
 }
 
@@ -860,9 +873,9 @@ hipError_t packed_attention_fwd(PackedArgs a, int dtype, int d, void* ws, hipStr
   const PackedPlan p = plan_of(a, dtype, d);
   if (p.row_tiles == 0) return hipSuccess;
   a.part_tiles = p.part_tiles;
-  a.units = p.units;
+  a.slots = p.slots;
   a.part_o = (float*)ws;
-  a.part_ml = (float2*)(a.part_o + (int64_t)a.Hkv * p.units * p.rows * d);
+  a.part_ml = (float2*)(a.part_o + (int64_t)a.Hkv * p.slots * p.rows * d);
   const int64_t grid = (int64_t)p.units * a.Hkv;
   if (d == 128) fwd_launch<128>(a, dtype, p.rows, grid, s);
   else fwd_launch<64>(a, dtype, p.rows, grid, s);

@@ -34,8 +34,8 @@ struct PackedArgs {
   float scale;
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
   // long keys shared out in parts of part_tiles 64-key tiles (0: one part), whose results meet in the workspace
-  int part_tiles, units;            // units: upper bound on (sequence, row tile, part) per key/value head
-  float* part_o; float2* part_ml;   // [Hkv * units][row tile][d] sums of p v, [Hkv * units][row tile] running maximum and sum of p
+  int part_tiles, slots;            // slots: upper bound on (sequence, row tile, part) of the sequences with more than one part, per key/value head
+  float* part_o; float2* part_ml;   // [Hkv * slots][row tile][d] sums of p v, [Hkv * slots][row tile] running maximum and sum of p
   // backward
   const void* d_o; void* dq; void* dk; void* dv;
   float2* stats;                    // [H][total_q] (lse, for bf16 in log2 units, rowsum(d_o o))
@@ -110,7 +110,7 @@ __device__ __forceinline__ bool find_unit(int nseq, int u, L&& load, C&& count, 
 struct PackedPlan {
   int rows;         // query rows of a workgroup's tile
   int part_tiles;   // 64-key tiles of a part, 0: keys are not shared out
-  int row_tiles, units;
+  int row_tiles, units, slots;   // upper bounds per key/value head: row tiles, (row tile, part), those of sequences with more than one part
   size_t ws;        // bytes
 };
 PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q, int max_k);

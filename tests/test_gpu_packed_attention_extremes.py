@@ -210,3 +210,17 @@ def test_gradients_of_large_scores(d, dtype, kw):
             "dv": rows * 2.0 ** -126 * np.nanmax(np.abs(p.do))}
     for n, g in zip(("dq", "dk", "dv"), grads):
         check(host64(g.contiguous()), ref[n], ref[n + "_tol"] + tiny[n], n)
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("count", [60, 130, 600])
+def test_few_long_caches_among_many_short_ones(d, count, dtype, hd):
+    """The partial results of the long ones lie together, whatever is before and between them; new tokens of none, one and two."""
+    rng = np.random.default_rng(count)
+    keys = rng.integers(0, 90, count)
+    keys[[0, 3, count // 2, count - 3, count - 2]] = [4000, 5100, 2500, 8111, 3000]
+    new = rng.integers(0, 3, count)
+    new[[0, 3, count // 2, count - 3, count - 2]] = [1, 0, 2, 1, 2]
+    p = Problem(d, dtype, hd, 8, 2, new, keys, True, slack=1, lead=2, tail=1, seed=count)
+    assert d.packed_attention_workspace_bytes(p.cfg) > 0
+    p.check_forward()

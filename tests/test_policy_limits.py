@@ -42,3 +42,12 @@ def test_gated_norm_of_more_workgroups_than_a_launch_takes():
 
 def test_policy_loss_of_more_samples_than_a_launch_takes():
     assert loss(B=1 << 24, n=4, nb=1 << 40) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("sequences", [1000, 20000])
+def test_workspace_is_for_sequences_that_are_shared_out(sequences):
+    """One new token of each of many sequences of 64 keys. Partial results have room for the sequences whose keys could be in more
+    than one part, not for all: with 512 workgroups' worth of parts, twice as many slots of 16 rows of 130 floats, and 2 x 8 more."""
+    cfg = packed(sequences=sequences, heads=32, kv_heads=8, head_dim=128, total_q=sequences, total_k=64 * sequences, max_q=1, q_row=4096, q_head=128,
+                 k_row=1024, k_head=128, v_row=1024, v_head=128, o_row=4096, o_head=128)
+    assert 0 < d.packed_attention_workspace_bytes(cfg) <= (2 * 512 + 16) * 16 * 130 * 4 + 256
