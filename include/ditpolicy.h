@@ -81,7 +81,7 @@ dit_status packed_attention(const dit_packed_config* cfg, const void* q, const v
  * call's. dq, dk and dv are laid out like q, k and v (whose (row, head) pieces must not overlap here). With p as
  * above, dv = p^T d_o, ds = p (d_o v^T - rowsum(d_o o)) scale, dq = ds k, dk = ds^T q; heads that share keys
  * add up. Key rows past k_lengths are left as they were; keys that no query sees get zeros. p comes from lse, of which fp32 holds
- * 2^-24 of its size: where |lse| is past 2^16 that is more than the rounding of bf16. As forward, a NaN or infinity in a
+ * 2^-24 of its size: where |lse| is past 2^16 that is more than the rounding of bf16, and past 2^28 p may be any number. As forward, a NaN or infinity in a
  * row of a sequence may reach the gradients of rows that the causal mask sets apart from it. */
 dit_status packed_attention_backward(const dit_packed_config* cfg, const void* q, const void* k, const void* v,
                                      const void* o, const float* lse, const void* d_o,

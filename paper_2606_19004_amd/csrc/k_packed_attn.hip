@@ -9,8 +9,9 @@
 // bf16: flash-style with v_mfma_f32_32x32x16_bf16, 4 waves of 32 rows, 64-key tiles of K and V in two LDS buffers
 // each. Scores are computed transposed (S^T = K Q^T), so that a lane owns one row and its probabilities are
 // operand B of O^T = V^T P^T as they stand; the exponentials of tile t share one instruction stream with the score
-// MFMAs of tile t + 1. Probabilities are rounded to bf16 for the second product (half a step, 2^-9 relative, of each:
-// averaged over the keys it is below the rounding of o itself); sums and maxima stay fp32.
+// MFMAs of tile t + 1. Probabilities are rounded to bf16 for the second product, by up to 2^-8 of each, because that is what the
+// matrix instruction takes at its full rate; sums and maxima stay fp32. o averages over the keys and its error with it, so the error is
+// of the size of o's own rounding: in the 2-norm o is off by 0.0019 to 0.0024 of itself, by 0.0016 to 0.0017 were only o rounded.
 // Bound by the matrix instructions and the exponentials between them (8 samples of 1101 to 2560 tokens, 24 heads of 128, no mask:
 // 372 to 403 us from card to card, 910 to 980 TFLOP/s, where a large library product runs at 1160 to 1230); few rows, below, by reading the keys once.
 #include <algorithm>
@@ -824,7 +825,8 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
 //          18 in parts of 4, 14 in parts of 2; sequences that fill the chip as above). Other tiles: only where they alone leave CUs without a workgroup, and
 //          128 rows only where a part is WORTH tiles shorter than the average sequence: their results are about 67 MB to write and
 //          read however the keys are cut (us whole / shared out: 1024 keys of 16 over 4 heads 23 / 38, 2048 of 8 over 1 38 / 40, of
-//          4 over 4 37 / 32, 4096 of 4 over 1 68 / 51, 8192 of 2 over 1 129 / 72).
+//          4 over 4 37 / 32, 4096 of 4 over 1 68 / 51, 8192 of 2 over 1 129 / 72). The host knows the average length alone, so a long
+//          sequence beside short ones stays whole where it would gain (4096 and 200 keys of 4 over 1: 70 / 56).
 PackedPlan packed_plan(int dtype, int nseq, int H, int Hkv, int d, int total_q, int total_k, int max_q, int max_k) {
   constexpr int CUS = 256, FEW_ROWS = 32, MIN_PART = 4, WHOLE = 12, WORTH = 26;
   PackedPlan p{};

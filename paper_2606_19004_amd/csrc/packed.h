@@ -65,8 +65,8 @@ __device__ __forceinline__ unsigned wave_scan(unsigned v) {
 // The sequence that unit u belongs to, where a sequence with what = load(i) (a struct of int) has count(what) units, and u's place
 // in it. Every wave finds it by itself, 64 sequences at a time: no host-made list of tiles, no empty workgroups where
 // lengths are unlike. What is known of the sequence comes from the lane that looked at it, with no further loads.
-// BLOCKS: how many times 64 sequences are loaded together (1000 sequences of 64 keys, 8 heads, one new token each: 191 us; one block at a
-// time, with a sum by LDS permutes, 239).
+// BLOCKS: how many times 64 sequences are loaded together (1000 sequences of 64 keys, 8 key/value heads of 128, one new token each: 191 to
+// 203 us from card to card; one block at a time, with a sum by LDS permutes, 239. Reading the keys and values once takes 53.)
 template <int BLOCKS, typename S, typename L, typename C>
 __device__ __forceinline__ bool find_unit_in(int nseq, int u, L&& load, C&& count, int& seq, int& local, S& what) {
   const int lane = threadIdx.x & 63;
