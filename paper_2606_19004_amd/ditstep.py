@@ -318,41 +318,35 @@ def dit_denoise_step_teacache(cfg, sw, blocks, t, t_next, noise_level, latent, x
 # policy update (include/ditpolicy.h)
 # ---------------------------------------------------------------------------
 NORM_KINDS = {"none": 0, "layer": 1, "rms": 2}
-
-
-def _elsewhere(t, dev):
-    raise ValueError(f"a tensor on {t.device} in a call on cuda:{dev}")
-
-
 _ROW_TYPES = {DIT_BF16: torch.bfloat16, DIT_F32: torch.float32}
 
 
-def _at(t, dev, dtype, shape, strides):
-    """The device pointer of a tensor (or None) that has to be on the current device, whose stream runs the call, and of this type,
-    shape and strides."""
+def _at(t, layout):
+    """The device pointer of a tensor (or None) whose (type, shape, strides, device) has to be `layout`: the device is the current one, whose
+    stream runs the call."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.shape != shape or t.stride() != strides:
-        _check_layout(t, dtype, shape, strides)
-    return t.data_ptr() if t.get_device() == dev else _elsewhere(t, dev)
+    if (t.dtype, t.shape, t.stride(), t.get_device()) != layout:
+        _check_layout(t, *layout)
+    return t.data_ptr()
 
 
 def _dense(t, dev, dtype, n):
     """The same of n elements without gaps (or more)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
-        _check_layout(t, dtype, (n,), (1,))
-    return t.data_ptr() if t.get_device() == dev else _elsewhere(t, dev)
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous() or t.get_device() != dev:
+        _check_layout(t, dtype, (n,), (1,), dev)
+    return t.data_ptr()
 
 
-def _check_layout(t, dtype, shape, strides):
+def _check_layout(t, dtype, shape, strides, dev):
     """What else may be read and written as `shape` at `strides`: more rows, any stride of an index that has one value, and, where the
     elements lie without gaps, as many of them in any contiguous shape."""
-    if dtype is None:   # (a config of an unknown type, which the library refuses)
-        return
-    if t.dtype is not dtype:
+    if dtype is not None and t.dtype is not dtype:   # (None: a config of an unknown type, which the library refuses)
         raise ValueError(f"a tensor of {t.dtype} where {dtype} is wanted")
+    if t.get_device() != dev:
+        raise ValueError(f"a tensor on {t.device} in a call on cuda:{dev}")
     if 0 in shape:
         return
     dense = [math.prod(shape[i + 1:]) for i in range(len(shape))]
@@ -365,7 +359,11 @@ def _check_layout(t, dtype, shape, strides):
 
 
 def _ws_args(ws, dev):
-    return (None, 0) if ws is None else (ws.data_ptr() if ws.get_device() == dev else _elsewhere(ws, dev), ws.numel())
+    if ws is None:
+        return None, 0
+    if ws.get_device() != dev:
+        _check_layout(ws, ws.dtype, (), (), dev)
+    return ws.data_ptr(), ws.numel()
 
 
 def packed_config(q, k, v, o, sequences, causal=False, scale=None, max_q=0) -> PackedConfig:
@@ -386,12 +384,12 @@ def packed_config(q, k, v, o, sequences, causal=False, scale=None, max_q=0) -> P
                         _dtype_code(q.dtype), scale, *strides)
 
 
-def _attention_layouts(cfg):
-    """(type, shape, strides) of q, k, v, o and their gradients"""
+def _attention_layouts(cfg, dev):
+    """Of q, k, v, o and their gradients."""
     dt, d = _ROW_TYPES.get(cfg.dtype), cfg.head_dim
     q, k = (cfg.total_q, cfg.heads, d), (cfg.total_k, cfg.kv_heads, d)
-    return (dt, q, (cfg.q_row, cfg.q_head, 1)), (dt, k, (cfg.k_row, cfg.k_head, 1)), (dt, k, (cfg.v_row, cfg.v_head, 1)), (
-        dt, q, (cfg.o_row, cfg.o_head, 1))
+    return (dt, q, (cfg.q_row, cfg.q_head, 1), dev), (dt, k, (cfg.k_row, cfg.k_head, 1), dev), (dt, k, (cfg.v_row, cfg.v_head, 1), dev), (
+        dt, q, (cfg.o_row, cfg.o_head, 1), dev)
 
 
 def packed_attention_workspace_bytes(cfg) -> int:
@@ -402,9 +400,9 @@ def packed_attention(cfg, q, k, v, o, lse=None, q_offsets=None, k_offsets=None, 
     """Tensors laid out as those cfg was made from; lse: fp32 [rows][heads]; offsets (one more than sequences) and lengths: device
     int32, or None (equal lengths)."""
     dev, s, i32 = _current_device(), cfg.sequences, torch.int32
-    lq, lk, lv, lo = _attention_layouts(cfg)
+    lq, lk, lv, lo = _attention_layouts(cfg, dev)
     qo, ko, kl = _dense(q_offsets, dev, i32, s + 1), _dense(k_offsets, dev, i32, s + 1), _dense(k_lengths, dev, i32, s)
-    _check(_lib.packed_attention(C.byref(cfg), _at(q, dev, *lq), _at(k, dev, *lk), _at(v, dev, *lv), qo, ko, kl, _at(o, dev, *lo),
+    _check(_lib.packed_attention(C.byref(cfg), _at(q, lq), _at(k, lk), _at(v, lv), qo, ko, kl, _at(o, lo),
                                  _dense(lse, dev, torch.float32, cfg.total_q * cfg.heads), *_ws_args(ws, dev), _s(stream)))
 
 
@@ -416,12 +414,12 @@ def packed_attention_backward(cfg, q, k, v, o, lse, d_o, dq, dk, dv, q_offsets=N
                               ws=None, stream=None):
     """d_o laid out like o, dq, dk, dv like q, k, v."""
     dev, s, i32 = _current_device(), cfg.sequences, torch.int32
-    lq, lk, lv, lo = _attention_layouts(cfg)
+    lq, lk, lv, lo = _attention_layouts(cfg, dev)
     qo, ko, kl = _dense(q_offsets, dev, i32, s + 1), _dense(k_offsets, dev, i32, s + 1), _dense(k_lengths, dev, i32, s)
     _check(_lib.packed_attention_backward(
-        C.byref(cfg), _at(q, dev, *lq), _at(k, dev, *lk), _at(v, dev, *lv), _at(o, dev, *lo),
-        _dense(lse, dev, torch.float32, cfg.total_q * cfg.heads), _at(d_o, dev, *lo), qo, ko, kl, _at(dq, dev, *lq), _at(dk, dev, *lk),
-        _at(dv, dev, *lv), *_ws_args(ws, dev), _s(stream)))
+        C.byref(cfg), _at(q, lq), _at(k, lk), _at(v, lv), _at(o, lo),
+        _dense(lse, dev, torch.float32, cfg.total_q * cfg.heads), _at(d_o, lo), qo, ko, kl, _at(dq, lq), _at(dk, lk),
+        _at(dv, lv), *_ws_args(ws, dev), _s(stream)))
 
 
 def gated_norm_config(x, sequences, post="none", pre="layer", eps=1e-6, residual_scale=1.0, y_row=None, h_row=None,
@@ -441,12 +439,11 @@ def gated_norm(cfg, x, y, x_out, h, gate=None, scale=None, shift=None, post_w=No
     """x, x_out, y, h: cfg's type, at its x_row, y_row, h_row; post_w, pre_w: [hidden], cfg's type; gate, scale, shift: fp32
     [sequences][hidden] at its mod_row; offsets: device int32 (one more than sequences), or None (equal lengths)."""
     dev, dt, f32, hidden, s = _current_device(), _ROW_TYPES.get(cfg.dtype), torch.float32, cfg.hidden, cfg.sequences
-    rows, xs, mods, ms = (cfg.rows, hidden), (cfg.x_row, 1), (s, hidden), (cfg.mod_row, 1)
-    off, g, sc, sh = _dense(offsets, dev, torch.int32, s + 1), _at(gate, dev, f32, mods, ms), _at(scale, dev, f32, mods, ms), _at(
-        shift, dev, f32, mods, ms)
-    _check(_lib.gated_norm(C.byref(cfg), _at(x, dev, dt, rows, xs), _at(y, dev, dt, rows, (cfg.y_row, 1)), _dense(post_w, dev, dt, hidden),
-                           _dense(pre_w, dev, dt, hidden), g, sc, sh, off, _at(x_out, dev, dt, rows, xs),
-                           _at(h, dev, dt, rows, (cfg.h_row, 1)), _s(stream)))
+    rows = (cfg.rows, hidden)
+    lx, lm = (dt, rows, (cfg.x_row, 1), dev), (f32, (s, hidden), (cfg.mod_row, 1), dev)
+    off, g, sc, sh = _dense(offsets, dev, torch.int32, s + 1), _at(gate, lm), _at(scale, lm), _at(shift, lm)
+    _check(_lib.gated_norm(C.byref(cfg), _at(x, lx), _at(y, (dt, rows, (cfg.y_row, 1), dev)), _dense(post_w, dev, dt, hidden),
+                           _dense(pre_w, dev, dt, hidden), g, sc, sh, off, _at(x_out, lx), _at(h, (dt, rows, (cfg.h_row, 1), dev)), _s(stream)))
 
 
 def gated_norm_backward_workspace_bytes(cfg) -> int:
@@ -457,13 +454,14 @@ def gated_norm_backward(cfg, x_out, y, dx_out, dh, dx, dy, gate=None, scale=None
                         dgate=None, dscale=None, dshift=None, dpost_w=None, dpre_w=None, ws=None, stream=None):
     """x_out: the forward call's output. Any gradient may be None; those of vectors and weights are fp32."""
     dev, dt, f32, hidden, s = _current_device(), _ROW_TYPES.get(cfg.dtype), torch.float32, cfg.hidden, cfg.sequences
-    lx, ly = (dt, (cfg.rows, hidden), (cfg.x_row, 1)), (dt, (cfg.rows, hidden), (cfg.y_row, 1))
-    lh, lm = (dt, (cfg.rows, hidden), (cfg.h_row, 1)), (f32, (s, hidden), (cfg.mod_row, 1))
-    off, g, sc = _dense(offsets, dev, torch.int32, s + 1), _at(gate, dev, *lm), _at(scale, dev, *lm)
+    rows = (cfg.rows, hidden)
+    lx, ly, lh = (dt, rows, (cfg.x_row, 1), dev), (dt, rows, (cfg.y_row, 1), dev), (dt, rows, (cfg.h_row, 1), dev)
+    lm = (f32, (s, hidden), (cfg.mod_row, 1), dev)
+    off, g, sc = _dense(offsets, dev, torch.int32, s + 1), _at(gate, lm), _at(scale, lm)
     _check(_lib.gated_norm_backward(
-        C.byref(cfg), _at(x_out, dev, *lx), _at(y, dev, *ly), _dense(post_w, dev, dt, hidden), _dense(pre_w, dev, dt, hidden), g, sc, off,
-        _at(dx_out, dev, *lx), _at(dh, dev, *lh), _at(dx, dev, *lx), _at(dy, dev, *ly), _at(dgate, dev, *lm), _at(dscale, dev, *lm),
-        _at(dshift, dev, *lm), _dense(dpost_w, dev, f32, hidden), _dense(dpre_w, dev, f32, hidden), *_ws_args(ws, dev), _s(stream)))
+        C.byref(cfg), _at(x_out, lx), _at(y, ly), _dense(post_w, dev, dt, hidden), _dense(pre_w, dev, dt, hidden), g, sc, off,
+        _at(dx_out, lx), _at(dh, lh), _at(dx, lx), _at(dy, ly), _at(dgate, lm), _at(dscale, lm),
+        _at(dshift, lm), _dense(dpost_w, dev, f32, hidden), _dense(dpre_w, dev, f32, hidden), *_ws_args(ws, dev), _s(stream)))
 
 
 def flow_policy_loss_workspace_bytes(batch, n_per_sample) -> int:
