@@ -69,7 +69,7 @@ size_t packed_attention_backward_workspace_bytes(const dit_packed_config* cfg);
  *              (a cache with room to grow); clamped to those rows
  *   lse        device [total_q][heads] fp32, or NULL
  * Keys outside the sequence are never read. A NaN or infinity in a key or value that the causal mask hides
- * from a query, but not from a later query of the same sequence, may still reach that query.
+ * from a query, but not from a later query of the same sequence, may still reach that query, if it sees any key.
  * Pointers and strides must keep 16-byte alignment of every (row, head); row strides are at least head_dim,
  * and o's (row, head) pieces must not overlap. DIT_ERR_UNSUPPORTED for a row stride of 2^24 elements or more
  * or a head stride of 2^40. */
@@ -82,7 +82,7 @@ dit_status packed_attention(const dit_packed_config* cfg, const void* q, const v
  * above, dv = p^T d_o, ds = p (d_o v^T - rowsum(d_o o)) scale, dq = ds k, dk = ds^T q; heads that share keys
  * add up. Key rows past k_lengths are left as they were; keys that no query sees get zeros. p comes from lse, of which fp32 holds
  * 2^-24 of its size: where |lse| is past 2^16 that is more than the rounding of bf16, and past 2^28 p may be any number. As forward, a NaN or infinity in a
- * row of a sequence may reach the gradients of rows that the causal mask sets apart from it. */
+ * row of a sequence may reach the gradients of rows that the causal mask sets apart from it, but dq of a query that sees no key is 0. */
 dit_status packed_attention_backward(const dit_packed_config* cfg, const void* q, const void* k, const void* v,
                                      const void* o, const float* lse, const void* d_o,
                                      const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths,

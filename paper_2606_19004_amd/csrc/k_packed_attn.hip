@@ -279,6 +279,11 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_bf16(PackedArgs a) {
     return;
   }
   const bool sees = vis > 0;
+  if (__ballot(!sees) != 0) {   // nothing of a value that is no number (0 times it is none either)
+#pragma unroll
+    for (int i = 0; i < NDB; i++)
+      if (!sees) o[i] = zero;
+  }
   const float inv = sees ? 1.0f / l_all : 0.f, log2_l = __builtin_amdgcn_logf(l_all);
   const float lse = !sees ? -INFINITY : c_row == c ? (m_run + log2_l) * LN2 : m_run * __builtin_amdgcn_rcpf(c_row) * a.scale;
   if (a.lse && real && half == 0) a.lse[(int64_t)(q0 + tok) * a.H + head] = lse;
@@ -444,6 +449,9 @@ __global__ void __launch_bounds__(256, 2) packed_fwd_f32(PackedArgs a) {
   if (row0 + wave * 16 + l16 >= rows) return;
   const bool sees = vis > 0;
   const float inv = sees ? 1.0f / l_run : 0.f;
+  if (!sees)   // nothing of a value that is no number
+#pragma unroll
+    for (int i = 0; i < NDB; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float lse = sees ? m_run + __builtin_amdgcn_logf(l_run) * LN2 : -INFINITY;
   float* orow = (float*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head;
   float* olse = a.lse ? a.lse + (int64_t)(q0 + tok) * a.H + head : nullptr;
@@ -547,6 +555,9 @@ __global__ void __launch_bounds__(256) packed_split_f32(PackedArgs a) {
   if (row0 + l16 >= rows || place < 0) return;
   const bool sees = vis > 0;
   float inv = sees ? 1.0f / l : 0.f;
+  if (!sees)   // nothing of a value that is no number
+#pragma unroll
+    for (int i = 0; i < NKC; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float* orow = (float*)a.o + (q0 + tok) * a.o_row + (int64_t)head * a.o_head;
   if (partial) {
     const int64_t slot = place * ROWS + l16;
@@ -744,7 +755,7 @@ __global__ void __launch_bounds__(256, 2) packed_few_bf16(PackedArgs a) {
   const float inv = sees ? 1.0f / l : 0.f;
   const float lse = sees ? fmaf(m, a.scale, __builtin_amdgcn_logf(l) * LN2) : -INFINITY;
 #pragma unroll
-  for (int e = 0; e < EPT; e++) acc[e] *= inv;
+  for (int e = 0; e < EPT; e++) acc[e] = sees ? acc[e] * inv : 0.f;   // (nothing of a value that is no number)
   if (a.lse && e0 == 0) a.lse[(int64_t)(q0 + tk) * a.H + hd] = lse;
 #pragma unroll
   for (int e = 0; e < EPT; e += 4) store4<u16>((u16*)a.o + (int64_t)(q0 + tk) * a.o_row + (int64_t)hd * a.o_head + e0 + e, acc + e);
@@ -808,8 +819,8 @@ __global__ void __launch_bounds__(256) packed_join(PackedArgs a, int d) {
   const bool sees = sees_keys(a, sq, tok);
   const float inv = sees ? 1.f / total : 0.f;
   T* orow = (T*)a.o + (int64_t)(q0 + tok) * a.o_row + (int64_t)head * a.o_head + e;
-  orow[0] = from_f32<T>(acc0 * inv);
-  if (d > 64) orow[1] = from_f32<T>(acc1 * inv);
+  orow[0] = from_f32<T>(sees ? acc0 * inv : 0.f);   // (nothing of a value that is no number)
+  if (d > 64) orow[1] = from_f32<T>(sees ? acc1 * inv : 0.f);
   if (a.lse && lane == 0)
     a.lse[(int64_t)(q0 + tok) * a.H + head] = sees ? fmaf(top, scale, __builtin_amdgcn_logf(total) * LN2) : -INFINITY;
 }

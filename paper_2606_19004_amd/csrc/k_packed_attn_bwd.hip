@@ -206,6 +206,11 @@ __device__ __forceinline__ void dq_bf16(const PackedArgs& a, int block, char* sm
         }
     }
   }
+  if (__ballot(vis <= 0) != 0) {   // rows that see no key: nothing of one that is no number
+#pragma unroll
+    for (int i = 0; i < NDB; i++)
+      if (vis <= 0) dq[i] = zero;
+  }
   __syncthreads();   // every wave is done with the K buffers
   store_columns<D>(smem + wave * 32 * RB, dq, a.scale, lane, [&](int r, int ch, uint4 v) {
     const int rr = row0 + wave * 32 + r;
@@ -465,6 +470,9 @@ __device__ __forceinline__ void dq_f32(const PackedArgs& a, int block, float* sm
     if (wave > 0) return;
   }
   if (mine >= rows) return;
+  if (vis <= 0)   // a row that sees no key: nothing of one that is no number
+#pragma unroll
+    for (int i = 0; i < NKC; i++) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float* out = (float*)a.dq + (q0 + tok) * a.q_row + (int64_t)head * a.q_head;
 #pragma unroll
   for (int i = 0; i < NKC; i++)

@@ -224,3 +224,17 @@ def test_few_long_caches_among_many_short_ones(d, count, dtype, hd):
     p = Problem(d, dtype, hd, 8, 2, new, keys, True, slack=1, lead=2, tail=1, seed=count)
     assert d.packed_attention_workspace_bytes(p.cfg) > 0
     p.check_forward()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("H,G,m,n", [(2, 1, 8, 5), (2, 1, 120, 70), (2, 1, 3050, 3000), (16, 16, 2112, 40)])
+def test_rows_that_see_no_key_are_empty_whatever_the_keys_hold(d, H, G, m, n, dtype, hd, bad):
+    """The first m - n of m causal queries: o = 0, lse = -inf and dq = 0, beside queries that see keys and values of no number."""
+    p = Problem(d, dtype, hd, H, G, [m], [n], True, layout="plain", seed=m)
+    p.tk[0], p.tv[0] = bad, bad
+    o, lse = p.forward()
+    assert np.all(o[:m - n] == 0.0) and np.all(np.isneginf(lse[:m - n]))
+    assert np.isnan(o[m - n:]).all()
+    dq = p.backward()[0]
+    assert bool((dq[:m - n] == 0.0).all())
