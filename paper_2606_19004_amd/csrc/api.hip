@@ -13,12 +13,16 @@
 #include <string>
 #include <vector>
 
+#include "../../include/ditint8.h"
 #include "../../include/ditpolicy.h"
 #include "../../include/ditstep.h"
+#include "../../include/ditupdate.h"
 #include "internal.h"
 #include "host_checks.h"
 #include "packed.h"
 #include "policy_checks.h"
+#include "update.h"
+#include "update_checks.h"
 
 using namespace dit;
 using dit::set_error;
@@ -1534,6 +1538,159 @@ dit_status flow_policy_loss(const float* x, const float* v, const float* x_next,
   TIMED("policy_loss_sums", 0, reads, hs(stream), policy_loss_sums(a, hs(stream)));
   TIMED("policy_loss_finish", 0, dv ? reads + 4.0 * batch * n : 0.0, hs(stream), policy_loss_finish(a, hs(stream)));
   return DIT_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// gradient norm, clipping, AdamW (ditupdate.h); linear layers in 8-bit integers (ditint8.h)
+// ---------------------------------------------------------------------------
+namespace {
+
+double gradient_bytes(const dit_gradient* g, int32_t n) {
+  double b = 0;
+  for (int32_t i = 0; i < n; i++) b += (double)g[i].count * esize(g[i].dtype);
+  return b;
+}
+
+// bytes of a row of in_features integers in the workspace: whole lines
+int64_t int8_row(const dit_int8_config* c) { return ((int64_t)c->in_features + 127) & ~(int64_t)127; }
+
+struct Int8Ws {
+  size_t scale, q, total;
+};
+Int8Ws int8_layout(const dit_int8_config* c) {
+  Int8Ws w;
+  w.scale = 0;
+  w.q = al256((size_t)c->rows * 4);
+  w.total = w.q + al256((size_t)c->rows * int8_row(c));
+  return w;
+}
+
+dit_status check_int8_call(const dit_int8_config* c, bool given, const void* x, const void* w, const void* w_scale, const void* bias,
+                           const void* y) {
+  if (!x || !w || !w_scale || !y) return set_error(DIT_ERR_INVALID_ARG, "x/w/w_scale/y NULL");
+  if (!aligned16(w) || (given && !aligned16(x))) return set_error(DIT_ERR_INVALID_ARG, "int8 rows must be 16-byte aligned");
+  dit_status st;
+  if ((st = check_offsets_aligned({w_scale}))) return st;
+  if ((st = check_elements({given ? nullptr : x, bias, y}, c->dtype))) return st;
+  return check_threads(int8_matmul_threads(c->rows, c->out_features));
+}
+
+dit_status run_int8_matmul(const dit_int8_config* c, const int8_t* x, int64_t x_row, const float* x_scale, const int8_t* w,
+                           const float* w_scale, const void* bias, void* y, hipStream_t s) {
+  Int8Args a{};
+  a.x = x;
+  a.x_scale = x_scale;
+  a.w = w;
+  a.w_scale = w_scale;
+  a.bias = bias;
+  a.y = y;
+  a.M = c->rows;
+  a.N = c->out_features;
+  a.K = c->in_features;
+  a.x_row = x_row;
+  a.w_row = c->w_row;
+  a.y_row = c->y_row;
+  const double M = a.M, N = a.N, K = a.K;
+  TIMED("int8_matmul", 2.0 * M * N * K, M * K + N * K + M * N * esize(c->dtype), s, int8_matmul_launch(a, c->dtype, c->act, s));
+  return DIT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t grad_norm_workspace_bytes(const dit_gradient* grads, int32_t n) {
+  int64_t total;
+  if (check_gradients(grads, n, false, &total)) return 0;
+  return al256((size_t)grad_norm_parts(grads, n, update_chunk(total)) * sizeof(double));
+}
+
+dit_status grad_norm(const dit_gradient* grads, int32_t n, double max_norm, double* norm, float* scale, void* ws, size_t ws_bytes,
+                     dit_stream stream) {
+  int64_t total;
+  dit_status st = check_gradients(grads, n, true, &total);
+  if (st) return st;
+  if (!(max_norm >= 0.0)) return set_error(DIT_ERR_DOMAIN, "max_norm %g (at least 0)", max_norm);
+  if (!norm && !scale) return set_error(DIT_ERR_INVALID_ARG, "no output wanted");
+  if (((uintptr_t)norm & 7) || ((uintptr_t)scale & 3)) return set_error(DIT_ERR_INVALID_ARG, "norm or scale not aligned to its type");
+  const int64_t chunk = update_chunk(total), parts = grad_norm_parts(grads, n, chunk);
+  if ((st = check_ws(ws, ws_bytes, al256((size_t)parts * sizeof(double))))) return st;
+  if (parts > 0)
+    TIMED("grad_norm", 0, gradient_bytes(grads, n), hs(stream), grad_norm_sums(grads, n, chunk, (double*)ws, hs(stream)));
+  TIMED("grad_norm_finish", 0, 8.0 * parts, hs(stream), grad_norm_finish((const double*)ws, parts, max_norm, norm, scale, hs(stream)));
+  return DIT_OK;
+}
+
+dit_status grad_clip(const dit_gradient* grads, int32_t n, const float* scale, dit_stream stream) {
+  int64_t total;
+  dit_status st = check_gradients(grads, n, true, &total);
+  if (st) return st;
+  if (!scale) return set_error(DIT_ERR_INVALID_ARG, "scale NULL");
+  if ((st = check_offsets_aligned({scale}))) return st;
+  if (total == 0) return DIT_OK;
+  TIMED("grad_clip", 0, 2.0 * gradient_bytes(grads, n), hs(stream), grad_clip_launch(grads, n, update_chunk(total), scale, hs(stream)));
+  return DIT_OK;
+}
+
+dit_status adamw_step(const dit_adamw_config* c, const dit_adamw_tensor* tensors, int32_t n, const float* scale,
+                      const int64_t* step_dev, dit_stream stream) {
+  int64_t total;
+  dit_status st = check_adamw(c, tensors, n, step_dev != nullptr, &total);
+  if (st) return st;
+  if ((st = check_offsets_aligned({scale}))) return st;
+  if ((uintptr_t)step_dev & 7) return set_error(DIT_ERR_INVALID_ARG, "step_dev not 8-byte aligned");
+  if (total == 0) return DIT_OK;
+  double bytes = 0;
+  for (int32_t i = 0; i < n; i++)
+    bytes += (double)tensors[i].count * (16 + 2 * esize(tensors[i].param_dtype) + esize(tensors[i].grad_dtype) + (tensors[i].copy ? 2 : 0));
+  TIMED("adamw_step", 0, bytes, hs(stream), adamw_launch(*c, tensors, n, update_chunk(total), scale, step_dev, hs(stream)));
+  return DIT_OK;
+}
+
+dit_status quantize_rows(const void* x, int32_t rows, int32_t cols, int64_t x_row, int32_t dtype, int8_t* q, int64_t q_row,
+                         float* scale, void* values, int64_t values_row, dit_stream stream) {
+  dit_status st = check_quantize(rows, cols, x_row, dtype, q_row, values != nullptr, values_row);
+  if (st) return st;
+  if (rows == 0 || cols == 0) return DIT_OK;
+  if (!x || !q || !scale) return set_error(DIT_ERR_INVALID_ARG, "x/q/scale NULL");
+  if ((st = check_elements({x, values}, dtype))) return st;
+  if ((st = check_offsets_aligned({scale}))) return st;
+  const QuantArgs a{x, q, scale, values, rows, cols, x_row, q_row, values_row};
+  TIMED("quantize_rows", 0, (double)rows * cols * (esize(dtype) * (values ? 2 : 1) + 1), hs(stream), quantize_rows_launch(a, dtype, hs(stream)));
+  return DIT_OK;
+}
+
+size_t int8_matmul_workspace_bytes(const dit_int8_config* c) { return check_int8(c, true) ? 0 : 0; }
+size_t int8_linear_workspace_bytes(const dit_int8_config* c) {
+  return check_int8(c, false) || c->rows == 0 || c->out_features == 0 ? 0 : int8_layout(c).total;
+}
+
+dit_status int8_matmul(const dit_int8_config* c, const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale,
+                       const void* bias, void* y, void* ws, size_t ws_bytes, dit_stream stream) {
+  dit_status st = check_int8(c, true);
+  if (st) return st;
+  if (c->rows == 0 || c->out_features == 0) return DIT_OK;
+  if ((st = check_int8_call(c, true, x, w, w_scale, bias, y))) return st;
+  if (!x_scale) return set_error(DIT_ERR_INVALID_ARG, "x_scale NULL");
+  if ((st = check_offsets_aligned({x_scale}))) return st;
+  if ((st = check_ws(ws, ws_bytes, int8_matmul_workspace_bytes(c)))) return st;
+  return run_int8_matmul(c, x, c->x_row, x_scale, w, w_scale, bias, y, hs(stream));
+}
+
+dit_status int8_linear(const dit_int8_config* c, const void* x, const int8_t* w, const float* w_scale, const void* bias, void* y,
+                       void* ws, size_t ws_bytes, dit_stream stream) {
+  dit_status st = check_int8(c, false);
+  if (st) return st;
+  if (c->rows == 0 || c->out_features == 0) return DIT_OK;
+  if ((st = check_int8_call(c, false, x, w, w_scale, bias, y))) return st;
+  if ((st = check_ws(ws, ws_bytes, int8_linear_workspace_bytes(c)))) return st;
+  const Int8Ws L = int8_layout(c);
+  float* x_scale = (float*)((char*)ws + L.scale);
+  int8_t* q = (int8_t*)ws + L.q;
+  if ((st = quantize_rows(x, c->rows, c->in_features, c->x_row, c->dtype, q, int8_row(c), x_scale, nullptr, 0, stream))) return st;
+  return run_int8_matmul(c, q, int8_row(c), x_scale, w, w_scale, bias, y, hs(stream));
 }
 
 }  // extern "C"

@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "packed.h"
+#include "vectors.h"
 
 namespace dit {
 namespace {
@@ -14,42 +15,6 @@ namespace {
 // The 8 successive elements of a row that a lane holds. VEC: D is a multiple of 8 and everything 16-byte aligned. Otherwise a lane
 // takes 16 bytes at the alignment of an element, which the memory unit allows; the one at the row's end loads its elements one by one
 // (the vectors of a chunk, and rows of up to 256 elements; longer rows: Raw) and stores 4, 2 and 1 of them.
-typedef unsigned u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
-typedef float f32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
-__device__ __forceinline__ void unpack8(const uint32_t* w, float* f) {
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void load8_any(const u16* p, float* f) {
-  const u32x4_any2 u = *(const u32x4_any2*)p;
-  const uint32_t w[4] = {u[0], u[1], u[2], u[3]};
-  unpack8(w, f);
-}
-__device__ __forceinline__ void load8_any(const float* p, float* f) {
-  const f32x4_any4 u = *(const f32x4_any4*)p, v = *(const f32x4_any4*)(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    f[i] = u[i];
-    f[4 + i] = v[i];
-  }
-}
-__device__ __forceinline__ void store8_any(u16* p, const float* f) {
-  *(u32x4_any2*)p = u32x4_any2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
-}
-__device__ __forceinline__ void store8_any(float* p, const float* f) {
-  *(f32x4_any4*)p = f32x4_any4{f[0], f[1], f[2], f[3]};
-  *(f32x4_any4*)(p + 4) = f32x4_any4{f[4], f[5], f[6], f[7]};
-}
-typedef unsigned u32x2_any2 __attribute__((ext_vector_type(2), aligned(2)));
-typedef unsigned u32_any2 __attribute__((aligned(2)));
-typedef float f32x2_any4 __attribute__((ext_vector_type(2), aligned(4)));
-__device__ __forceinline__ void store4_any(u16* p, const float* f) { *(u32x2_any2*)p = u32x2_any2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])}; }
-__device__ __forceinline__ void store4_any(float* p, const float* f) { *(f32x4_any4*)p = f32x4_any4{f[0], f[1], f[2], f[3]}; }
-__device__ __forceinline__ void store2_any(u16* p, const float* f) { *(u32_any2*)p = pack_bf16x2(f[0], f[1]); }
-__device__ __forceinline__ void store2_any(float* p, const float* f) { *(f32x2_any4*)p = f32x2_any4{f[0], f[1]}; }
 template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const T* p, int at, int D, float* f) {
 #pragma unroll

@@ -1,0 +1,292 @@
+// The end of a policy update: the 2-norm over the gradients of all weights, clipping, and the weights' AdamW step. All are
+// bound by memory. Tensors come as tables in the kernels' arguments (no copy to the device, nothing kept between
+// calls); a workgroup takes one chunk of one tensor.
+#include <algorithm>
+#include <cmath>
+
+#include "update.h"
+#include "vectors.h"
+
+namespace dit {
+namespace {
+
+constexpr int THREADS = 256;
+
+// ---- tables of tensors ----
+// first[e]: the workgroup that takes tensor e's first chunk; unused entries are past every workgroup.
+// A launch's arguments stay below 4 KB: 192 gradients, 64 weights.
+constexpr int GRADS = 192, WEIGHTS = 64;
+struct GradTable {
+  void* data[GRADS];
+  int64_t count[GRADS];   // elements, bf16 ones negated
+  int first[GRADS];
+};
+struct WeightTable {
+  void* param[WEIGHTS];
+  const void* grad[WEIGHTS];
+  float* m[WEIGHTS];
+  float* v[WEIGHTS];
+  void* copy[WEIGHTS];
+  int64_t count[WEIGHTS];
+  int first[WEIGHTS];
+  int types[WEIGHTS];     // bit 0: bf16 param, bit 1: bf16 grad
+};
+static_assert(sizeof(GradTable) + 64 <= 4096 && sizeof(WeightTable) + 96 <= 4096, "a launch's arguments");
+
+// The tensor that workgroup b works on: every lane looks at entries of its own, so that the search is one load long.
+template <int N> __device__ __forceinline__ int entry_of(const int* first, int b) {
+  const int lane = threadIdx.x & 63;
+  int f[N / 64], e = -1;
+#pragma unroll
+  for (int i = 0; i < N / 64; i++) f[i] = first[64 * i + lane];
+#pragma unroll
+  for (int i = 0; i < N / 64; i++) e += __popcll(__ballot(f[i] <= b));
+  return e;
+}
+
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// ---- norm ----
+// Squares are taken and summed in fp64 (a bf16 or fp32 value's square is exact there, and finite): four sums per thread in flight,
+// whose order is given by the chunk.
+template <typename T> __device__ double chunk_squares(const T* p, int64_t begin, int64_t end) {
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  constexpr int U = 4;
+  int64_t at = begin + 8 * threadIdx.x;
+  for (; at + (U - 1) * 8 * THREADS + 8 <= end; at += U * 8 * THREADS) {
+    float f[U][8];
+#pragma unroll
+    for (int u = 0; u < U; u++) load8_any(p + at + u * 8 * THREADS, f[u]);
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+      for (int i = 0; i < 8; i++) s[i & 3] = fma((double)f[u][i], (double)f[u][i], s[i & 3]);
+  }
+  for (; at < end; at += 8 * THREADS) {
+    if (at + 8 <= end) {
+      float f[8];
+      load8_any(p + at, f);
+#pragma unroll
+      for (int i = 0; i < 8; i++) s[i & 3] = fma((double)f[i], (double)f[i], s[i & 3]);
+    } else {
+      for (int i = 0; at + i < end; i++) {
+        const double d = to_f32(p[at + i]);
+        s[0] = fma(d, d, s[0]);
+      }
+    }
+  }
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+__global__ void __launch_bounds__(THREADS) norm_kernel(const GradTable t, int64_t chunk, double* parts) {
+  __shared__ double red[THREADS / 64];
+  const int b = blockIdx.x, e = entry_of<GRADS>(t.first, b);
+  const int64_t n = t.count[e], count = n < 0 ? -n : n;
+  const int64_t begin = (b - t.first[e]) * chunk, end = min(begin + chunk, count);
+  double s = n < 0 ? chunk_squares((const u16*)t.data[e], begin, end) : chunk_squares((const float*)t.data[e], begin, end);
+  s = wave_sum64(s);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) parts[b] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__global__ void __launch_bounds__(1024) norm_finish_kernel(const double* parts, int64_t n, double max_norm, double* norm, float* scale) {
+  __shared__ double red[16];
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += 1024) s += parts[i];
+  s = wave_sum64(s);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  s = 0.0;
+#pragma unroll
+  for (int w = 0; w < 16; w++) s += red[w];
+  const double r = sqrt(s);
+  if (norm) *norm = r;
+  if (scale) *scale = r < INFINITY ? (float)fmin(1.0, max_norm / (r + 1e-6)) : NAN;
+}
+
+// ---- clipping ----
+template <typename T> __device__ void chunk_scale(T* p, int64_t begin, int64_t end, float k) {
+  for (int64_t at = begin + 8 * threadIdx.x; at < end; at += 8 * THREADS) {
+    if (at + 8 <= end) {
+      float f[8];
+      load8_any(p + at, f);
+#pragma unroll
+      for (int i = 0; i < 8; i++) f[i] *= k;
+      store8_any(p + at, f);
+    } else {
+      for (int i = 0; at + i < end; i++) p[at + i] = from_f32<T>(to_f32(p[at + i]) * k);
+    }
+  }
+}
+__global__ void __launch_bounds__(THREADS) clip_kernel(const GradTable t, int64_t chunk, const float* scale) {
+  const float k = *scale;
+  if (k == 1.f) return;
+  const int b = blockIdx.x, e = entry_of<GRADS>(t.first, b);
+  const int64_t n = t.count[e], count = n < 0 ? -n : n;
+  const int64_t begin = (b - t.first[e]) * chunk, end = min(begin + chunk, count);
+  if (n < 0) chunk_scale((u16*)t.data[e], begin, end, k);
+  else chunk_scale((float*)t.data[e], begin, end, k);
+}
+
+// ---- AdamW ----
+struct Adam {
+  float beta1, rest1, beta2, rest2, eps, keep, step1, root2;
+  // with s = *scale: m = beta1 m + rest1 s g, v = beta2 v + rest2 (s g)^2, p = keep p - step1 m / (sqrt(v) root2 + eps),
+  // keep = 1 - lr weight_decay, step1 = lr / (1 - beta1^t), root2 = 1 / sqrt(1 - beta2^t)
+  __device__ __forceinline__ void apply(float g, float& m, float& v, float& p) const {
+    m = fmaf(rest1, g, beta1 * m);
+    v = fmaf(rest2 * g, g, beta2 * v);
+    p = fmaf(keep, p, -(step1 * m / fmaf(sqrtf(v), root2, eps)));
+  }
+};
+struct AdamArgs {
+  Adam a;                          // of the host's step number
+  const int64_t* step_dev;         // where that is on the device: with the logarithms of the betas (-inf for 0)
+  double lr, log_beta1, log_beta2;
+  const float* scale;
+};
+// step1 and root2 from t, in fp64: 1 - beta^t loses what a beta near 1 has
+__host__ __device__ __forceinline__ void set_step(Adam& a, double t, double lr, double log_beta1, double log_beta2) {
+  a.step1 = (float)(lr / -expm1(t * log_beta1));
+  a.root2 = (float)(1.0 / sqrt(-expm1(t * log_beta2)));
+}
+
+template <typename P, typename G>
+__device__ void chunk_adam(const Adam& a, float k, P* p, const G* g, float* m, float* v, u16* copy, int64_t begin, int64_t end) {
+  for (int64_t at = begin + 8 * threadIdx.x; at < end; at += 8 * THREADS) {
+    if (at + 8 <= end) {
+      float fp[8], fg[8], fm[8], fv[8];
+      load8_any(p + at, fp);
+      load8_any(g + at, fg);
+      load8_any(m + at, fm);
+      load8_any(v + at, fv);
+#pragma unroll
+      for (int i = 0; i < 8; i++) a.apply(k * fg[i], fm[i], fv[i], fp[i]);
+      store8_any(p + at, fp);
+      store8_any(m + at, fm);
+      store8_any(v + at, fv);
+      if (copy) store8_any(copy + at, fp);
+    } else {
+      for (int64_t i = at; i < end; i++) {
+        float fp = to_f32(p[i]), fm = m[i], fv = v[i];
+        a.apply(k * to_f32(g[i]), fm, fv, fp);
+        p[i] = from_f32<P>(fp);
+        m[i] = fm;
+        v[i] = fv;
+        if (copy) copy[i] = from_f32<u16>(fp);
+      }
+    }
+  }
+}
+__global__ void __launch_bounds__(THREADS) adamw_kernel(const WeightTable t, int64_t chunk, const AdamArgs args) {
+  const float k = args.scale ? *args.scale : 1.f;
+  if (k != k) return;
+  const int b = blockIdx.x, e = entry_of<WEIGHTS>(t.first, b);
+  const int64_t begin = (b - t.first[e]) * chunk, end = min(begin + chunk, t.count[e]);
+  Adam a = args.a;
+  if (args.step_dev) set_step(a, (double)*args.step_dev, args.lr, args.log_beta1, args.log_beta2);
+  void* p = t.param[e];
+  const void* g = t.grad[e];
+  float *m = t.m[e], *v = t.v[e];
+  u16* copy = (u16*)t.copy[e];
+  switch (t.types[e]) {
+    case 0: return chunk_adam(a, k, (float*)p, (const float*)g, m, v, copy, begin, end);
+    case 1: return chunk_adam(a, k, (u16*)p, (const float*)g, m, v, copy, begin, end);
+    case 2: return chunk_adam(a, k, (float*)p, (const u16*)g, m, v, copy, begin, end);
+    default: return chunk_adam(a, k, (u16*)p, (const u16*)g, m, v, copy, begin, end);
+  }
+}
+
+int64_t chunks_of(int64_t count, int64_t chunk) { return (count + chunk - 1) / chunk; }
+
+// Tables of successive tensors that have elements, a launch for each: launch(table, workgroups).
+template <typename F> hipError_t for_each_table(const dit_gradient* g, int n, int64_t chunk, F&& launch) {
+  for (int i = 0; i < n;) {
+    GradTable t;
+    int used = 0;
+    int64_t blocks = 0;
+    for (; i < n && used < GRADS; i++) {
+      if (g[i].count == 0) continue;
+      t.data[used] = g[i].data;
+      t.count[used] = g[i].dtype == DIT_BF16 ? -g[i].count : g[i].count;
+      t.first[used++] = (int)blocks;
+      blocks += chunks_of(g[i].count, chunk);
+    }
+    if (used == 0) break;
+    for (int k = used; k < GRADS; k++) {
+      t.data[k] = nullptr;
+      t.count[k] = 0;
+      t.first[k] = 0x7fffffff;
+    }
+    const hipError_t e = launch(t, (int)blocks);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+int64_t grad_norm_parts(const dit_gradient* g, int n, int64_t chunk) {
+  int64_t parts = 0;
+  for (int i = 0; i < n; i++) parts += chunks_of(g[i].count, chunk);
+  return parts;
+}
+
+hipError_t grad_norm_sums(const dit_gradient* g, int n, int64_t chunk, double* parts, hipStream_t s) {
+  return for_each_table(g, n, chunk, [&](const GradTable& t, int blocks) {
+    norm_kernel<<<blocks, THREADS, 0, s>>>(t, chunk, parts);
+    parts += blocks;
+    return hipGetLastError();
+  });
+}
+
+hipError_t grad_norm_finish(const double* parts, int64_t nparts, double max_norm, double* norm, float* scale, hipStream_t s) {
+  norm_finish_kernel<<<1, 1024, 0, s>>>(parts, nparts, max_norm, norm, scale);
+  return hipGetLastError();
+}
+
+hipError_t grad_clip_launch(const dit_gradient* g, int n, int64_t chunk, const float* scale, hipStream_t s) {
+  return for_each_table(g, n, chunk, [&](const GradTable& t, int blocks) {
+    clip_kernel<<<blocks, THREADS, 0, s>>>(t, chunk, scale);
+    return hipGetLastError();
+  });
+}
+
+hipError_t adamw_launch(const dit_adamw_config& c, const dit_adamw_tensor* w, int n, int64_t chunk, const float* scale,
+                        const int64_t* step_dev, hipStream_t s) {
+  AdamArgs a{{(float)c.beta1, (float)(1.0 - c.beta1), (float)c.beta2, (float)(1.0 - c.beta2), (float)c.eps,
+              (float)(1.0 - c.lr * c.weight_decay), 0.f, 0.f},
+             step_dev, c.lr, std::log(c.beta1), std::log(c.beta2), scale};
+  set_step(a.a, (double)c.step, c.lr, a.log_beta1, a.log_beta2);
+  for (int i = 0; i < n;) {
+    WeightTable t{};
+    int used = 0;
+    int64_t blocks = 0;
+    for (; i < n && used < WEIGHTS; i++) {
+      if (w[i].count == 0) continue;
+      t.param[used] = w[i].param;
+      t.grad[used] = w[i].grad;
+      t.m[used] = w[i].m;
+      t.v[used] = w[i].v;
+      t.copy[used] = w[i].copy;
+      t.count[used] = w[i].count;
+      t.types[used] = (w[i].param_dtype == DIT_BF16) | (w[i].grad_dtype == DIT_BF16) << 1;
+      t.first[used++] = (int)blocks;
+      blocks += chunks_of(w[i].count, chunk);
+    }
+    if (used == 0) break;
+    for (int k = used; k < WEIGHTS; k++) t.first[k] = 0x7fffffff;
+    adamw_kernel<<<(int)blocks, THREADS, 0, s>>>(t, chunk, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace dit

@@ -1,4 +1,4 @@
-"""Thin Python binding of libditstep.so (include/ditstep.h, include/ditpolicy.h).
+"""Thin Python binding of libditstep.so (include/ditstep.h, include/ditpolicy.h, include/ditupdate.h, include/ditint8.h).
 
 Argument marshalling only: every function takes torch tensors that already
 live on the GPU, passes their device pointers, sizes and the current HIP
@@ -33,7 +33,9 @@ EXPORTS = ("dit_abi_version", "dit_status_string", "dit_last_error_message", "di
            "dit_teacache_cache_bytes", "dit_denoise_step_teacache",
            "packed_attention_workspace_bytes", "packed_attention", "packed_attention_backward_workspace_bytes",
            "packed_attention_backward", "gated_norm", "gated_norm_backward_workspace_bytes", "gated_norm_backward",
-           "flow_policy_loss_workspace_bytes", "flow_policy_loss")
+           "flow_policy_loss_workspace_bytes", "flow_policy_loss",
+           "grad_norm_workspace_bytes", "grad_norm", "grad_clip", "adamw_step", "quantize_rows", "int8_matmul_workspace_bytes",
+           "int8_linear_workspace_bytes", "int8_matmul", "int8_linear")
 
 
 class DitError(RuntimeError):
@@ -77,6 +79,24 @@ class GatedNormConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("sequences", "rows", "hidden", "dtype", "post_norm", "pre_norm")] + [
         ("eps", C.c_float), ("residual_scale", C.c_float)] + [
         (n, C.c_int64) for n in ("x_row", "y_row", "h_row", "mod_row")]
+
+
+class Gradient(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("param", "grad", "m", "v", "copy")] + [
+        ("count", C.c_int64), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32)]
+
+
+class AdamwConfig(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [("step", C.c_int64)]
+
+
+class Int8Config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "in_features", "out_features", "dtype", "act")] + [
+        (n, C.c_int64) for n in ("x_row", "w_row", "y_row")]
 
 
 class KernelStat(C.Structure):
@@ -125,6 +145,15 @@ _sigs = {
     "gated_norm_backward": ([C.POINTER(GatedNormConfig)] + [_vp] * 17 + [_sz, _stream], _i32),
     "flow_policy_loss_workspace_bytes": ([_i32, _i64], _sz),
     "flow_policy_loss": ([_vp, _vp, _vp, _vp, _i32, _i64] + [C.c_double] * 3 + [_vp, _vp] + [C.c_double] * 4 + [ _vp, _vp, _vp, _vp, _vp, _sz, _stream], _i32),
+    "grad_norm_workspace_bytes": ([_vp, _i32], _sz),
+    "grad_norm": ([_vp, _i32, C.c_double, _vp, _vp, _vp, _sz, _stream], _i32),
+    "grad_clip": ([_vp, _i32, _vp, _stream], _i32),
+    "adamw_step": ([C.POINTER(AdamwConfig), _vp, _i32, _vp, _vp, _stream], _i32),
+    "quantize_rows": ([_vp, _i32, _i32, _i64, _i32, _vp, _i64, _vp, _vp, _i64, _stream], _i32),
+    "int8_matmul_workspace_bytes": ([C.POINTER(Int8Config)], _sz),
+    "int8_linear_workspace_bytes": ([C.POINTER(Int8Config)], _sz),
+    "int8_matmul": ([C.POINTER(Int8Config)] + [_vp] * 7 + [_sz, _stream], _i32),
+    "int8_linear": ([C.POINTER(Int8Config)] + [_vp] * 6 + [_sz, _stream], _i32),
 }
 for _name, (_args, _res) in _sigs.items():
     _fn = getattr(_lib, _name)
@@ -482,6 +511,192 @@ def flow_policy_loss(x, v, x_next, logp_old, adv, t, t_next, noise_level, loss, 
     _check(_lib.flow_policy_loss(px, pv, pn, pr, b, n, t, t_next, noise_level, old, pa, logp_scale, clip_low, clip_high, kl_weight,
                                  _dense(loss, dev, f64, 1), _dense(logp, dev, f64, b), _dense(ratio, dev, f64, b), dvp,
                                  *_ws_args(ws, dev), _s(stream)))
+
+
+# ---------------------------------------------------------------------------
+# the end of a policy update (include/ditupdate.h)
+# ---------------------------------------------------------------------------
+class TensorList:
+    """Descriptors of many tensors and the tensors themselves, for calls as often as these stay where they are."""
+
+    def __init__(self, array, count, device, keep):
+        self.array, self.count, self.device, self._keep = array, count, device, keep
+        self.bytes = None   # of grad_norm's workspace
+
+    def on_current_device(self):
+        if self.count and self.device != _current_device():
+            raise ValueError(f"tensors on cuda:{self.device} in a call on cuda:{_current_device()}")
+        return self.array, self.count
+
+
+def _apart(tensors):
+    """Refuses tensors that share memory."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors if t is not None and t.numel())
+    for (_, end), (start, _) in zip(spans, spans[1:]):
+        if start < end:
+            raise ValueError("tensors of a list share memory")
+
+
+def _one_device(tensors):
+    devices = {t.get_device() for t in tensors if t is not None}
+    if len(devices) > 1:
+        raise ValueError(f"tensors of a list are on several devices: {sorted(devices)}")
+    return devices.pop() if devices else -1
+
+
+def _flat(t, dtypes):
+    if t.dtype not in dtypes:
+        raise ValueError(f"a tensor of {t.dtype} where one of {[str(x) for x in dtypes]} is wanted")
+    if not t.is_contiguous():
+        raise ValueError(f"a tensor of shape {tuple(t.shape)} and strides {t.stride()} has gaps")
+    return t.data_ptr()
+
+
+_FLOATS = (torch.bfloat16, torch.float32)
+
+
+def grad_list(grads) -> TensorList:
+    """Gradients (bf16 or fp32, contiguous, any shapes; None is skipped) for grad_norm and grad_clip. The list holds their addresses:
+    make another one when gradients move."""
+    grads = [g for g in grads if g is not None]
+    array = (Gradient * max(len(grads), 1))(*[Gradient(_flat(g, _FLOATS), g.numel(), _dtype_code(g.dtype), 0) for g in grads])
+    _apart(grads)
+    return TensorList(array, len(grads), _one_device(grads), grads)
+
+
+def grad_norm_workspace_bytes(grads: TensorList) -> int:
+    if grads.bytes is None:
+        grads.bytes = _lib.grad_norm_workspace_bytes(grads.array, grads.count)
+    return grads.bytes
+
+
+def grad_norm(grads, max_norm, norm=None, scale=None, ws=None, stream=None):
+    """norm: one fp64, scale: one fp32 (device); either may be None."""
+    array, n = grads.on_current_device()
+    dev = _current_device()
+    _check(_lib.grad_norm(array, n, max_norm, _dense(norm, dev, torch.float64, 1), _dense(scale, dev, torch.float32, 1),
+                          *_ws_args(ws, dev), _s(stream)))
+
+
+def grad_clip(grads, scale, stream=None):
+    """Gradients times scale (one device fp32), in place."""
+    array, n = grads.on_current_device()
+    _check(_lib.grad_clip(array, n, _dense(scale, _current_device(), torch.float32, 1), _s(stream)))
+
+
+def adamw_list(params, grads, m, v, copies=None) -> TensorList:
+    """Weights (bf16 or fp32), their gradients (bf16 or fp32) and moments (fp32), all contiguous; copies: bf16 weights that follow
+    fp32 ones (a list whose entries may be None), or None. The list holds their addresses, as grad_list's."""
+    params, grads, m, v = (list(x) for x in (params, grads, m, v))
+    copies = [None] * len(params) if copies is None else list(copies)
+    if not len(params) == len(grads) == len(m) == len(v) == len(copies):
+        raise ValueError("lists of unlike lengths")
+    rows = []
+    for p, g, a, b, c in zip(params, grads, m, v, copies):
+        if any(t is not None and t.shape != p.shape for t in (g, a, b, c)):
+            raise ValueError(f"a weight of shape {tuple(p.shape)} and a tensor of another")
+        rows.append(AdamwTensor(_flat(p, _FLOATS), _flat(g, _FLOATS), _flat(a, (torch.float32,)), _flat(b, (torch.float32,)),
+                                None if c is None else _flat(c, (torch.bfloat16,)), p.numel(), _dtype_code(p.dtype), _dtype_code(g.dtype)))
+    keep = params + grads + m + v + copies
+    _apart(keep)
+    return TensorList((AdamwTensor * max(len(rows), 1))(*rows), len(rows), _one_device(keep), keep)
+
+
+def adamw_step(weights, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=1, scale=None, step_dev=None, stream=None):
+    """scale: grad_norm's (one device fp32), or None; step_dev: one device int64 that holds the step's number, or None (step)."""
+    array, n = weights.on_current_device()
+    dev = _current_device()
+    cfg = AdamwConfig(lr, beta1, beta2, eps, weight_decay, step)
+    _check(_lib.adamw_step(C.byref(cfg), array, n, _dense(scale, dev, torch.float32, 1), _dense(step_dev, dev, torch.int64, 1),
+                           _s(stream)))
+
+
+# ---------------------------------------------------------------------------
+# linear layers in 8-bit integers (include/ditint8.h)
+# ---------------------------------------------------------------------------
+ACTIVATIONS = {"none": 0, "gelu": 1}
+
+
+def int8_rows(rows, cols, device="cuda") -> torch.Tensor:
+    """[rows][cols] int8 whose rows start at multiples of 16 bytes, as int8_matmul and int8_linear want them."""
+    return torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=device)[:, :cols]
+
+
+def _row_stride(t):
+    """The row stride of a [rows][cols] tensor (of one row: any that is long enough)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _rows_of(t, name, dtypes):
+    if t.dim() != 2 or (t.numel() and t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} is [rows][columns] with the last index contiguous")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} is of {t.dtype}")
+
+
+def quantize_rows(x, q, scale, values=None, stream=None):
+    """x [rows][cols] bf16 or fp32 -> q (int8, the same shape), scale (fp32 [rows]) and, if given, values (x's type and shape): what q and
+    scale stand for. Row strides are free."""
+    dev = _current_device()
+    _rows_of(x, "x", _FLOATS)
+    _rows_of(q, "q", (torch.int8,))
+    for t in (x, q) if values is None else (x, q, values):
+        if t.shape != x.shape or t.get_device() != dev:
+            raise ValueError(f"a tensor of shape {tuple(t.shape)} on {t.device} for x of {tuple(x.shape)} in a call on cuda:{dev}")
+    if values is not None:
+        _rows_of(values, "values", (x.dtype,))
+    rows, cols = x.shape
+    _check(_lib.quantize_rows(_ptr(x), rows, cols, _row_stride(x), _dtype_code(x.dtype), _ptr(q), _row_stride(q),
+                              _dense(scale, dev, torch.float32, rows), _ptr(values), 0 if values is None else _row_stride(values), _s(stream)))
+
+
+def int8_config(x, w, y, act="none") -> Int8Config:
+    """x [rows][in] (bf16 or fp32: int8_linear, int8: int8_matmul), w [out][in] int8, y [rows][out] bf16 or fp32 (x's type, unless that is
+    int8); row strides are free, those of int8 rows multiples of 16 (int8_rows). act: none or gelu (its tanh form)."""
+    _rows_of(x, "x", (*_FLOATS, torch.int8))
+    _rows_of(w, "w", (torch.int8,))
+    _rows_of(y, "y", _FLOATS if x.dtype == torch.int8 else (x.dtype,))
+    if x.shape[1] != w.shape[1] or y.shape != (x.shape[0], w.shape[0]):
+        raise ValueError(f"shapes {tuple(x.shape)} x {tuple(w.shape)} -> {tuple(y.shape)}")
+
+    def int8_stride(t):   # of one row: any multiple of 16 that is long enough
+        return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+    return Int8Config(x.shape[0], x.shape[1], w.shape[0], _dtype_code(y.dtype), ACTIVATIONS[act],
+                      int8_stride(x) if x.dtype == torch.int8 else _row_stride(x), int8_stride(w), _row_stride(y))
+
+
+def _int8_at(t, rows, cols, row, dev):
+    """The device pointer of int8 rows laid out as the config says, whose storage reaches to the last row's 16-byte end."""
+    p = _at(t, (torch.int8, (rows, cols), (row, 1), dev))
+    if cols % 16 and t is not None and t.storage_offset() + (rows - 1) * row + -(-cols // 16) * 16 > t.untyped_storage().nbytes():
+        raise ValueError("the storage of int8 rows ends before the last row's next multiple of 16 bytes (int8_rows makes such rows)")
+    return p
+
+
+def int8_matmul_workspace_bytes(cfg) -> int:
+    return _lib.int8_matmul_workspace_bytes(C.byref(cfg))
+
+
+def int8_linear_workspace_bytes(cfg) -> int:
+    return _lib.int8_linear_workspace_bytes(C.byref(cfg))
+
+
+def int8_matmul(cfg, x, x_scale, w, w_scale, y, bias=None, ws=None, stream=None):
+    """Tensors laid out as those cfg was made from; x_scale [rows], w_scale [out] fp32; bias [out] of y's type, or None."""
+    dev, dt, f32 = _current_device(), _ROW_TYPES.get(cfg.dtype), torch.float32
+    M, K, N = cfg.rows, cfg.in_features, cfg.out_features
+    _check(_lib.int8_matmul(C.byref(cfg), _int8_at(x, M, K, cfg.x_row, dev), _dense(x_scale, dev, f32, M),
+                            _int8_at(w, N, K, cfg.w_row, dev), _dense(w_scale, dev, f32, N), _dense(bias, dev, dt, N),
+                            _at(y, (dt, (M, N), (cfg.y_row, 1), dev)), *_ws_args(ws, dev), _s(stream)))
+
+
+def int8_linear(cfg, x, w, w_scale, y, bias=None, ws=None, stream=None):
+    """int8_matmul of x rounded to integers, x of y's type."""
+    dev, dt, f32 = _current_device(), _ROW_TYPES.get(cfg.dtype), torch.float32
+    M, K, N = cfg.rows, cfg.in_features, cfg.out_features
+    _check(_lib.int8_linear(C.byref(cfg), _at(x, (dt, (M, K), (cfg.x_row, 1), dev)), _int8_at(w, N, K, cfg.w_row, dev),
+                            _dense(w_scale, dev, f32, N), _dense(bias, dev, dt, N), _at(y, (dt, (M, N), (cfg.y_row, 1), dev)),
+                            *_ws_args(ws, dev), _s(stream)))
 
 
 def dit_profile_begin():

@@ -1,0 +1,132 @@
+"""What the calls of ditupdate.h and ditint8.h refuse before any launch, and their workspace sizes (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+from paper_2606_19004_amd import ditstep as d
+
+lib = d.lib()
+OK, INVALID, SHAPE, DOMAIN, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3, 5, 7
+A = 1 << 20      # an aligned stand-in for a device pointer: every call here fails, or has nothing to do, before it is used
+NAN, INF = float("nan"), float("inf")
+
+
+def grads(*rows):
+    return (d.Gradient * max(len(rows), 1))(*[d.Gradient(*r) for r in rows]), len(rows)
+
+
+def norm(g, max_norm=1.0, norm=A, scale=A, ws=A, n=1 << 30):
+    return lib.grad_norm(*g, max_norm, norm, scale, ws, n, None)
+
+
+BAD_LISTS = [((None, 0), OK), ((None, 1), INVALID), ((None, -1), INVALID), (grads((A, -1, 0, 0)), INVALID), (grads((A, 8, 2, 0)), INVALID),
+             (grads((A, 8, 0, 1)), INVALID), (grads((A + 2, 8, 0, 0)), INVALID), (grads((A + 1, 8, 1, 0)), INVALID), (grads((None, 8, 0, 0)), INVALID),
+             (grads((A, (1 << 44) + 1, 0, 0)), UNSUPPORTED), (grads((A, 1 << 43, 0, 0), (A, 1 << 43, 1, 0), (A, 1, 1, 0)), UNSUPPORTED),
+             (grads((A, (1 << 63) - 1, 0, 0), (A, (1 << 63) - 1, 0, 0)), UNSUPPORTED), ((grads((A, 8, 0, 0))[0], (1 << 20) + 1), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("g,status", BAD_LISTS)
+def test_gradient_lists(g, status):
+    if status == OK:
+        assert lib.grad_clip(*g, A, None) == OK and d.lib().grad_norm_workspace_bytes(*g) == 0
+        return
+    assert norm(g) == status and lib.grad_clip(*g, A, None) == status
+    if g[0] is None or not any(x.data in (A + 1, A + 2, None) for x in g[0]):
+        assert lib.grad_norm_workspace_bytes(*g) == 0
+
+
+def test_norm_calls():
+    g = grads((A, 100000, 0, 0), (None, 0, 1, 0), (A, 5, 1, 0))
+    need = lib.grad_norm_workspace_bytes(*g)
+    assert need > 0 and need % 256 == 0
+    for bad in (-1.0, NAN, -INF):
+        assert norm(g, bad) == DOMAIN
+    assert norm(g, norm=None, scale=None) == INVALID and norm(g, norm=A + 4) == INVALID and norm(g, scale=A + 2) == INVALID
+    assert norm(g, ws=None) == WORKSPACE and norm(g, ws=A + 16) == WORKSPACE and norm(g, n=need - 1) == WORKSPACE
+    assert lib.grad_clip(*g, None, None) == INVALID and lib.grad_clip(*g, A + 1, None) == INVALID
+    assert lib.grad_clip(*grads((None, 0, 0, 0)), A, None) == OK
+
+
+def test_norm_workspace_is_small():
+    """A partial sum for every chunk: about 8192 and one for every tensor, however many elements there are."""
+    for rows in ([(A, 1 << 40, 1, 0)], [(A, 3, 0, 0)] * 5000, [(A, 1 << 30, 0, 0), (A, 7, 0, 0)] * 100):
+        assert lib.grad_norm_workspace_bytes(*grads(*rows)) <= 8 * (8192 + len(rows)) + 256
+
+
+def adam(rows=((A, A, A, A, A, 8, 0, 1),), scale=A, step_dev=None, **kw):
+    c = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=1)
+    c.update(kw)
+    cfg = d.AdamwConfig(*[c[n] for n, _ in d.AdamwConfig._fields_])
+    return lib.adamw_step(C.byref(cfg), (d.AdamwTensor * max(len(rows), 1))(*[d.AdamwTensor(*r) for r in rows]), len(rows), scale, step_dev, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(lr=NAN), DOMAIN), (dict(lr=INF), DOMAIN), (dict(weight_decay=INF), DOMAIN), (dict(beta1=1.0), DOMAIN), (dict(beta1=-0.1), DOMAIN),
+    (dict(beta2=1.0), DOMAIN), (dict(beta2=NAN), DOMAIN), (dict(eps=-1e-8), DOMAIN), (dict(eps=NAN), DOMAIN), (dict(step=0), DOMAIN), (dict(step=-5), DOMAIN),
+    (dict(scale=A + 1), INVALID), (dict(step_dev=A + 4), INVALID),
+    (dict(rows=[(None, A, A, A, A, 8, 0, 0)]), INVALID), (dict(rows=[(A, None, A, A, A, 8, 0, 0)]), INVALID),
+    (dict(rows=[(A, A, None, A, A, 8, 0, 0)]), INVALID), (dict(rows=[(A, A, A, None, A, 8, 0, 0)]), INVALID),
+    (dict(rows=[(A + 2, A, A, A, A, 8, 0, 0)]), INVALID), (dict(rows=[(A, A + 1, A, A, A, 8, 0, 1)]), INVALID),
+    (dict(rows=[(A, A, A + 2, A, A, 8, 0, 0)]), INVALID), (dict(rows=[(A, A, A, A + 2, A, 8, 0, 0)]), INVALID),
+    (dict(rows=[(A, A, A, A, A + 1, 8, 0, 0)]), INVALID), (dict(rows=[(A, A, A, A, A, 8, 2, 0)]), INVALID),
+    (dict(rows=[(A, A, A, A, A, 8, 0, 3)]), INVALID), (dict(rows=[(A, A, A, A, A, -8, 0, 0)]), INVALID),
+    (dict(rows=[(A, A, A, A, A, 1 << 45, 0, 0)]), UNSUPPORTED), (dict(rows=[(None, None, None, None, None, 0, 0, 0)]), OK), (dict(rows=[]), OK)])
+def test_adamw(kw, status):
+    assert adam(**kw) == status
+    assert lib.adamw_step(None, None, 0, None, None, None) == INVALID
+
+
+def rows(x=A, n=4, cols=10, x_row=10, dtype=1, q=A, q_row=10, scale=A, values=A, values_row=10):
+    return lib.quantize_rows(x, n, cols, x_row, dtype, q, q_row, scale, values, values_row, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n=-1), INVALID), (dict(cols=-1), INVALID), (dict(dtype=2), INVALID), (dict(x_row=9), INVALID), (dict(q_row=9), INVALID),
+    (dict(values_row=9), INVALID), (dict(x_row=-10), INVALID), (dict(q_row=1 << 30), UNSUPPORTED), (dict(x_row=(1 << 63) - 1), UNSUPPORTED),
+    (dict(x=None), INVALID), (dict(q=None), INVALID), (dict(scale=None), INVALID), (dict(x=A + 1), INVALID), (dict(values=A + 1), INVALID),
+    (dict(scale=A + 2), INVALID), (dict(dtype=0, x=A + 2), INVALID), (dict(n=0, x=None), OK), (dict(n=0, x=None, values=None, values_row=0), OK)])
+def test_quantize_rows(kw, status):
+    assert rows(**kw) == status
+
+
+def cfg8(**kw):
+    f = dict(rows=4, in_features=100, out_features=50, dtype=1, act=0, x_row=112, w_row=112, y_row=50)
+    f.update(kw)
+    return d.Int8Config(*[f[n] for n, _ in d.Int8Config._fields_])
+
+
+def matmul(c, x=A, xs=A, w=A, ws=A, bias=A, y=A, work=A, n=1 << 40):
+    return lib.int8_matmul(C.byref(c) if c else None, x, xs, w, ws, bias, y, work, n, None)
+
+
+def linear(c, x=A, w=A, ws=A, bias=A, y=A, work=A, n=1 << 40):
+    return lib.int8_linear(C.byref(c) if c else None, x, w, ws, bias, y, work, n, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rows=-1), INVALID), (dict(out_features=-1), INVALID), (dict(in_features=0), SHAPE), (dict(in_features=-3), SHAPE),
+    (dict(in_features=1 << 17, x_row=1 << 17, w_row=1 << 17), UNSUPPORTED), (dict(dtype=2), INVALID), (dict(act=2), INVALID), (dict(act=-1), INVALID),
+    (dict(x_row=96), INVALID), (dict(w_row=96), INVALID), (dict(y_row=49), INVALID), (dict(w_row=120), INVALID), (dict(w_row=1 << 23), UNSUPPORTED),
+    (dict(y_row=1 << 30), UNSUPPORTED), (dict(w_row=-(1 << 63)), INVALID), (dict(x_row=1 << 40), UNSUPPORTED),
+    (dict(rows=(1 << 31) - 1, out_features=(1 << 29), y_row=1 << 29), UNSUPPORTED)])
+def test_int8_config(kw, status):
+    c = cfg8(**kw)
+    assert matmul(c) == status and linear(c) == status
+    if "rows" not in kw or kw["rows"] < 0:
+        assert d.int8_matmul_workspace_bytes(c) == 0 and d.int8_linear_workspace_bytes(c) == 0
+
+
+def test_int8_calls():
+    c = cfg8()
+    assert matmul(None) == INVALID and linear(None) == INVALID
+    assert matmul(cfg8(x_row=120)) == INVALID and matmul(cfg8(x_row=1 << 23)) == UNSUPPORTED
+    for kw in (dict(x=None), dict(w=None), dict(ws=None), dict(y=None), dict(w=A + 8), dict(ws=A + 2), dict(bias=A + 1), dict(y=A + 1)):
+        assert matmul(c, **kw) == INVALID and linear(c, **kw) == INVALID, kw
+    assert matmul(c, xs=None) == INVALID and matmul(c, xs=A + 1) == INVALID and matmul(c, x=A + 8) == INVALID and linear(c, x=A + 1) == INVALID
+    assert linear(cfg8(dtype=0), x=A + 2) == INVALID and matmul(cfg8(dtype=0), y=A + 2) == INVALID
+    need = d.int8_linear_workspace_bytes(c)
+    assert need >= 4 * 128 + 4 * 4
+    assert linear(c, work=None) == WORKSPACE and linear(c, work=A + 16) == WORKSPACE and linear(c, n=need - 1) == WORKSPACE
+    for e in (cfg8(rows=0), cfg8(out_features=0, y_row=0)):
+        assert matmul(e, x=None, y=None, work=None, n=0) == OK and linear(e, x=None, y=None, work=None, n=0) == OK
+        assert d.int8_linear_workspace_bytes(e) == 0
