@@ -1,5 +1,6 @@
 // Linear layers in 8-bit integers on gfx950: rows to integers with a scale each, and the product of two such row sets.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_common.h"
 #include "update.h"
@@ -178,18 +179,21 @@ __device__ __forceinline__ u32x4_t rows_rsrc(const int8_t* p, int rows, int64_t 
                  (uint32_t)__builtin_amdgcn_readfirstlane((int)records), 0x00020000u};
 }
 
-// y of row m at features n .. n + 3 from their sums
-template <int ACT, typename T>
-__device__ __forceinline__ void finish4(const Int8Args& a, i32x4 c, int m, int n) {
-  const float xs = a.x_scale[m];
-  float v[4];
-#pragma unroll
-  for (int q = 0; q < 4; q++) {
-    const int nq = min(n + q, a.N - 1);
-    v[q] = (float)c[q] * xs * a.w_scale[nq];
-    if (a.bias) v[q] += to_f32(((const T*)a.bias)[nq]);
-    if (ACT) v[q] = gelu_tanh_f(v[q]);
-  }
+// What a feature contributes to its results.
+struct Channel {
+  float scale, bias;
+};
+template <typename T> __device__ __forceinline__ Channel channel(const Int8Args& a, int n) {
+  return Channel{a.w_scale[n], a.bias ? to_f32(((const T*)a.bias)[n]) : 0.f};
+}
+template <int ACT> __device__ __forceinline__ float finish(int sum, float x_scale, Channel c) {
+  // (two products and a sum, each rounded by itself in every form of the product)
+#pragma clang fp contract(off)
+  const float v = (float)sum * x_scale * c.scale + c.bias;
+  return ACT ? gelu_tanh_f(v) : v;
+}
+// four successive features of a row, as far as it goes
+template <typename T> __device__ __forceinline__ void store_features(const Int8Args& a, const float* v, int m, int n) {
   T* y = (T*)a.y + (int64_t)m * a.y_row + n;
   if (n + 4 <= a.N) {
     store4_any(y, v);
@@ -200,94 +204,485 @@ __device__ __forceinline__ void finish4(const Int8Args& a, i32x4 c, int m, int n
   }
 }
 
-// 64 x 64 tile, 4 waves of 32 x 32, k-tiles in a ring of three LDS stages (48 KB, three workgroups per CU).
-template <int ACT, typename T>
-__global__ void __launch_bounds__(256) int8_tile64_kernel(const Int8Args a, int total_tiles) {
-  constexpr int B = 64, STAGE = 2 * B * 128;
+constexpr uint32_t OUTSIDE = 0xC0000000u;   // an offset past any tile's records, also with what a burst adds
+
+// RING = 0 (256-row tiles): three LDS stages of x and two of w (160 KB), the pipeline of the bf16 GEMM's large tile, at
+// twice its depth per byte. RING > 0: a ring of RING stages of both.
+template <int BM, int BN, int WM, int WN, int RING, int ACT, typename T>
+__global__ void __launch_bounds__(WM * WN * 64) int8_gemm_kernel(const Int8Args a, int total_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) char smem[3 * STAGE];
+  constexpr bool TRI = RING == 0;
+  constexpr int NW = WM * WN, NT = NW * 64;
+  constexpr int WTM = BM / WM, WTN = BN / WN, TJ = WTM / 16, TI = WTN / 16;   // wave tile, its blocks along rows and features
+  constexpr int X_LOADS = BM / 8 / NW, W_LOADS = BN / 8 / NW;                 // 8-row groups that a wave loads per k-tile
+  constexpr int X_BYTES = BM * 128, W_BYTES = BN * 128;
+  static_assert(X_LOADS >= 1 && W_LOADS >= 1, "every wave loads at least one row group");
+  static_assert(TI % 2 == 0, "the paired store joins blocks 2p and 2p + 1");
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int per = gridDim.x >> 3;
   const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);   // XCD-aware, as in the bf16 kernel
   if (t >= total_tiles) return;
   int tm, tn;
-  tile_coords(t, cdiv(a.M, B), cdiv(a.N, B), tm, tn);
-  const int m0 = tm * B, n0 = tn * B;
+  tile_coords(t, cdiv(a.M, BM), cdiv(a.N, BN), tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const u32x4_t rx = rows_rsrc(a.x + (int64_t)m0 * a.x_row, min(B, a.M - m0), a.x_row, a.K);
-  const u32x4_t rw = rows_rsrc(a.w + (int64_t)n0 * a.w_row, min(B, a.N - n0), a.w_row, a.K);
-  const uint32_t OOB = 0x80000000u;
-  // a wave load fills 8 rows: lane -> row lane / 8, slot lane % 8, which holds chunk slot ^ swz(row)
-  uint32_t xoff[2], woff[2];
-  int chunk[2];
+  const int K = a.K, nk = (K + 127) / 128;
+
+  // a wave load fills 8 rows: lane -> row lane / 8, slot lane % 8, which holds chunk slot ^ swz(row); bursts carry -1024 i in
+  // their offsets and 4 KB that the base lacks
+  constexpr bool BX = X_LOADS == 3 || X_LOADS == 4, BW = W_LOADS == 3 || W_LOADS == 4;
+  const int lrow = lane >> 3;
+  u32x4_t rx = rows_rsrc(a.x + (int64_t)m0 * a.x_row - (BX ? 4096 : 0), min(BM, a.M - m0), a.x_row, K);
+  u32x4_t rw = rows_rsrc(a.w + (int64_t)n0 * a.w_row - (BW ? 4096 : 0), min(BN, a.N - n0), a.w_row, K);
+  if (BX) rx[2] += 4096;
+  if (BW) rw[2] += 4096;
+  uint32_t xoff[X_LOADS], woff[W_LOADS];
+  int xchunk[X_LOADS], wchunk[W_LOADS];
 #pragma unroll
-  for (int i = 0; i < 2; i++) {
-    const int r = 8 * (wave * 2 + i) + (lane >> 3);
-    chunk[i] = ((lane & 7) ^ swz(r)) * 16;
-    xoff[i] = m0 + r < a.M ? (uint32_t)(r * a.x_row) + chunk[i] : OOB;
-    woff[i] = n0 + r < a.N ? (uint32_t)(r * a.w_row) + chunk[i] : OOB;
+  for (int i = 0; i < X_LOADS; i++) {
+    const int r = 8 * (wave * X_LOADS + i) + lrow;
+    xchunk[i] = ((lane & 7) ^ swz(r)) * 16;
+    xoff[i] = m0 + r < a.M ? (uint32_t)(r * a.x_row) + xchunk[i] + (BX ? 4096u - 1024u * i : 0u) : OUTSIDE;
   }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
-  auto issue = [&](int kt, int st) {
-    const uint32_t base = lds0 + st * STAGE + wave * 2048;
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-      const bool in = kt * 128 + chunk[i] < a.K;
-      dma_b128(rx, base + i * 1024, in ? xoff[i] : OOB, kt * 128);
-      dma_b128(rw, base + B * 128 + i * 1024, in ? woff[i] : OOB, kt * 128);
+  for (int i = 0; i < W_LOADS; i++) {
+    const int r = 8 * (wave * W_LOADS + i) + lrow;
+    wchunk[i] = ((lane & 7) ^ swz(r)) * 16;
+    woff[i] = n0 + r < a.N ? (uint32_t)(r * a.w_row) + wchunk[i] + (BW ? 4096u - 1024u * i : 0u) : OUTSIDE;
+  }
+  // RING = 0: [W0][W1][X0][X1][X2], tile kt uses w stage kt % 2 and x stage kt % 3; else stage kt % RING of [W][X] pairs
+  auto stage_w = [&](int kt) -> uint32_t { return TRI ? (kt & 1) * W_BYTES : (kt % (RING + TRI)) * (X_BYTES + W_BYTES); };
+  auto stage_x = [&](int kt) -> uint32_t {
+    return TRI ? 2 * W_BYTES + (kt % 3) * X_BYTES : (kt % (RING + TRI)) * (X_BYTES + W_BYTES) + W_BYTES;
+  };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  // END: the tile may be the last one, whose chunks past the row's end read zeros
+  auto issue_x = [&](int kt, auto end_c) {
+    constexpr bool END = decltype(end_c)::value;
+    const uint32_t to = lds0 + stage_x(kt) + wave * X_LOADS * 1024;
+    uint32_t off[X_LOADS];
+#pragma unroll
+    for (int i = 0; i < X_LOADS; i++) off[i] = END && kt * 128 + xchunk[i] >= K ? OUTSIDE : xoff[i];
+    if constexpr (BX) {
+      dma_burst<X_LOADS>(rx, to, off, kt * 128);
+    } else {
+#pragma unroll
+      for (int i = 0; i < X_LOADS; i++) dma_b128(rx, to + i * 1024, off[i], kt * 128);
     }
   };
-  const int wm = wave >> 1, wn = wave & 1, r16 = lane & 15, kq = lane >> 4;
-  i32x4 acc[2][2] = {};
-  const int nk = (a.K + 127) / 128;
-  issue(0, 0);
-  if (nk > 1) issue(1, 1);
-  int st = 0;
-  for (int kt = 0; kt < nk; kt++) {
-    // tile kt has landed (the 4 loads of tile kt + 1 may be in flight) in every wave, and every wave is done reading
-    // tile kt - 1, whose stage takes tile kt + 2
-    if (kt + 1 < nk) __builtin_amdgcn_s_waitcnt(0x0f74);
-    else __builtin_amdgcn_s_waitcnt(0x0f70);
-    __syncthreads();
-    if (kt + 2 < nk) issue(kt + 2, st == 0 ? 2 : st - 1);
-    const char* sx = smem + st * STAGE;
-    const char* sw = sx + B * 128;
+  auto issue_w = [&](int kt, auto end_c) {
+    constexpr bool END = decltype(end_c)::value;
+    const uint32_t to = lds0 + stage_w(kt) + wave * W_LOADS * 1024;
+    uint32_t off[W_LOADS];
 #pragma unroll
-    for (int s = 0; s < 2; s++) {
-      i32x4 fw[2], fx[2];
+    for (int i = 0; i < W_LOADS; i++) off[i] = END && kt * 128 + wchunk[i] >= K ? OUTSIDE : woff[i];
+    if constexpr (BW) {
+      dma_burst<W_LOADS>(rw, to, off, kt * 128);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 2; i++) {
-        const int rw_ = 32 * wn + 16 * i + r16, rx_ = 32 * wm + 16 * i + r16;
-        fw[i] = *(const i32x4*)(sw + rw_ * 128 + (((4 * s + kq) ^ swz(rw_)) << 4));
-        fx[i] = *(const i32x4*)(sx + rx_ * 128 + (((4 * s + kq) ^ swz(rx_)) << 4));
-      }
-      if (kt + 1 == nk) {
-        const i32x4 mask = row_mask(kt * 128 + 64 * s + 16 * kq, a.K);
-#pragma unroll
-        for (int i = 0; i < 2; i++) fx[i] &= mask;
-      }
-#pragma unroll
-      for (int i = 0; i < 2; i++)
-#pragma unroll
-        for (int j = 0; j < 2; j++) acc[i][j] = mfma_i8(fw[i], fx[j], acc[i][j]);
+      for (int i = 0; i < W_LOADS; i++) dma_b128(rw, to + i * 1024, off[i], kt * 128);
     }
-    st = st == 2 ? 0 : st + 1;
+  };
+  using End = std::true_type;
+
+  i32x4 acc[TI][TJ];
+#pragma unroll
+  for (int i = 0; i < TI; i++)
+#pragma unroll
+    for (int j = 0; j < TJ; j++) acc[i][j] = i32x4{0, 0, 0, 0};
+  const int wm = wave / WN, wn = wave % WN;
+  const int frow = lane & 15, lkc = lane >> 4;   // row inside a 16-row block, 16-byte chunk inside a 64-byte step
+  int fwk[TI], fxk[TJ];
+#pragma unroll
+  for (int i = 0; i < TI; i++) fwk[i] = swz(wn * WTN + 16 * i + frow);
+#pragma unroll
+  for (int j = 0; j < TJ; j++) fxk[j] = swz(wm * WTM + 16 * j + frow);
+  const int wrow0 = (wn * WTN + frow) * 128, xrow0 = (wm * WTM + frow) * 128;
+  // fragments of step s, register-double-buffered so that step s + 1 loads while step s multiplies
+  i32x4 fw[2][TI], fx[2][TJ];
+  auto frags = [&](int kt, int s, int rb) {
+    const char* sx = smem + stage_x(kt);
+    const char* sw = smem + stage_w(kt);
+    const int c = 4 * s + lkc;
+#pragma unroll
+    for (int i = 0; i < TI; i++) fw[rb][i] = *(const i32x4*)(sw + wrow0 + i * 2048 + ((c ^ fwk[i]) << 4));
+#pragma unroll
+    for (int j = 0; j < TJ; j++) fx[rb][j] = *(const i32x4*)(sx + xrow0 + j * 2048 + ((c ^ fxk[j]) << 4));
+  };
+  auto mask_last = [&](int s) {   // of the last tile's step s, once its fragments are there
+    const i32x4 mask = row_mask((nk - 1) * 128 + 64 * s + 16 * lkc, K);
+#pragma unroll
+    for (int j = 0; j < TJ; j++) fx[s][j] &= mask;
+  };
+  auto multiply = [&](int rb, int i0, int i1) {
+#pragma unroll
+    for (int i = i0; i < i1; i++)
+#pragma unroll
+      for (int j = 0; j < TJ; j++) acc[i][j] = mfma_i8(fw[rb][i], fx[rb][j], acc[i][j]);
+  };
+
+  // What the epilogue needs of the features and rows, requested before the last k-tile: a feature for each thread, a row of each block.
+  // Branch-free: past the end they read the last one's.
+  static_assert(BN <= NT, "a thread for each feature");
+  Channel pre_c{0.f, 0.f};
+  float pre_x[TJ];
+  auto prefetch = [&]() {
+    pre_c = channel<T>(a, min(n0 + min(tid, BN - 1), a.N - 1));
+#pragma unroll
+    for (int j = 0; j < TJ; j++) pre_x[j] = a.x_scale[min(m0 + wm * WTM + 16 * j + frow, a.M - 1)];
+  };
+
+  if constexpr (TRI) {
+    // as in the bf16 kernel: the refill of an x stage in the first step, of a w stage after the barrier, which sits at the last step,
+    // whose fragments are in registers; a wave's issue priority falls from barrier to barrier
+    constexpr int NM = TI * TJ;
+    auto ktile = [&](int kt, auto ph_c) {
+      constexpr int PH = decltype(ph_c)::value;   // 0, 1: refill tile kt + 2 (1: the last one); 2: none; 3: last tile
+      using Kind = std::integral_constant<bool, PH == 1>;
+#pragma unroll
+      for (int s = 0; s < 2; s++) {
+        const int rb = s;
+        if (s == 0) {
+          __builtin_amdgcn_s_setprio(1);
+          frags(kt, 1, 1);
+          if constexpr (PH <= 1) issue_x(kt + 2, Kind());
+        } else if constexpr (PH < 3) {
+          if (PH < 2) __builtin_amdgcn_s_waitcnt(0x0070 | X_LOADS);
+          else __builtin_amdgcn_s_waitcnt(0);
+          __syncthreads();
+          __builtin_amdgcn_s_setprio(3);
+          if constexpr (PH <= 1) issue_w(kt + 2, Kind());
+          frags(kt + 1, 0, 0);
+        }
+        if constexpr (PH == 3) mask_last(s);
+        multiply(rb, 0, TI / 2);
+        if constexpr (PH < 3) {
+          if (s == 0) sched_step<NM / 2, PH <= 1 ? X_LOADS : 0, TI + TJ>();
+          else sched_step<NM / 2, PH <= 1 ? W_LOADS : 0, TI + TJ>();
+        }
+        if (s == 1) __builtin_amdgcn_s_setprio(2);
+        else __builtin_amdgcn_s_setprio(0);
+        multiply(rb, TI / 2, TI);
+      }
+    };
+    issue_x(0, End());
+    issue_w(0, End());
+    if (nk > 1) issue_x(1, End());
+    if (nk > 1) __builtin_amdgcn_s_waitcnt(0x0070 | X_LOADS);
+    else __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (nk > 1) issue_w(1, End());
+    frags(0, 0, 0);
+    for (int kt = 0; kt + 3 < nk; kt++) ktile(kt, std::integral_constant<int, 0>());
+    if (nk >= 3) ktile(nk - 3, std::integral_constant<int, 1>());
+    if (nk >= 2) ktile(nk - 2, std::integral_constant<int, 2>());
+    prefetch();
+    ktile(nk - 1, std::integral_constant<int, 3>());
+    __builtin_amdgcn_s_setprio(0);
+  } else {
+    // all stages are filled up front; the hand-over from tile kt to kt + 1 sits before the last step's products, whose fragments are in
+    // registers: tile kt + 1 has landed (the loads of the RING - 2 tiles after it stay in flight), barrier, and stage kt % RING takes
+    // tile kt + RING
+    constexpr int L = X_LOADS + W_LOADS;
+    static_assert((RING - 2) * L <= 15 && (RING - 1) * L <= 63, "the waits below");
+    auto wait_tiles = [&](int n) {   // at most the loads of n tiles in flight, LDS reads done
+      if (n >= RING - 2) __builtin_amdgcn_s_waitcnt(0x0070 | ((RING - 2) * L & 15));
+      else if (n == 2) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * L & 15));
+      else if (n == 1) __builtin_amdgcn_s_waitcnt(0x0070 | (L & 15));
+      else __builtin_amdgcn_s_waitcnt(0x0070);
+    };
+    auto step = [&](int kt, auto ph_c) {
+      constexpr int PH = decltype(ph_c)::value;   // 0: refill tile kt + RING; 1: none; 2: last tile
+      frags(kt, 1, 1);
+      if constexpr (PH == 2) mask_last(0);
+      multiply(0, 0, TI);
+      if constexpr (PH < 2) {
+        wait_tiles(PH == 0 ? RING - 2 : nk - 2 - kt);
+        __syncthreads();
+        if constexpr (PH == 0) {
+          issue_x(kt + RING, End());
+          issue_w(kt + RING, End());
+        }
+        frags(kt + 1, 0, 0);
+      }
+      if constexpr (PH == 2) mask_last(1);
+      multiply(1, 0, TI);
+    };
+    for (int kt = 0; kt < RING && kt < nk; kt++) {
+      issue_x(kt, End());
+      issue_w(kt, End());
+    }
+    if (nk >= RING) __builtin_amdgcn_s_waitcnt(0x0070 | ((RING - 1) * L & 15) | (((RING - 1) * L >> 4) << 14));
+    else wait_tiles(nk - 1);
+    __syncthreads();
+    frags(0, 0, 0);
+    int kt = 0;
+    for (; kt + RING < nk; kt++) step(kt, std::integral_constant<int, 0>());
+    for (; kt + 1 < nk; kt++) step(kt, std::integral_constant<int, 1>());
+    prefetch();
+    step(nk - 1, std::integral_constant<int, 2>());
   }
+
+  __syncthreads();   // every wave is done with the operand tiles
+  Channel* sc = (Channel*)smem;
+  if (tid < BN) sc[tid] = pre_c;
+  __syncthreads();
+  // block (i, j), register q: feature 16 i + 4 (lane / 16) + q, row 16 j + lane % 16. bf16: blocks i and i + 1 are regrouped so that a lane
+  // holds 8 adjacent features, stored with one 16-byte store, where y's rows are 16-byte aligned.
+  const bool pairs = sizeof(T) == 2 && a.N % 8 == 0 && a.y_row % 8 == 0 && (uintptr_t)a.y % 16 == 0;
+  const int pair_col = 16 * (lkc & 1) + 8 * (lkc >> 1);
+  auto values = [&](int i, int j, float* v) {
+    const int nl = wn * WTN + 16 * i + 4 * lkc;
 #pragma unroll
-  for (int j = 0; j < 2; j++) {
-    const int m = m0 + 32 * wm + 16 * j + r16;
+    for (int q = 0; q < 4; q++) v[q] = finish<ACT>(acc[i][j][q], pre_x[j], sc[nl + q]);
+  };
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-      const int n = n0 + 32 * wn + 16 * i + 4 * kq;
-      if (m < a.M && n < a.N) finish4<ACT, T>(a, acc[i][j], m, n);
+  for (int j = 0; j < TJ; j++) {
+    const int m = m0 + wm * WTM + 16 * j + frow;
+    if (m >= a.M) continue;   // the swap partners (lanes l and l ^ 16) share the row m
+    if (pairs) {
+#pragma unroll
+      for (int p = 0; p < TI / 2; p++) {
+        uint32_t w[2][2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          float v[4];
+          values(2 * p + e, j, v);
+          w[e][0] = pack_bf16x2(v[0], v[1]);
+          w[e][1] = pack_bf16x2(v[2], v[3]);
+        }
+        swap16(w[0][0], w[1][0]);
+        swap16(w[0][1], w[1][1]);
+        const int n = n0 + wn * WTN + 32 * p + pair_col;
+        if (n < a.N) *(uint4*)((u16*)a.y + (int64_t)m * a.y_row + n) = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < TI; i++) {
+        const int n = n0 + wn * WTN + 16 * i + 4 * lkc;
+        float v[4];
+        values(i, j, v);
+        if (n < a.N) store_features<T>(a, v, m, n);
+      }
     }
   }
 #endif
 }
 
-template <int ACT, typename T> hipError_t matmul(const Int8Args& a, hipStream_t s) {
-  const int64_t tiles = (int64_t)cdiv(a.M, 64) * cdiv(a.N, 64);
-  int8_tile64_kernel<ACT, T><<<8 * cdiv(tiles, 8), 256, 0, s>>>(a, (int)tiles);
+// B x B tile for few tiles: each of the 4 waves takes every 4th 128-byte slice of the whole tile, with two LDS stages of its own, so no barrier
+// stands in the k loop; the partial tiles meet in LDS. A quarter of the chain of the other forms per tile.
+template <int B, int ACT, typename T>
+__global__ void __launch_bounds__(256) int8_ksplit_kernel(const Int8Args a, int total_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int NB = B / 16, LD = B / 8, STAGE = 2 * B * 128;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int per = gridDim.x >> 3;
+  const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if (t >= total_tiles) return;
+  int tm, tn;
+  tile_coords(t, cdiv(a.M, B), cdiv(a.N, B), tm, tn);
+  const int m0 = tm * B, n0 = tn * B;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int K = a.K, nk = (K + 127) / 128;
+  const u32x4_t rx = rows_rsrc(a.x + (int64_t)m0 * a.x_row, min(B, a.M - m0), a.x_row, K);
+  const u32x4_t rw = rows_rsrc(a.w + (int64_t)n0 * a.w_row, min(B, a.N - n0), a.w_row, K);
+  uint32_t xoff[LD], woff[LD];
+#pragma unroll
+  for (int i = 0; i < LD; i++) {
+    const int r = 8 * i + (lane >> 3);
+    const uint32_t chunk = ((lane & 7) ^ swz(r)) * 16;
+    xoff[i] = m0 + r < a.M ? (uint32_t)(r * a.x_row) + chunk : OUTSIDE;
+    woff[i] = n0 + r < a.N ? (uint32_t)(r * a.w_row) + chunk : OUTSIDE;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + wave * 2 * STAGE;
+  auto issue = [&](int kt, int st) {
+    const uint32_t base = lds0 + st * STAGE;
+#pragma unroll
+    for (int i = 0; i < LD; i++) {
+      const bool in = kt * 128 + ((lane & 7) ^ swz(8 * i + (lane >> 3))) * 16 < K;
+      dma_b128(rx, base + i * 1024, in ? xoff[i] : OUTSIDE, kt * 128);
+      dma_b128(rw, base + B * 128 + i * 1024, in ? woff[i] : OUTSIDE, kt * 128);
+    }
+  };
+  const int r16 = lane & 15, kq = lane >> 4;
+  i32x4 acc[NB][NB];
+#pragma unroll
+  for (int i = 0; i < NB; i++)
+#pragma unroll
+    for (int j = 0; j < NB; j++) acc[i][j] = i32x4{0, 0, 0, 0};
+  if (wave < nk) issue(wave, 0);
+  if (wave + 4 < nk) issue(wave + 4, 1);
+  int st = 0;
+  for (int kt = wave; kt < nk; kt += 4) {
+    // this wave's slice kt has landed (the 2 LD loads of its next slice may be in flight)
+    if (kt + 4 >= nk) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else if (LD == 4) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    const char* sx = smem + wave * 2 * STAGE + st * STAGE;
+    const char* sw = sx + B * 128;
+    i32x4 fw[2][NB], fx[2][NB];
+#pragma unroll
+    for (int s = 0; s < 2; s++)
+#pragma unroll
+      for (int i = 0; i < NB; i++) {
+        const int r = 16 * i + r16;
+        fw[s][i] = *(const i32x4*)(sw + r * 128 + (((4 * s + kq) ^ swz(r)) << 4));
+        fx[s][i] = *(const i32x4*)(sx + r * 128 + (((4 * s + kq) ^ swz(r)) << 4));
+      }
+    if (kt + 8 < nk) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the fragments are in registers: the stage is free
+      issue(kt + 8, st);
+    }
+    if (kt + 1 == nk) {
+#pragma unroll
+      for (int s = 0; s < 2; s++) {
+        const i32x4 mask = row_mask(kt * 128 + 64 * s + 16 * kq, K);
+#pragma unroll
+        for (int i = 0; i < NB; i++) fx[s][i] &= mask;
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < 2; s++)
+#pragma unroll
+      for (int i = 0; i < NB; i++)
+#pragma unroll
+        for (int j = 0; j < NB; j++) acc[i][j] = mfma_i8(fw[s][i], fx[s][j], acc[i][j]);
+    st ^= 1;
+  }
+  __syncthreads();   // every wave's loads have landed and been read
+  i32x4* part = (i32x4*)smem;   // [block][wave][lane]
+#pragma unroll
+  for (int i = 0; i < NB; i++)
+#pragma unroll
+    for (int j = 0; j < NB; j++) part[((NB * i + j) * 4 + wave) * 64 + lane] = acc[i][j];
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < NB * NB / 4; q++) {
+    const int blk = wave * (NB * NB / 4) + q, i = blk / NB, j = blk % NB;
+    i32x4 c = part[(blk * 4) * 64 + lane];
+#pragma unroll
+    for (int g = 1; g < 4; g++) c += part[(blk * 4 + g) * 64 + lane];
+    const int m = m0 + 16 * j + r16, n = n0 + 16 * i + 4 * kq;
+    if (m < a.M && n < a.N) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) v[e] = finish<ACT>(c[e], a.x_scale[m], channel<T>(a, min(n + e, a.N - 1)));
+      store_features<T>(a, v, m, n);
+    }
+  }
+#endif
+}
+
+// Up to 16 MT rows: bound by reading w once. A workgroup takes 16 features, its waves share their k; w comes straight into registers, 64 bytes of
+// 16 rows per load, eight loads ahead, x from the L2.
+template <int MT, int WAVES, int ACT, typename T>
+__global__ void __launch_bounds__(WAVES * 64) int8_rows_kernel(const Int8Args a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ i32x4 part[MT][WAVES][64];
+  constexpr int AHEAD = 8;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n0 = blockIdx.x * 16, r16 = lane & 15, kq = lane >> 4, K = a.K;
+  const int8_t* w = a.w + (int64_t)min(n0 + r16, a.N - 1) * a.w_row;   // (rows past the end repeat the last and are not stored)
+  const int8_t* x[MT];
+#pragma unroll
+  for (int j = 0; j < MT; j++) x[j] = a.x + (int64_t)min(16 * j + r16, a.M - 1) * a.x_row;
+  i32x4 acc[MT];
+#pragma unroll
+  for (int j = 0; j < MT; j++) acc[j] = i32x4{0, 0, 0, 0};
+  const int steps = (K + 63) / 64;
+  auto load = [&](const int8_t* p, int step) {   // 16 bytes of step `step` of a row, zeros past its end
+    const int at = 64 * step + 16 * kq;
+    const i32x4 v = *(const i32x4*)(p + min(at, (K - 1) & ~15));
+    return v;
+  };
+  for (int s0 = wave; s0 < steps; s0 += AHEAD * WAVES) {
+    i32x4 fw[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; u++) fw[u] = load(w, min(s0 + u * WAVES, steps - 1));
+#pragma unroll
+    for (int u = 0; u < AHEAD; u++) {
+      const int step = s0 + u * WAVES;
+      const i32x4 mask = row_mask(64 * step + 16 * kq, K);   // all zeros past the end
+#pragma unroll
+      for (int j = 0; j < MT; j++) acc[j] = mfma_i8(fw[u], load(x[j], min(step, steps - 1)) & mask, acc[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < MT; j++) part[j][wave][lane] = acc[j];
+  __syncthreads();
+  if (wave >= MT) return;
+  i32x4 c = part[wave][0][lane];
+#pragma unroll
+  for (int g = 1; g < WAVES; g++) c += part[wave][g][lane];
+  const int m = 16 * wave + r16, n = n0 + 4 * kq;
+  if (m >= a.M || n >= a.N) return;
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; e++) v[e] = finish<ACT>(c[e], a.x_scale[m], channel<T>(a, min(n + e, a.N - 1)));
+  store_features<T>(a, v, m, n);
+#endif
+}
+
+enum Form { ROWS, KSPLIT_32, KSPLIT_64, RING_64, RING_128, LARGE_192, LARGE_256 };
+int64_t tiles_of(int M, int N, int bm, int bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn); }
+
+Form pick_form(int M, int N, int K) {
+  if (M <= 32) return ROWS;
+  const double kt = (K + 127) / 128;
+  const int64_t cus = cu_count();
+  auto rounds = [&](int bm, int bn, int64_t slots) { return (double)((tiles_of(M, N, bm, bn) + slots - 1) / slots); };
+  double best = rounds(256, 256, cus) * (1.2 * kt + 14.0);
+  Form pick = LARGE_256;
+  auto consider = [&](Form f, double cost) {
+    if (cost < best) best = cost, pick = f;
+  };
+  consider(LARGE_192, rounds(256, 192, cus) * 0.87 * (1.2 * kt + 14.0));
+  consider(RING_128, rounds(128, 128, cus) * (0.59 * kt + 7.0));
+  consider(KSPLIT_64, rounds(64, 64, cus) * (0.30 * kt + 7.0));
+  consider(KSPLIT_32, rounds(32, 32, 2 * cus) * (0.22 * kt + 3.0));
+  return pick;
+}
+
+template <int BM, int BN, int WM, int WN, int RING, int ACT, typename T> hipError_t launch_tiles(const Int8Args& a, hipStream_t s) {
+  constexpr size_t lds = RING == 0 ? (size_t)(2 * BN + 3 * BM) * 128 : (size_t)RING * (BM + BN) * 128;
+  static std::atomic<bool> attr_set[64] = {};
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(&int8_gemm_kernel<BM, BN, WM, WN, RING, ACT, T>), lds, attr_set);
+  if (e != hipSuccess) return e;
+  const int64_t tiles = tiles_of(a.M, a.N, BM, BN);
+  int8_gemm_kernel<BM, BN, WM, WN, RING, ACT, T><<<8 * cdiv(tiles, 8), WM * WN * 64, lds, s>>>(a, (int)tiles);
   return hipGetLastError();
+}
+template <int B, int ACT, typename T> hipError_t launch_ksplit(const Int8Args& a, hipStream_t s) {
+  constexpr size_t lds = (size_t)16 * B * 128;
+  static std::atomic<bool> attr_set[64] = {};
+  const hipError_t e = allow_lds(reinterpret_cast<const void*>(&int8_ksplit_kernel<B, ACT, T>), lds, attr_set);
+  if (e != hipSuccess) return e;
+  const int64_t tiles = tiles_of(a.M, a.N, B, B);
+  int8_ksplit_kernel<B, ACT, T><<<8 * cdiv(tiles, 8), 256, lds, s>>>(a, (int)tiles);
+  return hipGetLastError();
+}
+template <int WAVES, int ACT, typename T> hipError_t launch_rows(const Int8Args& a, hipStream_t s) {
+  if (a.M <= 16) int8_rows_kernel<1, WAVES, ACT, T><<<cdiv(a.N, 16), WAVES * 64, 0, s>>>(a);
+  else int8_rows_kernel<2, WAVES, ACT, T><<<cdiv(a.N, 16), WAVES * 64, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int ACT, typename T> hipError_t matmul(const Int8Args& a, hipStream_t s) {
+  switch (pick_form(a.M, a.N, a.K)) {
+    case ROWS: {
+      const int tiles = cdiv(a.N, 16), cus = cu_count();
+      if (tiles <= cus) return launch_rows<16, ACT, T>(a, s);
+      if (tiles <= 2 * cus) return launch_rows<8, ACT, T>(a, s);
+      return launch_rows<4, ACT, T>(a, s);
+    }
+    case KSPLIT_32: return launch_ksplit<32, ACT, T>(a, s);
+    case KSPLIT_64: return launch_ksplit<64, ACT, T>(a, s);
+    case RING_64: return launch_tiles<64, 64, 2, 2, 3, ACT, T>(a, s);
+    case RING_128: return launch_tiles<128, 128, 2, 4, 5, ACT, T>(a, s);
+    case LARGE_192: return launch_tiles<256, 192, 4, 2, 0, ACT, T>(a, s);
+    case LARGE_256: return launch_tiles<256, 256, 4, 2, 0, ACT, T>(a, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -296,7 +691,9 @@ hipError_t quantize_rows_launch(const QuantArgs& a, int dtype, hipStream_t s) {
   return dtype == DT_BF16 ? quantize_any<u16>(a, s) : quantize_any<float>(a, s);
 }
 
-int64_t int8_matmul_threads(int M, int N) { return 256 * 8 * (((int64_t)cdiv(M, 64) * cdiv(N, 64) + 7) / 8); }
+int64_t int8_matmul_threads(int M, int N) {
+  return M <= 32 ? 256 * std::max<int64_t>(cdiv(N, 16), 4 * cu_count()) : 256 * (tiles_of(M, N, 32, 32) + 8);
+}
 
 hipError_t int8_matmul_launch(const Int8Args& a, int dtype, int act, hipStream_t s) {
   if (dtype == DT_BF16) return act ? matmul<1, u16>(a, s) : matmul<0, u16>(a, s);
