@@ -1577,9 +1577,12 @@ dit_status check_int8_call(const dit_int8_config* c, bool given, const void* x, 
   return check_threads(int8_matmul_threads(c->rows, c->out_features));
 }
 
+// (raw, raw_row: rows that the product rounds by itself, in place of x and x_scale)
 dit_status run_int8_matmul(const dit_int8_config* c, const int8_t* x, int64_t x_row, const float* x_scale, const int8_t* w,
-                           const float* w_scale, const void* bias, void* y, hipStream_t s) {
+                           const float* w_scale, const void* bias, void* y, hipStream_t s, const void* raw = nullptr, int64_t raw_row = 0) {
   Int8Args a{};
+  a.raw = raw;
+  a.raw_row = raw_row;
   a.x = x;
   a.x_scale = x_scale;
   a.w = w;
@@ -1664,7 +1667,8 @@ dit_status quantize_rows(const void* x, int32_t rows, int32_t cols, int64_t x_ro
 
 size_t int8_matmul_workspace_bytes(const dit_int8_config* c) { return check_int8(c, true) ? 0 : 0; }
 size_t int8_linear_workspace_bytes(const dit_int8_config* c) {
-  return check_int8(c, false) || c->rows == 0 || c->out_features == 0 ? 0 : int8_layout(c).total;
+  if (check_int8(c, false) || c->rows == 0 || c->out_features == 0 || int8_takes_raw(c->rows, c->in_features)) return 0;
+  return int8_layout(c).total;
 }
 
 dit_status int8_matmul(const dit_int8_config* c, const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale,
@@ -1685,6 +1689,8 @@ dit_status int8_linear(const dit_int8_config* c, const void* x, const int8_t* w,
   if (st) return st;
   if (c->rows == 0 || c->out_features == 0) return DIT_OK;
   if ((st = check_int8_call(c, false, x, w, w_scale, bias, y))) return st;
+  if (int8_takes_raw(c->rows, c->in_features))
+    return run_int8_matmul(c, nullptr, 0, nullptr, w, w_scale, bias, y, hs(stream), x, c->x_row);
   if ((st = check_ws(ws, ws_bytes, int8_linear_workspace_bytes(c)))) return st;
   const Int8Ws L = int8_layout(c);
   float* x_scale = (float*)((char*)ws + L.scale);

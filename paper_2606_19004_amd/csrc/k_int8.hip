@@ -13,9 +13,9 @@ namespace {
 // rows to integers
 // ---------------------------------------------------------------------------
 // scale = max |x| / 127, correctly rounded and at least the smallest normal number, so that its reciprocal is finite.
-// q = the integer nearest to x / scale: r = rint(x (1 / scale)) is off by one at most, and only next to a half. What is left,
-// x - r scale, is exact in fp32: both are multiples of half a unit in the last place of scale, and their difference is below
-// 2^24 of these. Comparing it with scale / 2 decides, a tie for the even one.
+// q = the integer nearest to x / scale. x (1 / scale), rounded once to an integer, is that or its neighbour, which happens next to a half
+// only. What is left, x - q scale, is exact in fp32: both are multiples of half a unit in the last place of scale, and their
+// difference is below 2^24 of these. Where it is below scale / 2, q is right; elsewhere, which is rare, a tie goes to the even one.
 struct RowScale {
   float scale, inv, half;
   bool bad;   // the row holds a NaN or an infinity: scale NaN, integers 0
@@ -29,119 +29,174 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top) {
   r.half = 0.5f * r.scale;
   return r;
 }
-__device__ __forceinline__ float to_integer(float x, const RowScale& r) {
-  const float q = rintf(x * r.inv), left = fmaf(-q, r.scale, x), d = fabsf(left);
-  const bool odd = (int)q & 1;
-  return d > r.half || (d == r.half && odd) ? q + copysignf(1.f, left) : q;
-}
-__device__ __forceinline__ uint32_t pack4(const float* q) {
-  return ((uint32_t)(int)q[0] & 0xff) | ((uint32_t)(int)q[1] & 0xff) << 8 | ((uint32_t)(int)q[2] & 0xff) << 16 | (uint32_t)(int)q[3] << 24;
+constexpr float MAGIC = 12582912.f;   // 1.5 2^23: MAGIC + q has the integer q in its low bits
+// the low bytes of four words
+__device__ __forceinline__ uint32_t low_bytes(const float* t) {
+  const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(t[1]), __float_as_uint(t[0]), 0x0c0c0400u);
+  const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(t[3]), __float_as_uint(t[2]), 0x04000c0cu);
+  return lo | hi;
 }
 typedef unsigned u32x2_any1 __attribute__((ext_vector_type(2), aligned(1)));
 
-__device__ __forceinline__ uint32_t top_of(uint32_t top, const float* f) {
+// 8 successive elements of a row as they are stored, and the largest of their absolute values' bits
+template <typename T> struct Eight;
+template <> struct Eight<u16> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const u16* x) {
+    const u32x4_any2 u = *(const u32x4_any2*)x;
 #pragma unroll
-  for (int i = 0; i < 8; i++) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
-  return top;
-}
+    for (int i = 0; i < 4; i++) w[i] = u[i];
+  }
+  __device__ __forceinline__ void set(int i, u16 v) { w[i >> 1] = i & 1 ? w[i >> 1] | (uint32_t)v << 16 : v; }
+  __device__ __forceinline__ uint32_t top() const {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = __builtin_bit_cast(u16x2, w[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int i = 1; i < 4; i++) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    return (uint32_t)max(m[0], m[1]) << 16;
+  }
+  __device__ __forceinline__ void get(float* f) const { unpack8(w, f); }
+};
+template <> struct Eight<float> {
+  float v[8];
+  __device__ __forceinline__ void load(const float* x) { load8_any(x, v); }
+  __device__ __forceinline__ void set(int i, float f) { v[i] = f; }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+  }
+  __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+    for (int i = 0; i < 8; i++) f[i] = v[i];
+  }
+};
 template <typename T>
-__device__ __forceinline__ void load_row8(const T* x, int at, int cols, float* f) {
+__device__ __forceinline__ void load_row8(const T* x, int at, int cols, Eight<T>& e) {
   if (at + 8 <= cols) {
-    load8_any(x + at, f);
+    e.load(x + at);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++) f[i] = at + i < cols ? to_f32(x[at + i]) : 0.f;
+    for (int i = 0; i < 8; i++) e.set(i, at + i < cols ? x[at + i] : (T)0);
+  }
+}
+// t: MAGIC + q of 8 elements
+__device__ __forceinline__ void to_integers(const RowScale& r, const float* f, float* t) {
+  float far = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    t[i] = fmaf(f[i], r.inv, MAGIC);
+    far = fmaxf(far, fabsf(fmaf(MAGIC - t[i], r.scale, f[i])));
+  }
+  if (far >= r.half) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const float left = fmaf(MAGIC - t[i], r.scale, f[i]), d = fabsf(left);
+      if (d > r.half || (d == r.half && (__float_as_uint(t[i]) & 1))) t[i] += copysignf(1.f, left);
+    }
   }
 }
 template <typename T>
-__device__ __forceinline__ void store_row8(const RowScale& r, const float* f, int at, int cols, int8_t* q, T* values) {
-  float z[8], v[8];
+__device__ __forceinline__ void store_row8(const RowScale& r, const Eight<T>& e, int at, int cols, int8_t* q, T* values) {
+  if (at >= cols) return;
+  float f[8], t[8];
+  e.get(f);
+  to_integers(r, f, t);
+  if (r.bad) {
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    z[i] = r.bad ? 0.f : to_integer(f[i], r);
-    v[i] = r.bad ? NAN : z[i] * r.scale;
+    for (int i = 0; i < 8; i++) t[i] = MAGIC;
   }
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) v[i] = r.bad ? NAN : (t[i] - MAGIC) * r.scale;
   if (at + 8 <= cols) {
-    *(u32x2_any1*)(q + at) = u32x2_any1{pack4(z), pack4(z + 4)};
+    *(u32x2_any1*)(q + at) = u32x2_any1{low_bytes(t), low_bytes(t + 4)};
     if (values) store8_any(values + at, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; i++)
       if (at + i < cols) {
-        q[at + i] = (int8_t)(int)z[i];
+        q[at + i] = (int8_t)__float_as_uint(t[i]);
         if (values) values[at + i] = from_f32<T>(v[i]);
       }
   }
 }
-
-// LANES (64: a wave, 256: a workgroup) take a row, VECTORS x 8 elements each, in registers: one read.
-template <typename T, int LANES, int VECTORS>
-__global__ void __launch_bounds__(256) quantize_kernel(const QuantArgs a) {
-  __shared__ uint32_t red[4];
-  const int lane = threadIdx.x & (LANES - 1), per = 256 / LANES;
-  for (int64_t row = (int64_t)blockIdx.x * per + threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * per) {
-    const T* x = (const T*)a.x + row * a.x_row;
-    float f[VECTORS][8];
-    uint32_t top = 0;
+// the largest over LANES: part of a wave, or a workgroup of several
+template <int LANES> __device__ __forceinline__ uint32_t row_top(uint32_t top, uint32_t* red) {
+  constexpr int WAVES = LANES / 64;
 #pragma unroll
-    for (int k = 0; k < VECTORS; k++) load_row8(x, 8 * (lane + LANES * k), a.cols, f[k]);
-#pragma unroll
-    for (int k = 0; k < VECTORS; k++) top = top_of(top, f[k]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-    if (LANES == 256) {
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
-      __syncthreads();
-      top = max(max(red[0], red[1]), max(red[2], red[3]));
-    }
-    const RowScale r = row_scale(top);
-    if (lane == 0) a.scale[row] = r.bad ? NAN : r.scale;
-#pragma unroll
-    for (int k = 0; k < VECTORS; k++)
-      store_row8<T>(r, f[k], 8 * (lane + LANES * k), a.cols, a.q + row * a.q_row,
-                    a.values ? (T*)a.values + row * a.values_row : nullptr);
-  }
-}
-// Rows past 16384 elements: a workgroup reads them twice.
-template <typename T>
-__global__ void __launch_bounds__(256) quantize_long_kernel(const QuantArgs a) {
-  __shared__ uint32_t red[4];
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = (const T*)a.x + row * a.x_row;
-    uint32_t top = 0;
-    for (int64_t at = 8 * threadIdx.x; at < a.cols; at += 8 * 256) {
-      float f[8];
-      load_row8(x, (int)at, a.cols, f);
-      top = top_of(top, f);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  for (int o = LANES < 64 ? LANES / 2 : 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  if (WAVES > 1) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
     __syncthreads();
-    const RowScale r = row_scale(max(max(red[0], red[1]), max(red[2], red[3])));
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) top = max(top, red[w]);
+  }
+  return top;
+}
+
+// LANES (a wave or part of one, or a whole workgroup) take a row, VECTORS x 8 elements each, in registers: one read.
+template <typename T, int LANES, int VECTORS>
+__global__ void __launch_bounds__(LANES < 256 ? 256 : LANES) quantize_kernel(const QuantArgs a) {
+  __shared__ uint32_t red[LANES < 64 ? 1 : LANES / 64];
+  constexpr int PER = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup
+  const int lane = threadIdx.x % LANES;
+  for (int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * PER) {
+    const T* x = (const T*)a.x + row * a.x_row;
+    Eight<T> e[VECTORS];
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < VECTORS; k++) load_row8(x, 8 * (lane + LANES * k), a.cols, e[k]);
+#pragma unroll
+    for (int k = 0; k < VECTORS; k++) top = max(top, e[k].top());
+    const RowScale r = row_scale(row_top<LANES>(top, red));
+    if (lane == 0) a.scale[row] = r.bad ? NAN : r.scale;
+#pragma unroll
+    for (int k = 0; k < VECTORS; k++)
+      store_row8<T>(r, e[k], 8 * (lane + LANES * k), a.cols, a.q + row * a.q_row,
+                    a.values ? (T*)a.values + row * a.values_row : nullptr);
+  }
+}
+// Longer rows: a workgroup reads them twice.
+template <typename T>
+__global__ void __launch_bounds__(1024) quantize_long_kernel(const QuantArgs a) {
+  __shared__ uint32_t red[16];
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* x = (const T*)a.x + row * a.x_row;
+    Eight<T> e;
+    uint32_t top = 0;
+    for (int64_t at = 8 * threadIdx.x; at < a.cols; at += 8 * 1024) {
+      load_row8(x, (int)at, a.cols, e);
+      top = max(top, e.top());
+    }
+    const RowScale r = row_scale(row_top<1024>(top, red));
     if (threadIdx.x == 0) a.scale[row] = r.bad ? NAN : r.scale;
-    for (int64_t at = 8 * threadIdx.x; at < a.cols; at += 8 * 256) {
-      float f[8];
-      load_row8(x, (int)at, a.cols, f);
-      store_row8<T>(r, f, (int)at, a.cols, a.q + row * a.q_row, a.values ? (T*)a.values + row * a.values_row : nullptr);
+    for (int64_t at = 8 * threadIdx.x; at < a.cols; at += 8 * 1024) {
+      load_row8(x, (int)at, a.cols, e);
+      store_row8<T>(r, e, (int)at, a.cols, a.q + row * a.q_row, a.values ? (T*)a.values + row * a.values_row : nullptr);
     }
   }
 }
 
 template <typename T, int LANES, int VECTORS> void quantize(const QuantArgs& a, hipStream_t s) {
-  const int grid = (int)std::min<int64_t>(((int64_t)a.rows + 256 / LANES - 1) / (256 / LANES), 1 << 20);
-  quantize_kernel<T, LANES, VECTORS><<<grid, 256, 0, s>>>(a);
+  constexpr int PER = LANES < 256 ? 256 / LANES : 1;
+  const int grid = (int)std::min<int64_t>(((int64_t)a.rows + PER - 1) / PER, 1 << 20);
+  quantize_kernel<T, LANES, VECTORS><<<grid, LANES < 256 ? 256 : LANES, 0, s>>>(a);
 }
 template <typename T> hipError_t quantize_any(const QuantArgs& a, hipStream_t s) {
-  if (a.cols <= 512) quantize<T, 64, 1>(a, s);
+  if (a.cols <= 128) quantize<T, 16, 1>(a, s);
+  else if (a.cols <= 256) quantize<T, 32, 1>(a, s);
+  else if (a.cols <= 512) quantize<T, 64, 1>(a, s);
   else if (a.cols <= 1024) quantize<T, 64, 2>(a, s);
   else if (a.cols <= 2048) quantize<T, 256, 1>(a, s);
   else if (a.cols <= 4096) quantize<T, 256, 2>(a, s);
-  else if (a.cols <= 8192) quantize<T, 256, 4>(a, s);
-  else if (a.cols <= 16384) quantize<T, 256, 8>(a, s);
-  else quantize_long_kernel<T><<<std::min(a.rows, 1 << 20), 256, 0, s>>>(a);
+  else if (a.cols <= 8192) quantize<T, 512, 2>(a, s);
+  else if (a.cols <= 12288) quantize<T, 512, 3>(a, s);
+  else if (a.cols <= 16384) quantize<T, 512, 4>(a, s);
+  else if (a.cols <= 32768) quantize<T, 1024, 4>(a, s);
+  else quantize_long_kernel<T><<<std::min(a.rows, 1 << 20), 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -573,61 +628,147 @@ __global__ void __launch_bounds__(256) int8_ksplit_kernel(const Int8Args a, int 
 #endif
 }
 
-// Up to 16 MT rows: bound by reading w once. A workgroup takes 16 features, its waves share their k; w comes straight into registers, 64 bytes of
-// 16 rows per load, eight loads ahead, x from the L2.
-template <int MT, int WAVES, int ACT, typename T>
-__global__ void __launch_bounds__(WAVES * 64) int8_rows_kernel(const Int8Args a) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ i32x4 part[MT][WAVES][64];
-  constexpr int AHEAD = 8;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int n0 = blockIdx.x * 16, r16 = lane & 15, kq = lane >> 4, K = a.K;
-  const int8_t* w = a.w + (int64_t)min(n0 + r16, a.N - 1) * a.w_row;   // (rows past the end repeat the last and are not stored)
-  const int8_t* x[MT];
+// inclusive sum over the wave by VALU moves: the last lane has the total
+template <int CTRL, int ROWS> __device__ __forceinline__ int moved_up(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_total(int v) {
+  v += moved_up<0x111, 0xf>(v);
+  v += moved_up<0x112, 0xf>(v);
+  v += moved_up<0x114, 0xf>(v);
+  v += moved_up<0x118, 0xf>(v);
+  v += moved_up<0x142, 0xa>(v);
+  v += moved_up<0x143, 0xc>(v);
+  return v;
+}
+
+// One or two rows: bound by reading w once. A wave takes F features, 1 KB of each per step (16 bytes a lane), by v_dot4; x lies in LDS as
+// integers, zeros behind its end. SHARE: the four waves of a workgroup share the k of the same features (few features).
+// RAW: x comes in its own type and every workgroup rounds it by itself while its first weights are on their way: no launch before this one.
+constexpr int F = 4, STEP = 1024;
+constexpr int RAW_ELEMENTS = 16384;   // of all rows
+template <int ROWS, bool SHARE, bool RAW, int ACT, typename T>
+__global__ void __launch_bounds__(256) int8_few_rows_kernel(const Int8Args a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ int part[4][F][ROWS];
+  __shared__ uint32_t red[ROWS][4];
+  __shared__ float scales[ROWS];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int K = a.K, steps = (K + STEP - 1) / STEP, pad = steps * STEP;
+  const int n0 = blockIdx.x * (SHARE ? F : 4 * F), mine = SHARE ? n0 : n0 + wave * F;
+  const int8_t* w[F];
 #pragma unroll
-  for (int j = 0; j < MT; j++) x[j] = a.x + (int64_t)min(16 * j + r16, a.M - 1) * a.x_row;
-  i32x4 acc[MT];
+  for (int f = 0; f < F; f++) w[f] = a.w + (int64_t)min(mine + f, a.N - 1) * a.w_row;   // (features past the end repeat the last, unused)
+  constexpr int AHEAD = 4, STRIDE = SHARE ? 4 : 1;
+  const int first = SHARE ? wave : 0;
+  i32x4 fw[AHEAD][F];
+  auto load = [&](int step, i32x4* to) {
+    const int at = min(step * STEP + 16 * lane, (K - 1) & ~15);
 #pragma unroll
-  for (int j = 0; j < MT; j++) acc[j] = i32x4{0, 0, 0, 0};
-  const int steps = (K + 63) / 64;
-  auto load = [&](const int8_t* p, int step) {   // 16 bytes of step `step` of a row, zeros past its end
-    const int at = 64 * step + 16 * kq;
-    const i32x4 v = *(const i32x4*)(p + min(at, (K - 1) & ~15));
-    return v;
+    for (int f = 0; f < F; f++) to[f] = *(const i32x4*)(w[f] + at);
   };
-  for (int s0 = wave; s0 < steps; s0 += AHEAD * WAVES) {
-    i32x4 fw[AHEAD];
+  // (branch-free, so that what was requested before can be waited for alone; steps past the end repeat the last)
+  auto load_ahead = [&]() {
 #pragma unroll
-    for (int u = 0; u < AHEAD; u++) fw[u] = load(w, min(s0 + u * WAVES, steps - 1));
+    for (int u = 0; u < AHEAD; u++) load(min(first + u * STRIDE, steps - 1), fw[u]);
+  };
+
+  // x to LDS
+  if constexpr (RAW) {
+    constexpr int VECTORS = RAW_ELEMENTS / (ROWS * 2048);   // of 8 elements of a row that a thread holds
+    Eight<T> e[ROWS][VECTORS];
+#pragma unroll
+    for (int m = 0; m < ROWS; m++) {
+      const T* x = (const T*)a.raw + min(m, a.M - 1) * a.raw_row;
+#pragma unroll
+      for (int v = 0; v < VECTORS; v++) {
+        const int at = 8 * (tid + 256 * v);
+        if (K % 8 == 0) e[m][v].load(x + min(at, K - 8));   // (past the end: repeats the last ones, which does not change the largest)
+        else load_row8(x, at, K, e[m][v]);
+      }
+    }
+    load_ahead();
+#pragma unroll
+    for (int m = 0; m < ROWS; m++) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int v = 0; v < VECTORS; v++) top = max(top, e[m][v].top());
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+      if (lane == 0) red[m][wave] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < ROWS; m++) {
+      const RowScale r = row_scale(max(max(red[m][0], red[m][1]), max(red[m][2], red[m][3])));
+      if (tid == 0) scales[m] = r.bad ? NAN : r.scale;
+#pragma unroll
+      for (int v = 0; v < VECTORS; v++) {
+        const int at = 8 * (tid + 256 * v);
+        if (at >= pad) break;
+        float f[8], t[8];
+        e[m][v].get(f);
+        to_integers(r, f, t);
+        const bool none = r.bad || at >= K;   // (K % 8: the elements past the end were read as zeros)
+        *(uint2*)(smem + m * pad + at) = none ? make_uint2(0, 0) : make_uint2(low_bytes(t), low_bytes(t + 4));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int m = 0; m < ROWS; m++) {
+      const int8_t* x = a.x + min(m, a.M - 1) * a.x_row;
+      for (int at = 16 * tid; at < pad; at += 16 * 256)
+        *(i32x4*)(smem + m * pad + at) = *(const i32x4*)(x + min(at, (K - 1) & ~15)) & row_mask(at, K);
+      if (tid == 0) scales[m] = a.x_scale[min(m, a.M - 1)];
+    }
+    load_ahead();
+  }
+  __syncthreads();
+
+  int acc[F][ROWS];
+#pragma unroll
+  for (int f = 0; f < F; f++)
+#pragma unroll
+    for (int m = 0; m < ROWS; m++) acc[f][m] = 0;
+  for (int s = first; s < steps; s += AHEAD * STRIDE) {
 #pragma unroll
     for (int u = 0; u < AHEAD; u++) {
-      const int step = s0 + u * WAVES;
-      const i32x4 mask = row_mask(64 * step + 16 * kq, K);   // all zeros past the end
+      const int step = s + u * STRIDE;
+      if (step < steps) {
 #pragma unroll
-      for (int j = 0; j < MT; j++) acc[j] = mfma_i8(fw[u], load(x[j], min(step, steps - 1)) & mask, acc[j]);
+        for (int m = 0; m < ROWS; m++) {
+          const i32x4 x = *(const i32x4*)(smem + m * pad + step * STEP + 16 * lane);
+#pragma unroll
+          for (int f = 0; f < F; f++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) acc[f][m] = __builtin_amdgcn_sdot4(fw[u][f][i], x[i], acc[f][m], false);
+        }
+        if (step + AHEAD * STRIDE < steps) load(step + AHEAD * STRIDE, fw[u]);
+      }
     }
   }
 #pragma unroll
-  for (int j = 0; j < MT; j++) part[j][wave][lane] = acc[j];
+  for (int f = 0; f < F; f++)
+#pragma unroll
+    for (int m = 0; m < ROWS; m++) {
+      const int total = wave_total(acc[f][m]);
+      if (lane == 63) part[wave][f][m] = total;
+    }
   __syncthreads();
-  if (wave >= MT) return;
-  i32x4 c = part[wave][0][lane];
-#pragma unroll
-  for (int g = 1; g < WAVES; g++) c += part[wave][g][lane];
-  const int m = 16 * wave + r16, n = n0 + 4 * kq;
+  constexpr int WIDTH = SHARE ? F : 4 * F;   // features of the workgroup
+  if (tid >= WIDTH * ROWS) return;
+  const int m = tid / WIDTH, f = tid % WIDTH, n = n0 + f;
   if (m >= a.M || n >= a.N) return;
-  float v[4];
-#pragma unroll
-  for (int e = 0; e < 4; e++) v[e] = finish<ACT>(c[e], a.x_scale[m], channel<T>(a, min(n + e, a.N - 1)));
-  store_features<T>(a, v, m, n);
-#endif
+  const int sum = SHARE ? part[0][f][m] + part[1][f][m] + part[2][f][m] + part[3][f][m] : part[f / F][f % F][m];
+  ((T*)a.y)[(int64_t)m * a.y_row + n] = from_f32<T>(finish<ACT>(sum, scales[m], channel<T>(a, n)));
 }
 
-enum Form { ROWS, KSPLIT_32, KSPLIT_64, RING_64, RING_128, LARGE_192, LARGE_256 };
+enum Form { FEW_ROWS, KSPLIT_32, KSPLIT_64, RING_64, RING_128, LARGE_192, LARGE_256 };
 int64_t tiles_of(int M, int N, int bm, int bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn); }
 
+// rows of x in LDS
+size_t few_rows_lds(int M, int K) { return (size_t)M * ((K + STEP - 1) / STEP * STEP); }
+
 Form pick_form(int M, int N, int K) {
-  if (M <= 32) return ROWS;
+  if (M <= 2 && few_rows_lds(M, K) <= 61440) return FEW_ROWS;
   const double kt = (K + 127) / 128;
   const int64_t cus = cu_count();
   auto rounds = [&](int bm, int bn, int64_t slots) { return (double)((tiles_of(M, N, bm, bn) + slots - 1) / slots); };
@@ -661,20 +802,19 @@ template <int B, int ACT, typename T> hipError_t launch_ksplit(const Int8Args& a
   int8_ksplit_kernel<B, ACT, T><<<8 * cdiv(tiles, 8), 256, lds, s>>>(a, (int)tiles);
   return hipGetLastError();
 }
-template <int WAVES, int ACT, typename T> hipError_t launch_rows(const Int8Args& a, hipStream_t s) {
-  if (a.M <= 16) int8_rows_kernel<1, WAVES, ACT, T><<<cdiv(a.N, 16), WAVES * 64, 0, s>>>(a);
-  else int8_rows_kernel<2, WAVES, ACT, T><<<cdiv(a.N, 16), WAVES * 64, 0, s>>>(a);
+template <int ROWS, bool RAW, int ACT, typename T> hipError_t launch_few(const Int8Args& a, hipStream_t s) {
+  const size_t lds = few_rows_lds(a.M, a.K);
+  if (cdiv(a.N, 4 * F) >= 2 * cu_count()) int8_few_rows_kernel<ROWS, false, RAW, ACT, T><<<cdiv(a.N, 4 * F), 256, lds, s>>>(a);
+  else int8_few_rows_kernel<ROWS, true, RAW, ACT, T><<<cdiv(a.N, F), 256, lds, s>>>(a);
   return hipGetLastError();
+}
+template <bool RAW, int ACT, typename T> hipError_t launch_few_rows(const Int8Args& a, hipStream_t s) {
+  return a.M == 1 ? launch_few<1, RAW, ACT, T>(a, s) : launch_few<2, RAW, ACT, T>(a, s);
 }
 
 template <int ACT, typename T> hipError_t matmul(const Int8Args& a, hipStream_t s) {
   switch (pick_form(a.M, a.N, a.K)) {
-    case ROWS: {
-      const int tiles = cdiv(a.N, 16), cus = cu_count();
-      if (tiles <= cus) return launch_rows<16, ACT, T>(a, s);
-      if (tiles <= 2 * cus) return launch_rows<8, ACT, T>(a, s);
-      return launch_rows<4, ACT, T>(a, s);
-    }
+    case FEW_ROWS: return launch_few_rows<false, ACT, T>(a, s);
     case KSPLIT_32: return launch_ksplit<32, ACT, T>(a, s);
     case KSPLIT_64: return launch_ksplit<64, ACT, T>(a, s);
     case RING_64: return launch_tiles<64, 64, 2, 2, 3, ACT, T>(a, s);
@@ -692,10 +832,16 @@ hipError_t quantize_rows_launch(const QuantArgs& a, int dtype, hipStream_t s) {
 }
 
 int64_t int8_matmul_threads(int M, int N) {
-  return M <= 32 ? 256 * std::max<int64_t>(cdiv(N, 16), 4 * cu_count()) : 256 * (tiles_of(M, N, 32, 32) + 8);
+  return M <= 2 ? 256 * std::max<int64_t>(cdiv(N, 4 * F), 2 * cu_count()) : 256 * (tiles_of(M, N, 32, 32) + 8);
 }
 
+bool int8_takes_raw(int M, int K) { return M <= 2 && (int64_t)M * K <= RAW_ELEMENTS; }
+
 hipError_t int8_matmul_launch(const Int8Args& a, int dtype, int act, hipStream_t s) {
+  if (a.raw) {
+    if (dtype == DT_BF16) return act ? launch_few_rows<true, 1, u16>(a, s) : launch_few_rows<true, 0, u16>(a, s);
+    return act ? launch_few_rows<true, 1, float>(a, s) : launch_few_rows<true, 0, float>(a, s);
+  }
   if (dtype == DT_BF16) return act ? matmul<1, u16>(a, s) : matmul<0, u16>(a, s);
   return act ? matmul<1, float>(a, s) : matmul<0, float>(a, s);
 }

@@ -14,33 +14,34 @@ constexpr int THREADS = 256;
 
 // ---- tables of tensors ----
 // first[e]: the workgroup that takes tensor e's first chunk; unused entries are past every workgroup.
-// A launch's arguments stay below 4 KB: 192 gradients, 64 weights.
-constexpr int GRADS = 192, WEIGHTS = 64;
-struct GradTable {
-  void* data[GRADS];
-  int64_t count[GRADS];   // elements, bf16 ones negated
-  int first[GRADS];
+// A launch's arguments stay below 4 KB: 192 gradients, 64 weights. Short lists take smaller tables, which the host copies faster.
+constexpr int GRADS = 192, WEIGHTS = 64, FEW = 24;
+template <int N> struct GradTable {
+  void* data[N];
+  int64_t count[N];   // elements, bf16 ones negated
+  int first[N];
 };
-struct WeightTable {
-  void* param[WEIGHTS];
-  const void* grad[WEIGHTS];
-  float* m[WEIGHTS];
-  float* v[WEIGHTS];
-  void* copy[WEIGHTS];
-  int64_t count[WEIGHTS];
-  int first[WEIGHTS];
-  int types[WEIGHTS];     // bit 0: bf16 param, bit 1: bf16 grad
+template <int N> struct WeightTable {
+  void* param[N];
+  const void* grad[N];
+  float* m[N];
+  float* v[N];
+  void* copy[N];
+  int64_t count[N];
+  int first[N];
+  int types[N];       // bit 0: bf16 param, bit 1: bf16 grad
 };
-static_assert(sizeof(GradTable) + 64 <= 4096 && sizeof(WeightTable) + 96 <= 4096, "a launch's arguments");
+static_assert(sizeof(GradTable<GRADS>) + 64 <= 4096 && sizeof(WeightTable<WEIGHTS>) + 96 <= 4096, "a launch's arguments");
 
 // The tensor that workgroup b works on: every lane looks at entries of its own, so that the search is one load long.
 template <int N> __device__ __forceinline__ int entry_of(const int* first, int b) {
+  constexpr int LOADS = (N + 63) / 64;
   const int lane = threadIdx.x & 63;
-  int f[N / 64], e = -1;
+  int f[LOADS], e = -1;
 #pragma unroll
-  for (int i = 0; i < N / 64; i++) f[i] = first[64 * i + lane];
+  for (int i = 0; i < LOADS; i++) f[i] = first[min(64 * i + lane, N - 1)];
 #pragma unroll
-  for (int i = 0; i < N / 64; i++) e += __popcll(__ballot(f[i] <= b));
+  for (int i = 0; i < LOADS; i++) e += __popcll(__ballot(64 * i + lane < N && f[i] <= b));
   return e;
 }
 
@@ -82,9 +83,10 @@ template <typename T> __device__ double chunk_squares(const T* p, int64_t begin,
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-__global__ void __launch_bounds__(THREADS) norm_kernel(const GradTable t, int64_t chunk, double* parts) {
+template <int N>
+__global__ void __launch_bounds__(THREADS) norm_kernel(const GradTable<N> t, int64_t chunk, double* parts) {
   __shared__ double red[THREADS / 64];
-  const int b = blockIdx.x, e = entry_of<GRADS>(t.first, b);
+  const int b = blockIdx.x, e = entry_of<N>(t.first, b);
   const int64_t n = t.count[e], count = n < 0 ? -n : n;
   const int64_t begin = (b - t.first[e]) * chunk, end = min(begin + chunk, count);
   double s = n < 0 ? chunk_squares((const u16*)t.data[e], begin, end) : chunk_squares((const float*)t.data[e], begin, end);
@@ -96,8 +98,13 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const GradTable t, int64_
 
 __global__ void __launch_bounds__(1024) norm_finish_kernel(const double* parts, int64_t n, double max_norm, double* norm, float* scale) {
   __shared__ double red[16];
-  double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 1024) s += parts[i];
+  double p[8], s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += 8 * 1024) {   // eight loads in flight; what is past the end reads the last and does not count
+#pragma unroll
+    for (int u = 0; u < 8; u++) p[u] = parts[min(i + 1024 * u, n - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; u++) s += i + 1024 * u < n ? p[u] : 0.0;
+  }
   s = wave_sum64(s);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -124,10 +131,11 @@ template <typename T> __device__ void chunk_scale(T* p, int64_t begin, int64_t e
     }
   }
 }
-__global__ void __launch_bounds__(THREADS) clip_kernel(const GradTable t, int64_t chunk, const float* scale) {
+template <int N>
+__global__ void __launch_bounds__(THREADS) clip_kernel(const GradTable<N> t, int64_t chunk, const float* scale) {
   const float k = *scale;
   if (k == 1.f) return;
-  const int b = blockIdx.x, e = entry_of<GRADS>(t.first, b);
+  const int b = blockIdx.x, e = entry_of<N>(t.first, b);
   const int64_t n = t.count[e], count = n < 0 ? -n : n;
   const int64_t begin = (b - t.first[e]) * chunk, end = min(begin + chunk, count);
   if (n < 0) chunk_scale((u16*)t.data[e], begin, end, k);
@@ -184,10 +192,11 @@ __device__ void chunk_adam(const Adam& a, float k, P* p, const G* g, float* m, f
     }
   }
 }
-__global__ void __launch_bounds__(THREADS) adamw_kernel(const WeightTable t, int64_t chunk, const AdamArgs args) {
+template <int N>
+__global__ void __launch_bounds__(THREADS) adamw_kernel(const WeightTable<N> t, int64_t chunk, const AdamArgs args) {
   const float k = args.scale ? *args.scale : 1.f;
   if (k != k) return;
-  const int b = blockIdx.x, e = entry_of<WEIGHTS>(t.first, b);
+  const int b = blockIdx.x, e = entry_of<N>(t.first, b);
   const int64_t begin = (b - t.first[e]) * chunk, end = min(begin + chunk, t.count[e]);
   Adam a = args.a;
   if (args.step_dev) set_step(a, (double)*args.step_dev, args.lr, args.log_beta1, args.log_beta2);
@@ -206,12 +215,12 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const WeightTable t, int
 int64_t chunks_of(int64_t count, int64_t chunk) { return (count + chunk - 1) / chunk; }
 
 // Tables of successive tensors that have elements, a launch for each: launch(table, workgroups).
-template <typename F> hipError_t for_each_table(const dit_gradient* g, int n, int64_t chunk, F&& launch) {
+template <int N, typename F> hipError_t for_each_table(const dit_gradient* g, int n, int64_t chunk, F&& launch) {
   for (int i = 0; i < n;) {
-    GradTable t;
+    GradTable<N> t{};
     int used = 0;
     int64_t blocks = 0;
-    for (; i < n && used < GRADS; i++) {
+    for (; i < n && used < N; i++) {
       if (g[i].count == 0) continue;
       t.data[used] = g[i].data;
       t.count[used] = g[i].dtype == DIT_BF16 ? -g[i].count : g[i].count;
@@ -219,12 +228,47 @@ template <typename F> hipError_t for_each_table(const dit_gradient* g, int n, in
       blocks += chunks_of(g[i].count, chunk);
     }
     if (used == 0) break;
-    for (int k = used; k < GRADS; k++) {
-      t.data[k] = nullptr;
-      t.count[k] = 0;
-      t.first[k] = 0x7fffffff;
-    }
+    for (int k = used; k < N; k++) t.first[k] = 0x7fffffff;
     const hipError_t e = launch(t, (int)blocks);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <int N> hipError_t norm_sums(const dit_gradient* g, int n, int64_t chunk, double* parts, hipStream_t s) {
+  return for_each_table<N>(g, n, chunk, [&](const GradTable<N>& t, int blocks) {
+    norm_kernel<N><<<blocks, THREADS, 0, s>>>(t, chunk, parts);
+    parts += blocks;
+    return hipGetLastError();
+  });
+}
+template <int N> hipError_t clip(const dit_gradient* g, int n, int64_t chunk, const float* scale, hipStream_t s) {
+  return for_each_table<N>(g, n, chunk, [&](const GradTable<N>& t, int blocks) {
+    clip_kernel<N><<<blocks, THREADS, 0, s>>>(t, chunk, scale);
+    return hipGetLastError();
+  });
+}
+template <int N> hipError_t adamw(const AdamArgs& a, const dit_adamw_tensor* w, int n, int64_t chunk, hipStream_t s) {
+  for (int i = 0; i < n;) {
+    WeightTable<N> t{};
+    int used = 0;
+    int64_t blocks = 0;
+    for (; i < n && used < N; i++) {
+      if (w[i].count == 0) continue;
+      t.param[used] = w[i].param;
+      t.grad[used] = w[i].grad;
+      t.m[used] = w[i].m;
+      t.v[used] = w[i].v;
+      t.copy[used] = w[i].copy;
+      t.count[used] = w[i].count;
+      t.types[used] = (w[i].param_dtype == DIT_BF16) | (w[i].grad_dtype == DIT_BF16) << 1;
+      t.first[used++] = (int)blocks;
+      blocks += chunks_of(w[i].count, chunk);
+    }
+    if (used == 0) break;
+    for (int k = used; k < N; k++) t.first[k] = 0x7fffffff;
+    adamw_kernel<N><<<(int)blocks, THREADS, 0, s>>>(t, chunk, a);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -239,11 +283,7 @@ int64_t grad_norm_parts(const dit_gradient* g, int n, int64_t chunk) {
 }
 
 hipError_t grad_norm_sums(const dit_gradient* g, int n, int64_t chunk, double* parts, hipStream_t s) {
-  return for_each_table(g, n, chunk, [&](const GradTable& t, int blocks) {
-    norm_kernel<<<blocks, THREADS, 0, s>>>(t, chunk, parts);
-    parts += blocks;
-    return hipGetLastError();
-  });
+  return n <= FEW ? norm_sums<FEW>(g, n, chunk, parts, s) : norm_sums<GRADS>(g, n, chunk, parts, s);
 }
 
 hipError_t grad_norm_finish(const double* parts, int64_t nparts, double max_norm, double* norm, float* scale, hipStream_t s) {
@@ -252,10 +292,7 @@ hipError_t grad_norm_finish(const double* parts, int64_t nparts, double max_norm
 }
 
 hipError_t grad_clip_launch(const dit_gradient* g, int n, int64_t chunk, const float* scale, hipStream_t s) {
-  return for_each_table(g, n, chunk, [&](const GradTable& t, int blocks) {
-    clip_kernel<<<blocks, THREADS, 0, s>>>(t, chunk, scale);
-    return hipGetLastError();
-  });
+  return n <= FEW ? clip<FEW>(g, n, chunk, scale, s) : clip<GRADS>(g, n, chunk, scale, s);
 }
 
 hipError_t adamw_launch(const dit_adamw_config& c, const dit_adamw_tensor* w, int n, int64_t chunk, const float* scale,
@@ -264,29 +301,7 @@ hipError_t adamw_launch(const dit_adamw_config& c, const dit_adamw_tensor* w, in
               (float)(1.0 - c.lr * c.weight_decay), 0.f, 0.f},
              step_dev, c.lr, std::log(c.beta1), std::log(c.beta2), scale};
   set_step(a.a, (double)c.step, c.lr, a.log_beta1, a.log_beta2);
-  for (int i = 0; i < n;) {
-    WeightTable t{};
-    int used = 0;
-    int64_t blocks = 0;
-    for (; i < n && used < WEIGHTS; i++) {
-      if (w[i].count == 0) continue;
-      t.param[used] = w[i].param;
-      t.grad[used] = w[i].grad;
-      t.m[used] = w[i].m;
-      t.v[used] = w[i].v;
-      t.copy[used] = w[i].copy;
-      t.count[used] = w[i].count;
-      t.types[used] = (w[i].param_dtype == DIT_BF16) | (w[i].grad_dtype == DIT_BF16) << 1;
-      t.first[used++] = (int)blocks;
-      blocks += chunks_of(w[i].count, chunk);
-    }
-    if (used == 0) break;
-    for (int k = used; k < WEIGHTS; k++) t.first[k] = 0x7fffffff;
-    adamw_kernel<<<(int)blocks, THREADS, 0, s>>>(t, chunk, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  return n <= FEW ? adamw<FEW>(a, w, n, chunk, s) : adamw<WEIGHTS>(a, w, n, chunk, s);
 }
 
 }  // namespace dit

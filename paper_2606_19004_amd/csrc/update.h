@@ -25,8 +25,10 @@ struct Int8Args {
   const int8_t* x; const float* x_scale; const int8_t* w; const float* w_scale; const void* bias; void* y;
   int M, N, K;
   int64_t x_row, w_row, y_row;
+  const void* raw; int64_t raw_row;   // rows that are not integers yet, in place of x and x_scale (where int8_takes_raw), or null
 };
 int64_t int8_matmul_threads(int M, int N);   // of the largest launch: one takes fewer than 2^32
+bool int8_takes_raw(int M, int K);           // whether a product rounds its few rows by itself
 hipError_t int8_matmul_launch(const Int8Args& a, int dtype, int act, hipStream_t s);
 
 }  // namespace dit

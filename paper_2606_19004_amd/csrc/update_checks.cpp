@@ -33,7 +33,7 @@ dit_status check_count(int64_t count, int32_t i, int64_t* total) {
 
 int64_t update_chunk(int64_t total) {
   const int64_t unit = 2048;
-  return unit * std::max<int64_t>(2, (total + unit * 8192 - 1) / (unit * 8192));
+  return unit * std::max<int64_t>(1, (total + unit * 8192 - 1) / (unit * 8192));
 }
 
 dit_status check_gradients(const dit_gradient* g, int32_t n, bool data, int64_t* total) {

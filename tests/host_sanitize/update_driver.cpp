@@ -33,7 +33,7 @@ void lists() {
       EXPECT(ok == (a >= 0 && b >= 0 && a <= (int64_t)1 << 44 && b <= ((int64_t)1 << 44) - a));
       if (!ok) continue;
       const int64_t chunk = update_chunk(total);
-      EXPECT(chunk % 2048 == 0 && chunk >= 4096 && (total + chunk - 1) / chunk <= 8192);
+      EXPECT(chunk % 2048 == 0 && chunk >= 2048 && (total + chunk - 1) / chunk <= 8192);
       dit_adamw_config c{1e-3, 0.9, 0.999, 1e-8, 0.0, 1};
       dit_adamw_tensor t[2] = {{x, x, x, x, nullptr, a, DIT_F32, DIT_F32}, {x, x, x, x, x, b, DIT_BF16, DIT_BF16}};
       EXPECT(check_adamw(&c, t, 2, false, &total) == DIT_OK);

@@ -71,7 +71,7 @@ class Problem:
         assert off.max() <= 0, off.max()
 
 
-SIZES = [(1, 1, 1), (1, 16, 16), (1, 100, 3), (2, 17, 5), (1, 3072, 640), (3, 128, 64), (5, 129, 65), (16, 1000, 100), (17, 64, 33), (31, 255, 127),
+SIZES = [(1, 1, 1), (1, 16, 16), (1, 5000, 9000), (2, 1024, 4200), (2, 1025, 77), (4, 3000, 8200), (6, 4097, 40), (8, 2048, 8300), (8, 7680, 21), (8, 7681, 21), (9, 640, 50), (1, 100, 3), (2, 17, 5), (1, 3072, 640), (3, 128, 64), (5, 129, 65), (16, 1000, 100), (17, 64, 33), (31, 255, 127),
          (33, 333, 129), (64, 512, 64), (65, 127, 257), (100, 2050, 48), (127, 384, 130), (128, 256, 128), (129, 640, 513), (255, 1001, 515),
          (256, 768, 256), (300, 4096, 320), (520, 300, 1030), (1000, 160, 72), (1300, 90, 700)]
 
@@ -114,7 +114,8 @@ def test_scales_that_are_not_finite(d, M):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("M,K,N,act", [(1, 3072, 384, "none"), (1, 77, 9, "gelu"), (4, 1000, 100, "gelu"), (20, 513, 70, "none"), (130, 2049, 257, "gelu"),
+@pytest.mark.parametrize("M,K,N,act", [(1, 3072, 384, "none"), (1, 16384, 40, "none"), (1, 16385, 40, "gelu"), (2, 8192, 33, "gelu"), (3, 4096, 8200, "none"),
+                                       (3, 5461, 9, "gelu"), (4, 4096, 20, "none"), (8, 2048, 8210, "gelu"), (7, 1033, 50, "none"), (8, 2049, 30, "none"), (1, 77, 9, "gelu"), (4, 1000, 100, "gelu"), (20, 513, 70, "none"), (130, 2049, 257, "gelu"),
                                        (300, 20000, 33, "none"), (600, 256, 512, "gelu")])
 def test_linear_is_the_product_of_rounded_rows(d, M, K, N, act, dtype):
     """Bit for bit, with x at a row stride of its own."""
