@@ -769,18 +769,25 @@ size_t few_rows_lds(int M, int K) { return (size_t)M * ((K + STEP - 1) / STEP * 
 
 Form pick_form(int M, int N, int K) {
   if (M <= 2 && few_rows_lds(M, K) <= 61440) return FEW_ROWS;
+  // Estimated times, us. What a CU takes per k-tile: 1.25 for a 256 x 256 tile (near the matrix rate), 0.5 for 128 x 128 and 0.24 for 64 x 64
+  // (LDS reads), 0.23 and 0.09 for those whose waves share k; beside it each round's first loads and stores. Measured (us, in this order: 32 and 64
+  // with shared k, 64, 128, 256 x 192, 256): 128 x 12288 -> 3072: 19 / 22 / 28 / 48 / 77 / 97; 333 x 3072 -> 9216: 35 / 35 / 22 / 16 / 25 / 31;
+  // 512 x 4096 -> 4096: 26 / 21 / 16 / 20 / 31 / 38; 1280 x 3072 -> 9216: 120 / 116 / 69 / 56 / 35 / 38; 1280 x 12288 -> 3072:
+  // 137 / 100 / 94 / 62 / 98 / 117; 20480 x 3072 -> 12288: 2307 / 2043 / 1181 / 962 / 640 / 610.
   const double kt = (K + 127) / 128;
   const int64_t cus = cu_count();
-  auto rounds = [&](int bm, int bn, int64_t slots) { return (double)((tiles_of(M, N, bm, bn) + slots - 1) / slots); };
-  double best = rounds(256, 256, cus) * (1.2 * kt + 14.0);
+  auto rounds = [&](int bm, int bn) { return (double)((tiles_of(M, N, bm, bn) + cus - 1) / cus); };
+  auto shares = [&](int b, double slots) { return std::max(1.0, tiles_of(M, N, b, b) / (slots * cus)); };
+  double best = rounds(256, 256) * (1.25 * kt + 11.0);
   Form pick = LARGE_256;
   auto consider = [&](Form f, double cost) {
     if (cost < best) best = cost, pick = f;
   };
-  consider(LARGE_192, rounds(256, 192, cus) * 0.87 * (1.2 * kt + 14.0));
-  consider(RING_128, rounds(128, 128, cus) * (0.59 * kt + 7.0));
-  consider(KSPLIT_64, rounds(64, 64, cus) * (0.30 * kt + 7.0));
-  consider(KSPLIT_32, rounds(32, 32, 2 * cus) * (0.22 * kt + 3.0));
+  consider(LARGE_192, rounds(256, 192) * 0.87 * (1.25 * kt + 11.0));
+  consider(RING_128, rounds(128, 128) * (0.5 * kt + 4.5));
+  consider(RING_64, 3.0 + kt * std::max(0.27, 0.235 * shares(64, 1)));
+  consider(KSPLIT_64, rounds(64, 64) * (0.23 * kt + 3.0));
+  consider(KSPLIT_32, 2.5 + shares(32, 2) * (0.185 * kt + 0.7));
   return pick;
 }
 
@@ -818,7 +825,7 @@ template <int ACT, typename T> hipError_t matmul(const Int8Args& a, hipStream_t 
     case KSPLIT_32: return launch_ksplit<32, ACT, T>(a, s);
     case KSPLIT_64: return launch_ksplit<64, ACT, T>(a, s);
     case RING_64: return launch_tiles<64, 64, 2, 2, 3, ACT, T>(a, s);
-    case RING_128: return launch_tiles<128, 128, 2, 4, 5, ACT, T>(a, s);
+    case RING_128: return launch_tiles<128, 128, 2, 4, 4, ACT, T>(a, s);
     case LARGE_192: return launch_tiles<256, 192, 4, 2, 0, ACT, T>(a, s);
     case LARGE_256: return launch_tiles<256, 256, 4, 2, 0, ACT, T>(a, s);
   }

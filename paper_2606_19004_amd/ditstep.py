@@ -634,20 +634,27 @@ def _rows_of(t, name, dtypes):
         raise ValueError(f"{name} is of {t.dtype}")
 
 
+_ROW_CODES = {torch.bfloat16: DIT_BF16, torch.float32: DIT_F32}
+
+
 def quantize_rows(x, q, scale, values=None, stream=None):
     """x [rows][cols] bf16 or fp32 -> q (int8, the same shape), scale (fp32 [rows]) and, if given, values (x's type and shape): what q and
     scale stand for. Row strides are free."""
-    dev = _current_device()
-    _rows_of(x, "x", _FLOATS)
-    _rows_of(q, "q", (torch.int8,))
-    for t in (x, q) if values is None else (x, q, values):
-        if t.shape != x.shape or t.get_device() != dev:
-            raise ValueError(f"a tensor of shape {tuple(t.shape)} on {t.device} for x of {tuple(x.shape)} in a call on cuda:{dev}")
-    if values is not None:
-        _rows_of(values, "values", (x.dtype,))
-    rows, cols = x.shape
-    _check(_lib.quantize_rows(_ptr(x), rows, cols, _row_stride(x), _dtype_code(x.dtype), _ptr(q), _row_stride(q),
-                              _dense(scale, dev, torch.float32, rows), _ptr(values), 0 if values is None else _row_stride(values), _s(stream)))
+    dev, shape, dt = _current_device(), x.shape, x.dtype
+    for t, want in ((x, dt), (q, torch.int8)) if values is None else ((x, dt), (q, torch.int8), (values, dt)):
+        if t.shape != shape or t.dtype is not want or t.get_device() != dev:
+            raise ValueError(f"a tensor of {t.dtype}, shape {tuple(t.shape)}, on {t.device} for x of {dt}, {tuple(shape)} in a call on cuda:{dev}")
+    code = _ROW_CODES.get(dt)
+    if code is None or len(shape) != 2:
+        raise ValueError(f"x of {dt} and shape {tuple(shape)}: [rows][cols] of bf16 or fp32 is wanted")
+    rows, cols = shape
+    sx, sq, sv = x.stride(), q.stride(), (0, 1) if values is None else values.stride()
+    if cols > 1 and not sx[1] == sq[1] == sv[1] == 1:
+        raise ValueError("the last index of x, q and values is contiguous")
+    if rows == 1:   # any row stride that is long enough
+        sx, sq, sv = (max(sx[0], cols),), (max(sq[0], cols),), (max(sv[0], cols),)
+    _check(_lib.quantize_rows(x.data_ptr(), rows, cols, sx[0], code, q.data_ptr(), sq[0], _dense(scale, dev, torch.float32, rows),
+                              None if values is None else values.data_ptr(), sv[0], _s(stream)))
 
 
 def int8_config(x, w, y, act="none") -> Int8Config:
@@ -665,12 +672,25 @@ def int8_config(x, w, y, act="none") -> Int8Config:
                       int8_stride(x) if x.dtype == torch.int8 else _row_stride(x), int8_stride(w), _row_stride(y))
 
 
-def _int8_at(t, rows, cols, row, dev):
-    """The device pointer of int8 rows laid out as the config says, whose storage reaches to the last row's 16-byte end."""
-    p = _at(t, (torch.int8, (rows, cols), (row, 1), dev))
-    if cols % 16 and t is not None and t.storage_offset() + (rows - 1) * row + -(-cols // 16) * 16 > t.untyped_storage().nbytes():
+def _int8_at(t, layout):
+    """The device pointer of int8 rows of that layout, whose storage reaches to the last row's 16-byte end."""
+    p = _at(t, layout)
+    rows, cols = layout[1]
+    if cols % 16 and t is not None and t.storage_offset() + (rows - 1) * layout[2][0] + -(-cols // 16) * 16 > t.untyped_storage().nbytes():
         raise ValueError("the storage of int8 rows ends before the last row's next multiple of 16 bytes (int8_rows makes such rows)")
     return p
+
+
+def _int8_layouts(cfg, dev):
+    """Of x as integers and in y's type, w and y; with the type and the sizes. Kept with the config, for as long as it says the same."""
+    key = bytes(cfg), dev
+    kept = cfg.__dict__.get("_layouts")
+    if kept is None or kept[0] != key:
+        dt, i8, M, K, N = _ROW_TYPES.get(cfg.dtype), torch.int8, cfg.rows, cfg.in_features, cfg.out_features
+        x, w, y = (cfg.x_row, 1), (cfg.w_row, 1), (cfg.y_row, 1)
+        kept = key, ((i8, (M, K), x, dev), (dt, (M, K), x, dev), (i8, (N, K), w, dev), (dt, (M, N), y, dev), dt, M, N)
+        cfg._layouts = kept
+    return kept[1]
 
 
 def int8_matmul_workspace_bytes(cfg) -> int:
@@ -683,20 +703,18 @@ def int8_linear_workspace_bytes(cfg) -> int:
 
 def int8_matmul(cfg, x, x_scale, w, w_scale, y, bias=None, ws=None, stream=None):
     """Tensors laid out as those cfg was made from; x_scale [rows], w_scale [out] fp32; bias [out] of y's type, or None."""
-    dev, dt, f32 = _current_device(), _ROW_TYPES.get(cfg.dtype), torch.float32
-    M, K, N = cfg.rows, cfg.in_features, cfg.out_features
-    _check(_lib.int8_matmul(C.byref(cfg), _int8_at(x, M, K, cfg.x_row, dev), _dense(x_scale, dev, f32, M),
-                            _int8_at(w, N, K, cfg.w_row, dev), _dense(w_scale, dev, f32, N), _dense(bias, dev, dt, N),
-                            _at(y, (dt, (M, N), (cfg.y_row, 1), dev)), *_ws_args(ws, dev), _s(stream)))
+    dev = _current_device()
+    lx, _, lw, ly, dt, M, N = _int8_layouts(cfg, dev)
+    _check(_lib.int8_matmul(C.byref(cfg), _int8_at(x, lx), _dense(x_scale, dev, torch.float32, M), _int8_at(w, lw),
+                            _dense(w_scale, dev, torch.float32, N), _dense(bias, dev, dt, N), _at(y, ly), *_ws_args(ws, dev), _s(stream)))
 
 
 def int8_linear(cfg, x, w, w_scale, y, bias=None, ws=None, stream=None):
     """int8_matmul of x rounded to integers, x of y's type."""
-    dev, dt, f32 = _current_device(), _ROW_TYPES.get(cfg.dtype), torch.float32
-    M, K, N = cfg.rows, cfg.in_features, cfg.out_features
-    _check(_lib.int8_linear(C.byref(cfg), _at(x, (dt, (M, K), (cfg.x_row, 1), dev)), _int8_at(w, N, K, cfg.w_row, dev),
-                            _dense(w_scale, dev, f32, N), _dense(bias, dev, dt, N), _at(y, (dt, (M, N), (cfg.y_row, 1), dev)),
-                            *_ws_args(ws, dev), _s(stream)))
+    dev = _current_device()
+    _, lx, lw, ly, dt, _, N = _int8_layouts(cfg, dev)
+    _check(_lib.int8_linear(C.byref(cfg), _at(x, lx), _int8_at(w, lw), _dense(w_scale, dev, torch.float32, N), _dense(bias, dev, dt, N),
+                            _at(y, ly), *_ws_args(ws, dev), _s(stream)))
 
 
 def dit_profile_begin():
