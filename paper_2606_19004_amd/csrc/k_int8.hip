@@ -435,33 +435,59 @@ __global__ void __launch_bounds__(WM * WN * 64) int8_gemm_kernel(const Int8Args 
     ktile(nk - 1, std::integral_constant<int, 3>());
     __builtin_amdgcn_s_setprio(0);
   } else {
-    // all stages are filled up front; the hand-over from tile kt to kt + 1 sits before the last step's products, whose fragments are in
-    // registers: tile kt + 1 has landed (the loads of the RING - 2 tiles after it stay in flight), barrier, and stage kt % RING takes
-    // tile kt + RING
+    // All stages are filled up front. The hand-over from tile kt to kt + 1 sits before the last step's products, whose fragments are in
+    // registers: tile kt + 1 has landed (the loads of the RING - 2 tiles after it stay in flight), barrier. Stage kt % RING then takes tile
+    // kt + RING. SPREAD: w between the products of that step, x between those of the next, so that the loads' issue does not stand before the
+    // products (128 x 12288 -> 3072 48 -> 43 us, 512 x 4096 -> 4096 20.5 -> 17.7; where the whole chip is busy its clock falls to 1.6 GHz
+    // and nothing is gained: 1280 x 12288 -> 3072 62 and 63). Tiles of 64, of which a CU holds three, are faster without (28 and 31).
     constexpr int L = X_LOADS + W_LOADS;
-    static_assert((RING - 2) * L <= 15 && (RING - 1) * L <= 63, "the waits below");
+    constexpr bool SPREAD = BM * BN > 64 * 64;
+    static_assert((RING - 2) * L <= 15 && (RING - 1) * L <= 63 && X_LOADS <= TI && W_LOADS <= TI, "the waits and places below");
     auto wait_tiles = [&](int n) {   // at most the loads of n tiles in flight, LDS reads done
       if (n >= RING - 2) __builtin_amdgcn_s_waitcnt(0x0070 | ((RING - 2) * L & 15));
       else if (n == 2) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * L & 15));
       else if (n == 1) __builtin_amdgcn_s_waitcnt(0x0070 | (L & 15));
       else __builtin_amdgcn_s_waitcnt(0x0070);
     };
-    auto step = [&](int kt, auto ph_c) {
-      constexpr int PH = decltype(ph_c)::value;   // 0: refill tile kt + RING; 1: none; 2: last tile
-      frags(kt, 1, 1);
-      if constexpr (PH == 2) mask_last(0);
-      multiply(0, 0, TI);
-      if constexpr (PH < 2) {
-        wait_tiles(PH == 0 ? RING - 2 : nk - 2 - kt);
-        __syncthreads();
-        if constexpr (PH == 0) {
-          issue_x(kt + RING, End());
-          issue_w(kt + RING, End());
-        }
-        frags(kt + 1, 0, 0);
+    // the products of a step, with the refill of one operand by tile `to` between them
+    auto products = [&](int rb, auto op_c, int to) {
+      constexpr int OP = decltype(op_c)::value;   // 0: none, 1: w, 2: x
+#pragma unroll
+      for (int i = 0; i < TI; i++) {
+        multiply(rb, i, i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (OP == 1)
+          if (i < W_LOADS) dma_b128(rw, lds0 + stage_w(to) + (wave * W_LOADS + i) * 1024, to * 128 + wchunk[i] >= K ? OUTSIDE : woff[i], to * 128);
+        if constexpr (OP == 2)
+          if (i < X_LOADS) dma_b128(rx, lds0 + stage_x(to) + (wave * X_LOADS + i) * 1024, to * 128 + xchunk[i] >= K ? OUTSIDE : xoff[i], to * 128);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (PH == 2) mask_last(1);
-      multiply(1, 0, TI);
+    };
+    using None = std::integral_constant<int, 0>;
+    using OfW = std::integral_constant<int, 1>;
+    using OfX = std::integral_constant<int, 2>;
+    auto step = [&](int kt, auto x_c, auto w_c) {   // a tile that is not the last
+      constexpr bool REFILL = decltype(w_c)::value != 0;
+      frags(kt, 1, 1);
+      if constexpr (SPREAD) {
+        __builtin_amdgcn_sched_barrier(0);
+        products(0, x_c, kt - 1 + RING);
+      } else {
+        multiply(0, 0, TI);
+      }
+      wait_tiles(REFILL ? RING - 2 : nk - 2 - kt);
+      __syncthreads();
+      if constexpr (REFILL && !SPREAD) {
+        issue_x(kt + RING, End());
+        issue_w(kt + RING, End());
+      }
+      frags(kt + 1, 0, 0);
+      if constexpr (SPREAD) {
+        __builtin_amdgcn_sched_barrier(0);
+        products(1, w_c, kt + RING);
+      } else {
+        multiply(1, 0, TI);
+      }
     };
     for (int kt = 0; kt < RING && kt < nk; kt++) {
       issue_x(kt, End());
@@ -472,10 +498,22 @@ __global__ void __launch_bounds__(WM * WN * 64) int8_gemm_kernel(const Int8Args 
     __syncthreads();
     frags(0, 0, 0);
     int kt = 0;
-    for (; kt + RING < nk; kt++) step(kt, std::integral_constant<int, 0>());
-    for (; kt + 1 < nk; kt++) step(kt, std::integral_constant<int, 1>());
+    if constexpr (SPREAD) {
+      if (nk > RING) {
+        step(0, None(), OfW());
+        for (kt = 1; kt + RING < nk; kt++) step(kt, OfX(), OfW());
+        step(kt++, OfX(), None());
+      }
+    } else {
+      for (; kt + RING < nk; kt++) step(kt, OfX(), OfW());
+    }
+    for (; kt + 1 < nk; kt++) step(kt, None(), None());
     prefetch();
-    step(nk - 1, std::integral_constant<int, 2>());
+    frags(nk - 1, 1, 1);
+    mask_last(0);
+    multiply(0, 0, TI);
+    mask_last(1);
+    multiply(1, 0, TI);
   }
 
   __syncthreads();   // every wave is done with the operand tiles
@@ -771,8 +809,8 @@ Form pick_form(int M, int N, int K) {
   if (M <= 2 && few_rows_lds(M, K) <= 61440) return FEW_ROWS;
   // Estimated times, us. What a CU takes per k-tile: 1.25 for a 256 x 256 tile (near the matrix rate), 0.5 for 128 x 128 and 0.24 for 64 x 64
   // (LDS reads), 0.23 and 0.09 for those whose waves share k; beside it each round's first loads and stores. Measured (us, in this order: 32 and 64
-  // with shared k, 64, 128, 256 x 192, 256): 128 x 12288 -> 3072: 19 / 22 / 28 / 48 / 77 / 97; 333 x 3072 -> 9216: 35 / 35 / 22 / 16 / 25 / 31;
-  // 512 x 4096 -> 4096: 26 / 21 / 16 / 20 / 31 / 38; 1280 x 3072 -> 9216: 120 / 116 / 69 / 56 / 35 / 38; 1280 x 12288 -> 3072:
+  // with shared k, 64, 128, 256 x 192, 256): 128 x 12288 -> 3072: 19 / 22 / 28 / 43 / 77 / 97; 333 x 3072 -> 9216: 35 / 35 / 22 / 16 / 25 / 31;
+  // 512 x 4096 -> 4096: 26 / 21 / 16 / 18 / 31 / 38; 1280 x 3072 -> 9216: 120 / 116 / 69 / 56 / 35 / 38; 1280 x 12288 -> 3072:
   // 137 / 100 / 94 / 62 / 98 / 117; 20480 x 3072 -> 12288: 2307 / 2043 / 1181 / 962 / 640 / 610.
   const double kt = (K + 127) / 128;
   const int64_t cus = cu_count();
