@@ -1213,6 +1213,8 @@ dit_status dit_debug_gemm_plan(const dit_block_config* c, int32_t batch, int32_t
 #ifdef DITSTEP_DEBUG
 // Debug builds, for tests: whether group_reward_stats_async checks the rewards in its statistics launch. Host only.
 int32_t dit_debug_reward_check_in_launch(int32_t groups, int32_t n) { return reward_check_in_launch(groups, n); }
+// The form that int8_matmul gives a product (an Int8Form). Host only.
+int32_t dit_debug_int8_form(int32_t rows, int32_t in_features, int32_t out_features) { return int8_form(rows, out_features, in_features); }
 #endif
 
 dit_status dit_profile_begin(void) {

@@ -799,14 +799,15 @@ __global__ void __launch_bounds__(256) int8_few_rows_kernel(const Int8Args a) {
   ((T*)a.y)[(int64_t)m * a.y_row + n] = from_f32<T>(finish<ACT>(sum, scales[m], channel<T>(a, n)));
 }
 
-enum Form { FEW_ROWS, KSPLIT_32, KSPLIT_64, RING_64, RING_128, LARGE_192, LARGE_256 };
 int64_t tiles_of(int M, int N, int bm, int bn) { return (int64_t)cdiv(M, bm) * cdiv(N, bn); }
 
 // rows of x in LDS
 size_t few_rows_lds(int M, int K) { return (size_t)M * ((K + STEP - 1) / STEP * STEP); }
 
-Form pick_form(int M, int N, int K) {
-  if (M <= 2 && few_rows_lds(M, K) <= 61440) return FEW_ROWS;
+}  // namespace
+
+Int8Form int8_form(int M, int N, int K) {
+  if (M <= 2 && few_rows_lds(M, K) <= 61440) return INT8_FEW_ROWS;
   // Estimated times, us. What a CU takes per k-tile: 1.25 for a 256 x 256 tile (near the matrix rate), 0.5 for 128 x 128 and 0.24 for 64 x 64
   // (LDS reads), 0.23 and 0.09 for those whose waves share k; beside it each round's first loads and stores. Measured (us, in this order: 32 and 64
   // with shared k, 64, 128, 256 x 192, 256): 128 x 12288 -> 3072: 19 / 22 / 28 / 43 / 77 / 97; 333 x 3072 -> 9216: 35 / 35 / 22 / 16 / 25 / 31;
@@ -817,17 +818,19 @@ Form pick_form(int M, int N, int K) {
   auto rounds = [&](int bm, int bn) { return (double)((tiles_of(M, N, bm, bn) + cus - 1) / cus); };
   auto shares = [&](int b, double slots) { return std::max(1.0, tiles_of(M, N, b, b) / (slots * cus)); };
   double best = rounds(256, 256) * (1.25 * kt + 11.0);
-  Form pick = LARGE_256;
-  auto consider = [&](Form f, double cost) {
+  Int8Form pick = INT8_LARGE_256;
+  auto consider = [&](Int8Form f, double cost) {
     if (cost < best) best = cost, pick = f;
   };
-  consider(LARGE_192, rounds(256, 192) * 0.87 * (1.25 * kt + 11.0));
-  consider(RING_128, rounds(128, 128) * (0.5 * kt + 4.5));
-  consider(RING_64, 3.0 + kt * std::max(0.27, 0.235 * shares(64, 1)));
-  consider(KSPLIT_64, rounds(64, 64) * (0.23 * kt + 3.0));
-  consider(KSPLIT_32, 2.5 + shares(32, 2) * (0.185 * kt + 0.7));
+  consider(INT8_LARGE_192, rounds(256, 192) * (1.09 * kt + 8.5));
+  consider(INT8_RING_128, rounds(128, 128) * (0.5 * kt + 4.5));
+  consider(INT8_RING_64, 3.0 + std::max(0.27 * kt, shares(64, 1) * std::max(0.235 * kt, 0.9 + 0.1 * kt)));
+  consider(INT8_KSPLIT_64, rounds(64, 64) * (0.23 * kt + 3.0));
+  consider(INT8_KSPLIT_32, 2.5 + shares(32, 2) * (0.185 * kt + 0.7));
   return pick;
 }
+
+namespace {
 
 template <int BM, int BN, int WM, int WN, int RING, int ACT, typename T> hipError_t launch_tiles(const Int8Args& a, hipStream_t s) {
   constexpr size_t lds = RING == 0 ? (size_t)(2 * BN + 3 * BM) * 128 : (size_t)RING * (BM + BN) * 128;
@@ -858,14 +861,14 @@ template <bool RAW, int ACT, typename T> hipError_t launch_few_rows(const Int8Ar
 }
 
 template <int ACT, typename T> hipError_t matmul(const Int8Args& a, hipStream_t s) {
-  switch (pick_form(a.M, a.N, a.K)) {
-    case FEW_ROWS: return launch_few_rows<false, ACT, T>(a, s);
-    case KSPLIT_32: return launch_ksplit<32, ACT, T>(a, s);
-    case KSPLIT_64: return launch_ksplit<64, ACT, T>(a, s);
-    case RING_64: return launch_tiles<64, 64, 2, 2, 3, ACT, T>(a, s);
-    case RING_128: return launch_tiles<128, 128, 2, 4, 4, ACT, T>(a, s);
-    case LARGE_192: return launch_tiles<256, 192, 4, 2, 0, ACT, T>(a, s);
-    case LARGE_256: return launch_tiles<256, 256, 4, 2, 0, ACT, T>(a, s);
+  switch (int8_form(a.M, a.N, a.K)) {
+    case INT8_FEW_ROWS: return launch_few_rows<false, ACT, T>(a, s);
+    case INT8_KSPLIT_32: return launch_ksplit<32, ACT, T>(a, s);
+    case INT8_KSPLIT_64: return launch_ksplit<64, ACT, T>(a, s);
+    case INT8_RING_64: return launch_tiles<64, 64, 2, 2, 3, ACT, T>(a, s);
+    case INT8_RING_128: return launch_tiles<128, 128, 2, 4, 4, ACT, T>(a, s);
+    case INT8_LARGE_192: return launch_tiles<256, 192, 4, 2, 0, ACT, T>(a, s);
+    case INT8_LARGE_256: return launch_tiles<256, 256, 4, 2, 0, ACT, T>(a, s);
   }
   return hipErrorInvalidValue;
 }

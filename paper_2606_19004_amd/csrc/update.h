@@ -27,6 +27,10 @@ struct Int8Args {
   int64_t x_row, w_row, y_row;
   const void* raw; int64_t raw_row;   // rows that are not integers yet, in place of x and x_scale (where int8_takes_raw), or null
 };
+// How a product runs: one or two rows by dot products; tiles of 32 or 64 whose waves share k; of 64 or 128 with rings of LDS stages; of 256 x 192
+// or 256 x 256
+enum Int8Form { INT8_FEW_ROWS, INT8_KSPLIT_32, INT8_KSPLIT_64, INT8_RING_64, INT8_RING_128, INT8_LARGE_192, INT8_LARGE_256 };
+Int8Form int8_form(int M, int N, int K);
 int64_t int8_matmul_threads(int M, int N);   // of the largest launch: one takes fewer than 2^32
 bool int8_takes_raw(int M, int K);           // whether a product rounds its few rows by itself
 hipError_t int8_matmul_launch(const Int8Args& a, int dtype, int act, hipStream_t s);

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import operator
 import os
 
 import torch
@@ -529,39 +530,53 @@ class TensorList:
         return self.array, self.count
 
 
-def _apart(tensors):
-    """Refuses tensors that share memory."""
-    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors if t is not None and t.numel())
-    for (_, end), (start, _) in zip(spans, spans[1:]):
-        if start < end:
-            raise ValueError("tensors of a list share memory")
+def _apart(starts, ends):
+    """Refuses pieces of memory that overlap: none do where the i-th smallest end is never past the start that follows it (of all
+    starts, i + 1-th: were two pieces to overlap at a start, fewer pieces would have ended there than the condition says)."""
+    starts.sort()
+    ends.sort()
+    if any(map(operator.gt, ends, starts[1:])):
+        raise ValueError("tensors of a list share memory")
 
 
-def _one_device(tensors):
-    devices = {t.get_device() for t in tensors if t is not None}
-    if len(devices) > 1:
-        raise ValueError(f"tensors of a list are on several devices: {sorted(devices)}")
-    return devices.pop() if devices else -1
+def _list_of(struct, words, count, device, keep):
+    """words: the structs' fields, 64 bits each (two 32-bit fields in one)."""
+    array = (struct * max(count, 1))()
+    if count:
+        C.memmove(array, (C.c_uint64 * len(words))(*words), 8 * len(words))
+    return TensorList(array, count, device, keep)
 
 
-def _flat(t, dtypes):
-    if t.dtype not in dtypes:
-        raise ValueError(f"a tensor of {t.dtype} where one of {[str(x) for x in dtypes]} is wanted")
-    if not t.is_contiguous():
-        raise ValueError(f"a tensor of shape {tuple(t.shape)} and strides {t.stride()} has gaps")
-    return t.data_ptr()
+_ROW_CODES = {torch.bfloat16: DIT_BF16, torch.float32: DIT_F32}
+_SIZES = {torch.bfloat16: 2, torch.float32: 4}
+
+
+def _piece(t, device, dtypes, starts, ends):
+    """The address of a tensor without gaps, of one of dtypes, on `device`; where it starts and ends is noted."""
+    if t.dtype not in dtypes or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"a tensor of {t.dtype}, shape {tuple(t.shape)} and strides {t.stride()} on {t.device}: one without gaps, of "
+                         f"{[str(x) for x in dtypes]}, on the list's device is wanted")
+    p, n = t.data_ptr(), t.numel()
+    if n:
+        starts.append(p)
+        ends.append(p + n * _SIZES[t.dtype])
+    return p or 0
 
 
 _FLOATS = (torch.bfloat16, torch.float32)
+_F32, _BF16 = (torch.float32,), (torch.bfloat16,)
 
 
 def grad_list(grads) -> TensorList:
     """Gradients (bf16 or fp32, contiguous, any shapes; None is skipped) for grad_norm and grad_clip. The list holds their addresses:
     make another one when gradients move."""
     grads = [g for g in grads if g is not None]
-    array = (Gradient * max(len(grads), 1))(*[Gradient(_flat(g, _FLOATS), g.numel(), _dtype_code(g.dtype), 0) for g in grads])
-    _apart(grads)
-    return TensorList(array, len(grads), _one_device(grads), grads)
+    device = grads[0].get_device() if grads else -1
+    words, starts, ends = [], [], []
+    for g in grads:
+        words += (_piece(g, device, _FLOATS, starts, ends), g.numel(), _ROW_CODES[g.dtype])
+    _apart(starts, ends)
+    return _list_of(Gradient, words, len(grads), device, grads)
 
 
 def grad_norm_workspace_bytes(grads: TensorList) -> int:
@@ -591,15 +606,16 @@ def adamw_list(params, grads, m, v, copies=None) -> TensorList:
     copies = [None] * len(params) if copies is None else list(copies)
     if not len(params) == len(grads) == len(m) == len(v) == len(copies):
         raise ValueError("lists of unlike lengths")
-    rows = []
+    device = params[0].get_device() if params else -1
+    words, starts, ends = [], [], []
     for p, g, a, b, c in zip(params, grads, m, v, copies):
-        if any(t is not None and t.shape != p.shape for t in (g, a, b, c)):
+        if not p.shape == g.shape == a.shape == b.shape or (c is not None and c.shape != p.shape):
             raise ValueError(f"a weight of shape {tuple(p.shape)} and a tensor of another")
-        rows.append(AdamwTensor(_flat(p, _FLOATS), _flat(g, _FLOATS), _flat(a, (torch.float32,)), _flat(b, (torch.float32,)),
-                                None if c is None else _flat(c, (torch.bfloat16,)), p.numel(), _dtype_code(p.dtype), _dtype_code(g.dtype)))
-    keep = params + grads + m + v + copies
-    _apart(keep)
-    return TensorList((AdamwTensor * max(len(rows), 1))(*rows), len(rows), _one_device(keep), keep)
+        words += (_piece(p, device, _FLOATS, starts, ends), _piece(g, device, _FLOATS, starts, ends), _piece(a, device, _F32, starts, ends),
+                  _piece(b, device, _F32, starts, ends), 0 if c is None else _piece(c, device, _BF16, starts, ends), p.numel(),
+                  _ROW_CODES[p.dtype] | _ROW_CODES[g.dtype] << 32)
+    _apart(starts, ends)
+    return _list_of(AdamwTensor, words, len(params), device, params + grads + m + v + copies)
 
 
 def adamw_step(weights, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=1, scale=None, step_dev=None, stream=None):
@@ -632,9 +648,6 @@ def _rows_of(t, name, dtypes):
         raise ValueError(f"{name} is [rows][columns] with the last index contiguous")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} is of {t.dtype}")
-
-
-_ROW_CODES = {torch.bfloat16: DIT_BF16, torch.float32: DIT_F32}
 
 
 def quantize_rows(x, q, scale, values=None, stream=None):

@@ -82,6 +82,22 @@ def test_sizes(d, M, K, N, dtype):
     Problem(d, M, K, N, dtype, gelu=(M + N) % 2 == 0, bias=M % 3 != 0).check()
 
 
+# every form at sizes that do not fill its tiles: one k-tile, two, three, and more than its stages, rows of w that end inside 16 bytes
+FORMS = [("few rows", 1, 61440, 50), ("few rows", 2, 30720, 9), ("few rows", 2, 2049, 8210), ("32, shared k", 1, 61441, 50), ("32, shared k", 3, 700, 9000),
+         ("32, shared k", 190, 3001, 2100), ("64, shared k", 250, 12001, 3001), ("64", 300, 2001, 4000), ("64", 513, 260, 11665), ("64", 4100, 130, 4100),
+         ("128", 333, 3001, 9215), ("128", 1427, 1120, 2271), ("128", 1959, 72, 1734), ("128", 2478, 131, 1471), ("128", 2642, 365, 1396),
+         ("128", 942, 505, 3198), ("128", 527, 566, 5683), ("128", 1477, 732, 2335), ("256 x 192", 7000, 131, 8001), ("256 x 192", 1401, 315, 6787),
+         ("256 x 192", 2807, 2847, 8364), ("256 x 256", 9003, 90, 3001), ("256 x 256", 5000, 200, 2500), ("256 x 256", 4000, 333, 8009), ("256 x 256", 7901, 639, 6935)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("form,M,K,N", FORMS)
+def test_every_form(d, form, M, K, N, dtype):
+    from tests.plan_util import int8_form
+    assert int8_form(M, K, N) == form
+    Problem(d, M, K, N, dtype, gelu=K % 2 == 0, bias=M % 2 == 1, pad=16 * (N % 2), ypad=3 * (M % 2)).check()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("M,K,N", [(1, 200, 30), (7, 47, 19), (40, 1100, 70), (200, 130, 300), (700, 333, 260)])
 def test_strides_and_what_lies_between_rows(d, M, K, N, dtype):
@@ -114,7 +130,7 @@ def test_scales_that_are_not_finite(d, M):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("M,K,N,act", [(1, 3072, 384, "none"), (1, 16384, 40, "none"), (1, 16385, 40, "gelu"), (2, 8192, 33, "gelu"), (3, 4096, 8200, "none"),
+@pytest.mark.parametrize("M,K,N,act", [(1, 3072, 384, "none"), (1, 16384, 40, "none"), (1, 16385, 40, "gelu"), (1, 3000, 9000, "gelu"), (2, 8191, 8300, "none"), (2, 8192, 50, "none"), (2, 8193, 50, "none"), (1, 5, 3, "none"), (2, 8, 2, "none"), (2, 8192, 33, "gelu"), (3, 4096, 8200, "none"),
                                        (3, 5461, 9, "gelu"), (4, 4096, 20, "none"), (8, 2048, 8210, "gelu"), (7, 1033, 50, "none"), (8, 2049, 30, "none"), (1, 77, 9, "gelu"), (4, 1000, 100, "gelu"), (20, 513, 70, "none"), (130, 2049, 257, "gelu"),
                                        (300, 20000, 33, "none"), (600, 256, 512, "gelu")])
 def test_linear_is_the_product_of_rounded_rows(d, M, K, N, act, dtype):
