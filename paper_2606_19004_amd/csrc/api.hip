@@ -1669,7 +1669,7 @@ dit_status quantize_rows(const void* x, int32_t rows, int32_t cols, int64_t x_ro
 
 size_t int8_matmul_workspace_bytes(const dit_int8_config* c) { return check_int8(c, true) ? 0 : 0; }
 size_t int8_linear_workspace_bytes(const dit_int8_config* c) {
-  if (check_int8(c, false) || c->rows == 0 || c->out_features == 0 || int8_takes_raw(c->rows, c->in_features)) return 0;
+  if (check_int8(c, false) || c->rows == 0 || c->out_features == 0 || int8_takes_raw(c->rows, c->out_features, c->in_features)) return 0;
   return int8_layout(c).total;
 }
 
@@ -1691,7 +1691,7 @@ dit_status int8_linear(const dit_int8_config* c, const void* x, const int8_t* w,
   if (st) return st;
   if (c->rows == 0 || c->out_features == 0) return DIT_OK;
   if ((st = check_int8_call(c, false, x, w, w_scale, bias, y))) return st;
-  if (int8_takes_raw(c->rows, c->in_features))
+  if (int8_takes_raw(c->rows, c->out_features, c->in_features))
     return run_int8_matmul(c, nullptr, 0, nullptr, w, w_scale, bias, y, hs(stream), x, c->x_row);
   if ((st = check_ws(ws, ws_bytes, int8_linear_workspace_bytes(c)))) return st;
   const Int8Ws L = int8_layout(c);

@@ -666,6 +666,115 @@ __global__ void __launch_bounds__(256) int8_ksplit_kernel(const Int8Args a, int 
 #endif
 }
 
+// Small products of rows that are not integers yet, in one launch: a 32 x 32 tile as above, whose workgroup first rounds its 32 rows of x into
+// LDS, eight lanes to a row, while its first slices of w are on their way. Bound by latency: the launch, x, w, the sums. Against a launch that
+// rounds the rows and one that multiplies (us, as eager calls and in a graph): 3 x 256 -> 256 6.6 and 4.0 for 9.6 and 6.1, 500 x 256 -> 1024 6.7 and
+// 6.4 for 9.6 and 8.7, 500 x 512 -> 1024 9.5 and 9.3 for 10.1 and 9.2; rows of 1001 (333 of them, 515 features) took 12.4 for 10.0 and 7.9.
+constexpr int RAW_K = 512;   // longest rows
+template <int VECTORS, int ACT, typename T>
+__global__ void __launch_bounds__(256) int8_small_kernel(const Int8Args a, int total_tiles) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int B = 32, STAGE = B * 128;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // x [k-tile][row][128], then two stages of w for each wave
+  __shared__ float scales[B];
+  const int per = gridDim.x >> 3;
+  const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if (t >= total_tiles) return;
+  int tm, tn;
+  tile_coords(t, cdiv(a.M, B), cdiv(a.N, B), tm, tn);
+  const int m0 = tm * B, n0 = tn * B;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int K = a.K, nk = (K + 127) / 128;
+  const u32x4_t rw = rows_rsrc(a.w + (int64_t)n0 * a.w_row, min(B, a.N - n0), a.w_row, K);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + nk * STAGE + wave * 2 * STAGE;
+  auto issue = [&](int kt, int st) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int r = 8 * i + (lane >> 3), chunk = ((lane & 7) ^ swz(r)) * 16;
+      const bool in = kt * 128 + chunk < K && n0 + r < a.N;
+      dma_b128(rw, lds0 + st * STAGE + i * 1024, in ? (uint32_t)(r * a.w_row) + chunk : OUTSIDE, kt * 128);
+    }
+  };
+  const int row = tid >> 3, part = tid & 7;   // elements 8 (part + 8 v) .. + 7 of a row; rows past the end repeat the last and are not stored
+  const T* x = (const T*)a.raw + min(m0 + row, a.M - 1) * a.raw_row;
+  Eight<T> e[VECTORS];
+#pragma unroll
+  for (int v = 0; v < VECTORS; v++) {
+    const int at = 8 * (part + 8 * v);
+    if (K % 8 == 0) e[v].load(x + min(at, K - 8));   // (past the end: repeats the last ones, which does not change the largest)
+    else load_row8(x, at, K, e[v]);
+  }
+  if (wave < nk) issue(wave, 0);
+  if (wave + 4 < nk) issue(wave + 4, 1);
+  uint32_t top = 0;
+#pragma unroll
+  for (int v = 0; v < VECTORS; v++) top = max(top, e[v].top());
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  const RowScale r = row_scale(top);
+  if (part == 0) scales[row] = r.bad ? NAN : r.scale;
+#pragma unroll
+  for (int v = 0; v < VECTORS; v++) {
+    const int at = 8 * (part + 8 * v);
+    if (at >= nk * 128) break;
+    float f[8], z[8];
+    e[v].get(f);
+    to_integers(r, f, z);
+    const bool none = r.bad || at >= K;
+    *(uint2*)(smem + (at >> 7) * STAGE + row * 128 + ((((at >> 4) & 7) ^ swz(row)) << 4) + (at & 8)) =
+        none ? make_uint2(0, 0) : make_uint2(low_bytes(z), low_bytes(z + 4));
+  }
+  __syncthreads();
+
+  const int r16 = lane & 15, kq = lane >> 4;
+  i32x4 acc[2][2] = {};
+  int st = 0;
+  for (int kt = wave; kt < nk; kt += 4) {
+    if (kt + 4 >= nk) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");   // (the 4 loads of this wave's next slice may be in flight)
+    const char* sx = smem + kt * STAGE;
+    const char* sw = smem + nk * STAGE + (wave * 2 + st) * STAGE;
+    i32x4 fw[2][2], fx[2][2];
+#pragma unroll
+    for (int s = 0; s < 2; s++)
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        const int fr = 16 * i + r16;
+        fw[s][i] = *(const i32x4*)(sw + fr * 128 + (((4 * s + kq) ^ swz(fr)) << 4));
+        fx[s][i] = *(const i32x4*)(sx + fr * 128 + (((4 * s + kq) ^ swz(fr)) << 4));
+      }
+    if (kt + 8 < nk) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the fragments are in registers: the stage is free
+      issue(kt + 8, st);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; s++)
+#pragma unroll
+      for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int j = 0; j < 2; j++) acc[i][j] = mfma_i8(fw[s][i], fx[s][j], acc[i][j]);
+    st ^= 1;
+  }
+  __syncthreads();   // x and w have been read
+  i32x4* sums = (i32x4*)smem;   // [block][wave][lane]
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+#pragma unroll
+    for (int j = 0; j < 2; j++) sums[((2 * i + j) * 4 + wave) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  i32x4 c = sums[(wave * 4) * 64 + lane];   // wave q finishes block (q / 2, q % 2)
+#pragma unroll
+  for (int g = 1; g < 4; g++) c += sums[(wave * 4 + g) * 64 + lane];
+  const int ml = 16 * (wave & 1) + r16, m = m0 + ml, n = n0 + 16 * (wave >> 1) + 4 * kq;
+  if (m < a.M && n < a.N) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = finish<ACT>(c[e], scales[ml], channel<T>(a, min(n + e, a.N - 1)));
+    store_features<T>(a, v, m, n);
+  }
+#endif
+}
+
 // inclusive sum over the wave by VALU moves: the last lane has the total
 template <int CTRL, int ROWS> __device__ __forceinline__ int moved_up(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
 __device__ __forceinline__ int wave_total(int v) {
@@ -860,6 +969,17 @@ template <bool RAW, int ACT, typename T> hipError_t launch_few_rows(const Int8Ar
   return a.M == 1 ? launch_few<1, RAW, ACT, T>(a, s) : launch_few<2, RAW, ACT, T>(a, s);
 }
 
+template <int VECTORS, int ACT, typename T> hipError_t launch_small(const Int8Args& a, hipStream_t s) {
+  const size_t lds = (size_t)((a.K + 127) / 128 + 8) * 4096;   // (more than the 16 KB that the sums take; at most 64)
+  const int64_t tiles = tiles_of(a.M, a.N, 32, 32);
+  int8_small_kernel<VECTORS, ACT, T><<<8 * cdiv(tiles, 8), 256, lds, s>>>(a, (int)tiles);
+  return hipGetLastError();
+}
+template <int ACT, typename T> hipError_t launch_raw(const Int8Args& a, hipStream_t s) {
+  if (a.M <= 2) return launch_few_rows<true, ACT, T>(a, s);
+  return a.K <= RAW_K / 2 ? launch_small<RAW_K / 128, ACT, T>(a, s) : launch_small<RAW_K / 64, ACT, T>(a, s);
+}
+
 template <int ACT, typename T> hipError_t matmul(const Int8Args& a, hipStream_t s) {
   switch (int8_form(a.M, a.N, a.K)) {
     case INT8_FEW_ROWS: return launch_few_rows<false, ACT, T>(a, s);
@@ -883,12 +1003,15 @@ int64_t int8_matmul_threads(int M, int N) {
   return M <= 2 ? 256 * std::max<int64_t>(cdiv(N, 4 * F), 2 * cu_count()) : 256 * (tiles_of(M, N, 32, 32) + 8);
 }
 
-bool int8_takes_raw(int M, int K) { return M <= 2 && (int64_t)M * K <= RAW_ELEMENTS; }
+bool int8_takes_raw(int M, int N, int K) {
+  if (M <= 2) return (int64_t)M * K <= RAW_ELEMENTS;
+  return K <= RAW_K && tiles_of(M, N, 32, 32) <= 2 * cu_count();
+}
 
 hipError_t int8_matmul_launch(const Int8Args& a, int dtype, int act, hipStream_t s) {
   if (a.raw) {
-    if (dtype == DT_BF16) return act ? launch_few_rows<true, 1, u16>(a, s) : launch_few_rows<true, 0, u16>(a, s);
-    return act ? launch_few_rows<true, 1, float>(a, s) : launch_few_rows<true, 0, float>(a, s);
+    if (dtype == DT_BF16) return act ? launch_raw<1, u16>(a, s) : launch_raw<0, u16>(a, s);
+    return act ? launch_raw<1, float>(a, s) : launch_raw<0, float>(a, s);
   }
   if (dtype == DT_BF16) return act ? matmul<1, u16>(a, s) : matmul<0, u16>(a, s);
   return act ? matmul<1, float>(a, s) : matmul<0, float>(a, s);

@@ -130,7 +130,9 @@ def test_scales_that_are_not_finite(d, M):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("M,K,N,act", [(1, 3072, 384, "none"), (1, 16384, 40, "none"), (1, 16385, 40, "gelu"), (1, 3000, 9000, "gelu"), (2, 8191, 8300, "none"), (2, 8192, 50, "none"), (2, 8193, 50, "none"), (1, 5, 3, "none"), (2, 8, 2, "none"), (2, 8192, 33, "gelu"), (3, 4096, 8200, "none"),
+@pytest.mark.parametrize("M,K,N,act", [(1, 3072, 384, "none"), (1, 16384, 40, "none"), (1, 16385, 40, "gelu"), (1, 3000, 9000, "gelu"), (2, 8191, 8300, "none"), (2, 8192, 50, "none"), (2, 8193, 50, "none"), (1, 5, 3, "none"), (2, 8, 2, "none"),
+                                       (33, 512, 70, "gelu"), (500, 511, 1000, "none"), (64, 9, 40, "none"), (3, 130, 16384, "gelu"), (3, 130, 16416, "none"),
+                                       (100, 256, 100, "none"), (47, 257, 33, "gelu"), (5, 128, 31, "none"), (300, 1, 20, "none"), (2, 8192, 33, "gelu"), (3, 4096, 8200, "none"),
                                        (3, 5461, 9, "gelu"), (4, 4096, 20, "none"), (8, 2048, 8210, "gelu"), (7, 1033, 50, "none"), (8, 2049, 30, "none"), (1, 77, 9, "gelu"), (4, 1000, 100, "gelu"), (20, 513, 70, "none"), (130, 2049, 257, "gelu"),
                                        (300, 20000, 33, "none"), (600, 256, 512, "gelu")])
 def test_linear_is_the_product_of_rounded_rows(d, M, K, N, act, dtype):

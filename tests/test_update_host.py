@@ -124,9 +124,11 @@ def test_int8_calls():
         assert matmul(c, **kw) == INVALID and linear(c, **kw) == INVALID, kw
     assert matmul(c, xs=None) == INVALID and matmul(c, xs=A + 1) == INVALID and matmul(c, x=A + 8) == INVALID and linear(c, x=A + 1) == INVALID
     assert linear(cfg8(dtype=0), x=A + 2) == INVALID and matmul(cfg8(dtype=0), y=A + 2) == INVALID
-    assert d.int8_linear_workspace_bytes(cfg8(rows=2)) == 0      # one or two rows are rounded by the product itself
+    # one or two rows, and small products of short rows, are rounded by the product itself
+    assert d.int8_linear_workspace_bytes(cfg8(rows=2, in_features=8000, x_row=8000, w_row=8000)) == 0 and d.int8_linear_workspace_bytes(c) == 0
+    c = cfg8(in_features=600, x_row=608, w_row=608)
     need = d.int8_linear_workspace_bytes(c)
-    assert need >= 4 * 128 + 4 * 4
+    assert need >= 4 * 640 + 4 * 4
     assert linear(c, work=None) == WORKSPACE and linear(c, work=A + 16) == WORKSPACE and linear(c, n=need - 1) == WORKSPACE
     for e in (cfg8(rows=0), cfg8(out_features=0, y_row=0)):
         assert matmul(e, x=None, y=None, work=None, n=0) == OK and linear(e, x=None, y=None, work=None, n=0) == OK
