@@ -1,6 +1,8 @@
 // The end of a policy update: the 2-norm over the gradients of all weights, clipping, and the weights' AdamW step. All are
-// bound by memory. Tensors come as tables in the kernels' arguments (no copy to the device, nothing kept between
-// calls); a workgroup takes one chunk of one tensor.
+// bound by memory (a large copy runs at 5.0 TB/s). 340 M weights, bf16 gradients, fp32 master weights with bf16 copies: norm 118-123 us (5.5 TB/s), clip
+// 271 (5.0), AdamW 1912 (5.0). Tensors come as tables in the kernels' arguments (no copy to the device, nothing kept between calls); a workgroup
+// takes one chunk of one tensor. About 8192 chunks, of 2048 elements at least: 2.4 M fp32 weights in 20 tensors: AdamW 14.0 us (4.7 TB/s;
+// chunks of 4096 15.3), norm 6.3, clip 5.2.
 #include <algorithm>
 #include <cmath>
 
@@ -14,7 +16,8 @@ constexpr int THREADS = 256;
 
 // ---- tables of tensors ----
 // first[e]: the workgroup that takes tensor e's first chunk; unused entries are past every workgroup.
-// A launch's arguments stay below 4 KB: 192 gradients, 64 weights. Short lists take smaller tables, which the host copies faster.
+// A launch's arguments stay below 4 KB: 192 gradients, 64 weights. Short lists take smaller tables, which the host copies faster (20 tensors: norm
+// and clip 15.1 -> 13.1 us). Long lists of small tensors pay for their launches: 1200 tensors, 9 M weights, AdamW 133 us in 19 of them.
 constexpr int GRADS = 192, WEIGHTS = 64, FEW = 24;
 template <int N> struct GradTable {
   void* data[N];
@@ -52,6 +55,7 @@ __device__ __forceinline__ double wave_sum64(double v) {
 }
 
 // ---- norm ----
+// Two launches: sums of the chunks, then one workgroup that adds them up (2-5 us, most of it the launch; joining them needs counters that start at zero).
 // Squares are taken and summed in fp64 (a bf16 or fp32 value's square is exact there, and finite): four sums per thread in flight,
 // whose order is given by the chunk.
 template <typename T> __device__ double chunk_squares(const T* p, int64_t begin, int64_t end) {
@@ -98,13 +102,8 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const GradTable<N> t, int
 
 __global__ void __launch_bounds__(1024) norm_finish_kernel(const double* parts, int64_t n, double max_norm, double* norm, float* scale) {
   __shared__ double red[16];
-  double p[8], s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += 8 * 1024) {   // eight loads in flight; what is past the end reads the last and does not count
-#pragma unroll
-    for (int u = 0; u < 8; u++) p[u] = parts[min(i + 1024 * u, n - 1)];
-#pragma unroll
-    for (int u = 0; u < 8; u++) s += i + 1024 * u < n ? p[u] : 0.0;
-  }
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += 1024) s += parts[i];
   s = wave_sum64(s);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -143,6 +142,8 @@ __global__ void __launch_bounds__(THREADS) clip_kernel(const GradTable<N> t, int
 }
 
 // ---- AdamW ----
+// One pass: 28 bytes move for a weight of the master form. Rounding to bf16 weights is to nearest: without master weights a step below
+// half a unit in the last place is lost.
 struct Adam {
   float beta1, rest1, beta2, rest2, eps, keep, step1, root2;
   // with s = *scale: m = beta1 m + rest1 s g, v = beta2 v + rest2 (s g)^2, p = keep p - step1 m / (sqrt(v) root2 + eps),
