@@ -26,7 +26,8 @@ extern "C" {
  *   q[i][j]  = the integer nearest to x[i][j] / scale[i], of two as near the even one (the quotient itself is rounded, not an
  *              fp32 quotient), in -127..127
  *   values[i][j] = q[i][j] scale[i], rounded to dtype: what the integers stand for (an update that follows an 8-bit
- *              rollout runs its own products with these)
+ *              rollout runs its own products with these; 127 scale may round past the largest fp32 number, to infinity, where
+ *              max |x| is the largest)
  * A row that holds a NaN or an infinity gets scale NaN, q 0 and values NaN. q is int8 at row stride q_row; values (may be
  * NULL, may be x itself at its stride) has row stride values_row. Strides are at least cols; elements past cols are left as
  * they were. Tensors need the alignment of their type only. rows == 0 or cols == 0: no-op. */

@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "gemm_common.h"
+#include "packed.h"
 #include "update.h"
 #include "vectors.h"
 
@@ -785,18 +786,6 @@ __global__ void __launch_bounds__(256) int8_small_kernel(const Int8Args a, int t
 #endif
 }
 
-// inclusive sum over the wave by VALU moves: the last lane has the total
-template <int CTRL, int ROWS> __device__ __forceinline__ int moved_up(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
-__device__ __forceinline__ int wave_total(int v) {
-  v += moved_up<0x111, 0xf>(v);
-  v += moved_up<0x112, 0xf>(v);
-  v += moved_up<0x114, 0xf>(v);
-  v += moved_up<0x118, 0xf>(v);
-  v += moved_up<0x142, 0xa>(v);
-  v += moved_up<0x143, 0xc>(v);
-  return v;
-}
-
 // One or two rows: bound by reading w once. A wave takes F features, 1 KB of each per step (16 bytes a lane), by v_dot4; x lies in LDS as
 // integers, zeros behind its end. SHARE: the four waves of a workgroup share the k of the same features (few features).
 // RAW: x comes in its own type and every workgroup rounds it by itself while its first weights are on their way: no launch before this one.
@@ -909,7 +898,7 @@ __global__ void __launch_bounds__(256) int8_few_rows_kernel(const Int8Args a) {
   for (int f = 0; f < F; f++)
 #pragma unroll
     for (int m = 0; m < ROWS; m++) {
-      const int total = wave_total(acc[f][m]);
+      const int total = (int)wave_scan((unsigned)acc[f][m]);   // in the last lane
       if (lane == 63) part[wave][f][m] = total;
     }
   __syncthreads();

@@ -145,24 +145,24 @@ __global__ void __launch_bounds__(THREADS) clip_kernel(const GradTable<N> t, int
 // One pass: 28 bytes move for a weight of the master form. Rounding to bf16 weights is to nearest: without master weights a step below
 // half a unit in the last place is lost.
 struct Adam {
-  float beta1, rest1, beta2, rest2, eps, keep, step1, root2;
-  // with s = *scale: m = beta1 m + rest1 s g, v = beta2 v + rest2 (s g)^2, p = keep p - step1 m / (sqrt(v) root2 + eps),
-  // keep = 1 - lr weight_decay, step1 = lr / (1 - beta1^t), root2 = 1 / sqrt(1 - beta2^t)
+  float beta1, rest1, beta2, rest2, eps, lr, decay, mean1, root2;
+  // with s = *scale: m = beta1 m + rest1 s g, v = beta2 v + rest2 (s g)^2, p -= lr (mean1 m / (sqrt(v) root2 + eps) + decay p),
+  // mean1 = 1 / (1 - beta1^t), root2 = 1 / sqrt(1 - beta2^t). (p (1 - lr decay) would lose every decay below 2^-25.)
   __device__ __forceinline__ void apply(float g, float& m, float& v, float& p) const {
     m = fmaf(rest1, g, beta1 * m);
     v = fmaf(rest2 * g, g, beta2 * v);
-    p = fmaf(keep, p, -(step1 * m / fmaf(sqrtf(v), root2, eps)));
+    p = fmaf(-lr, fmaf(decay, p, mean1 * m / fmaf(sqrtf(v), root2, eps)), p);
   }
 };
 struct AdamArgs {
   Adam a;                          // of the host's step number
   const int64_t* step_dev;         // where that is on the device: with the logarithms of the betas (-inf for 0)
-  double lr, log_beta1, log_beta2;
+  double log_beta1, log_beta2;
   const float* scale;
 };
-// step1 and root2 from t, in fp64: 1 - beta^t loses what a beta near 1 has
-__host__ __device__ __forceinline__ void set_step(Adam& a, double t, double lr, double log_beta1, double log_beta2) {
-  a.step1 = (float)(lr / -expm1(t * log_beta1));
+// mean1 and root2 from t, in fp64: 1 - beta^t loses what a beta near 1 has
+__host__ __device__ __forceinline__ void set_step(Adam& a, double t, double log_beta1, double log_beta2) {
+  a.mean1 = (float)(1.0 / -expm1(t * log_beta1));
   a.root2 = (float)(1.0 / sqrt(-expm1(t * log_beta2)));
 }
 
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const WeightTable<N> t, 
   const int b = blockIdx.x, e = entry_of<N>(t.first, b);
   const int64_t begin = (b - t.first[e]) * chunk, end = min(begin + chunk, t.count[e]);
   Adam a = args.a;
-  if (args.step_dev) set_step(a, (double)*args.step_dev, args.lr, args.log_beta1, args.log_beta2);
+  if (args.step_dev) set_step(a, (double)*args.step_dev, args.log_beta1, args.log_beta2);
   void* p = t.param[e];
   const void* g = t.grad[e];
   float *m = t.m[e], *v = t.v[e];
@@ -299,9 +299,9 @@ hipError_t grad_clip_launch(const dit_gradient* g, int n, int64_t chunk, const f
 hipError_t adamw_launch(const dit_adamw_config& c, const dit_adamw_tensor* w, int n, int64_t chunk, const float* scale,
                         const int64_t* step_dev, hipStream_t s) {
   AdamArgs a{{(float)c.beta1, (float)(1.0 - c.beta1), (float)c.beta2, (float)(1.0 - c.beta2), (float)c.eps,
-              (float)(1.0 - c.lr * c.weight_decay), 0.f, 0.f},
-             step_dev, c.lr, std::log(c.beta1), std::log(c.beta2), scale};
-  set_step(a.a, (double)c.step, c.lr, a.log_beta1, a.log_beta2);
+              (float)c.lr, (float)c.weight_decay, 0.f, 0.f},
+             step_dev, std::log(c.beta1), std::log(c.beta2), scale};
+  set_step(a.a, (double)c.step, a.log_beta1, a.log_beta2);
   return n <= FEW ? adamw<FEW>(a, w, n, chunk, s) : adamw<WEIGHTS>(a, w, n, chunk, s);
 }
 

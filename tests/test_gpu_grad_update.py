@@ -182,6 +182,22 @@ def test_adamw_settings(d, change):
         check_adam((p, m, v, None), old, 1.0, h, h["step"])
 
 
+def test_a_small_decay_is_not_lost(d):
+    """lr weight_decay = 2^-27, below what 1 - lr weight_decay can hold, beside steps of any size: the weights move by lr weight_decay p
+    on average. p lies in [64, 128), where a unit is 2^-17: the decay is 0.094 units on average, so it turns the rounding of that share of the
+    weights (sums of unlike steps), and the mean over 2^20 of them is off by sqrt(0.094) units / 2^10, 0.3%, per standard deviation."""
+    n, lr, decay = 1 << 20, 2.0 ** -15, 2.0 ** -12
+    g = torch.Generator(device="cuda").manual_seed(2)
+    start, grad, mean, square = 64 * torch.rand(n, generator=g, device="cuda") + 64, *(torch.randn(n, generator=g, device="cuda") for _ in range(3))
+    out = []
+    for wd in (0.0, decay):
+        p, m, v = start.clone(), mean.clone(), square.square() + 0.1
+        d.adamw_step(d.adamw_list([p], [grad], [m], [v]), lr=lr, weight_decay=wd, step=5)
+        out.append(p.double())
+    moved, want = float((out[0] - out[1]).mean()), lr * decay * float(start.double().mean())
+    assert abs(moved - want) <= 0.02 * want
+
+
 def test_a_gradient_of_zero_and_a_zero_state(d):
     """v = 0: the step is m / eps times lr, here 0; nothing is NaN."""
     p, g, m, v = (torch.zeros(100, device="cuda") for _ in range(4))

@@ -157,6 +157,34 @@ def test_linear_is_the_product_of_rounded_rows(d, M, K, N, act, dtype):
         assert torch.isnan(y[1].float()).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,K,N", [(1, 3072, 9000), (2, 700, 40), (1, 701, 17), (5, 512, 40), (40, 300, 2000), (5, 600, 40), (300, 3000, 70)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_linear_of_a_row_that_is_not_finite(d, M, K, N, bad, dtype):
+    """NaN in that row of y, the bits of the rows alone in all others, wherever the value stands; a row of zeros gives the bias."""
+    x = torch.randn(M, K, device="cuda").to(TYPES[dtype])
+    if M > 2:
+        x[2] = 0.0
+    w, ws = d.int8_rows(N, K), torch.empty(N, device="cuda")
+    d.quantize_rows(torch.randn(N, K, device="cuda"), w, ws)
+    bias, y = torch.randn(N, device="cuda").to(x.dtype), torch.empty(M, N, dtype=x.dtype, device="cuda")
+    cfg = d.int8_config(x, w, y)
+    space = d.workspace(d.int8_linear_workspace_bytes(cfg))
+    d.int8_linear(cfg, x, w, ws, y, bias=bias, ws=space)
+    want = y.clone()
+    assert torch.isfinite(want.float()).all()
+    if M > 2:
+        assert torch.equal(want[2], bias)
+    for row, col in ((M - 1, 0), (0, K - 1), (M // 2, K // 2)):
+        kept = x[row, col].clone()
+        x[row, col] = bad
+        d.int8_linear(cfg, x, w, ws, y, bias=bias, ws=space)
+        assert torch.isnan(y[row].float()).all()
+        rest = torch.arange(M, device="cuda") != row
+        assert torch.equal(y[rest], want[rest])
+        x[row, col] = kept
+
+
 @pytest.mark.parametrize("M,N", [(3, 5), (40, 70), (300, 300)])
 def test_offsets_past_32_bits(d, M, N):
     """Rows of x, w and y that start past 2^32 bytes."""
