@@ -273,7 +273,7 @@ constexpr uint32_t OUTSIDE = 0xC0000000u;   // an offset past any tile's records
 // Bound by the matrix units, at the clock that the chip's power leaves: 20480 x 3072 -> 12288 in 610 us (590-640 from card to card), 2540
 // TOP/s (a library product of these integers: 720 us), with gelu 640. A 256 x 256 tile takes 2380 cycles per k-tile, 2048 of them the products'
 // (one of 128 x 128: 1030 and 512; more stages or fewer LDS reads per product did not change that), 2.3 GHz on few CUs and 1.6-1.7 on all.
-// y's rows are stored 16 bytes a lane where their length and stride allow (features a multiple of 8); else 20480 x 3072 -> 12287 takes 710 us.
+// bf16 rows of y that do not start at multiples of 4 bytes cost stores of parts of a word: 20480 x 3072 -> 12287 706 us, -> 12284 624.
 template <int BM, int BN, int WM, int WN, int RING, int ACT, typename T>
 __global__ void __launch_bounds__(WM * WN * 64) int8_gemm_kernel(const Int8Args a, int total_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -532,8 +532,8 @@ __global__ void __launch_bounds__(WM * WN * 64) int8_gemm_kernel(const Int8Args 
   if (tid < BN) sc[tid] = pre_c;
   __syncthreads();
   // block (i, j), register q: feature 16 i + 4 (lane / 16) + q, row 16 j + lane % 16. bf16: blocks i and i + 1 are regrouped so that a lane
-  // holds 8 adjacent features, stored with one 16-byte store, where y's rows are 16-byte aligned.
-  const bool pairs = sizeof(T) == 2 && a.N % 8 == 0 && a.y_row % 8 == 0 && (uintptr_t)a.y % 16 == 0;
+  // holds 8 adjacent features, stored with one 16-byte store at any alignment.
+  constexpr bool PAIRS = sizeof(T) == 2;
   const int pair_col = 16 * (lkc & 1) + 8 * (lkc >> 1);
   auto values = [&](int i, int j, float* v) {
     const int nl = wn * WTN + 16 * i + 4 * lkc;
@@ -544,7 +544,7 @@ __global__ void __launch_bounds__(WM * WN * 64) int8_gemm_kernel(const Int8Args 
   for (int j = 0; j < TJ; j++) {
     const int m = m0 + wm * WTM + 16 * j + frow;
     if (m >= a.M) continue;   // the swap partners (lanes l and l ^ 16) share the row m
-    if (pairs) {
+    if constexpr (PAIRS) {
 #pragma unroll
       for (int p = 0; p < TI / 2; p++) {
         uint32_t w[2][2];
@@ -558,7 +558,14 @@ __global__ void __launch_bounds__(WM * WN * 64) int8_gemm_kernel(const Int8Args 
         swap16(w[0][0], w[1][0]);
         swap16(w[0][1], w[1][1]);
         const int n = n0 + wn * WTN + 32 * p + pair_col;
-        if (n < a.N) *(uint4*)((u16*)a.y + (int64_t)m * a.y_row + n) = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
+        u16* y = (u16*)a.y + (int64_t)m * a.y_row + n;
+        if (n + 8 <= a.N) {
+          *(u32x4_any2*)y = u32x4_any2{w[0][0], w[0][1], w[1][0], w[1][1]};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; e++)
+            if (n + e < a.N) y[e] = (u16)(w[e >> 2][(e >> 1) & 1] >> (16 * (e & 1)));
+        }
       }
     } else {
 #pragma unroll
