@@ -16,7 +16,6 @@ def debug_lib():
         _lib = C.CDLL(LIB)
         _lib.dit_debug_gemm_plan.argtypes = [C.POINTER(ditstep.BlockConfig), C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
         _lib.dit_debug_reward_check_in_launch.argtypes = [C.c_int32, C.c_int32]
-        _lib.dit_debug_int8_form.argtypes = [C.c_int32, C.c_int32, C.c_int32]
     return _lib
 
 
@@ -30,11 +29,3 @@ def gemm_plan(cfg, batch, op, latent_dim=64):
     out = (C.c_int32 * 5)()
     assert debug_lib().dit_debug_gemm_plan(C.byref(cfg), batch, latent_dim, OPS.index(op), out) == 0
     return tuple(out)
-
-
-INT8_FORMS = ("few rows", "32, shared k", "64, shared k", "64", "128", "256 x 192", "256 x 256")
-
-
-def int8_form(rows, in_features, out_features):
-    """The form that an 8-bit product takes: see INT8_FORMS."""
-    return INT8_FORMS[debug_lib().dit_debug_int8_form(rows, in_features, out_features)]

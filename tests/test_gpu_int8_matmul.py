@@ -93,7 +93,7 @@ FORMS = [("few rows", 1, 61440, 50), ("few rows", 2, 30720, 9), ("few rows", 2, 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("form,M,K,N", FORMS)
 def test_every_form(d, form, M, K, N, dtype):
-    from tests.plan_util import int8_form
+    from tests.int8_util import int8_form
     assert int8_form(M, K, N) == form
     Problem(d, M, K, N, dtype, gelu=K % 2 == 0, bias=M % 2 == 1, pad=16 * (N % 2), ypad=3 * (M % 2)).check()
 

@@ -1,7 +1,7 @@
 """The form that an 8-bit product takes (no GPU needed): each is the choice somewhere, and the sizes that the rule was measured at keep theirs."""
 import pytest
 
-from tests.plan_util import INT8_FORMS, int8_form
+from tests.int8_util import INT8_FORMS, int8_form
 
 CHOICES = [((1, 61440, 5), "few rows"), ((1, 61441, 5), "32, shared k"), ((2, 30720, 5), "few rows"), ((2, 30721, 5), "32, shared k"), ((2, 3072, 12288), "few rows"),
            ((3, 3072, 12288), "32, shared k"), ((128, 12288, 3072), "32, shared k"), ((256, 12288, 3072), "64, shared k"), ((512, 4096, 4096), "64"),
