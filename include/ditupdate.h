@@ -57,10 +57,10 @@ typedef struct {
 } dit_adamw_tensor;
 
 typedef struct {
-  double lr;            /* finite */
+  double lr;            /* finite in fp32 */
   double beta1, beta2;  /* 0 <= beta < 1 */
-  double eps;           /* >= 0, finite */
-  double weight_decay;  /* finite */
+  double eps;           /* 0 or in the range of normal fp32 numbers */
+  double weight_decay;  /* finite in fp32 */
   int64_t step;         /* t >= 1: this step's number (without step_dev) */
 } dit_adamw_config;
 
@@ -70,8 +70,8 @@ typedef struct {
  * in fp32, rounded once to the types of param and copy. Nothing changes where *scale is NaN: a step whose gradients are not
  * finite is left out.
  *   scale     device fp32 (grad_norm's), or NULL
- *   step_dev  device int64 holding t (a captured step, which the caller counts on the device), or NULL: cfg's; it must be
- *             1 or more where it is read */
+ *   step_dev  device int64 holding t (a captured step, which the caller counts on the device), or NULL: cfg's. Nothing
+ *             changes where it is below 1 */
 dit_status adamw_step(const dit_adamw_config* cfg, const dit_adamw_tensor* tensors, int32_t n, const float* scale,
                       const int64_t* step_dev, dit_stream stream);
 

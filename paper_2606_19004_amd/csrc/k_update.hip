@@ -200,7 +200,11 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const WeightTable<N> t, 
   const int b = blockIdx.x, e = entry_of<N>(t.first, b);
   const int64_t begin = (b - t.first[e]) * chunk, end = min(begin + chunk, t.count[e]);
   Adam a = args.a;
-  if (args.step_dev) set_step(a, (double)*args.step_dev, args.log_beta1, args.log_beta2);
+  if (args.step_dev) {
+    const int64_t step = *args.step_dev;
+    if (step < 1) return;   // (1 - beta^t is 0 or negative)
+    set_step(a, (double)step, args.log_beta1, args.log_beta2);
+  }
   void* p = t.param[e];
   const void* g = t.grad[e];
   float *m = t.m[e], *v = t.v[e];

@@ -2,6 +2,7 @@
 #include "update_checks.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <initializer_list>
 
@@ -51,10 +52,13 @@ dit_status check_gradients(const dit_gradient* g, int32_t n, bool data, int64_t*
 dit_status check_adamw(const dit_adamw_config* c, const dit_adamw_tensor* t, int32_t n, bool step_dev, int64_t* total) {
   *total = 0;
   if (!c) return set_error(DIT_ERR_INVALID_ARG, "config is NULL");
-  if (!std::isfinite(c->lr) || !std::isfinite(c->weight_decay)) return set_error(DIT_ERR_DOMAIN, "lr or weight_decay not finite");
+  // (the kernel's numbers are fp32: an eps that rounds to 0 there would make 0 / 0 of a weight that has had no gradient)
+  if (!(std::fabs(c->lr) <= FLT_MAX) || !(std::fabs(c->weight_decay) <= FLT_MAX))
+    return set_error(DIT_ERR_DOMAIN, "lr or weight_decay not finite in fp32");
   if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0))
     return set_error(DIT_ERR_DOMAIN, "beta1 and beta2 must be in [0, 1)");
-  if (!(c->eps >= 0.0) || !std::isfinite(c->eps)) return set_error(DIT_ERR_DOMAIN, "eps must be >= 0 and finite");
+  if (c->eps != 0.0 && !(c->eps >= FLT_MIN && c->eps <= FLT_MAX))
+    return set_error(DIT_ERR_DOMAIN, "eps must be 0 or a positive normal fp32 number");
   if (!step_dev && c->step < 1) return set_error(DIT_ERR_DOMAIN, "step %lld (from 1 on)", (long long)c->step);
   dit_status st = check_list(t, n);
   for (int32_t i = 0; !st && i < n; i++) {

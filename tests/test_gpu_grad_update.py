@@ -182,6 +182,17 @@ def test_adamw_settings(d, change):
         check_adam((p, m, v, None), old, 1.0, h, h["step"])
 
 
+@pytest.mark.parametrize("step", [0, -1, -2 ** 63])
+def test_a_device_step_below_1_changes_nothing(d, step):
+    tensors = [torch.randn(5000, device="cuda") for _ in range(4)]
+    tensors[3].square_()
+    copy = torch.zeros(5000, dtype=torch.bfloat16, device="cuda")
+    old = [t.clone() for t in tensors] + [copy.clone()]
+    d.adamw_step(d.adamw_list(*([t] for t in tensors), [copy]), step_dev=torch.tensor([step], device="cuda"), **{**HYPER, "step": 0})
+    for t, before in zip([*tensors, copy], old):
+        assert torch.equal(t, before)
+
+
 def test_a_small_decay_is_not_lost(d):
     """lr weight_decay = 2^-27, below what 1 - lr weight_decay can hold, beside steps of unlike sizes. p lies in [64, 128), where a unit is 2^-17:
     the decay is 0.094 units on average and turns the rounding of the weights whose step ends that near a half. So the weights move, on average, by

@@ -76,6 +76,11 @@ def test_adamw(kw, status):
     assert lib.adamw_step(None, None, 0, None, None, None) == INVALID
 
 
+@pytest.mark.parametrize("kw", [dict(lr=1e39), dict(lr=-1e300), dict(weight_decay=4e38), dict(eps=1e39), dict(eps=1e-50), dict(eps=1e-38)])
+def test_adamw_numbers_that_fp32_does_not_hold(kw):
+    assert adam(**kw) == DOMAIN
+
+
 def rows(x=A, n=4, cols=10, x_row=10, dtype=1, q=A, q_row=10, scale=A, values=A, values_row=10):
     return lib.quantize_rows(x, n, cols, x_row, dtype, q, q_row, scale, values, values_row, None)
 
