@@ -18,9 +18,10 @@ namespace {
 // scale = max |x| / 127, correctly rounded and at least the smallest normal number, so that its reciprocal is finite.
 // q = the integer nearest to x / scale. x (1 / scale), rounded once to an integer, is that or its neighbour, which happens next to a half
 // only. What is left, x - q scale, is exact in fp32: both are multiples of half a unit in the last place of scale, and their
-// difference is below 2^24 of these. Where it is below scale / 2, q is right; elsewhere, which is rare, a tie goes to the even one.
+// difference is below 2^24 of these. Where twice that is below scale, q is right; elsewhere, which is rare, a tie goes to the even one. (What is
+// left is doubled, which is exact. Half of the scale is not: below 2^-125 a scale is a multiple of 2^-149, the smallest unit there is.)
 struct RowScale {
-  float scale, inv, half;
+  float scale, inv;
   bool bad;   // the row holds a NaN or an infinity: scale NaN, integers 0
 };
 // top: the largest |x| of the row, as bits (which order like the values, NaN last)
@@ -29,7 +30,6 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top) {
   r.bad = top >= 0x7f800000u;
   r.scale = fmaxf(__uint_as_float(r.bad ? 0u : top) / 127.f, 0x1p-126f);
   r.inv = 1.f / r.scale;
-  r.half = 0.5f * r.scale;
   return r;
 }
 constexpr float MAGIC = 12582912.f;   // 1.5 2^23: MAGIC + q has the integer q in its low bits
@@ -92,11 +92,11 @@ __device__ __forceinline__ void to_integers(const RowScale& r, const float* f, f
     t[i] = fmaf(f[i], r.inv, MAGIC);
     far = fmaxf(far, fabsf(fmaf(MAGIC - t[i], r.scale, f[i])));
   }
-  if (far >= r.half) {
+  if (2.f * far >= r.scale) {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      const float left = fmaf(MAGIC - t[i], r.scale, f[i]), d = fabsf(left);
-      if (d > r.half || (d == r.half && (__float_as_uint(t[i]) & 1))) t[i] += copysignf(1.f, left);
+      const float left = fmaf(MAGIC - t[i], r.scale, f[i]), d = 2.f * fabsf(left);
+      if (d > r.scale || (d == r.scale && (__float_as_uint(t[i]) & 1))) t[i] += copysignf(1.f, left);
     }
   }
 }
