@@ -58,7 +58,7 @@ typedef struct {
 
 typedef struct {
   double lr;            /* finite in fp32 */
-  double beta1, beta2;  /* 0 <= beta < 1 */
+  double beta1, beta2;  /* 0 <= beta < 1, also where it is rounded to fp32 (1 - 2^-25 is not): the means are fp32 numbers */
   double eps;           /* 0 or in the range of normal fp32 numbers */
   double weight_decay;  /* finite in fp32 */
   int64_t step;         /* t >= 1: this step's number (without step_dev) */
@@ -67,8 +67,8 @@ typedef struct {
 /* With g' = *scale g (scale NULL: 1),
  *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
  *   param -= lr ( (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay param ),
- * in fp32, rounded once to the types of param and copy. Nothing changes where *scale is NaN: a step whose gradients are not
- * finite is left out.
+ * in fp32, rounded once to the types of param and copy. The betas count to 2^-24 of 1 - beta; each step rounds the means twice, by 2^-24 of
+ * them at most, and squares below 2^-149 vanish in v. Nothing changes where *scale is NaN: a step whose gradients are not finite is left out.
  *   scale     device fp32 (grad_norm's), or NULL
  *   step_dev  device int64 holding t (a captured step, which the caller counts on the device), or NULL: cfg's. Nothing
  *             changes where it is below 1 */

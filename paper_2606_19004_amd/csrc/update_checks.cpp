@@ -55,8 +55,10 @@ dit_status check_adamw(const dit_adamw_config* c, const dit_adamw_tensor* t, int
   // (the kernel's numbers are fp32: an eps that rounds to 0 there would make 0 / 0 of a weight that has had no gradient)
   if (!(std::fabs(c->lr) <= FLT_MAX) || !(std::fabs(c->weight_decay) <= FLT_MAX))
     return set_error(DIT_ERR_DOMAIN, "lr or weight_decay not finite in fp32");
-  if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0))
-    return set_error(DIT_ERR_DOMAIN, "beta1 and beta2 must be in [0, 1)");
+  // (a mean in fp32 times a beta that rounds to 1 there stays as it is)
+  for (double beta : {c->beta1, c->beta2})
+    if (!(beta >= 0.0 && beta < 1.0) || !((float)beta < 1.f))
+      return set_error(DIT_ERR_DOMAIN, "beta1 and beta2 must be in [0, 1), also as fp32 numbers");
   if (c->eps != 0.0 && !(c->eps >= FLT_MIN && c->eps <= FLT_MAX))
     return set_error(DIT_ERR_DOMAIN, "eps must be 0 or a positive normal fp32 number");
   if (!step_dev && c->step < 1) return set_error(DIT_ERR_DOMAIN, "step %lld (from 1 on)", (long long)c->step);
