@@ -601,11 +601,14 @@ def grad_clip(grads, scale, stream=None):
 
 def adamw_list(params, grads, m, v, copies=None) -> TensorList:
     """Weights (bf16 or fp32), their gradients (bf16 or fp32) and moments (fp32), all contiguous; copies: bf16 weights that follow
-    fp32 ones (a list whose entries may be None), or None. The list holds their addresses, as grad_list's."""
+    fp32 ones (a list whose entries may be None), or None. A weight whose gradient is None is left out, as in grad_list. The list holds
+    their addresses, as grad_list's."""
     params, grads, m, v = (list(x) for x in (params, grads, m, v))
     copies = [None] * len(params) if copies is None else list(copies)
     if not len(params) == len(grads) == len(m) == len(v) == len(copies):
         raise ValueError("lists of unlike lengths")
+    if any(g is None for g in grads):
+        params, grads, m, v, copies = ([x for x, g in zip(row, grads) if g is not None] for row in (params, grads, m, v, copies))
     device = params[0].get_device() if params else -1
     words, starts, ends = [], [], []
     for p, g, a, b, c in zip(params, grads, m, v, copies):
