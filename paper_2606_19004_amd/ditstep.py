@@ -539,6 +539,14 @@ def _apart(starts, ends):
         raise ValueError("tensors of a list share memory")
 
 
+def _joined(starts, ends):
+    """The pieces that overlapping ones make together: one ends where the i-th smallest end is not past the start that follows it."""
+    starts.sort()
+    ends.sort()
+    cuts = [i for i in range(1, len(starts)) if ends[i - 1] <= starts[i]]
+    return starts[:1] + [starts[i] for i in cuts], [ends[i - 1] for i in cuts] + ends[-1:]
+
+
 def _list_of(struct, words, count, device, keep):
     """words: the structs' fields, 64 bits each (two 32-bit fields in one)."""
     array = (struct * max(count, 1))()
@@ -601,8 +609,8 @@ def grad_clip(grads, scale, stream=None):
 
 def adamw_list(params, grads, m, v, copies=None) -> TensorList:
     """Weights (bf16 or fp32), their gradients (bf16 or fp32) and moments (fp32), all contiguous; copies: bf16 weights that follow
-    fp32 ones (a list whose entries may be None), or None. A weight whose gradient is None is left out, as in grad_list. The list holds
-    their addresses, as grad_list's."""
+    fp32 ones (a list whose entries may be None), or None. A weight whose gradient is None is left out, as in grad_list. Gradients
+    are read only and may share memory with each other. The list holds addresses, as grad_list's."""
     params, grads, m, v = (list(x) for x in (params, grads, m, v))
     copies = [None] * len(params) if copies is None else list(copies)
     if not len(params) == len(grads) == len(m) == len(v) == len(copies):
@@ -610,14 +618,15 @@ def adamw_list(params, grads, m, v, copies=None) -> TensorList:
     if any(g is None for g in grads):
         params, grads, m, v, copies = ([x for x, g in zip(row, grads) if g is not None] for row in (params, grads, m, v, copies))
     device = params[0].get_device() if params else -1
-    words, starts, ends = [], [], []
+    words, starts, ends, g_starts, g_ends = [], [], [], [], []
     for p, g, a, b, c in zip(params, grads, m, v, copies):
         if not p.shape == g.shape == a.shape == b.shape or (c is not None and c.shape != p.shape):
             raise ValueError(f"a weight of shape {tuple(p.shape)} and a tensor of another")
-        words += (_piece(p, device, _FLOATS, starts, ends), _piece(g, device, _FLOATS, starts, ends), _piece(a, device, _F32, starts, ends),
+        words += (_piece(p, device, _FLOATS, starts, ends), _piece(g, device, _FLOATS, g_starts, g_ends), _piece(a, device, _F32, starts, ends),
                   _piece(b, device, _F32, starts, ends), 0 if c is None else _piece(c, device, _BF16, starts, ends), p.numel(),
                   _ROW_CODES[p.dtype] | _ROW_CODES[g.dtype] << 32)
-    _apart(starts, ends)
+    g_starts, g_ends = _joined(g_starts, g_ends)
+    _apart(starts + g_starts, ends + g_ends)
     return _list_of(AdamwTensor, words, len(params), device, params + grads + m + v + copies)
 
 
