@@ -188,6 +188,13 @@ def _s(stream) -> int | None:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
+def _size(n) -> int:
+    """A size that the library takes as a 32-bit integer, into which a larger one would wrap."""
+    if n >= 1 << 31:
+        raise ValueError(f"a size of {n} (at most 2^31 - 1)")
+    return n
+
+
 def _dtype_code(dtype) -> int:
     if dtype in ("bf16", torch.bfloat16, DIT_BF16):
         return DIT_BF16
@@ -266,12 +273,12 @@ def flow_logprob(x, v, x_next, t, t_next, noise_level, logp, stream=None):
     logp: [batch] fp64 device tensor."""
     b = x.shape[0] if x.dim() > 0 else 0
     n = x.numel() // b if b else 0
-    _check(_lib.flow_logprob(_ptr(x), _ptr(v), _ptr(x_next), b, n, t, t_next, noise_level, _ptr(logp), _s(stream)))
+    _check(_lib.flow_logprob(_ptr(x), _ptr(v), _ptr(x_next), _size(b), n, t, t_next, noise_level, _ptr(logp), _s(stream)))
 
 
 def group_reward_stats(rewards, adv_eps=1e-4, k_select=0, mean=None, std=None, adv=None, order=None, selected=None,
                        stream=None):
-    g, n = rewards.shape
+    g, n = map(_size, rewards.shape)
     _check(_lib.group_reward_stats(_ptr(rewards), g, n, adv_eps, k_select, _ptr(mean), _ptr(std), _ptr(adv),
                                    _ptr(order), _ptr(selected), _s(stream)))
 
@@ -279,7 +286,7 @@ def group_reward_stats(rewards, adv_eps=1e-4, k_select=0, mean=None, std=None, a
 def group_reward_stats_async(rewards, status, adv_eps=1e-4, k_select=0, mean=None, std=None, adv=None, order=None,
                              selected=None, stream=None):
     """status: one-element int32 device tensor; holds DIT_OK or DIT_ERR_NAN once the stream has run."""
-    g, n = rewards.shape
+    g, n = map(_size, rewards.shape)
     _check(_lib.group_reward_stats_async(_ptr(rewards), g, n, adv_eps, k_select, _ptr(mean), _ptr(std), _ptr(adv),
                                          _ptr(order), _ptr(selected), _ptr(status), _s(stream)))
 
@@ -410,7 +417,7 @@ def packed_config(q, k, v, o, sequences, causal=False, scale=None, max_q=0) -> P
     if scale is None:
         scale = 1.0 / math.sqrt(d)
     strides = [s for t in (q, k, v, o) for s in (t.stride(0), t.stride(1))]
-    return PackedConfig(sequences, q.shape[1], k.shape[1], d, q.shape[0], k.shape[0], max_q, int(bool(causal)),
+    return PackedConfig(sequences, _size(q.shape[1]), _size(k.shape[1]), _size(d), _size(q.shape[0]), _size(k.shape[0]), max_q, int(bool(causal)),
                         _dtype_code(q.dtype), scale, *strides)
 
 
@@ -457,7 +464,7 @@ def gated_norm_config(x, sequences, post="none", pre="layer", eps=1e-6, residual
     """x [rows][hidden] (a row stride is fine); row strides of y and h are x's, that of gate, scale and shift is hidden, unless given."""
     if x.dim() != 2 or (x.numel() and x.stride(1) != 1):
         raise ValueError("x is [rows][hidden] with the last index contiguous")
-    rows, hidden = x.shape
+    rows, hidden = map(_size, x.shape)
     row = x.stride(0) if rows > 1 else max(x.stride(0), hidden)
     return GatedNormConfig(sequences, rows, hidden, _dtype_code(x.dtype), NORM_KINDS[post], NORM_KINDS[pre], eps,
                            residual_scale, row, row if y_row is None else y_row, row if h_row is None else h_row,
@@ -495,14 +502,14 @@ def gated_norm_backward(cfg, x_out, y, dx_out, dh, dx, dy, gate=None, scale=None
 
 
 def flow_policy_loss_workspace_bytes(batch, n_per_sample) -> int:
-    return _lib.flow_policy_loss_workspace_bytes(batch, n_per_sample)
+    return _lib.flow_policy_loss_workspace_bytes(_size(batch), n_per_sample)
 
 
 def flow_policy_loss(x, v, x_next, logp_old, adv, t, t_next, noise_level, loss, dv=None, logp=None, ratio=None,
                      v_ref=None, logp_scale=None, clip_low=0.2, clip_high=0.2, kl_weight=0.0, ws=None, stream=None):
     """x, v, x_next, v_ref, dv: [batch][n] fp32 (any trailing shape, contiguous); logp_old, logp, ratio: [batch] fp64; adv: [batch]
     fp32; loss: one fp64. logp_scale None: 1 / n."""
-    b = x.shape[0] if x.dim() > 0 else 0
+    b = _size(x.shape[0]) if x.dim() > 0 else 0
     n = x.numel() // b if b else 0
     if logp_scale is None:
         logp_scale = 1.0 / max(n, 1)
@@ -673,6 +680,8 @@ def quantize_rows(x, q, scale, values=None, stream=None):
     if code is None or len(shape) != 2:
         raise ValueError(f"x of {dt} and shape {tuple(shape)}: [rows][cols] of bf16 or fp32 is wanted")
     rows, cols = shape
+    if (rows | cols) >> 31:
+        _size(max(shape))
     sx, sq, sv = x.stride(), q.stride(), (0, 1) if values is None else values.stride()
     if cols > 1 and not sx[1] == sq[1] == sv[1] == 1:
         raise ValueError("the last index of x, q and values is contiguous")
@@ -693,7 +702,7 @@ def int8_config(x, w, y, act="none") -> Int8Config:
 
     def int8_stride(t):   # of one row: any multiple of 16 that is long enough
         return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
-    return Int8Config(x.shape[0], x.shape[1], w.shape[0], _dtype_code(y.dtype), ACTIVATIONS[act],
+    return Int8Config(_size(x.shape[0]), _size(x.shape[1]), _size(w.shape[0]), _dtype_code(y.dtype), ACTIVATIONS[act],
                       int8_stride(x) if x.dtype == torch.int8 else _row_stride(x), int8_stride(w), _row_stride(y))
 
 
