@@ -37,7 +37,7 @@ dit_status quantize_rows(const void* x, int32_t rows, int32_t cols, int64_t x_ro
 typedef enum { DIT_ACT_NONE = 0, DIT_ACT_GELU_TANH = 1 } dit_activation;
 
 typedef struct {
-  int32_t rows;          /* of x and y, >= 0 */
+  int32_t rows;          /* of x and y, >= 0; y has at most 2^23 - 8 tiles of 256 x 256 results (2^39 of them) */
   int32_t in_features;   /* 1 .. 131071: the sums fit 32 bits whatever the integers are */
   int32_t out_features;  /* >= 0 */
   int32_t dtype;         /* dit_dtype of y and bias, and of int8_linear's x */

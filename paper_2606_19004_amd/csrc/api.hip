@@ -1576,7 +1576,7 @@ dit_status check_int8_call(const dit_int8_config* c, bool given, const void* x, 
   dit_status st;
   if ((st = check_offsets_aligned({w_scale}))) return st;
   if ((st = check_elements({given ? nullptr : x, bias, y}, c->dtype))) return st;
-  return check_threads(int8_matmul_threads(c->rows, c->out_features));
+  return check_threads(int8_matmul_threads(c->rows, c->out_features, c->in_features));
 }
 
 // (raw, raw_row: rows that the product rounds by itself, in place of x and x_scale)

@@ -923,10 +923,31 @@ int64_t tiles_of(int M, int N, int bm, int bn) { return (int64_t)cdiv(M, bm) * c
 // rows of x in LDS
 size_t few_rows_lds(int M, int K) { return (size_t)M * ((K + STEP - 1) / STEP * STEP); }
 
+// of one or two rows: whether waves of a workgroup share k, and its workgroups
+bool few_rows_share(int N) { return cdiv(N, 4 * F) < 2 * cu_count(); }
+int few_rows_blocks(int N) { return cdiv(N, few_rows_share(N) ? F : 4 * F); }
+
+int64_t tile_blocks(int M, int N, int bm, int bn) { return (tiles_of(M, N, bm, bn) + 7) / 8 * 8; }
+
+int64_t form_threads(Int8Form f, int M, int N) {
+  switch (f) {
+    case INT8_FEW_ROWS: return 256 * (int64_t)few_rows_blocks(N);
+    case INT8_KSPLIT_32: return 256 * tile_blocks(M, N, 32, 32);
+    case INT8_KSPLIT_64:
+    case INT8_RING_64: return 256 * tile_blocks(M, N, 64, 64);
+    case INT8_RING_128: return 512 * tile_blocks(M, N, 128, 128);
+    case INT8_LARGE_192: return 512 * tile_blocks(M, N, 256, 192);
+    case INT8_LARGE_256: return 512 * tile_blocks(M, N, 256, 256);
+  }
+  return INT64_MAX;
+}
+// a launch takes fewer than 2^32 threads
+bool fits(Int8Form f, int M, int N) { return form_threads(f, M, N) < int64_t(1) << 32; }
+
 }  // namespace
 
 Int8Form int8_form(int M, int N, int K) {
-  if (M <= 2 && few_rows_lds(M, K) <= 61440) return INT8_FEW_ROWS;
+  if (M <= 2 && few_rows_lds(M, K) <= 61440 && fits(INT8_FEW_ROWS, M, N)) return INT8_FEW_ROWS;
   // Estimated times, us. What a CU takes per k-tile: 1.25 for a 256 x 256 tile (near the matrix rate), 0.5 for 128 x 128 and 0.24 for 64 x 64
   // (LDS reads), 0.23 and 0.09 for those whose waves share k; beside it each round's first loads and stores. Measured (us, in this order: 32 and 64
   // with shared k, 64, 128, 256 x 192, 256): 128 x 12288 -> 3072: 19 / 22 / 28 / 43 / 77 / 97; 333 x 3072 -> 9216: 35 / 35 / 22 / 16 / 25 / 31;
@@ -939,7 +960,7 @@ Int8Form int8_form(int M, int N, int K) {
   double best = rounds(256, 256) * (1.25 * kt + 11.0);
   Int8Form pick = INT8_LARGE_256;
   auto consider = [&](Int8Form f, double cost) {
-    if (cost < best) best = cost, pick = f;
+    if (cost < best && fits(f, M, N)) best = cost, pick = f;
   };
   consider(INT8_LARGE_192, rounds(256, 192) * (1.09 * kt + 8.5));
   consider(INT8_RING_128, rounds(128, 128) * (0.5 * kt + 4.5));
@@ -957,7 +978,7 @@ template <int BM, int BN, int WM, int WN, int RING, int ACT, typename T> hipErro
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(&int8_gemm_kernel<BM, BN, WM, WN, RING, ACT, T>), lds, attr_set);
   if (e != hipSuccess) return e;
   const int64_t tiles = tiles_of(a.M, a.N, BM, BN);
-  int8_gemm_kernel<BM, BN, WM, WN, RING, ACT, T><<<8 * cdiv(tiles, 8), WM * WN * 64, lds, s>>>(a, (int)tiles);
+  int8_gemm_kernel<BM, BN, WM, WN, RING, ACT, T><<<(int)tile_blocks(a.M, a.N, BM, BN), WM * WN * 64, lds, s>>>(a, (int)tiles);
   return hipGetLastError();
 }
 template <int B, int ACT, typename T> hipError_t launch_ksplit(const Int8Args& a, hipStream_t s) {
@@ -966,13 +987,13 @@ template <int B, int ACT, typename T> hipError_t launch_ksplit(const Int8Args& a
   const hipError_t e = allow_lds(reinterpret_cast<const void*>(&int8_ksplit_kernel<B, ACT, T>), lds, attr_set);
   if (e != hipSuccess) return e;
   const int64_t tiles = tiles_of(a.M, a.N, B, B);
-  int8_ksplit_kernel<B, ACT, T><<<8 * cdiv(tiles, 8), 256, lds, s>>>(a, (int)tiles);
+  int8_ksplit_kernel<B, ACT, T><<<(int)tile_blocks(a.M, a.N, B, B), 256, lds, s>>>(a, (int)tiles);
   return hipGetLastError();
 }
 template <int ROWS, bool RAW, int ACT, typename T> hipError_t launch_few(const Int8Args& a, hipStream_t s) {
   const size_t lds = few_rows_lds(a.M, a.K);
-  if (cdiv(a.N, 4 * F) >= 2 * cu_count()) int8_few_rows_kernel<ROWS, false, RAW, ACT, T><<<cdiv(a.N, 4 * F), 256, lds, s>>>(a);
-  else int8_few_rows_kernel<ROWS, true, RAW, ACT, T><<<cdiv(a.N, F), 256, lds, s>>>(a);
+  if (few_rows_share(a.N)) int8_few_rows_kernel<ROWS, true, RAW, ACT, T><<<few_rows_blocks(a.N), 256, lds, s>>>(a);
+  else int8_few_rows_kernel<ROWS, false, RAW, ACT, T><<<few_rows_blocks(a.N), 256, lds, s>>>(a);
   return hipGetLastError();
 }
 template <bool RAW, int ACT, typename T> hipError_t launch_few_rows(const Int8Args& a, hipStream_t s) {
@@ -982,7 +1003,7 @@ template <bool RAW, int ACT, typename T> hipError_t launch_few_rows(const Int8Ar
 template <int VECTORS, int ACT, typename T> hipError_t launch_small(const Int8Args& a, hipStream_t s) {
   const size_t lds = (size_t)((a.K + 127) / 128 + 8) * 4096;   // (more than the 16 KB that the sums take; at most 64)
   const int64_t tiles = tiles_of(a.M, a.N, 32, 32);
-  int8_small_kernel<VECTORS, ACT, T><<<8 * cdiv(tiles, 8), 256, lds, s>>>(a, (int)tiles);
+  int8_small_kernel<VECTORS, ACT, T><<<(int)tile_blocks(a.M, a.N, 32, 32), 256, lds, s>>>(a, (int)tiles);
   return hipGetLastError();
 }
 template <int ACT, typename T> hipError_t launch_raw(const Int8Args& a, hipStream_t s) {
@@ -1009,12 +1030,11 @@ hipError_t quantize_rows_launch(const QuantArgs& a, int dtype, hipStream_t s) {
   return dtype == DT_BF16 ? quantize_any<u16>(a, s) : quantize_any<float>(a, s);
 }
 
-int64_t int8_matmul_threads(int M, int N) {
-  return M <= 2 ? 256 * std::max<int64_t>(cdiv(N, 4 * F), 2 * cu_count()) : 256 * (tiles_of(M, N, 32, 32) + 8);
-}
+// (a product that rounds its own rows has the threads of this form, or 512 small tiles)
+int64_t int8_matmul_threads(int M, int N, int K) { return form_threads(int8_form(M, N, K), M, N); }
 
 bool int8_takes_raw(int M, int N, int K) {
-  if (M <= 2) return (int64_t)M * K <= RAW_ELEMENTS;
+  if (M <= 2) return (int64_t)M * K <= RAW_ELEMENTS && fits(INT8_FEW_ROWS, M, N);
   return K <= RAW_K && tiles_of(M, N, 32, 32) <= 2 * cu_count();
 }
 

@@ -31,7 +31,7 @@ struct Int8Args {
 // or 256 x 256
 enum Int8Form { INT8_FEW_ROWS, INT8_KSPLIT_32, INT8_KSPLIT_64, INT8_RING_64, INT8_RING_128, INT8_LARGE_192, INT8_LARGE_256 };
 Int8Form int8_form(int M, int N, int K);
-int64_t int8_matmul_threads(int M, int N);   // of the largest launch: one takes fewer than 2^32
+int64_t int8_matmul_threads(int M, int N, int K);   // of the product's launch: one takes fewer than 2^32
 bool int8_takes_raw(int M, int N, int K);    // whether a product rounds its rows by itself
 hipError_t int8_matmul_launch(const Int8Args& a, int dtype, int act, hipStream_t s);
 
