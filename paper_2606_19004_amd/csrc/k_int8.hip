@@ -454,10 +454,9 @@ __global__ void __launch_bounds__(WM * WN * 64) int8_gemm_kernel(const Int8Args 
     // and nothing is gained: 1280 x 12288 -> 3072 62 and 63). Tiles of 64, of which a CU holds three, are faster without (28 and 31).
     constexpr int L = X_LOADS + W_LOADS;
     constexpr bool SPREAD = BM * BN > 64 * 64;
-    static_assert((RING - 2) * L <= 15 && (RING - 1) * L <= 63 && X_LOADS <= TI && W_LOADS <= TI, "the waits and places below");
+    static_assert(RING <= 4 && (RING - 2) * L <= 15 && (RING - 1) * L <= 63 && X_LOADS <= TI && W_LOADS <= TI, "the waits and places below");
     auto wait_tiles = [&](int n) {   // at most the loads of n tiles in flight, LDS reads done
       if (n >= RING - 2) __builtin_amdgcn_s_waitcnt(0x0070 | ((RING - 2) * L & 15));
-      else if (n == 2) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * L & 15));
       else if (n == 1) __builtin_amdgcn_s_waitcnt(0x0070 | (L & 15));
       else __builtin_amdgcn_s_waitcnt(0x0070);
     };
@@ -686,15 +685,16 @@ __global__ void __launch_bounds__(256) int8_ksplit_kernel(const Int8Args a, int 
 }
 
 // Small products of rows that are not integers yet, in one launch: a 32 x 32 tile as above, whose workgroup first rounds its 32 rows of x into
-// LDS, eight lanes to a row, while its first slices of w are on their way. Bound by latency: the launch, x, w, the sums. Against a launch that
+// LDS, eight lanes to a row, while its slices of w are on their way. Bound by latency: the launch, x, w, the sums. Against a launch that
 // rounds the rows and one that multiplies (us, as eager calls and in a graph): 3 x 256 -> 256 6.6 and 4.0 for 9.6 and 6.1, 500 x 256 -> 1024 6.7 and
 // 6.4 for 9.6 and 8.7, 500 x 512 -> 1024 9.5 and 9.3 for 10.1 and 9.2; rows of 1001 (333 of them, 515 features) took 12.4 for 10.0 and 7.9.
-constexpr int RAW_K = 512;   // longest rows
+constexpr int RAW_K = 512;   // longest rows: four k-tiles, one for each wave
+static_assert(RAW_K <= 4 * 128, "a wave has one slice of k at most");
 template <int VECTORS, int ACT, typename T>
 __global__ void __launch_bounds__(256) int8_small_kernel(const Int8Args a, int total_tiles) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int B = 32, STAGE = B * 128;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];   // x [k-tile][row][128], then two stages of w for each wave
+  extern __shared__ __attribute__((aligned(1024))) char smem[];   // x [k-tile][row][128], then each wave's slice of w
   __shared__ float scales[B];
   const int per = gridDim.x >> 3;
   const int t = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
@@ -705,13 +705,13 @@ __global__ void __launch_bounds__(256) int8_small_kernel(const Int8Args a, int t
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int K = a.K, nk = (K + 127) / 128;
   const u32x4_t rw = rows_rsrc(a.w + (int64_t)n0 * a.w_row, min(B, a.N - n0), a.w_row, K);
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + nk * STAGE + wave * 2 * STAGE;
-  auto issue = [&](int kt, int st) {
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem + (nk + wave) * STAGE;
+  auto issue = [&](int kt) {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
       const int r = 8 * i + (lane >> 3), chunk = ((lane & 7) ^ swz(r)) * 16;
       const bool in = kt * 128 + chunk < K && n0 + r < a.N;
-      dma_b128(rw, lds0 + st * STAGE + i * 1024, in ? (uint32_t)(r * a.w_row) + chunk : OUTSIDE, kt * 128);
+      dma_b128(rw, lds0 + i * 1024, in ? (uint32_t)(r * a.w_row) + chunk : OUTSIDE, kt * 128);
     }
   };
   const int row = tid >> 3, part = tid & 7;   // elements 8 (part + 8 v) .. + 7 of a row; rows past the end repeat the last and are not stored
@@ -723,8 +723,7 @@ __global__ void __launch_bounds__(256) int8_small_kernel(const Int8Args a, int t
     if (K % 8 == 0) e[v].load(x + min(at, K - 8));   // (past the end: repeats the last ones, which does not change the largest)
     else load_row8(x, at, K, e[v]);
   }
-  if (wave < nk) issue(wave, 0);
-  if (wave + 4 < nk) issue(wave + 4, 1);
+  if (wave < nk) issue(wave);
   uint32_t top = 0;
 #pragma unroll
   for (int v = 0; v < VECTORS; v++) top = max(top, e[v].top());
@@ -747,12 +746,10 @@ __global__ void __launch_bounds__(256) int8_small_kernel(const Int8Args a, int t
 
   const int r16 = lane & 15, kq = lane >> 4;
   i32x4 acc[2][2] = {};
-  int st = 0;
-  for (int kt = wave; kt < nk; kt += 4) {
-    if (kt + 4 >= nk) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(4)" ::: "memory");   // (the 4 loads of this wave's next slice may be in flight)
-    const char* sx = smem + kt * STAGE;
-    const char* sw = smem + nk * STAGE + (wave * 2 + st) * STAGE;
+  if (wave < nk) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const char* sx = smem + wave * STAGE;
+    const char* sw = smem + (nk + wave) * STAGE;
     i32x4 fw[2][2], fx[2][2];
 #pragma unroll
     for (int s = 0; s < 2; s++)
@@ -762,17 +759,12 @@ __global__ void __launch_bounds__(256) int8_small_kernel(const Int8Args a, int t
         fw[s][i] = *(const i32x4*)(sw + fr * 128 + (((4 * s + kq) ^ swz(fr)) << 4));
         fx[s][i] = *(const i32x4*)(sx + fr * 128 + (((4 * s + kq) ^ swz(fr)) << 4));
       }
-    if (kt + 8 < nk) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the fragments are in registers: the stage is free
-      issue(kt + 8, st);
-    }
 #pragma unroll
     for (int s = 0; s < 2; s++)
 #pragma unroll
       for (int i = 0; i < 2; i++)
 #pragma unroll
         for (int j = 0; j < 2; j++) acc[i][j] = mfma_i8(fw[s][i], fx[s][j], acc[i][j]);
-    st ^= 1;
   }
   __syncthreads();   // x and w have been read
   i32x4* sums = (i32x4*)smem;   // [block][wave][lane]
@@ -1001,7 +993,7 @@ template <bool RAW, int ACT, typename T> hipError_t launch_few_rows(const Int8Ar
 }
 
 template <int VECTORS, int ACT, typename T> hipError_t launch_small(const Int8Args& a, hipStream_t s) {
-  const size_t lds = (size_t)((a.K + 127) / 128 + 8) * 4096;   // (more than the 16 KB that the sums take; at most 64)
+  const size_t lds = (size_t)((a.K + 127) / 128 + 4) * 4096;   // 20 to 32 KB (the sums take 16)
   const int64_t tiles = tiles_of(a.M, a.N, 32, 32);
   int8_small_kernel<VECTORS, ACT, T><<<(int)tile_blocks(a.M, a.N, 32, 32), 256, lds, s>>>(a, (int)tiles);
   return hipGetLastError();
