@@ -272,7 +272,7 @@ constexpr uint32_t OUTSIDE = 0xC0000000u;   // an offset past any tile's records
 // twice its depth per byte. RING > 0: a ring of RING stages of both.
 // Bound by the matrix units, at the clock that the chip's power leaves: 20480 x 3072 -> 12288 in 610 us (590-640 from card to card), 2540
 // TOP/s (a library product of these integers: 720 us), with gelu 640. A 256 x 256 tile takes 2380 cycles per k-tile, 2048 of them the products'
-// (one of 128 x 128: 1030 and 512; more stages, fewer LDS reads per product or two tiles to a barrier did not help), 2.3 GHz on few CUs and 1.6-1.7 on all.
+// (one of 128 x 128: 1030 and 512; more stages, fewer LDS reads per product or two tiles to a barrier did not help), 2.3 GHz on few CUs and 1.6-1.75 on all.
 // bf16 rows of y that do not start at multiples of 4 bytes cost stores of parts of a word: on one card 20480 x 3072 -> 12288 624 us, -> 12284 634,
 // -> 12287 752.
 template <int BM, int BN, int WM, int WN, int RING, int ACT, typename T>

@@ -1,8 +1,8 @@
 // The end of a policy update: the 2-norm over the gradients of all weights, clipping, and the weights' AdamW step. All are
 // bound by memory (a large copy runs at 5.0 TB/s). 340 M weights, bf16 gradients, fp32 master weights with bf16 copies: norm 118-123 us (5.5 TB/s), clip
-// 271 (5.0), AdamW 1912 (5.0). Tensors come as tables in the kernels' arguments (no copy to the device, nothing kept between calls); a workgroup
-// takes one chunk of one tensor. About 8192 chunks, of 2048 elements at least: 2.4 M fp32 weights in 20 tensors: AdamW 14.0 us (4.7 TB/s;
-// chunks of 4096 15.3), norm 6.3, clip 5.2.
+// 271 (5.0), AdamW 1895 (5.0), of bf16 weights without masters 1497 (5.0). Tensors come as tables in the kernels' arguments (no copy to the device,
+// nothing kept between calls); a workgroup takes one chunk of one tensor. About 8192 chunks, of 2048 elements at least:
+// 2.4 M fp32 weights in 20 tensors: AdamW 12.4-14.0 us (4.7-5.3 TB/s; chunks of 4096 15.3), norm 6.3, clip 5.2.
 #include <algorithm>
 #include <cmath>
 
@@ -17,7 +17,7 @@ constexpr int THREADS = 256;
 // ---- tables of tensors ----
 // first[e]: the workgroup that takes tensor e's first chunk; unused entries are past every workgroup.
 // A launch's arguments stay below 4 KB: 192 gradients, 64 weights. Short lists take smaller tables, which the host copies faster (20 tensors: norm
-// and clip 15.1 -> 13.1 us). Long lists of small tensors pay for their launches: 1200 tensors, 9 M weights, AdamW 133 us in 19 of them.
+// and clip 15.1 -> 13.1 us). Long lists of small tensors pay for their launches: 1200 tensors, 9 M weights, AdamW 111-133 us in 19 of them.
 constexpr int GRADS = 192, WEIGHTS = 64, FEW = 24;
 template <int N> struct GradTable {
   void* data[N];
@@ -142,7 +142,8 @@ __global__ void __launch_bounds__(THREADS) clip_kernel(const GradTable<N> t, int
 }
 
 // ---- AdamW ----
-// One pass: 28 bytes move for a weight of the master form. Rounding to bf16 weights is to nearest: without master weights a step below
+// One pass: 28 bytes move for a weight of the master form. The step's number on the device, from which every thread computes its two factors in
+// fp64, costs 0.5 us of 12.4 (2.4 M fp32 weights) and nothing of 1895 (340 M). Rounding to bf16 weights is to nearest: without master weights a step below
 // half a unit in the last place is lost.
 // A beta is the sum of two fp32 numbers, so that what a mean keeps and what is added to it have the weights beta and 1 - beta to 2^-24 of 1 - beta.
 // (One fp32 number is off by up to 1.7e-4 of 1 - 0.9999, in every step to the same side.)
